@@ -344,6 +344,130 @@ int lamp_attn_decode(const uint16_t *q, const uint16_t *k, const uint16_t *v,
                      const struct lamp_fwd_extra *extra, void *stream);
 
 /*
+ * Serving: what surrounds the attention of a layer, from the projections'
+ * outputs to the attention over an 8-bit paged cache.  Three operators, each
+ * asynchronous on `stream`, each allocating nothing (but lamp_attn_cache
+ * without a workspace), each usable in a captured graph: the lengths and the
+ * block table are read on the device.
+ *
+ * lamp_rows: rows of d channels (contiguous, 16-byte aligned) of B x N tokens
+ * and `heads` heads, element (b, n, h, c) at p + b*batch + n*token + h*head + c
+ * (strides in elements; multiples of 8 for bf16, of 4 for fp32).
+ */
+typedef struct lamp_rows {
+    void *p;
+    int64_t batch, token, head;
+    int heads;
+} lamp_rows;
+
+/*
+ * lamp_qk_norm_rope -- RMS norm of every query and key head, then the position
+ * rotation, in one pass: for each row x of d channels
+ *   y = x (mean x^2 + eps)^(-1/2) gain     (q_gain / k_gain NULL: y = x)
+ *   y'_c = y_c cos_c - y_{c+h} sin_c,  y'_{c+h} = y_{c+h} cos_c + y_c sin_c
+ * for c < h = rot/2, channels from rot on as they are (rope NULL: no rotation),
+ * in fp32 with one final rounding to bf16.
+ *
+ * in[0..2] / out[0..2]: queries, keys, values; heads = 0 (both) leaves one
+ * out.  Values are copied (rounded to bf16).  in_f32: the inputs are fp32
+ * (else bf16); outputs are bf16.  Outputs may have any strides, e.g. in
+ * [B][N][H][d] and out [B][H][N][d], what lamp_attn_fwd reads; an output may
+ * be its own input (same pointer, strides and type), not overlap one otherwise.
+ * gain_f32: bit 0, the gain of the queries is fp32 (else bf16), bit 1, that of
+ * the keys.  rope: [npos][rot] fp32, the row of a position holds rot/2 cosines,
+ * then rot/2 sines; rot a positive multiple of 16, at most d.  positions: int32
+ * [B][N], or NULL: token n is at position n.  A token whose position lies
+ * outside the table has NaN in its rotated channels.
+ * Built: d in {64, 128, 256}, B*N up to 2^25.  B = 0 or N = 0 returns LAMP_OK.
+ */
+int lamp_qk_norm_rope(const lamp_rows *in, const lamp_rows *out, int B, int N, int d, int in_f32,
+                      const void *q_gain, const void *k_gain, unsigned gain_f32,
+                      const float *rope, int npos, int rot, const int32_t *positions, double eps, void *stream);
+
+/*
+ * An 8-bit paged cache.  k [pages][Hkv][page][d] and v [pages][Hkv][d][page]
+ * (transposed within the page) hold e4m3 codes, k_scale and v_scale
+ * [pages][Hkv] fp32 powers of two: an element's value is code * scale.  page:
+ * 16, 32, 64, 128 or 256 tokens; d in {64, 128, 256}; 16-byte aligned.
+ */
+typedef struct lamp_cache {
+    uint8_t *k, *v;
+    float *k_scale, *v_scale;
+    int pages, Hkv, page, d;
+} lamp_cache;
+
+/*
+ * A ragged batch of S sequences and T new tokens.  q_start (int32 [S+1],
+ * non-decreasing, from 0 to at most T): sequence s has the new tokens
+ * [q_start[s], q_start[s+1]); NULL: T = S, one token each.  kv_lens (int32
+ * [S]): its keys, the new tokens included, so that token i of its n new ones is
+ * at position kv_lens[s] - n + i.  table (int32 [S][width], rows table_stride
+ * elements apart): table[s][j] is the page of the positions [j*page,
+ * (j+1)*page); entries that no call reads or writes may hold anything.  Tokens
+ * from q_start[S] on belong to no sequence: nothing is written for them.
+ * All DEVICE memory; values that break these rules give wrong results, never an
+ * access outside the arrays.  Built: T up to 2^23, S*Hkv up to 2^22, width*page
+ * up to 2^30, T*Hq up to 2^27.  S = 0 or T = 0 returns LAMP_OK.
+ */
+typedef struct lamp_batch {
+    const int32_t *table;
+    int64_t table_stride;
+    const int32_t *kv_lens, *q_start;
+    int S, T, width;
+} lamp_batch;
+
+/*
+ * lamp_kv_append -- append the batch's new keys and values to the cache; the
+ * keys normed (k_gain, eps) and rotated (rope) on the way, as in
+ * lamp_qk_norm_rope, by their own positions.
+ *
+ * k, v: [T][Hkv][d] bf16 or (in_f32) fp32, strides in elements as in lamp_rows.
+ * For each (page, head) that receives tokens, keys and values apart: let `need`
+ * be the smallest power of two (at least 2^-100) with max |new| <= 448 need.
+ * The scale becomes need if the first new token opens the page, else the larger
+ * of need and the old scale, the codes already there being rescaled (exactly,
+ * but for values that become subnormal, which round to nearest even).  New
+ * elements are rounded once, from fp32 to e4m3, to nearest even.  What is not
+ * finite takes no part in `need` and is stored as NaN, as are the rotated
+ * channels of keys at positions outside the rope table.  Slots behind the new
+ * tokens keep what they hold.
+ *
+ * Tokens whose table entry is missing (outside [0, pages), or beyond width) or
+ * whose position is negative are dropped.  No page may receive tokens of two
+ * sequences in one call.
+ */
+int lamp_kv_append(const void *k, const void *v, int in_f32, int64_t k_token, int64_t k_head, int64_t v_token,
+                   int64_t v_head, const lamp_cache *cache, const lamp_batch *batch, const void *k_gain, int gain_f32,
+                   const float *rope, int npos, int rot, double eps, void *stream);
+
+/*
+ * lamp_attn_cache -- softmax attention of the batch's new tokens over the
+ * cache (their own keys appended first): ragged prompts, chunks and single
+ * tokens in one call.
+ *
+ * q [T][Hq][d] bf16 (strides q_token, q_head); o [T][Hq][d] bf16 and lse
+ * [T][Hq] fp32 (natural log), dense.  Query head h reads kv head h / (Hq/Hkv).
+ * The token at position p sees keys j < kv_lens[s] with j <= p (causal) and
+ * j > p - window (window > 0; requires causal).  Logits are scale * q.k.
+ * Products of bf16 queries and 8-bit keys are exact and summed in fp32; the
+ * softmax is in fp32; probabilities times the values' scale are rounded to
+ * bf16 for the product with the values, which is summed in fp32.
+ * A row that sees no key has o = 0 and lse = -infinity; one that sees a key of
+ * a missing page (or beyond the table) is NaN.  A NaN or an infinity, of a key,
+ * a value or a query, reaches only rows that see it.
+ *
+ * workspace: at least lamp_attn_cache_workspace_size(...) bytes, 256-byte
+ * aligned, or NULL: the library's per-device workspace, as for lamp_attn_fwd.
+ * Results do not depend on its contents and repeat bit for bit.
+ */
+int lamp_attn_cache(const uint16_t *q, int64_t q_token, int64_t q_head, int Hq, const lamp_cache *cache,
+                    const lamp_batch *batch, int causal, int window, double scale, uint16_t *o, float *lse,
+                    void *workspace, size_t workspace_bytes, void *stream);
+
+/* Bytes of workspace lamp_attn_cache needs (0 for sizes it refuses, and where none is needed). */
+size_t lamp_attn_cache_workspace_size(int T, int S, int Hq, int Hkv, int d, int page, int width);
+
+/*
  * lamp_attn_logits8 -- the 8-bit logits alone (Alg. 1, first accumulation;
  * Sec. 4.1 recursive FMA summation rounded to e4m3 after every step).
  * Writes the e4m3 codes of rows [row0, row0 + nrows) of every (b, h):

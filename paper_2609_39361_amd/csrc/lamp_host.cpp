@@ -12,6 +12,7 @@
 #include "lamp.h"
 #include "lamp_decode.h"
 #include "lamp_kernels.h"
+#include "lamp_serve.h"
 
 namespace {
 
@@ -886,6 +887,216 @@ int lamp_get_sim_tables(int device, uint16_t *sim8, uint32_t *sim16)
     if (e == hipSuccess && sim16) e = hipMemcpy(sim16, st->sim16, lamp::SIM16_TABLE * sizeof(uint32_t), hipMemcpyDeviceToHost);
     (void)hipSetDevice(prev);
     if (e != hipSuccess) return fail(LAMP_ERR_HIP, "lamp_get_sim_tables: %s", hipGetErrorString(e));
+    return LAMP_OK;
+}
+
+// --- serving ------------------------------------------------------------------
+
+static bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+// Rows of d channels with 16-byte loads: the pointer and every stride.
+static int check_rows(const char *name, const void *p, bool f32, const int64_t *strides, int n)
+{
+    if (!p) return fail(LAMP_ERR_INVALID_ARG, "null pointer: %s", name);
+    bool ok = aligned16(p);
+    for (int i = 0; i < n; ++i) ok = ok && strides[i] % (f32 ? 4 : 8) == 0;
+    if (!ok) return fail(LAMP_ERR_INVALID_ARG, "%s: rows are not aligned to 16 bytes", name);
+    return LAMP_OK;
+}
+
+static int check_rope(const float *rope, int npos, int rot, int d)
+{
+    if (!rope) return LAMP_OK;
+    if (npos <= 0) return fail(LAMP_ERR_INVALID_ARG, "npos=%d rows of the rope table", npos);
+    if (rot <= 0 || rot % 16 || rot > d)
+        return fail(LAMP_ERR_INVALID_ARG, "rot=%d is not a multiple of 16 up to d=%d", rot, d);
+    if (!aligned16(rope)) return fail(LAMP_ERR_INVALID_ARG, "rope table not aligned to 16 bytes");
+    return LAMP_OK;
+}
+
+static int check_eps(double eps)
+{
+    if (!(eps >= 0.0) || std::isinf(eps)) return fail(LAMP_ERR_INVALID_ARG, "eps must be finite and >= 0");
+    return LAMP_OK;
+}
+
+static int check_d(int d)
+{
+    if (d != 64 && d != 128 && d != 256) return fail(LAMP_ERR_UNSUPPORTED, "head dimension %d not built (64, 128, 256)", d);
+    return LAMP_OK;
+}
+
+int lamp_qk_norm_rope(const lamp_rows *in, const lamp_rows *out, int B, int N, int d, int in_f32, const void *q_gain,
+                      const void *k_gain, unsigned gain_f32, const float *rope, int npos, int rot,
+                      const int32_t *positions, double eps, void *stream)
+{
+    if (!in || !out) return fail(LAMP_ERR_INVALID_ARG, "null pointer: in, out");
+    if (B < 0 || N < 0) return fail(LAMP_ERR_INVALID_ARG, "invalid sizes (B=%d N=%d)", B, N);
+    int rc = check_d(d);
+    if (!rc) rc = check_rope(rope, npos, rot, d);
+    if (!rc) rc = check_eps(eps);
+    if (rc) return rc;
+    if (gain_f32 & ~3u) return fail(LAMP_ERR_INVALID_ARG, "unknown bits in gain_f32 0x%x", gain_f32);
+    if ((q_gain && !aligned16(q_gain)) || (k_gain && !aligned16(k_gain)))
+        return fail(LAMP_ERR_INVALID_ARG, "gains not aligned to 16 bytes");
+    if (B == 0 || N == 0) return LAMP_OK;
+    static const char *const names[3] = {"q", "k", "v"};
+    lamp::NormRopeParams p{};
+    int64_t heads = 0;
+    for (int i = 0; i < 3; ++i) {
+        if (in[i].heads < 0 || in[i].heads != out[i].heads)
+            return fail(LAMP_ERR_INVALID_ARG, "%s: %d heads in, %d out", names[i], in[i].heads, out[i].heads);
+        p.H[i] = in[i].heads;
+        heads += in[i].heads;
+        if (in[i].heads == 0) continue;
+        const int64_t is[3] = {in[i].batch, in[i].token, in[i].head}, os[3] = {out[i].batch, out[i].token, out[i].head};
+        rc = check_rows(names[i], in[i].p, in_f32 != 0, is, 3);
+        if (!rc) rc = check_rows(names[i], out[i].p, false, os, 3);
+        if (rc) return rc;
+        p.in[i] = {in[i].p, in[i].batch, in[i].token, in[i].head};
+        p.out[i] = {static_cast<uint16_t *>(out[i].p), out[i].batch, out[i].token, out[i].head};
+    }
+    if (heads == 0) return LAMP_OK;
+    if (heads > 65536 || (int64_t)B * N > (int64_t)1 << 25)
+        return fail(LAMP_ERR_UNSUPPORTED, "B*N above 2^25 or more than 65536 heads");
+    p.w[0] = q_gain;
+    p.w[1] = k_gain;
+    p.w_f32[0] = (int)(gain_f32 & 1u);
+    p.w_f32[1] = (int)(gain_f32 >> 1 & 1u);
+    p.rope = rope;
+    p.npos = npos;
+    p.rot = rope ? rot : 0;
+    p.positions = positions;
+    p.B = B;
+    p.N = N;
+    p.eps = (float)eps;
+    HIP_TRY(lamp::launch_norm_rope(d, in_f32 != 0, p, static_cast<hipStream_t>(stream)));
+    return LAMP_OK;
+}
+
+// The cache and the batch of a serving call; *b is filled in.
+static int check_paged(const lamp_cache *c, const lamp_batch *n, lamp::PagedBatch *b)
+{
+    if (!c || !n) return fail(LAMP_ERR_INVALID_ARG, "null pointer: cache, batch");
+    int rc = check_d(c->d);
+    if (rc) return rc;
+    int ps = 4;
+    while (ps < 8 && (1 << ps) != c->page) ++ps;
+    if ((1 << ps) != c->page) return fail(LAMP_ERR_UNSUPPORTED, "page of %d tokens not built (16, 32, 64, 128, 256)", c->page);
+    if (c->pages <= 0 || c->Hkv <= 0) return fail(LAMP_ERR_INVALID_ARG, "invalid sizes (pages=%d Hkv=%d)", c->pages, c->Hkv);
+    if (c->Hkv > 65535) return fail(LAMP_ERR_UNSUPPORTED, "Hkv=%d above 65535", c->Hkv);
+    if (!c->k || !c->v || !c->k_scale || !c->v_scale) return fail(LAMP_ERR_INVALID_ARG, "null pointer in the cache");
+    if (!aligned16(c->k) || !aligned16(c->v)) return fail(LAMP_ERR_INVALID_ARG, "cache not aligned to 16 bytes");
+    if (n->S < 0 || n->T < 0 || n->width < 0) return fail(LAMP_ERR_INVALID_ARG, "invalid sizes (S=%d T=%d width=%d)", n->S, n->T, n->width);
+    if (!n->q_start && n->T != n->S) return fail(LAMP_ERR_INVALID_ARG, "without q_start T=%d must equal S=%d", n->T, n->S);
+    if (n->S > 0 && n->T > 0 && ((!n->table && n->width > 0) || !n->kv_lens))
+        return fail(LAMP_ERR_INVALID_ARG, "null pointer in the batch");
+    if (n->T > 1 << 23 || (int64_t)n->S * c->Hkv > 1 << 22 || ((int64_t)n->width << ps) > (int64_t)1 << 30)
+        return fail(LAMP_ERR_UNSUPPORTED, "T above 2^23, S*Hkv above 2^22 or width*page above 2^30");
+    *b = {n->table, n->kv_lens, n->q_start, n->table_stride, n->S, n->T, n->width, c->pages, ps, c->Hkv};
+    return LAMP_OK;
+}
+
+int lamp_kv_append(const void *k, const void *v, int in_f32, int64_t k_token, int64_t k_head, int64_t v_token,
+                   int64_t v_head, const lamp_cache *cache, const lamp_batch *batch, const void *k_gain, int gain_f32,
+                   const float *rope, int npos, int rot, double eps, void *stream)
+{
+    lamp::AppendParams p{};
+    int rc = check_paged(cache, batch, &p.b);
+    if (!rc) rc = check_rope(rope, npos, rot, cache->d);
+    if (!rc) rc = check_eps(eps);
+    if (rc) return rc;
+    if (k_gain && !aligned16(k_gain)) return fail(LAMP_ERR_INVALID_ARG, "gain not aligned to 16 bytes");
+    if (batch->S == 0 || batch->T == 0) return LAMP_OK;
+    const int64_t ks[2] = {k_token, k_head}, vs[2] = {v_token, v_head};
+    rc = check_rows("k", k, in_f32 != 0, ks, 2);
+    if (!rc) rc = check_rows("v", v, in_f32 != 0, vs, 2);
+    if (rc) return rc;
+    p.k = k;
+    p.v = v;
+    p.k_st = k_token;
+    p.k_sh = k_head;
+    p.v_st = v_token;
+    p.v_sh = v_head;
+    p.kc = cache->k;
+    p.vc = cache->v;
+    p.ks = cache->k_scale;
+    p.vs = cache->v_scale;
+    p.w = k_gain;
+    p.w_f32 = gain_f32 != 0;
+    p.rope = rope;
+    p.npos = npos;
+    p.rot = rope ? rot : 0;
+    p.eps = (float)eps;
+    HIP_TRY(lamp::launch_kv_append(cache->d, in_f32 != 0, p, static_cast<hipStream_t>(stream)));
+    return LAMP_OK;
+}
+
+// Workspace of lamp_attn_cache: the partial outputs of split row tiles, none
+// where no sequence can be split.
+static size_t cache_attn_ws(int d, int page, int width)
+{
+    const size_t rows = (size_t)lamp::cache_attn_slots((int64_t)width * page) * lamp::CACHE_ROWS;
+    return align256(rows * d * 4) + align256(rows * 2 * 4);
+}
+
+size_t lamp_attn_cache_workspace_size(int T, int S, int Hq, int Hkv, int d, int page, int width)
+{
+    if (T <= 0 || S <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv || width <= 0) return 0;
+    if ((d != 64 && d != 128 && d != 256) || page < 16 || page > 256 || (page & (page - 1))) return 0;
+    if ((int64_t)width * page > (int64_t)1 << 30) return 0;
+    return cache_attn_ws(d, page, width);
+}
+
+int lamp_attn_cache(const uint16_t *q, int64_t q_token, int64_t q_head, int Hq, const lamp_cache *cache,
+                    const lamp_batch *batch, int causal, int window, double scale, uint16_t *o, float *lse,
+                    void *workspace, size_t workspace_bytes, void *stream)
+{
+    lamp::CacheAttnParams p{};
+    int rc = check_paged(cache, batch, &p.b);
+    if (rc) return rc;
+    if (Hq <= 0 || Hq % cache->Hkv) return fail(LAMP_ERR_INVALID_ARG, "Hq=%d is not a multiple of Hkv=%d", Hq, cache->Hkv);
+    if (causal != 0 && causal != 1) return fail(LAMP_ERR_INVALID_ARG, "causal must be 0 or 1");
+    if (window < 0) return fail(LAMP_ERR_INVALID_ARG, "window must be >= 0");
+    if (window > 0 && !causal) return fail(LAMP_ERR_INVALID_ARG, "a sliding window requires causal=1");
+    if (!std::isfinite(scale)) return fail(LAMP_ERR_INVALID_ARG, "scale must be finite");
+    if ((int64_t)batch->T * Hq > (int64_t)1 << 27 || Hq > 65536)
+        return fail(LAMP_ERR_UNSUPPORTED, "T*Hq above 2^27 or Hq above 65536");
+    if (batch->S == 0 || batch->T == 0) return LAMP_OK;
+    const int64_t qs[2] = {q_token, q_head};
+    rc = check_rows("q", q, false, qs, 2);
+    if (rc) return rc;
+    if (!o || !lse) return fail(LAMP_ERR_INVALID_ARG, "null pointer among o, lse");
+    if (!aligned16(o)) return fail(LAMP_ERR_INVALID_ARG, "o not aligned to 16 bytes");
+    p.q = q;
+    p.q_st = q_token;
+    p.q_sh = q_head;
+    p.kc = cache->k;
+    p.vc = cache->v;
+    p.ks = cache->k_scale;
+    p.vs = cache->v_scale;
+    p.o = o;
+    p.lse = lse;
+    p.Hq = Hq;
+    p.causal = causal;
+    p.window = window < 1 << 30 ? window : 1 << 30;   // (no key lies farther back)
+    p.scale_log2 = (float)(scale * 1.4426950408889634);
+    p.slots = lamp::cache_attn_slots((int64_t)batch->width * cache->page);
+    const size_t need = cache_attn_ws(cache->d, cache->page, batch->width);
+    if (p.slots > 0) {
+        lamp_fwd_extra extra{};
+        extra.workspace = workspace;
+        extra.workspace_bytes = workspace_bytes;
+        int dev = 0;
+        rc = current_device(&dev);
+        if (rc) return rc;
+        void *base = nullptr;
+        rc = call_ws(dev, &extra, need, static_cast<hipStream_t>(stream), &base);
+        if (rc) return rc;
+        p.part = static_cast<float *>(base);
+        p.part_ml = p.part + align256((size_t)p.slots * lamp::CACHE_ROWS * cache->d * 4) / 4;
+    }
+    HIP_TRY(lamp::launch_cache_attn(cache->d, p, static_cast<hipStream_t>(stream)));
     return LAMP_OK;
 }
 

@@ -5,6 +5,8 @@ kernels of the library.  PyTorch provides device memory and the stream.  The
 library must have been built (python -m paper_2609_39361_amd.build); there is
 no fallback path.
 """
+import collections
+import contextlib
 import ctypes
 import math
 import os
@@ -71,6 +73,15 @@ def lib():
         L.lamp_attn_decode.restype = i32
         L.lamp_attn_logits_sim.argtypes = [P, P] + [i32] * 10 + [P, P]
         L.lamp_attn_logits_sim.restype = i32
+        i64 = ctypes.c_int64
+        L.lamp_qk_norm_rope.argtypes = [P, P, i32, i32, i32, i32, P, P, ctypes.c_uint, P, i32, i32, P, f64, P]
+        L.lamp_qk_norm_rope.restype = i32
+        L.lamp_kv_append.argtypes = [P, P, i32, i64, i64, i64, i64, P, P, P, i32, P, i32, i32, f64, P]
+        L.lamp_kv_append.restype = i32
+        L.lamp_attn_cache.argtypes = [P, i64, i64, i32, P, P, i32, i32, f64, P, P, P, sz, P]
+        L.lamp_attn_cache.restype = i32
+        L.lamp_attn_cache_workspace_size.argtypes = [i32] * 7
+        L.lamp_attn_cache_workspace_size.restype = sz
         L.lamp_get_sim_tables.argtypes = [i32, P, P]
         L.lamp_get_sim_tables.restype = i32
         L.lamp_attn_fwd_workspace_size.argtypes = [i32] * 8
@@ -322,6 +333,238 @@ def attn_decode(q, k, v, causal=True, window=0, tk=64, delta=2.0 ** -8, tau=0.5,
     del keep
     _check(rc)
     return o, lse, mask
+
+
+# --- serving: norms with rotation, the 8-bit paged cache, attention over it ----
+
+class Rows(ctypes.Structure):
+    """struct lamp_rows (include/lamp.h)."""
+    _fields_ = [("p", ctypes.c_void_p), ("batch", ctypes.c_int64), ("token", ctypes.c_int64), ("head", ctypes.c_int64),
+                ("heads", ctypes.c_int)]
+
+
+class _Cache(ctypes.Structure):
+    """struct lamp_cache (include/lamp.h)."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("pages", ctypes.c_int), ("Hkv", ctypes.c_int), ("page", ctypes.c_int), ("d", ctypes.c_int)]
+
+
+class _Batch(ctypes.Structure):
+    """struct lamp_batch (include/lamp.h)."""
+    _fields_ = [("table", ctypes.c_void_p), ("table_stride", ctypes.c_int64), ("kv_lens", ctypes.c_void_p),
+                ("q_start", ctypes.c_void_p), ("S", ctypes.c_int), ("T", ctypes.c_int), ("width", ctypes.c_int)]
+
+
+# An 8-bit paged cache: codes k [pages,Hkv,page,d] and v [pages,Hkv,d,page] (float8_e4m3fn, V
+# transposed within its page), scales k_scale and v_scale [pages,Hkv] (fp32 powers of two)
+KVCache = collections.namedtuple("KVCache", "k v k_scale v_scale")
+
+_FLOATS = (torch.bfloat16, torch.float32)
+
+
+def kv_cache(pages, Hkv, d, page=64, device="cuda"):
+    """An empty KVCache of `pages` pages of `page` tokens (zero codes and scales)."""
+    z = dict(device=device)
+    return KVCache(torch.zeros((pages, Hkv, page, d), dtype=torch.uint8, **z).view(torch.float8_e4m3fn),
+                   torch.zeros((pages, Hkv, d, page), dtype=torch.uint8, **z).view(torch.float8_e4m3fn),
+                   torch.zeros((pages, Hkv), dtype=torch.float32, **z), torch.zeros((pages, Hkv), dtype=torch.float32, **z))
+
+
+def rope_table(n, rot, base=1e6, device="cuda"):
+    """The rotation's table of positions 0 .. n-1: fp32 [n, rot], rot/2 cosines then rot/2 sines of
+    position * base^(-2i/rot) (angles in fp64)."""
+    inv = base ** (-torch.arange(0, rot, 2, dtype=torch.float64, device=device) / rot)
+    ang = torch.arange(n, dtype=torch.float64, device=device)[:, None] * inv
+    return torch.cat([ang.cos(), ang.sin()], dim=-1).float()
+
+
+def _on(device):
+    """The device made current, if it is not."""
+    return contextlib.nullcontext() if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+
+
+def _check_tensor(t, name, dtypes, device, shape=None):
+    """A CUDA tensor on `device` of one of `dtypes`, contiguous in its last dimension (`shape`: of that shape, dense)."""
+    if not isinstance(t, torch.Tensor) or t.dtype not in dtypes or t.device != device:
+        raise ValueError("%s must be a %s tensor on %s" % (name, " or ".join(str(x) for x in dtypes), device))
+    if shape is not None and (t.shape != shape or not t.is_contiguous()):
+        raise ValueError("%s must be contiguous, of shape %s" % (name, tuple(shape)))
+    if t.dim() and t.stride(-1) != 1 and t.shape[-1] > 1:
+        raise ValueError("%s must be contiguous in its last dimension" % name)
+
+
+def _strides(t):
+    """Strides in elements; 0 where only one index exists."""
+    return tuple(s if n > 1 else 0 for s, n in zip(t.stride(), t.shape))
+
+
+def _check_norm_rope(dev, d, gains, rope):
+    for name, w in gains:
+        if w is not None:
+            _check_tensor(w, name, _FLOATS, dev, (d,))
+    if rope is not None:
+        _check_tensor(rope, "rope", (torch.float32,), dev)
+        if rope.dim() != 2 or not rope.is_contiguous():
+            raise ValueError("rope must be a contiguous [positions, rot] table")
+    return (None, 0, 0) if rope is None else (rope.data_ptr(), rope.shape[0], rope.shape[1])
+
+
+def qk_norm_rope(q, k=None, v=None, q_weight=None, k_weight=None, rope=None, positions=None, eps=1e-6, out=None):
+    """RMS norm of every query and key head by the gains q_weight / k_weight [d] (None: not normed), then
+    the rotation by `rope` (a table as of rope_table, None: not rotated), in one pass.
+
+    Inputs bf16 or fp32 (all the same), outputs bf16; the last dimension contiguous, rows of 16-byte
+    alignment (slices of a fused projection are fine).  Prompts: q [B,N,Hq,d], k and v [B,N,Hkv,d] give
+    [B,H,N,d], what attn_fwd reads.  Tokens of a serving step: q [T,Hq,d], k and v [T,Hkv,d] give [T,H,d].
+    `positions`: int32 [B,N] or [T]; default 0 .. N-1.  v is laid out (and rounded) with them.  `out`: the
+    tensors to write into (None where the input is None), of the outputs' shapes with any strides; tokens
+    may be written in place.  Returns (q, k, v), None for what was not given."""
+    ins = (q, k, v)
+    if not isinstance(q, torch.Tensor) or q.dim() not in (3, 4) or not q.is_cuda or q.dtype not in _FLOATS:
+        raise ValueError("q must be a bf16 or fp32 CUDA tensor [B,N,Hq,d] or [T,Hq,d]")
+    dev, prompt, d = q.device, q.dim() == 4, q.shape[-1]
+    lead = q.shape[:-2]
+    B, N = lead if prompt else (1, lead[0])
+    for t, name in zip(ins, "qkv"):
+        if t is not None:
+            _check_tensor(t, name, (q.dtype,), dev)
+            if t.dim() != q.dim() or t.shape[:-2] != lead or t.shape[-1] != d:
+                raise ValueError("%s shape %s does not match q %s" % (name, tuple(t.shape), tuple(q.shape)))
+    if k is not None and v is not None and k.shape != v.shape:
+        raise ValueError("v shape %s differs from k %s" % (tuple(v.shape), tuple(k.shape)))
+    table, npos, rot = _check_norm_rope(dev, d, (("q_weight", q_weight), ("k_weight", k_weight)), rope)
+    if positions is not None:
+        _check_tensor(positions, "positions", (torch.int32,), dev, lead)
+    outs = []
+    for i, t in enumerate(ins):
+        o = None if out is None else out[i]
+        shape = None if t is None else ((B, t.shape[2], N, d) if prompt else tuple(t.shape))
+        if (t is None) != (o is None) and out is not None:
+            raise ValueError("out must hold one tensor for each input")
+        if o is not None:
+            _check_tensor(o, "out[%d]" % i, (torch.bfloat16,), dev)
+            if tuple(o.shape) != shape:
+                raise ValueError("out[%d] must be of shape %s" % (i, shape))
+        elif t is not None:
+            o = torch.empty(shape, dtype=torch.bfloat16, device=dev)
+        outs.append(o)
+    if B * N and q.shape[-2]:
+        ri, ro = (Rows * 3)(), (Rows * 3)()
+        for i, (t, o) in enumerate(zip(ins, outs)):
+            if t is not None:
+                st, so = _strides(t), _strides(o)
+                if prompt:
+                    ri[i] = (t.data_ptr(), st[0], st[1], st[2], t.shape[2])
+                    ro[i] = (o.data_ptr(), so[0], so[2], so[1], t.shape[2])
+                else:
+                    ri[i] = (t.data_ptr(), 0, st[0], st[1], t.shape[1])
+                    ro[i] = (o.data_ptr(), 0, so[0], so[1], t.shape[1])
+        f32 = torch.float32
+        with _on(dev):
+            _check(lib().lamp_qk_norm_rope(
+                ri, ro, B, N, d, int(q.dtype == f32), None if q_weight is None else q_weight.data_ptr(),
+                None if k_weight is None else k_weight.data_ptr(),
+                int(q_weight is not None and q_weight.dtype == f32) + 2 * int(k_weight is not None and k_weight.dtype == f32),
+                table, npos, rot, None if positions is None else positions.data_ptr(), float(eps), _stream(dev)))
+    return tuple(outs)
+
+
+def _paged(cache, block_table, kv_lens, q_start, T):
+    """(lamp_cache, lamp_batch) of a call, checked."""
+    kc, vc, ks, vs = cache
+    if not isinstance(kc, torch.Tensor) or kc.dim() != 4 or not kc.is_cuda:
+        raise ValueError("cache.k must be a float8_e4m3fn CUDA tensor [pages,Hkv,page,d]")
+    dev = kc.device
+    pages, Hkv, page, d = kc.shape
+    fp8 = (torch.float8_e4m3fn,)
+    _check_tensor(kc, "cache.k", fp8, dev, kc.shape)
+    _check_tensor(vc, "cache.v", fp8, dev, (pages, Hkv, d, page))
+    _check_tensor(ks, "cache.k_scale", (torch.float32,), dev, (pages, Hkv))
+    _check_tensor(vs, "cache.v_scale", (torch.float32,), dev, (pages, Hkv))
+    i32 = (torch.int32,)
+    _check_tensor(block_table, "block_table", i32, dev)
+    if block_table.dim() != 2:
+        raise ValueError("block_table must be [S, pages of a sequence]")
+    S, width = block_table.shape
+    _check_tensor(kv_lens, "kv_lens", i32, dev, (S,))
+    if q_start is not None:
+        _check_tensor(q_start, "q_start", i32, dev, (S + 1,))
+    elif T != S:
+        raise ValueError("without q_start there is one token for each of the %d sequences, not %d" % (S, T))
+    c = _Cache(kc.data_ptr(), vc.data_ptr(), ks.data_ptr(), vs.data_ptr(), pages, Hkv, page, d)
+    b = _Batch(block_table.data_ptr(), block_table.stride(0), kv_lens.data_ptr(),
+               None if q_start is None else q_start.data_ptr(), S, T, width)
+    return c, b, dev
+
+
+def kv_append(k, v, cache, block_table, kv_lens, q_start=None, k_weight=None, rope=None, eps=1e-6):
+    """Append new keys and values [T,Hkv,d] (bf16 or fp32, token and head strides free) to a KVCache; the
+    keys normed by k_weight and rotated by `rope` on the way (None: not), in fp32 with one rounding to e4m3.
+
+    Sequence s has the tokens q_start[s] .. q_start[s+1]-1 (int32 [S+1]; None: token s alone), its length
+    with them is kv_lens[s] (int32 [S]) and its pages are block_table[s] (int32 [S,width]).  A page's scale
+    is the smallest power of two under which its largest element fits e4m3; when later tokens need a
+    larger one, the codes there are rescaled.  Tokens without a page in the table are dropped.  All of it
+    is read on the device, so that a captured call follows lengths that change.  Returns the cache."""
+    if not isinstance(k, torch.Tensor) or not isinstance(v, torch.Tensor) or k.dim() != 3 or k.shape != v.shape:
+        raise ValueError("k and v [T,Hkv,d] expected")
+    c, b, dev = _paged(cache, block_table, kv_lens, q_start, k.shape[0])
+    _check_tensor(k, "k", _FLOATS, dev)
+    _check_tensor(v, "v", (k.dtype,), dev)
+    if k.shape[1:] != (c.Hkv, c.d):
+        raise ValueError("k of %d heads and d = %d, a cache of %d and %d" % (k.shape[1], k.shape[2], c.Hkv, c.d))
+    table, npos, rot = _check_norm_rope(dev, c.d, (("k_weight", k_weight),), rope)
+    f32 = torch.float32
+    with _on(dev):
+        _check(lib().lamp_kv_append(
+            k.data_ptr(), v.data_ptr(), int(k.dtype == f32), *_strides(k)[:2], *_strides(v)[:2],
+            ctypes.byref(c), ctypes.byref(b), None if k_weight is None else k_weight.data_ptr(),
+            int(k_weight is not None and k_weight.dtype == f32), table, npos, rot, float(eps), _stream(dev)))
+    return cache
+
+
+def attn_cache_workspace_size(T, S, Hq, Hkv, d, page, width):
+    """Bytes of workspace one attn_cache call needs (0: none)."""
+    return int(lib().lamp_attn_cache_workspace_size(T, S, Hq, Hkv, d, page, width))
+
+
+def attn_cache(q, cache, block_table, kv_lens, q_start=None, causal=True, window=0, scale=None, out=None,
+               workspace=None):
+    """Softmax attention of new tokens q [T,Hq,d] (bf16, token and head strides free) over a KVCache that
+    holds their own keys already: (o bf16 [T,Hq,d], lse fp32 [T,Hq]).
+
+    block_table, kv_lens and q_start as for kv_append: prompts, chunks and single tokens of any lengths in
+    one call.  The token at position p sees the sequence's keys j <= p (causal) with j > p - window
+    (window > 0).  `scale` of the logits: default 1/sqrt(d).  A row that sees no key has o = 0 and
+    lse = -inf; tokens behind q_start[S] are left as they are in `out` = (o, lse).  `workspace`: a device
+    tensor of attn_cache_workspace_size(...) bytes; by default one of torch's, on the current stream."""
+    if not isinstance(q, torch.Tensor) or q.dim() != 3:
+        raise ValueError("q [T,Hq,d] expected")
+    T, Hq, d = q.shape
+    c, b, dev = _paged(cache, block_table, kv_lens, q_start, T)
+    _check_tensor(q, "q", (torch.bfloat16,), dev)
+    if d != c.d:
+        raise ValueError("q of d = %d, a cache of %d" % (d, c.d))
+    if out is None:
+        o = torch.empty((T, Hq, d), dtype=torch.bfloat16, device=dev)
+        lse = torch.empty((T, Hq), dtype=torch.float32, device=dev)
+    else:
+        o, lse = out
+        _check_out(o, "o", (T, Hq, d), torch.bfloat16, dev)
+        _check_out(lse, "lse", (T, Hq), torch.float32, dev)
+    L = lib()
+    if workspace is None:
+        need = L.lamp_attn_cache_workspace_size(T, b.S, Hq, c.Hkv, d, c.page, b.width)
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    elif workspace.device != dev or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on the inputs' device")
+    with _on(dev):
+        _check(L.lamp_attn_cache(
+            q.data_ptr(), *_strides(q)[:2], Hq, ctypes.byref(c), ctypes.byref(b), int(causal), int(window),
+            d ** -0.5 if scale is None else float(scale), o.data_ptr(), lse.data_ptr(),
+            None if workspace is None else workspace.data_ptr(),
+            0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(dev)))
+    return o, lse
 
 
 def logits8(q, k, causal=True, window=0, row0=0, nrows=None, sr_seed=None):
