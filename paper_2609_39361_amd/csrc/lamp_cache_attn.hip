@@ -13,165 +13,12 @@
 // is of the unrounded probabilities.
 #include <hip/hip_runtime.h>
 
-#include "lamp_serve.h"
+#include "lamp_cache_plan.h"
 
 namespace lamp {
 namespace {
 
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-
-constexpr float NEG_INF = -__builtin_inff();
-constexpr int TILE = 64;       // keys of the plan's tiles
-constexpr int MIN_TILES = 4;   // least tiles of a piece (one a wave)
-constexpr int TARGET = 512;    // workgroups that fill the 256 CUs (two fit in each one's registers)
-
-// The key range of one sequence is cut in pieces when its row tiles alone do
-// not fill the device: with `total` the key tiles of all (sequence, row tile,
-// kv head) triples, pieces hold about total / TARGET tiles.  Every workgroup
-// works the plan out for itself from the lengths (no planning launch, and a
-// captured graph follows lengths that change).
-struct Unit {
-    int s;           // sequence (-1: none)
-    int tile, head;  // row tile, kv head
-    int piece, pieces;
-    int slot;        // partial output (first piece's slot + piece) where pieces > 1
-};
-
-struct SeqPlan {
-    int a, n;        // first new token, new tokens
-    int all, len;    // keys, and those in the table's reach
-    int pos0;        // position of the first new token
-    int tiles;       // row tiles
-    int kt;          // key tiles that a row tile visits at most
-};
-
-__device__ __forceinline__ SeqPlan seq_plan(const CacheAttnParams &p, int s, int G)
-{
-    SeqPlan r;
-    r.a = p.b.q_start ? p.b.q_start[s] : s;
-    const int e = p.b.q_start ? p.b.q_start[s + 1] : s + 1;
-    const int len = p.b.kv_lens[s] > 0 ? p.b.kv_lens[s] : 0;
-    r.n = r.a >= 0 && e <= p.b.T && e > r.a ? e - r.a : 0;
-    r.pos0 = len - r.n;
-    const int64_t reach = (int64_t)p.b.width << p.b.page_shift;
-    r.all = len;
-    r.len = len < reach ? len : (int)reach;
-    r.tiles = (int)(((int64_t)r.n * G + CACHE_ROWS - 1) / CACHE_ROWS);
-    r.kt = (r.len + TILE - 1) / TILE;
-    if (p.window > 0) {
-        const int64_t span = ((int64_t)p.window + CACHE_ROWS - 1 + TILE - 1) / TILE + 1;
-        if (span < r.kt) r.kt = (int)span;
-    }
-    return r;
-}
-
-__device__ __forceinline__ int64_t wave_sum(int64_t v)
-{
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) v += __shfl_xor(v, m, 64);
-    return v;
-}
-
-// Tiles of a piece, from the lengths of every sequence (by one wave).
-__device__ int piece_tiles(const CacheAttnParams &p, int G)
-{
-    int64_t total = 0;
-    for (int s = threadIdx.x & 63; s < p.b.S; s += 64) {
-        const SeqPlan r = seq_plan(p, s, G);
-        total += (int64_t)r.tiles * r.kt;
-    }
-    total = wave_sum(total) * p.b.Hkv;
-    const int64_t c = (total + TARGET - 1) / TARGET;
-    return (int)(c < MIN_TILES ? MIN_TILES : (c < 1 << 24 ? c : 1 << 24));
-}
-
-// Unit x of the plan; with `joined`, unit x among the (row tile, kv head) pairs
-// of split sequences instead (piece 0, slot of the first piece).
-__device__ Unit find_unit(const CacheAttnParams &p, int G, int64_t x, bool joined)
-{
-    const int lane = threadIdx.x & 63;
-    const int chunk = piece_tiles(p, G);
-    int64_t units = 0, slots = 0;   // of the sequences before this round of 64
-    for (int s0 = 0; s0 < p.b.S; s0 += 64) {
-        const int s = s0 + lane;
-        int64_t pairs = 0;
-        int c = 1;
-        if (s < p.b.S) {
-            const SeqPlan r = seq_plan(p, s, G);
-            pairs = (int64_t)r.tiles * p.b.Hkv;
-            c = (r.kt + chunk - 1) / chunk;
-            c = c < 1 ? 1 : c;
-        }
-        const int64_t u = joined ? (c > 1 ? pairs : 0) : pairs * c, sl = c > 1 ? pairs * c : 0;
-        int64_t ui = u, si = sl;   // inclusive prefix sums
-#pragma unroll
-        for (int m = 1; m < 64; m <<= 1) {
-            const int64_t a = __shfl_up(ui, m, 64), b = __shfl_up(si, m, 64);
-            if (lane >= m) ui += a, si += b;
-        }
-        const uint64_t hit = __ballot(x < units + ui);
-        if (hit) {
-            const int l = __builtin_ctzll(hit);   // the first sequence that ends behind x
-            const int64_t local = x - (units + __shfl(ui - u, l, 64));
-            const int64_t slot0 = slots + __shfl(si - sl, l, 64);
-            const int cs = __shfl(c, l, 64);
-            Unit r;
-            r.s = s0 + l;
-            r.pieces = cs;
-            r.piece = joined ? 0 : (int)(local % cs);
-            const int64_t pair = joined ? local : local / cs;
-            r.head = (int)(pair % p.b.Hkv);
-            r.tile = (int)(pair / p.b.Hkv);
-            const int64_t slot = slot0 + pair * cs + r.piece;
-            if (cs > 1 && slot + (joined ? cs : 1) > p.slots) break;   // (lengths that break the contract)
-            r.slot = (int)slot;
-            return r;
-        }
-        units += __shfl(ui, 63, 64);
-        slots += __shfl(si, 63, 64);
-    }
-    return {-1, 0, 0, 0, 0, 0};
-}
-
-__device__ __forceinline__ uint32_t pack2(float a, float b)
-{
-    bf16x2 v;
-    v[0] = (__bf16)a;
-    v[1] = (__bf16)b;
-    return __builtin_bit_cast(uint32_t, v);
-}
-
-// 8 codes as bf16 (exact).
-__device__ __forceinline__ bf16x8 widen(uint32_t lo, uint32_t hi)
-{
-    u32x4 r;
-    r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false));
-    r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true));
-    r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false));
-    r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true));
-    return __builtin_bit_cast(bf16x8, r);
-}
-
-// The high bit of each byte that holds the NaN code (0x7F or 0xFF).
-__device__ __forceinline__ uint32_t nan_bytes(uint32_t c)
-{
-    return ((c & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
-}
-
-// Bytes of a word of 4 keys from `k` that lie in [lo, hi).
-__device__ __forceinline__ uint32_t byte_mask(int k, int lo, int hi)
-{
-    const int a = lo - k, e = hi - k;
-    const uint32_t below = e >= 4 ? ~0u : (e <= 0 ? 0u : (1u << (8 * e)) - 1u);
-    const uint32_t from = a <= 0 ? ~0u : (a >= 4 ? 0u : ~0u << (8 * a));
-    return below & from;
-}
-
-// One unit: CACHE_ROWS query rows (row = token * G + head of the group) of one
+// One unit: FewRows::ROWS query rows (row = token * G + head of the group) of one
 // sequence and kv head against one piece of its keys; the 4 waves take key
 // tiles of KT in turn, each with its own m, l and o, and join them at the end.
 //
@@ -195,25 +42,26 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(CacheAttnParams p)
     constexpr int OS = D + 4;          // row stride of the joining buffer
     __shared__ float obuf[4 * 16 * OS];
     __shared__ float ml[4 * 16 * 2];
+    __shared__ uint32_t marks[FewRows::ROWS][D / 32];   // rows and channels that see NaN values (mark_nan)
 
     const int G = p.Hq / p.b.Hkv;
-    const Unit u = find_unit(p, G, blockIdx.x, false);
+    const Unit u = find_unit<FewRows>(p, G, blockIdx.x, false);
     if (u.s < 0) return;
-    const SeqPlan sq = seq_plan(p, u.s, G);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
+    const SeqPlan sq = seq_plan<FewRows>(p, u.s, G);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
+    if (threadIdx.x < FewRows::ROWS * (D / 32)) marks[0][threadIdx.x] = 0;
+    __syncthreads();
     const int rows = sq.n * G;
-    const int r0 = u.tile * CACHE_ROWS, rlast = (r0 + CACHE_ROWS < rows ? r0 + CACHE_ROWS : rows) - 1;
+    const int r0 = u.tile * FewRows::ROWS, rlast = (r0 + FewRows::ROWS < rows ? r0 + FewRows::ROWS : rows) - 1;
     const int row = r0 + n < rows ? r0 + n : rlast;   // (missing rows repeat the last, and are not written)
     const int tok = row / G, qh = u.head * G + row - tok * G;
     const int pos = sq.pos0 + tok;                    // may be negative: sees nothing
     const int pmin = sq.pos0 + r0 / G, pmax = sq.pos0 + rlast / G;
-    // keys that this row sees, that some row sees, that every row sees
-    const int hi = p.causal ? (pos + 1 < sq.len ? pos + 1 : sq.len) : sq.len;
-    const int lo = p.window > 0 && pos - p.window + 1 > 0 ? pos - p.window + 1 : 0;
-    const int hi_any = p.causal ? (pmax + 1 < sq.len ? pmax + 1 : sq.len) : sq.len;
-    const int lo_any = p.window > 0 && pmin - p.window + 1 > 0 ? pmin - p.window + 1 : 0;
-    const int hi_all = p.causal ? (pmin + 1 < sq.len ? pmin + 1 : sq.len) : sq.len;
-    const int lo_all = p.window > 0 && pmax - p.window + 1 > 0 ? pmax - p.window + 1 : 0;
+    // keys that a position sees: this row's, those that some row sees, that every row sees
+    auto upto = [&](int x) { return p.causal ? (x + 1 < sq.len ? x + 1 : sq.len) : sq.len; };
+    auto from = [&](int x) { return p.window > 0 && x - p.window + 1 > 0 ? x - p.window + 1 : 0; };
+    const int hi = upto(pos), lo = from(pos);
+    const int hi_any = upto(pmax), lo_any = from(pmin), hi_all = upto(pmin), lo_all = from(pmax);
     const int t0 = lo_any / KT, t1 = hi_any > lo_any ? (hi_any + KT - 1) / KT : t0;
     const int beg = t0 + (int)((int64_t)(t1 - t0) * u.piece / u.pieces);
     const int end = t0 + (int)((int64_t)(t1 - t0) * (u.piece + 1) / u.pieces);
@@ -348,9 +196,8 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(CacheAttnParams p)
         }
         if (partial) {
             // Values that no row sees (behind the sequence's end, before the
-            // window, of a missing page) are whatever memory holds: zero them,
-            // as 0 * NaN is NaN.  Values that some rows see may hold NaN for
-            // the others: those are zeroed too and counted by row and channel.
+            // window, of a missing page) are whatever memory holds: zeroed, as
+            // 0 * NaN is NaN; NaN that some rows see is marked.
             uint32_t some = 0;
 #pragma unroll
             for (int w = 0; w < VW; ++w) {
@@ -361,35 +208,18 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(CacheAttnParams p)
                     some |= nan_bytes(vreg[i][w]);
                 }
             }
-            if (__ballot(some != 0)) {
-                bf16x8 vis[KPL / 8];
+            if (some) {
 #pragma unroll
-                for (int k = 0; k < KPL / 8; ++k) {
-                    u32x4 w;
+                for (int i = 0; i < DT; ++i)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int key = key0 + 8 * k + 2 * e;
-                        w[e] = (key >= lo && key < hi ? 0x3F80u : 0u) | (key + 1 >= lo && key + 1 < hi ? 0x3F800000u : 0u);
+                    for (int w = 0; w < VW; ++w) {
+                        const uint32_t nan = nan_bytes(vreg[i][w]);
+                        mark_nan<D>(marks, nan, 16 * i + n, key0 + 4 * w, rlast + 1 - r0, [&](int r, int key) {
+                            const int rp = sq.pos0 + (r0 + r) / G;
+                            return key >= from(rp) && key < upto(rp);
+                        });
+                        vreg[i][w] &= ~((nan >> 7) * 0xFFu);
                     }
-                    vis[k] = __builtin_bit_cast(bf16x8, w);
-                }
-#pragma unroll
-                for (int i = 0; i < DT; ++i) {
-                    f32x4 count = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                    for (int k = 0; k < KPL / 8; ++k) {
-                        uint32_t one[2];
-#pragma unroll
-                        for (int w = 0; w < 2; ++w) {
-                            const uint32_t b = nan_bytes(vreg[i][2 * k + w]);
-                            one[w] = (b >> 7) * 0x38u;   // e4m3 1.0 where NaN
-                            vreg[i][2 * k + w] &= ~((b >> 7) * 0xFFu);
-                        }
-                        count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(one[0], one[1]), vis[k], count, 0, 0, 0);
-                    }
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) o[i][e] = count[e] > 0.0f ? __builtin_nanf("") : o[i][e];
-                }
             }
         }
 #pragma unroll
@@ -430,8 +260,11 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(CacheAttnParams p)
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] += ow[e] * f;
         }
+        const uint32_t nan = marks[r][d >> 5] >> (d & 31);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = nan >> e & 1u ? __builtin_nanf("") : v[e];
         if (u.pieces > 1) {
-            const int64_t at_row = (int64_t)u.slot * CACHE_ROWS + r;
+            const int64_t at_row = (int64_t)u.slot * FewRows::ROWS + r;
             *reinterpret_cast<f32x4 *>(p.part + at_row * D + d) = v;
             if (d == 0) {
                 p.part_ml[at_row * 2] = mx;
@@ -442,86 +275,164 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(CacheAttnParams p)
             const int64_t orow = (int64_t)(sq.a + i) * p.Hq + u.head * G + gr - i * G;
             const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
             *reinterpret_cast<u32x2 *>(p.o + orow * D + d) = u32x2{pack2(v[0] * inv, v[1] * inv), pack2(v[2] * inv, v[3] * inv)};
-            if (d == 0) p.lse[orow] = sum == 0.0f ? NEG_INF : (mx + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+            if (d == 0) p.lse[orow] = sum == 0.0f ? NEG_INF : (mx + __builtin_amdgcn_logf(sum)) * LN2;
         }
     }
 }
 
-// The pieces of one row tile and kv head joined; 4 rows to a workgroup, one a
-// wave, whose lanes hold D/64 channels each.
-template <int D>
+// The pieces of the rows of a split (row tile, kv head) joined: a workgroup
+// takes a row, its waves the pieces in turn (BY = 256: few rows of many
+// pieces), or 16 rows, a wave 4 of them one after another (BY = 64: many rows
+// of few pieces).  A lane holds D/64 channels.
+template <class F, int D, int BY>
 __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnParams p)
 {
-    constexpr int C = D / 64;
+    constexpr int C = D / 64, W = BY / 64, ROWS = W > 1 ? 1 : 4;
+    __shared__ float obuf[W > 1 ? 4 * D : 1], lbuf[4];
     const int G = p.Hq / p.b.Hkv;
-    const Unit u = find_unit(p, G, blockIdx.x, true);
+    const Unit u = find_unit<F>(p, G, blockIdx.x, true);
     if (u.s < 0) return;
-    const SeqPlan sq = seq_plan(p, u.s, G);
-    const int lane = threadIdx.x & 63, r = (int)blockIdx.y * 4 + (threadIdx.x >> 6), gr = u.tile * CACHE_ROWS + r;
-    if (gr >= sq.n * G) return;
-    const int64_t base = (int64_t)u.slot * CACHE_ROWS + r;
-    float mx = NEG_INF;
-    for (int c = lane; c < u.pieces; c += 64) mx = fmaxf(mx, p.part_ml[(base + (int64_t)c * CACHE_ROWS) * 2]);
+    const SeqPlan sq = seq_plan<F>(p, u.s, G);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    for (int k = 0; k < ROWS; ++k) {
+        const int r = W > 1 ? (int)blockIdx.y : (int)blockIdx.y * 16 + wave * 4 + k, gr = u.tile * F::ROWS + r;
+        if (gr >= sq.n * G) return;   // (the whole workgroup where it shares a row)
+        const int64_t base = (int64_t)u.slot * F::ROWS + r;
+        float mx = NEG_INF;
+        for (int c = lane; c < u.pieces; c += 64) mx = fmaxf(mx, p.part_ml[(base + (int64_t)c * F::ROWS) * 2]);
 #pragma unroll
-    for (int k = 1; k < 64; k <<= 1) mx = fmaxf(mx, __shfl_xor(mx, k, 64));
-    const float ms = mx == NEG_INF ? 0.0f : mx;
-    float sum = 0.0f, v[C] = {};
-    for (int c = 0; c < u.pieces; ++c) {
-        const int64_t at = base + (int64_t)c * CACHE_ROWS;
-        const float f = __builtin_amdgcn_exp2f(p.part_ml[at * 2] - ms);
-        sum += p.part_ml[at * 2 + 1] * f;
+        for (int x = 1; x < 64; x <<= 1) mx = fmaxf(mx, __shfl_xor(mx, x, 64));
+        const float ms = mx == NEG_INF ? 0.0f : mx;
+        float sum = 0.0f, v[C] = {};
+        // rounds of 16 pieces of the wave, whose weights 16 lanes work out
+        for (int c0 = W > 1 ? wave : 0; c0 < u.pieces; c0 += 16 * W) {
+            const int c = c0 + (lane & 15) * W;
+            const int64_t at = (base + (int64_t)(c < u.pieces ? c : 0) * F::ROWS) * 2;
+            const float f = c < u.pieces ? __builtin_amdgcn_exp2f(p.part_ml[at] - ms) : 0.0f;
+            const float fl = c < u.pieces ? p.part_ml[at + 1] * f : 0.0f;
 #pragma unroll
-        for (int k = 0; k < C; ++k) v[k] += p.part[at * D + 64 * k + lane] * f;
+            for (int j = 0; j < 16; ++j) {
+                if (c0 + j * W < u.pieces) {
+                    const float *o = p.part + (base + (int64_t)(c0 + j * W) * F::ROWS) * D + C * lane;
+                    const float fj = __shfl(f, j, 64);
+                    sum += __shfl(fl, j, 64);
+#pragma unroll
+                    for (int e = 0; e < C; ++e) v[e] += o[e] * fj;
+                }
+            }
+        }
+        if constexpr (W > 1) {
+#pragma unroll
+            for (int e = 0; e < C; ++e) obuf[wave * D + C * lane + e] = v[e];
+            if (lane == 0) lbuf[wave] = sum;
+            __syncthreads();
+            if (wave != 0) return;
+            sum = lbuf[0] + lbuf[1] + lbuf[2] + lbuf[3];
+#pragma unroll
+            for (int e = 0; e < C; ++e) {
+                const int d = C * lane + e;
+                v[e] = obuf[d] + obuf[D + d] + obuf[2 * D + d] + obuf[3 * D + d];
+            }
+        }
+        const int i = gr / G;
+        const int64_t orow = (int64_t)(sq.a + i) * p.Hq + u.head * G + gr - i * G;
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        uint16_t *o = p.o + orow * D + C * lane;
+        if constexpr (C == 1) {
+            *o = (uint16_t)pack2(v[0] * inv, 0.0f);
+        } else {
+#pragma unroll
+            for (int e = 0; e < C; e += 2) *reinterpret_cast<uint32_t *>(o + e) = pack2(v[e] * inv, v[e + 1] * inv);
+        }
+        if (lane == 0) p.lse[orow] = sum == 0.0f ? NEG_INF : (mx + __builtin_amdgcn_logf(sum)) * LN2;
     }
-    const int i = gr / G;
-    const int64_t orow = (int64_t)(sq.a + i) * p.Hq + u.head * G + gr - i * G;
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-#pragma unroll
-    for (int k = 0; k < C; ++k) {
-        const uint32_t b = pack2(v[k] * inv, 0.0f);
-        p.o[orow * D + 64 * k + lane] = (uint16_t)b;
-    }
-    if (lane == 0) p.lse[orow] = sum == 0.0f ? NEG_INF : (mx + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
 }
 
-// Row tiles times kv heads that the batch can have at most.
-int64_t max_pairs(const CacheAttnParams &p)
+template <class F>
+unsigned join_pairs(const CacheAttnParams &p)
 {
-    const int G = p.Hq / p.b.Hkv;
-    return ((int64_t)p.b.T * G / CACHE_ROWS + p.b.S) * p.b.Hkv;
+    const int64_t pairs = max_pairs<F>(p);
+    return (unsigned)(pairs < F::TARGET ? pairs : F::TARGET);
 }
 
-// A sequence of kt key tiles and `pairs` row tiles times heads is cut in
-// c = ceil(kt / chunk) < 1 + kt / chunk pieces, and sum(pairs kt) / chunk <=
-// TARGET: below max_pairs + TARGET units in all.
 template <int D, int KT>
-hipError_t launch(const CacheAttnParams &p, hipStream_t s)
+hipError_t launch_few(const CacheAttnParams &p, hipStream_t s)
 {
-    const int64_t pairs = max_pairs(p);
-    cache_attn_kernel<D, KT><<<dim3((unsigned)(p.slots ? pairs + TARGET : pairs)), 256, 0, s>>>(p);
-    if (p.slots) {
-        const dim3 grid((unsigned)(pairs < TARGET ? pairs : TARGET), CACHE_ROWS / 4);
-        cache_join_kernel<D><<<grid, 256, 0, s>>>(p);
-    }
+    cache_attn_kernel<D, KT><<<dim3((unsigned)max_units<FewRows>(p)), 256, 0, s>>>(p);
+    if (p.slots) cache_join_kernel<FewRows, D, 256><<<dim3(join_pairs<FewRows>(p), FewRows::ROWS), 256, 0, s>>>(p);
     return hipGetLastError();
 }
 
-} // namespace
-
-// Where c >= 2, c < 2 kt / chunk: below 2 TARGET partial outputs, of below
-// TARGET row tiles times heads.  Sequences of one piece need none.
-int cache_attn_slots(int64_t keys)
+template <int D>
+hipError_t launch_many(const CacheAttnParams &p, hipStream_t s)
 {
-    return (keys + TILE - 1) / TILE > MIN_TILES ? 2 * TARGET : 0;
+    const hipError_t e = launch_cache_prompt(D, p, s);
+    if (e != hipSuccess) return e;
+    if (p.slots) cache_join_kernel<ManyRows, D, 64><<<dim3(join_pairs<ManyRows>(p), ManyRows::ROWS / 16), 256, 0, s>>>(p);
+    return hipGetLastError();
 }
 
-hipError_t launch_cache_attn(int D, const CacheAttnParams &p, hipStream_t s)
+// Partial outputs of form F.
+template <class F>
+int slots_of(int64_t T, int64_t S, int G, int Hkv, int64_t keys)
 {
-    switch (D) {
-    case 64: return launch<64, 64>(p, s);
-    case 128: return launch<128, 64>(p, s);
-    default: return launch<256, 32>(p, s);
+    if ((keys + TILE - 1) / TILE <= F::MIN_TILES) return 0;
+    const int64_t units = (T * G / F::ROWS + S) * Hkv + F::TARGET;
+    return (int)(units < 2 * F::TARGET ? units : 2 * F::TARGET);
+}
+
+// Sequences of at most this many rows take the form for few rows.
+constexpr int FEW = 64;
+
+struct Choice {
+    bool few, many;
+    int64_t limit;   // rows up to which a sequence is among the few
+};
+
+// From what the host knows: no sequence has more than T G rows, and they have
+// T G / S on average.  Either form is right for any sequence.
+Choice choose(int64_t T, int64_t S, int G)
+{
+    if (T * G <= FEW || T * G <= FewRows::ROWS * S) return {true, false, T * G};
+    if (S == 1) return {false, true, 0};
+    return {true, true, FEW};
+}
+
+size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+} // namespace
+
+size_t cache_attn_workspace(int D, int64_t T, int64_t S, int G, int Hkv, int64_t keys)
+{
+    const Choice c = choose(T, S, G);
+    const size_t few = c.few ? (size_t)slots_of<FewRows>(T, S, G, Hkv, keys) * FewRows::ROWS : 0;
+    const size_t many = c.many ? (size_t)slots_of<ManyRows>(T, S, G, Hkv, keys) * ManyRows::ROWS : 0;
+    const size_t rows = few > many ? few : many;   // (one form after the other)
+    return align256(rows * D * 4) + align256(rows * 2 * 4);
+}
+
+hipError_t launch_cache_attn(int D, const CacheAttnParams &params, hipStream_t s)
+{
+    CacheAttnParams p = params;
+    const int64_t T = p.b.T, S = p.b.S, keys = (int64_t)p.b.width << p.b.page_shift;
+    const int G = p.Hq / p.b.Hkv;
+    const Choice c = choose(T, S, G);
+    if (c.many) {
+        p.rows_above = c.limit;
+        p.rows_upto = T * G;
+        p.slots = slots_of<ManyRows>(T, S, G, p.b.Hkv, keys);
+        p.part_ml = p.part + align256((size_t)p.slots * ManyRows::ROWS * D * 4) / 4;
+        const hipError_t e = D == 64 ? launch_many<64>(p, s) : (D == 128 ? launch_many<128>(p, s) : launch_many<256>(p, s));
+        if (e != hipSuccess) return e;
     }
+    if (c.few) {
+        p.rows_above = 0;
+        p.rows_upto = c.limit;
+        p.slots = slots_of<FewRows>(T, S, G, p.b.Hkv, keys);
+        p.part_ml = p.part + align256((size_t)p.slots * FewRows::ROWS * D * 4) / 4;
+        return D == 64 ? launch_few<64, 64>(p, s) : (D == 128 ? launch_few<128, 64>(p, s) : launch_few<256, 32>(p, s));
+    }
+    return hipSuccess;
 }
 
 } // namespace lamp

@@ -1032,20 +1032,13 @@ int lamp_kv_append(const void *k, const void *v, int in_f32, int64_t k_token, in
     return LAMP_OK;
 }
 
-// Workspace of lamp_attn_cache: the partial outputs of split row tiles, none
-// where no sequence can be split.
-static size_t cache_attn_ws(int d, int page, int width)
-{
-    const size_t rows = (size_t)lamp::cache_attn_slots((int64_t)width * page) * lamp::CACHE_ROWS;
-    return align256(rows * d * 4) + align256(rows * 2 * 4);
-}
-
 size_t lamp_attn_cache_workspace_size(int T, int S, int Hq, int Hkv, int d, int page, int width)
 {
     if (T <= 0 || S <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv || width <= 0) return 0;
     if ((d != 64 && d != 128 && d != 256) || page < 16 || page > 256 || (page & (page - 1))) return 0;
     if ((int64_t)width * page > (int64_t)1 << 30) return 0;
-    return cache_attn_ws(d, page, width);
+    if (T > 1 << 23 || (int64_t)S * Hkv > 1 << 22 || (int64_t)T * Hq > (int64_t)1 << 27) return 0;
+    return lamp::cache_attn_workspace(d, T, S, Hq / Hkv, Hkv, (int64_t)width * page);
 }
 
 int lamp_attn_cache(const uint16_t *q, int64_t q_token, int64_t q_head, int Hq, const lamp_cache *cache,
@@ -1081,9 +1074,9 @@ int lamp_attn_cache(const uint16_t *q, int64_t q_token, int64_t q_head, int Hq, 
     p.causal = causal;
     p.window = window < 1 << 30 ? window : 1 << 30;   // (no key lies farther back)
     p.scale_log2 = (float)(scale * 1.4426950408889634);
-    p.slots = lamp::cache_attn_slots((int64_t)batch->width * cache->page);
-    const size_t need = cache_attn_ws(cache->d, cache->page, batch->width);
-    if (p.slots > 0) {
+    const size_t need = lamp::cache_attn_workspace(cache->d, batch->T, batch->S, Hq / cache->Hkv, cache->Hkv,
+                                                   (int64_t)batch->width * cache->page);
+    if (need > 0) {
         lamp_fwd_extra extra{};
         extra.workspace = workspace;
         extra.workspace_bytes = workspace_bytes;
@@ -1094,7 +1087,6 @@ int lamp_attn_cache(const uint16_t *q, int64_t q_token, int64_t q_head, int Hq, 
         rc = call_ws(dev, &extra, need, static_cast<hipStream_t>(stream), &base);
         if (rc) return rc;
         p.part = static_cast<float *>(base);
-        p.part_ml = p.part + align256((size_t)p.slots * lamp::CACHE_ROWS * cache->d * 4) / 4;
     }
     HIP_TRY(lamp::launch_cache_attn(cache->d, p, static_cast<hipStream_t>(stream)));
     return LAMP_OK;

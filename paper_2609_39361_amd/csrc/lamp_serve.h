@@ -70,18 +70,19 @@ struct CacheAttnParams {
     const float *ks, *vs;
     uint16_t *o;              // [T][Hq][D] bf16
     float *lse;               // [T][Hq]
-    float *part;              // partial outputs of split row tiles: [slots][rows][D] (workspace)
-    float *part_ml;           // their running maxima and sums [slots][rows][2]
+    float *part;              // partial outputs of split row tiles: [slots][rows of a tile][D] (workspace)
+    float *part_ml;           // their running maxima and sums [slots][rows of a tile][2]
     int Hq, causal, window;
     float scale_log2;         // logit scale times log2(e)
+    int64_t rows_above, rows_upto;   // the launch takes the sequences with this many rows (new tokens times heads of a group)
     int slots;                // partial outputs that the workspace holds
 };
 
-// Query rows of one workgroup of the split form.
-constexpr int CACHE_ROWS = 16;
-
-// Partial outputs that a call over sequences of at most `keys` keys may need.
-int cache_attn_slots(int64_t keys);
+// Bytes of workspace a call over sequences of at most `keys` keys needs.
+size_t cache_attn_workspace(int D, int64_t T, int64_t S, int G, int Hkv, int64_t keys);
+// p.part: that workspace (null where it needs none).
 hipError_t launch_cache_attn(int D, const CacheAttnParams &p, hipStream_t s);
+// The form for many rows a sequence (lamp_cache_prompt.hip), of launch_cache_attn.
+hipError_t launch_cache_prompt(int D, const CacheAttnParams &p, hipStream_t s);
 
 } // namespace lamp
