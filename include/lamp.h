@@ -352,7 +352,8 @@ int lamp_attn_decode(const uint16_t *q, const uint16_t *k, const uint16_t *v,
  *
  * lamp_rows: rows of d channels (contiguous, 16-byte aligned) of B x N tokens
  * and `heads` heads, element (b, n, h, c) at p + b*batch + n*token + h*head + c
- * (strides in elements; multiples of 8 for bf16, of 4 for fp32).
+ * (strides in elements; those of more than one index multiples of 8 for bf16,
+ * of 4 for fp32).
  */
 typedef struct lamp_rows {
     void *p;

@@ -13,320 +13,76 @@
 // is of the unrounded probabilities.
 #include <hip/hip_runtime.h>
 
-#include "lamp_cache_plan.h"
+#include "lamp_cache_few.h"
 
 namespace lamp {
 namespace {
 
-// One unit: FewRows::ROWS query rows (row = token * G + head of the group) of one
-// sequence and kv head against one piece of its keys; the 4 waves take key
-// tiles of KT in turn, each with its own m, l and o, and join them at the end.
-//
-// The transposed products S^T = K Q^T and O^T = V^T P^T (16x16x32) leave a
-// lane (row n = lane % 16, g = lane / 16) with the logits of the KT/4
-// consecutive keys from g KT/4, which is what it then holds as P^T's operand:
-// P moves through no LDS.  For that, row m of the K operand t is key
-// (m / 4) KT/4 + 4 t + m % 4, and both products take their summed axis in the
-// order that makes a lane's bytes contiguous: K's channels g D/4 .. of a key,
-// V's KT/4 keys of a channel (V is stored transposed within its page).  Codes
-// go from global memory straight to registers in 16-byte loads; the next
-// tile's are requested as soon as this tile's have been used.
 template <int D, int KT>
-__global__ __launch_bounds__(256) void cache_attn_kernel(CacheAttnParams p)
+__global__ __launch_bounds__(256) void cache_few_kernel(CacheAttnParams p)
 {
-    constexpr int NT = KT / 16;        // K operands of a tile
-    constexpr int KPL = KT / 4;        // keys of a lane
-    constexpr int KW = D / 16;         // words of a lane's channels of one key
-    constexpr int VW = KPL / 4;        // words of a lane's keys of one channel
-    constexpr int DT = D / 16;         // 16-channel tiles of o
-    constexpr int OS = D + 4;          // row stride of the joining buffer
-    __shared__ float obuf[4 * 16 * OS];
-    __shared__ float ml[4 * 16 * 2];
-    __shared__ uint32_t marks[FewRows::ROWS][D / 32];   // rows and channels that see NaN values (mark_nan)
-
-    const int G = p.Hq / p.b.Hkv;
-    const Unit u = find_unit<FewRows>(p, G, blockIdx.x, false);
-    if (u.s < 0) return;
-    const SeqPlan sq = seq_plan<FewRows>(p, u.s, G);
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
-    if (threadIdx.x < FewRows::ROWS * (D / 32)) marks[0][threadIdx.x] = 0;
-    __syncthreads();
-    const int rows = sq.n * G;
-    const int r0 = u.tile * FewRows::ROWS, rlast = (r0 + FewRows::ROWS < rows ? r0 + FewRows::ROWS : rows) - 1;
-    const int row = r0 + n < rows ? r0 + n : rlast;   // (missing rows repeat the last, and are not written)
-    const int tok = row / G, qh = u.head * G + row - tok * G;
-    const int pos = sq.pos0 + tok;                    // may be negative: sees nothing
-    const int pmin = sq.pos0 + r0 / G, pmax = sq.pos0 + rlast / G;
-    // keys that a position sees: this row's, those that some row sees, that every row sees
-    auto upto = [&](int x) { return p.causal ? (x + 1 < sq.len ? x + 1 : sq.len) : sq.len; };
-    auto from = [&](int x) { return p.window > 0 && x - p.window + 1 > 0 ? x - p.window + 1 : 0; };
-    const int hi = upto(pos), lo = from(pos);
-    const int hi_any = upto(pmax), lo_any = from(pmin), hi_all = upto(pmin), lo_all = from(pmax);
-    const int t0 = lo_any / KT, t1 = hi_any > lo_any ? (hi_any + KT - 1) / KT : t0;
-    const int beg = t0 + (int)((int64_t)(t1 - t0) * u.piece / u.pieces);
-    const int end = t0 + (int)((int64_t)(t1 - t0) * (u.piece + 1) / u.pieces);
-
-    bf16x8 qf[D / 32];
-    {
-        const uint16_t *q = p.q + (int64_t)(sq.a + tok) * p.q_st + (int64_t)qh * p.q_sh + g * (D / 4);
-#pragma unroll
-        for (int k = 0; k < D / 32; ++k) qf[k] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(q + 8 * k));
-    }
-
-    const int *table = p.b.table + u.s * p.b.table_stride;
-    const int ps = p.b.page_shift, pmask = (1 << ps) - 1;
-    // page of the KPL keys from `key` (a page holds them whole): UNSEEN by every row, or MISSING where the table names none
-    constexpr int UNSEEN = -2, MISSING = -1;
-    auto page_at = [&](int key) {
-        if (key >= hi_any || key + KPL <= lo_any) return UNSEEN;
-        const int pg = table[key >> ps];
-        return pg >= 0 && pg < p.b.pages ? pg : MISSING;
-    };
-    const int kgrp = ((n >> 2) * KPL);   // the lane's key group as a row of K, its first key in the tile
-    uint32_t kreg[NT][KW], vreg[DT][VW];
-    float kscale = 0.0f, vscale = 0.0f;
-    int pgk, pgv;
-
-    auto load_k = [&](int t) {
-        const int key = t * KT + kgrp + (n & 3);
-        const uint8_t *c = p.kc + ((int64_t)(pgk < 0 ? 0 : pgk) * p.b.Hkv + u.head) * ((int64_t)D << ps)
-                           + (int64_t)(key & pmask) * D + g * (D / 4);
-#pragma unroll
-        for (int i = 0; i < NT; ++i)
-#pragma unroll
-            for (int w = 0; w < KW; w += 4) {
-                const u32x4 x = *reinterpret_cast<const u32x4 *>(c + 4 * i * D + 4 * w);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) kreg[i][w + e] = x[e];
-            }
-    };
-    auto load_v = [&](int t) {
-        const int64_t at = (int64_t)(pgv < 0 ? 0 : pgv) * p.b.Hkv + u.head;
-        kscale = p.ks[at] * p.scale_log2;
-        vscale = pgv < 0 ? 1.0f : p.vs[at];   // (its probabilities are 0 or NaN)
-        const uint8_t *c = p.vc + at * ((int64_t)D << ps) + (int64_t)n * (1 << ps) + ((t * KT + g * KPL) & pmask);
-#pragma unroll
-        for (int i = 0; i < DT; ++i) {
-            const uint8_t *ci = c + ((int64_t)(16 * i) << ps);
-            if constexpr (VW == 4) {
-                const u32x4 x = *reinterpret_cast<const u32x4 *>(ci);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) vreg[i][e] = x[e];
-            } else {
-                const u32x2 x = *reinterpret_cast<const u32x2 *>(ci);
-                vreg[i][0] = x[0];
-                vreg[i][1] = x[1];
-            }
-        }
-    };
-
-    f32x4 o[DT];
-#pragma unroll
-    for (int i = 0; i < DT; ++i) o[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    // l: of this lane's keys.  A row that sees keys beyond the table's reach is NaN.
-    float m = NEG_INF, l = (p.causal && pos + 1 < sq.all ? pos + 1 : sq.all) > sq.len ? __builtin_nanf("") : 0.0f;
-
-    int t = beg + wave;
-    bool bad = false;
-    if (t < end) {
-        pgk = page_at(t * KT + kgrp);
-        pgv = page_at(t * KT + g * KPL);
-        load_k(t);
-        load_v(t);
-        bad = pgv == MISSING;
-    }
-    for (; t < end; t += 4) {
-        const int next = t + 4;
-        if (next < end) {
-            pgk = page_at(next * KT + kgrp);
-            pgv = page_at(next * KT + g * KPL);
-        }
-        f32x4 acc[NT];
-#pragma unroll
-        for (int i = 0; i < NT; ++i) {
-            acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int k = 0; k < D / 32; ++k)
-                acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(kreg[i][2 * k], kreg[i][2 * k + 1]), qf[k], acc[i], 0, 0, 0);
-        }
-        if (next < end) load_k(next);
-        const int key0 = t * KT + g * KPL;   // the lane's keys: key0 + 4 i + e
-        const bool partial = t * KT < lo_all || t * KT + KT > hi_all || __ballot(bad) != 0;   // (of the whole wave)
-        float x[KPL];
-#pragma unroll
-        for (int i = 0; i < NT; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) x[4 * i + e] = acc[i][e] * kscale;
-        if (partial) {
-#pragma unroll
-            for (int i = 0; i < KPL; ++i) {
-                const int key = key0 + i;
-                x[i] = key < lo || key >= hi ? NEG_INF : (bad ? __builtin_nanf("") : x[i]);
-            }
-        }
-        float mt = x[0];
-#pragma unroll
-        for (int i = 1; i < KPL; ++i) mt = fmaxf(mt, x[i]);
-        mt = fmaxf(mt, __shfl_xor(mt, 16, 64));
-        mt = fmaxf(mt, __shfl_xor(mt, 32, 64));
-        const float mn = fmaxf(m, mt);
-        const float ms = mn == NEG_INF ? 0.0f : mn;   // (a row that has seen no key yet)
-        const float alpha = __builtin_amdgcn_exp2f(m - ms);
-        m = mn;
-        float sum = 0.0f;
-#pragma unroll
-        for (int i = 0; i < KPL; ++i) {
-            x[i] = __builtin_amdgcn_exp2f(x[i] - ms);
-            sum += x[i];
-        }
-        l = l * alpha + sum;
-        if (__ballot(alpha != 1.0f)) {
-#pragma unroll
-            for (int i = 0; i < DT; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[i][e] *= alpha;
-        }
-        bf16x8 pf[KPL / 8];
-#pragma unroll
-        for (int k = 0; k < KPL / 8; ++k) {
-            u32x4 w;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = pack2(x[8 * k + 2 * e] * vscale, x[8 * k + 2 * e + 1] * vscale);
-            pf[k] = __builtin_bit_cast(bf16x8, w);
-        }
-        if (partial) {
-            // Values that no row sees (behind the sequence's end, before the
-            // window, of a missing page) are whatever memory holds: zeroed, as
-            // 0 * NaN is NaN; NaN that some rows see is marked.
-            uint32_t some = 0;
-#pragma unroll
-            for (int w = 0; w < VW; ++w) {
-                const uint32_t see = bad ? 0u : byte_mask(key0 + 4 * w, lo_any, hi_any);
-#pragma unroll
-                for (int i = 0; i < DT; ++i) {
-                    vreg[i][w] &= see;
-                    some |= nan_bytes(vreg[i][w]);
-                }
-            }
-            if (some) {
-#pragma unroll
-                for (int i = 0; i < DT; ++i)
-#pragma unroll
-                    for (int w = 0; w < VW; ++w) {
-                        const uint32_t nan = nan_bytes(vreg[i][w]);
-                        mark_nan<D>(marks, nan, 16 * i + n, key0 + 4 * w, rlast + 1 - r0, [&](int r, int key) {
-                            const int rp = sq.pos0 + (r0 + r) / G;
-                            return key >= from(rp) && key < upto(rp);
-                        });
-                        vreg[i][w] &= ~((nan >> 7) * 0xFFu);
-                    }
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < DT; ++i)
-#pragma unroll
-            for (int k = 0; k < KPL / 8; ++k)
-                o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(vreg[i][2 * k], vreg[i][2 * k + 1]), pf[k], o[i], 0, 0, 0);
-        if (next < end) {
-            load_v(next);
-            bad = pgv == MISSING;
-        }
-    }
-
-    // join the waves
-    l += __shfl_xor(l, 16, 64);
-    l += __shfl_xor(l, 32, 64);
-    if (g == 0) {
-        ml[(wave * 16 + n) * 2] = m;
-        ml[(wave * 16 + n) * 2 + 1] = l;
-    }
-#pragma unroll
-    for (int i = 0; i < DT; ++i) *reinterpret_cast<f32x4 *>(&obuf[(wave * 16 + n) * OS + 16 * i + 4 * g]) = o[i];
-    __syncthreads();
-    for (int at = threadIdx.x * 4; at < 16 * D; at += 1024) {
-        const int r = at / D, d = at - r * D;
-        if (r0 + r >= rows) continue;
-        float mx = NEG_INF;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) mx = fmaxf(mx, ml[(w * 16 + r) * 2]);
-        const float ms = mx == NEG_INF ? 0.0f : mx;
-        float sum = 0.0f;
-        f32x4 v = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const float f = __builtin_amdgcn_exp2f(ml[(w * 16 + r) * 2] - ms);
-            sum += ml[(w * 16 + r) * 2 + 1] * f;
-            const f32x4 ow = *reinterpret_cast<const f32x4 *>(&obuf[(w * 16 + r) * OS + d]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] += ow[e] * f;
-        }
-        const uint32_t nan = marks[r][d >> 5] >> (d & 31);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = nan >> e & 1u ? __builtin_nanf("") : v[e];
-        if (u.pieces > 1) {
-            const int64_t at_row = (int64_t)u.slot * FewRows::ROWS + r;
-            *reinterpret_cast<f32x4 *>(p.part + at_row * D + d) = v;
-            if (d == 0) {
-                p.part_ml[at_row * 2] = mx;
-                p.part_ml[at_row * 2 + 1] = sum;
-            }
-        } else {
-            const int gr = r0 + r, i = gr / G;
-            const int64_t orow = (int64_t)(sq.a + i) * p.Hq + u.head * G + gr - i * G;
-            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-            *reinterpret_cast<u32x2 *>(p.o + orow * D + d) = u32x2{pack2(v[0] * inv, v[1] * inv), pack2(v[2] * inv, v[3] * inv)};
-            if (d == 0) p.lse[orow] = sum == 0.0f ? NEG_INF : (mx + __builtin_amdgcn_logf(sum)) * LN2;
-        }
-    }
+    __shared__ FewShared<D, 4> sh;
+    cache_few<D, KT, 4>(p, (int)blockIdx.x, sh);
 }
 
-// The pieces of the rows of a split (row tile, kv head) joined: a workgroup
-// takes a row, its waves the pieces in turn (BY = 256: few rows of many
-// pieces), or 16 rows, a wave 4 of them one after another (BY = 64: many rows
-// of few pieces).  A lane holds D/64 channels.
-template <class F, int D, int BY>
+// The pieces of the rows of split row tiles joined.  The workgroups of a row
+// tile's c partial outputs share its rows, the k-th those with row % c = k.
+// Few rows (many pieces): a workgroup's waves take the pieces in turn, a row
+// after another; many rows (few pieces): MANY_BY workgroups for each partial
+// output, a wave takes whole rows.  A lane holds D/64 channels.
+constexpr int MANY_BY = 8;
+
+template <int D>
 __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnParams p)
 {
-    constexpr int C = D / 64, W = BY / 64, ROWS = W > 1 ? 1 : 4;
-    __shared__ float obuf[W > 1 ? 4 * D : 1], lbuf[4];
-    const int G = p.Hq / p.b.Hkv;
-    const Unit u = find_unit<F>(p, G, blockIdx.x, true);
-    if (u.s < 0) return;
-    const SeqPlan sq = seq_plan<F>(p, u.s, G);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    for (int k = 0; k < ROWS; ++k) {
-        const int r = W > 1 ? (int)blockIdx.y : (int)blockIdx.y * 16 + wave * 4 + k, gr = u.tile * F::ROWS + r;
-        if (gr >= sq.n * G) return;   // (the whole workgroup where it shares a row)
-        const int64_t base = (int64_t)u.slot * F::ROWS + r;
+    constexpr int C = D / 64;
+    __shared__ float obuf[4 * D], lbuf[4];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), G = p.Hq / p.b.Hkv;
+    const bool many = (int)blockIdx.x >= p.slots[0];
+    const int form = many ? 1 : 0, x = many ? ((int)blockIdx.x - p.slots[0]) / MANY_BY : (int)blockIdx.x;
+    const int tile_rows = many ? ManyRows::ROWS : FewRows::ROWS;
+    if (x >= p.counts[form]) return;
+    const PartInfo i = static_cast<const PartInfo *>(p.info[form])[x];
+    // (whatever tables that break their rules leave here, nothing outside the arrays is touched)
+    const int slot0 = x - i.piece;
+    if (i.piece < 0 || i.pieces <= i.piece || slot0 < 0 || i.pieces > p.slots[form] - slot0 || i.head < 0 || i.head >= p.b.Hkv || i.token < 0
+        || i.row0 < 0 || i.rows < 0 || i.rows > tile_rows || i.token + (i.row0 + (int64_t)i.rows - 1) / G >= p.b.T)
+        return;
+    const float *part = p.part[form], *ml = p.part_ml[form];
+    const int share = many ? ((int)blockIdx.x - p.slots[0]) % MANY_BY * 4 + wave : 0, shares = many ? 4 * MANY_BY : 1;
+    const int first = many ? 0 : wave, step = many ? 1 : 4;   // the wave's pieces
+    for (int r = i.piece + i.pieces * share; r < i.rows; r += i.pieces * shares) {
+        const int64_t base = (int64_t)slot0 * tile_rows + r;
         float mx = NEG_INF;
-        for (int c = lane; c < u.pieces; c += 64) mx = fmaxf(mx, p.part_ml[(base + (int64_t)c * F::ROWS) * 2]);
+        for (int c = lane; c < i.pieces; c += 64) mx = fmaxf(mx, ml[(base + (int64_t)c * tile_rows) * 2]);
 #pragma unroll
-        for (int x = 1; x < 64; x <<= 1) mx = fmaxf(mx, __shfl_xor(mx, x, 64));
+        for (int k = 1; k < 64; k <<= 1) mx = fmaxf(mx, __shfl_xor(mx, k, 64));
         const float ms = mx == NEG_INF ? 0.0f : mx;
         float sum = 0.0f, v[C] = {};
-        // rounds of 16 pieces of the wave, whose weights 16 lanes work out
-        for (int c0 = W > 1 ? wave : 0; c0 < u.pieces; c0 += 16 * W) {
-            const int c = c0 + (lane & 15) * W;
-            const int64_t at = (base + (int64_t)(c < u.pieces ? c : 0) * F::ROWS) * 2;
-            const float f = c < u.pieces ? __builtin_amdgcn_exp2f(p.part_ml[at] - ms) : 0.0f;
-            const float fl = c < u.pieces ? p.part_ml[at + 1] * f : 0.0f;
+        // rounds of 16 of the wave's pieces, whose weights 16 lanes work out
+        for (int c0 = first; c0 < i.pieces; c0 += 16 * step) {
+            const int c = c0 + (lane & 15) * step;
+            const int64_t at = (base + (int64_t)(c < i.pieces ? c : 0) * tile_rows) * 2;
+            const float f = c < i.pieces ? __builtin_amdgcn_exp2f(ml[at] - ms) : 0.0f;
+            const float fl = c < i.pieces ? ml[at + 1] * f : 0.0f;
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
-                if (c0 + j * W < u.pieces) {
-                    const float *o = p.part + (base + (int64_t)(c0 + j * W) * F::ROWS) * D + C * lane;
-                    const float fj = __shfl(f, j, 64);
-                    sum += __shfl(fl, j, 64);
+                if (c0 + j * step < i.pieces) {
+                    const float *o = part + (base + (int64_t)(c0 + j * step) * tile_rows) * D + C * lane;
+                    const float fj = __builtin_bit_cast(float, lane_value(__builtin_bit_cast(int, f), j));
+                    sum += __builtin_bit_cast(float, lane_value(__builtin_bit_cast(int, fl), j));
 #pragma unroll
                     for (int e = 0; e < C; ++e) v[e] += o[e] * fj;
                 }
             }
         }
-        if constexpr (W > 1) {
+        if (!many) {
+            __syncthreads();   // (the row before has been read)
 #pragma unroll
             for (int e = 0; e < C; ++e) obuf[wave * D + C * lane + e] = v[e];
             if (lane == 0) lbuf[wave] = sum;
             __syncthreads();
-            if (wave != 0) return;
+            if (wave != 0) continue;
             sum = lbuf[0] + lbuf[1] + lbuf[2] + lbuf[3];
 #pragma unroll
             for (int e = 0; e < C; ++e) {
@@ -334,8 +90,8 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnParams p)
                 v[e] = obuf[d] + obuf[D + d] + obuf[2 * D + d] + obuf[3 * D + d];
             }
         }
-        const int i = gr / G;
-        const int64_t orow = (int64_t)(sq.a + i) * p.Hq + u.head * G + gr - i * G;
+        const int gr = i.row0 + r, t = gr / G;
+        const int64_t orow = (int64_t)(i.token + t) * p.Hq + i.head * G + gr - t * G;
         const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
         uint16_t *o = p.o + orow * D + C * lane;
         if constexpr (C == 1) {
@@ -348,91 +104,116 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnParams p)
     }
 }
 
-template <class F>
-unsigned join_pairs(const CacheAttnParams &p)
-{
-    const int64_t pairs = max_pairs<F>(p);
-    return (unsigned)(pairs < F::TARGET ? pairs : F::TARGET);
-}
-
 template <int D, int KT>
-hipError_t launch_few(const CacheAttnParams &p, hipStream_t s)
+hipError_t launch(const CacheAttnParams &p, hipStream_t s)
 {
-    cache_attn_kernel<D, KT><<<dim3((unsigned)max_units<FewRows>(p)), 256, 0, s>>>(p);
-    if (p.slots) cache_join_kernel<FewRows, D, 256><<<dim3(join_pairs<FewRows>(p), FewRows::ROWS), 256, 0, s>>>(p);
+    if (p.units[1]) {
+        const hipError_t e = launch_cache_prompt(D, p, s);
+        if (e != hipSuccess) return e;
+    } else {
+        cache_few_kernel<D, KT><<<dim3((unsigned)p.units[0]), 256, 0, s>>>(p);
+    }
+    const int joins = p.slots[0] + MANY_BY * p.slots[1];
+    if (joins) cache_join_kernel<D><<<dim3((unsigned)joins), 256, 0, s>>>(p);
     return hipGetLastError();
-}
-
-template <int D>
-hipError_t launch_many(const CacheAttnParams &p, hipStream_t s)
-{
-    const hipError_t e = launch_cache_prompt(D, p, s);
-    if (e != hipSuccess) return e;
-    if (p.slots) cache_join_kernel<ManyRows, D, 64><<<dim3(join_pairs<ManyRows>(p), ManyRows::ROWS / 16), 256, 0, s>>>(p);
-    return hipGetLastError();
-}
-
-// Partial outputs of form F.
-template <class F>
-int slots_of(int64_t T, int64_t S, int G, int Hkv, int64_t keys)
-{
-    if ((keys + TILE - 1) / TILE <= F::MIN_TILES) return 0;
-    const int64_t units = (T * G / F::ROWS + S) * Hkv + F::TARGET;
-    return (int)(units < 2 * F::TARGET ? units : 2 * F::TARGET);
-}
-
-// Sequences of at most this many rows take the form for few rows.
-constexpr int FEW = 64;
-
-struct Choice {
-    bool few, many;
-    int64_t limit;   // rows up to which a sequence is among the few
-};
-
-// From what the host knows: no sequence has more than T G rows, and they have
-// T G / S on average.  Either form is right for any sequence.
-Choice choose(int64_t T, int64_t S, int G)
-{
-    if (T * G <= FEW || T * G <= FewRows::ROWS * S) return {true, false, T * G};
-    if (S == 1) return {false, true, 0};
-    return {true, true, FEW};
 }
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+// Sequences of at most this many rows take the form for few rows, where a batch
+// holds both.
+constexpr int FEW = 64;
+
+// Bounds of a call from what the host knows: no sequence has more than T G
+// rows, and they have T G / S on average.  Either form is right for any
+// sequence: which takes which is a matter of time only.
+struct Bounds {
+    int above[2], upto[2], units[2], slots[2];
+};
+
+// A sequence of kt key tiles and `pairs` row tiles times heads is cut in
+// c = ceil(kt / chunk) < 1 + kt / chunk pieces, and sum(pairs kt) / chunk <=
+// TARGET: below sum(pairs) + TARGET units, and at most kt / MIN_TILES + 1 a
+// pair.  Where c >= 2, c < 2 kt / chunk: below 2 TARGET partial outputs.
+// Sequences no longer than one piece need none.
+template <class F>
+void bound(Bounds &b, int64_t pairs, int64_t keys)
+{
+    const int64_t most = ((keys + TILE - 1) / TILE + F::MIN_TILES - 1) / F::MIN_TILES;   // pieces of a pair
+    const int64_t a = pairs + F::TARGET, c = pairs * (most > 1 ? most : 1), units = a < c ? a : c;
+    b.units[F::FORM] = (int)units;
+    b.slots[F::FORM] = most <= 1 ? 0 : (int)(units < 2 * F::TARGET ? units : 2 * F::TARGET);
+}
+
+Bounds bounds(int64_t T, int64_t S, int G, int Hkv, int64_t keys)
+{
+    Bounds b = {};
+    const int64_t rows = T * G;
+    const bool few = rows <= FEW || rows <= FewRows::ROWS * S;   // (short sequences, whatever q_start says)
+    const bool both = !few && S > 1;
+    const int64_t limit = few ? rows : (both ? FEW : 0);         // rows up to which a sequence is among the few
+    if (few || both) {
+        const int64_t most = rows / FewRows::ROWS + S, each = S * ((limit + FewRows::ROWS - 1) / FewRows::ROWS);
+        b.upto[0] = (int)limit;
+        bound<FewRows>(b, (most < each ? most : each) * Hkv, keys);
+    }
+    if (!few) {
+        b.above[1] = (int)limit;
+        b.upto[1] = (int)rows;
+        bound<ManyRows>(b, (rows / ManyRows::ROWS + S) * Hkv, keys);
+    }
+    return b;
+}
+
+// The workspace: counts, infos, running maxima and sums, partial outputs.
+struct Layout {
+    size_t info[2], ml[2], part[2], total;
+};
+
+Layout layout(const Bounds &b, int D)
+{
+    Layout l = {};
+    size_t at = 256;
+    const size_t rows[2] = {(size_t)b.slots[0] * FewRows::ROWS, (size_t)b.slots[1] * ManyRows::ROWS};
+    auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at += align256(bytes);
+        return here;
+    };
+    for (int f = 0; f < 2; ++f) l.info[f] = take(b.slots[f] * sizeof(PartInfo));
+    for (int f = 0; f < 2; ++f) l.ml[f] = take(rows[f] * 2 * sizeof(float));
+    for (int f = 0; f < 2; ++f) l.part[f] = take(rows[f] * D * sizeof(float));
+    l.total = b.slots[0] + b.slots[1] ? at : 0;
+    return l;
+}
 
 } // namespace
 
 size_t cache_attn_workspace(int D, int64_t T, int64_t S, int G, int Hkv, int64_t keys)
 {
-    const Choice c = choose(T, S, G);
-    const size_t few = c.few ? (size_t)slots_of<FewRows>(T, S, G, Hkv, keys) * FewRows::ROWS : 0;
-    const size_t many = c.many ? (size_t)slots_of<ManyRows>(T, S, G, Hkv, keys) * ManyRows::ROWS : 0;
-    const size_t rows = few > many ? few : many;   // (one form after the other)
-    return align256(rows * D * 4) + align256(rows * 2 * 4);
+    return layout(bounds(T, S, G, Hkv, keys), D).total;
 }
 
-hipError_t launch_cache_attn(int D, const CacheAttnParams &params, hipStream_t s)
+hipError_t launch_cache_attn(int D, CacheAttnParams &p, void *ws, hipStream_t s)
 {
-    CacheAttnParams p = params;
-    const int64_t T = p.b.T, S = p.b.S, keys = (int64_t)p.b.width << p.b.page_shift;
-    const int G = p.Hq / p.b.Hkv;
-    const Choice c = choose(T, S, G);
-    if (c.many) {
-        p.rows_above = c.limit;
-        p.rows_upto = T * G;
-        p.slots = slots_of<ManyRows>(T, S, G, p.b.Hkv, keys);
-        p.part_ml = p.part + align256((size_t)p.slots * ManyRows::ROWS * D * 4) / 4;
-        const hipError_t e = D == 64 ? launch_many<64>(p, s) : (D == 128 ? launch_many<128>(p, s) : launch_many<256>(p, s));
-        if (e != hipSuccess) return e;
+    const Bounds b = bounds(p.b.T, p.b.S, p.Hq / p.b.Hkv, p.b.Hkv, (int64_t)p.b.width << p.b.page_shift);
+    const Layout l = layout(b, D);
+    char *base = static_cast<char *>(ws);
+    p.counts = reinterpret_cast<int *>(base);
+    for (int f = 0; f < 2; ++f) {
+        p.rows_above[f] = b.above[f];
+        p.rows_upto[f] = b.upto[f];
+        p.units[f] = b.units[f];
+        p.slots[f] = b.slots[f];
+        p.info[f] = base + l.info[f];
+        p.part_ml[f] = reinterpret_cast<float *>(base + l.ml[f]);
+        p.part[f] = reinterpret_cast<float *>(base + l.part[f]);
     }
-    if (c.few) {
-        p.rows_above = 0;
-        p.rows_upto = c.limit;
-        p.slots = slots_of<FewRows>(T, S, G, p.b.Hkv, keys);
-        p.part_ml = p.part + align256((size_t)p.slots * FewRows::ROWS * D * 4) / 4;
-        return D == 64 ? launch_few<64, 64>(p, s) : (D == 128 ? launch_few<128, 64>(p, s) : launch_few<256, 32>(p, s));
+    switch (D) {
+    case 64: return launch<64, 64>(p, s);
+    case 128: return launch<128, 64>(p, s);
+    default: return launch<256, 32>(p, s);
     }
-    return hipSuccess;
 }
 
 } // namespace lamp

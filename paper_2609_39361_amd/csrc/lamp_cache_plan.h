@@ -3,6 +3,10 @@
 #pragma once
 #include <hip/hip_runtime.h>
 
+#include <limits.h>
+
+#include <type_traits>
+
 #include "lamp_serve.h"
 
 namespace lamp {
@@ -19,21 +23,21 @@ constexpr float NEG_INF = -__builtin_inff();
 constexpr float LN2 = 0.6931471805599453f;
 constexpr int TILE = 64;       // keys of the plan's tiles
 
-// The two forms of the attention kernel.  ROWS: query rows of a workgroup (row
-// = token * G + head of the group); TARGET: workgroups that fill the 256 CUs;
-// MIN_TILES: least key tiles of a piece.
-struct FewRows {       // single tokens and short chunks (lamp_cache_attn.hip)
-    static constexpr int ROWS = 16, TARGET = 512, MIN_TILES = 4;
+// The two forms of the attention.  ROWS: query rows of a workgroup (row = token
+// * G + head of the group); TARGET: workgroups that fill the 256 CUs; MIN_TILES:
+// least key tiles of a piece.
+struct FewRows {       // single tokens and short chunks (lamp_cache_few.h)
+    static constexpr int ROWS = 16, TARGET = 512, MIN_TILES = 4, FORM = 0;
 };
 struct ManyRows {      // prompts (lamp_cache_prompt.hip)
-    static constexpr int ROWS = 256, TARGET = 256, MIN_TILES = 8;
+    static constexpr int ROWS = 256, TARGET = 256, MIN_TILES = 8, FORM = 1;
 };
 
 // The key range of one sequence is cut in pieces when its row tiles alone do
 // not fill the device: with `total` the key tiles of all (sequence, row tile,
-// kv head) triples, pieces hold about total / target tiles.  Every workgroup
-// works the plan out for itself from the lengths (no planning launch, and a
-// captured graph follows lengths that change).
+// kv head) triples of a form, pieces hold about total / TARGET tiles.  Every
+// workgroup works the plan out for itself from the lengths (no planning launch,
+// and a captured graph follows lengths that change).
 struct Unit {
     int s;           // sequence (-1: none)
     int tile, head;  // row tile, kv head
@@ -58,88 +62,109 @@ __device__ __forceinline__ SeqPlan seq_plan(const CacheAttnParams &p, int s, int
     const int len = p.b.kv_lens[s] > 0 ? p.b.kv_lens[s] : 0;
     r.n = r.a >= 0 && e <= p.b.T && e > r.a ? e - r.a : 0;
     r.pos0 = len - r.n;
-    const int64_t reach = (int64_t)p.b.width << p.b.page_shift;
+    const int reach = p.b.width << p.b.page_shift;   // (at most 2^30)
     r.all = len;
-    r.len = len < reach ? len : (int)reach;
-    const int64_t rows = (int64_t)r.n * G;
-    r.tiles = rows > p.rows_above && rows <= p.rows_upto ? (int)((rows + F::ROWS - 1) / F::ROWS) : 0;
+    r.len = len < reach ? len : reach;
+    const int rows = r.n * G;                        // (at most 2^27)
+    r.tiles = rows > p.rows_above[F::FORM] && rows <= p.rows_upto[F::FORM] ? (rows + F::ROWS - 1) / F::ROWS : 0;
     r.kt = (r.len + TILE - 1) / TILE;
     if (p.window > 0) {
-        const int64_t span = ((int64_t)p.window + F::ROWS - 1 + TILE - 1) / TILE + 1;
-        if (span < r.kt) r.kt = (int)span;
+        const int span = (p.window + F::ROWS - 1 + TILE - 1) / TILE + 1;
+        if (span < r.kt) r.kt = span;
     }
     return r;
 }
 
-__device__ __forceinline__ int64_t wave_sum(int64_t v)
+// Inclusive sum over the wave's lanes.
+template <class T>
+__device__ __forceinline__ T wave_scan(T v)
 {
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) v += __shfl_xor(v, m, 64);
+    const T zero = 0;
+    auto step = [&](auto ctrl, auto rows) {
+        const int x = __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, zero), __builtin_bit_cast(int, v), decltype(ctrl)::value,
+                                                  decltype(rows)::value, 0xf, false);
+        v += __builtin_bit_cast(T, x);
+    };
+    step(std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xf>{});   // row_shr:1
+    step(std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xf>{});   // row_shr:2
+    step(std::integral_constant<int, 0x114>{}, std::integral_constant<int, 0xf>{});   // row_shr:4
+    step(std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xf>{});   // row_shr:8
+    step(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});   // row_bcast:15
+    step(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});   // row_bcast:31
     return v;
 }
 
-// Tiles of a piece, from the lengths of every sequence (by one wave).
-template <class F>
-__device__ int piece_tiles(const CacheAttnParams &p, int G)
+__device__ __forceinline__ int lane_value(int v, int lane)
 {
-    int64_t total = 0;
-    for (int s = threadIdx.x & 63; s < p.b.S; s += 64) {
-        const SeqPlan r = seq_plan<F>(p, s, G);
-        total += (int64_t)r.tiles * r.kt;
-    }
-    total = wave_sum(total) * p.b.Hkv;
-    const int64_t c = (total + F::TARGET - 1) / F::TARGET;
-    return (int)(c < F::MIN_TILES ? F::MIN_TILES : (c < 1 << 24 ? c : 1 << 24));
+    return __builtin_amdgcn_readlane(v, lane);
 }
 
-// Unit x of the plan; with `joined`, unit x among the (row tile, kv head) pairs
-// of split sequences instead (piece 0, slot of the first piece).
+// Unit x of form F (by every wave, the same in each).  The workgroup of unit 0
+// also writes how many partial outputs the form has.
 template <class F>
-__device__ Unit find_unit(const CacheAttnParams &p, int G, int64_t x, bool joined)
+__device__ Unit find_unit(const CacheAttnParams &p, int G, int x)
 {
     const int lane = threadIdx.x & 63;
-    const int chunk = piece_tiles<F>(p, G);
-    int64_t units = 0, slots = 0;   // of the sequences before this round of 64
+    SeqPlan first;   // of the first 64 sequences
+    float total = 0.0f;
+    for (int s = lane; s < p.b.S; s += 64) {
+        const SeqPlan r = seq_plan<F>(p, s, G);
+        if (s == lane) first = r;
+        total += (float)r.tiles * (float)r.kt;
+    }
+    total = __builtin_bit_cast(float, lane_value(__builtin_bit_cast(int, wave_scan(total)), 63)) * (float)p.b.Hkv;
+    // (rounded up by more than the sum's fp32 rounding, so that the bound of the units holds)
+    const float want = total * (1.0001f / F::TARGET);
+    const int chunk = want < F::MIN_TILES ? F::MIN_TILES : (want < 1e8f ? (int)want + 1 : 100000000);
+    int units = 0, slots = 0;   // of the sequences before this round of 64
+    Unit found = {-1, 0, 0, 0, 0, 0};
     for (int s0 = 0; s0 < p.b.S; s0 += 64) {
         const int s = s0 + lane;
-        int64_t pairs = 0;
-        int c = 1, tiles = 0;
+        int tiles = 0, c = 1;
         if (s < p.b.S) {
-            const SeqPlan r = seq_plan<F>(p, s, G);
+            const SeqPlan r = s0 == 0 ? first : seq_plan<F>(p, s, G);
             tiles = r.tiles;
-            pairs = (int64_t)tiles * p.b.Hkv;
             c = (r.kt + chunk - 1) / chunk;
             c = c < 1 ? 1 : c;
         }
-        const int64_t u = joined ? (c > 1 ? pairs : 0) : pairs * c, sl = c > 1 ? pairs * c : 0;
-        int64_t ui = u, si = sl;   // inclusive prefix sums
-#pragma unroll
-        for (int m = 1; m < 64; m <<= 1) {
-            const int64_t a = __shfl_up(ui, m, 64), b = __shfl_up(si, m, 64);
-            if (lane >= m) ui += a, si += b;
-        }
-        const uint64_t hit = __ballot(x < units + ui);
+        const int pairs = tiles * p.b.Hkv, u = pairs * c, sl = c > 1 ? u : 0;
+        const int ui = wave_scan(u), si = wave_scan(sl);
+        const uint64_t hit = __ballot(x >= units + ui - u && x < units + ui);
         if (hit) {
-            const int l = __builtin_ctzll(hit);   // the first sequence that ends behind x
-            const int64_t local = x - (units + __shfl(ui - u, l, 64));
-            const int64_t slot0 = slots + __shfl(si - sl, l, 64);
-            const int cs = __shfl(c, l, 64);
-            Unit r;
-            r.s = s0 + l;
-            r.pieces = cs;
-            r.piece = joined ? 0 : (int)(local % cs);
-            const int64_t pair = joined ? local : local / cs;
-            r.head = (int)(pair % p.b.Hkv);
-            r.tile = __shfl(tiles, l, 64) - 1 - (int)(pair / p.b.Hkv);   // (causal: the last row tiles see most keys, and start first)
-            const int64_t slot = slot0 + pair * cs + r.piece;
-            if (cs > 1 && slot + (joined ? cs : 1) > p.slots) break;   // (lengths that break the contract)
-            r.slot = (int)slot;
-            return r;
+            const int l = __builtin_ctzll(hit);
+            const int cs = lane_value(c, l), local = x - (units + lane_value(ui - u, l)), pair = local / cs;
+            const int slot = slots + lane_value(si - sl, l) + local;
+            // (tables that break their rules may count past the bounds: such units are left out)
+            if (local >= 0 && pair < lane_value(pairs, l) && (cs == 1 || (slot >= 0 && slot < p.slots[F::FORM]))) {
+                found.s = s0 + l;
+                found.pieces = cs;
+                found.piece = local - pair * cs;
+                found.head = pair % p.b.Hkv;
+                found.tile = lane_value(tiles, l) - 1 - pair / p.b.Hkv;   // (causal: the last row tiles see most keys, and start first)
+                found.slot = slot;
+            }
+            if (x != 0) return found;
         }
-        units += __shfl(ui, 63, 64);
-        slots += __shfl(si, 63, 64);
+        units += lane_value(ui, 63);
+        slots += lane_value(si, 63);
     }
-    return {-1, 0, 0, 0, 0, 0};
+    if (x == 0 && p.slots[F::FORM] && threadIdx.x == 0) p.counts[F::FORM] = slots;
+    return found;
+}
+
+// What cache_join_kernel needs to know of a partial output; each unit writes its own.
+struct PartInfo {
+    int token, row0, rows, head;   // first token of the sequence, rows [row0, row0 + rows) of it
+    int piece, pieces, unused[2];
+};
+
+template <class F>
+__device__ __forceinline__ void write_info(const CacheAttnParams &p, const Unit &u, int token, int row0, int rows)
+{
+    if (u.pieces > 1 && threadIdx.x == 0) {
+        PartInfo *i = static_cast<PartInfo *>(p.info[F::FORM]) + u.slot;
+        *i = {token, row0, rows, u.head, u.piece, u.pieces, {0, 0}};
+    }
 }
 
 __device__ __forceinline__ uint32_t pack2(float a, float b)
@@ -189,25 +214,6 @@ __device__ __forceinline__ void mark_nan(uint32_t (*marks)[D / 32], uint32_t nan
         for (int r = 0; r < rows; ++r)
             if (sees(r, k)) atomicOr(&marks[r][d >> 5], 1u << (d & 31));
     }
-}
-
-// Row tiles times kv heads that the batch can have at most.
-template <class F>
-int64_t max_pairs(const CacheAttnParams &p)
-{
-    const int G = p.Hq / p.b.Hkv;
-    return ((int64_t)p.b.T * G / F::ROWS + p.b.S) * p.b.Hkv;
-}
-
-// A sequence of kt key tiles and `pairs` row tiles times heads is cut in
-// c = ceil(kt / chunk) < 1 + kt / chunk pieces, and sum(pairs kt) / chunk <=
-// TARGET: below max_pairs + TARGET units in all.  Where c >= 2, c < 2 kt / chunk:
-// below 2 TARGET partial outputs, of below TARGET row tiles times heads.
-// Sequences no longer than one piece need none.
-template <class F>
-int max_units(const CacheAttnParams &p)
-{
-    return (int)(max_pairs<F>(p) + (p.slots ? F::TARGET : 0));
 }
 
 } // namespace

@@ -4,8 +4,7 @@
 //
 // A workgroup of 8 waves takes 256 query rows, 32 a wave, and walks over key
 // tiles.  Its threads widen the tile's codes to bf16 once for all rows and lay
-// them out in LDS (two buffers: the next tile is written while this one is
-// used, one barrier a tile).  The transposed products S^T = K Q^T and
+// them out in LDS.  The transposed products S^T = K Q^T and
 // O^T = V^T P^T (32x32x16) leave a lane (row n = lane % 32, half = lane / 32)
 // with the logits of half of the row's keys, which is also the operand of the
 // second product: row m of a 32-key operand of K is key swap(m), m with bits 2
@@ -14,12 +13,23 @@
 // between the two halves a tile.
 //
 // Both LDS layouts are rows of 16-byte units (K: 8 channels of a key, keys in
-// operand order; V: 8 keys of a channel), the unit's place exchanged with the
-// row's low bits, so that the lanes reading one unit of consecutive rows use
-// all banks.
+// operand order; V: 8 keys of a channel) with one unit of padding, so that the
+// lanes reading one unit of consecutive rows use all banks, at addresses that
+// differ by constants.
+//
+// A wave alternates between a phase for the matrix cores (o += V^T P^T of the
+// tile before, then S^T of this one, with the widening and storing of its share
+// of the next tile between the products) and one for the vector unit (the
+// softmax of this tile).  A barrier ends every phase and the upper four waves,
+// which share the four SIMDs with the lower four, run one phase behind: while
+// one wave of a SIMD multiplies, the other exponentiates.  With phases numbered
+// so that the lower half multiplies for tile t in phase 2 t and the upper in
+// 2 t + 1, K of tile t + 1 and V of tile t are stored in phases 2 t and 2 t + 1
+// and read in 2 t + 2 and 2 t + 3; K of t - 1 and V of t - 2, whose buffers they
+// take, were last read in phase 2 t - 1: two buffers of each do.
 #include <hip/hip_runtime.h>
 
-#include "lamp_cache_plan.h"
+#include "lamp_cache_few.h"
 
 namespace lamp {
 namespace {
@@ -31,37 +41,45 @@ constexpr int WAVES = 8, THREADS = 64 * WAVES;
 // and o is rescaled a few times a row instead of at every tile.
 constexpr float LAZY = 8.0f;
 
+constexpr int AHEAD = 6;   // operands in flight from LDS
+
 __device__ __forceinline__ int swap23(int m)
 {
     return (m & ~12) | ((m & 4) << 1) | ((m & 8) >> 1);
 }
 
 template <int D, int KT>
-__global__ __launch_bounds__(THREADS, 2) void cache_prompt_kernel(CacheAttnParams p)
+struct PromptShared {
+    u32x4 k[2][KT * (D / 8 + 1)];
+    u32x4 v[2][D * (KT / 8 + 1)];
+    float meta[4][KT / 16][2];                        // logit factor (scale, log2 e, key scale) and value scale of each group of 16 keys
+    uint32_t marks[ManyRows::ROWS][D / 32];           // rows and channels that see NaN values (mark_nan)
+    int marked;
+};
+
+// WIDE: a page holds whole tiles, so that a tile's page, scales and addresses
+// are the same for all threads (otherwise for each group of 16 keys).
+template <int D, int KT, bool WIDE>
+__device__ __forceinline__ void cache_prompt(const CacheAttnParams &p, int x, PromptShared<D, KT> &sh)
 {
     constexpr int NB = KT / 32;                 // 32-key operands of K
     constexpr int DB = D / 32;                  // 32-channel tiles of o
     constexpr int KU = D / 8, VU = KT / 8;      // 16-byte units of a row of K and V in LDS
-    // the unit's place in row m of K, d of V (8 units fill the banks once: 2 rows of V where it has 4)
-    auto k_at = [](int m, int unit) { return m * KU + (unit ^ (m & (KU < 16 ? KU - 1 : 15))); };
-    auto v_at = [](int d, int unit) { return d * VU + (unit ^ (VU < 8 ? (d >> 1) & (VU - 1) : d & (VU - 1))); };
+    constexpr auto k_at = [](int m, int unit) { return m * (KU + 1) + unit; };   // of row m
+    constexpr auto v_at = [](int d, int unit) { return d * (VU + 1) + unit; };
     constexpr int NG = KT / 16;                 // groups of 16 keys (each in one page)
     constexpr int CH = KT * D / 16;             // 16-byte chunks of codes of one tile of K (and of V)
     constexpr int PER = (CH + THREADS - 1) / THREADS;   // chunks of K of a thread, and of V
-    __shared__ u32x4 kbuf[2][KT * KU];
-    __shared__ u32x4 vbuf[2][D * VU];
-    __shared__ float meta[2][NG][2];            // logit factor (scale, log2 e, key scale) and value scale of each group
-    __shared__ uint32_t marks[ManyRows::ROWS][D / 32];   // rows and channels that see NaN values (mark_nan)
-    __shared__ int marked;
 
     const int G = p.Hq / p.b.Hkv;
-    const Unit u = find_unit<ManyRows>(p, G, blockIdx.x, false);
+    const Unit u = find_unit<ManyRows>(p, G, x);
     if (u.s < 0) return;
     const SeqPlan sq = seq_plan<ManyRows>(p, u.s, G);
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 31, half = lane >> 5;
     const int rows = sq.n * G, r0 = u.tile * ManyRows::ROWS;
     const int rend = r0 + ManyRows::ROWS < rows ? r0 + ManyRows::ROWS : rows;
+    write_info<ManyRows>(p, u, sq.a, r0, rend - r0);
     // keys that rows from ra to rb (inclusive) see: some of them [lo, hi), all of them [lo_all, hi_all)
     auto upto = [&](int pos) { return p.causal ? (pos + 1 < sq.len ? pos + 1 : sq.len) : sq.len; };
     auto from = [&](int pos) { return p.window > 0 && pos - p.window + 1 > 0 ? pos - p.window + 1 : 0; };
@@ -93,90 +111,124 @@ __global__ __launch_bounds__(THREADS, 2) void cache_prompt_kernel(CacheAttnParam
     }
     const float scale = fabsf(p.scale_log2);
 
-    // --- staging: this thread's chunks of a tile
+    // --- staging.  Straight-line code, so that no load is waited for before it
+    // is used: tiles beyond the last repeat it (nothing reads what that stores),
+    // places beyond the table's width read its last entry (no row sees them).
     const int *table = p.b.table + u.s * p.b.table_stride;
     const int ps = p.b.page_shift, pmask = (1 << ps) - 1;
-    constexpr int UNSEEN = -2, MISSING = -1;
-    auto page_at = [&](int key) {   // of the 16 keys from `key`
-        if (key >= hi_any || key + 16 <= lo_any) return UNSEEN;
-        const int pg = table[key >> ps];
-        return pg >= 0 && pg < p.b.pages ? pg : MISSING;
+    auto entry = [&](int key) {   // of the table, for the 16 keys from `key`
+        const int at = key >> ps;
+        return table[at < p.b.width ? at : p.b.width - 1];
     };
-    // chunk i of K: key, 16 channels; of V: channel, 16 keys
-    auto k_key = [&](int i) { return (tid + i * THREADS) / (D / 16); };
-    auto k_chunk = [&](int i) { return (tid + i * THREADS) % (D / 16); };
-    auto v_chan = [&](int i) { return (tid + i * THREADS) / NG; };
-    auto v_group = [&](int i) { return (tid + i * THREADS) % NG; };
-    auto mine = [&](int i) { return CH % THREADS == 0 || tid + i * THREADS < CH; };
+    auto held = [&](int pg) { return pg >= 0 && pg < p.b.pages; };
+    auto seen = [&](int key) { return key < hi_any && key + 16 > lo_any; };   // by some row
+    auto tile = [&](int t) { return t < end ? t : end - 1; };
+    // chunk i of K: 16 channels of a key; of V: 16 keys of a channel (two threads share one where a tile has fewer than threads)
+    int kkey[PER], kch[PER], vch[PER], vgr[PER];
+    // their bytes in a page, but for the tile's place in it (a tile is part of a page or holds whole ones)
+    int koff[PER], voff[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int c = (tid + i * THREADS) % CH;
+        kkey[i] = c / (D / 16);
+        kch[i] = c % (D / 16);
+        vch[i] = c / NG;
+        vgr[i] = c % NG;
+        koff[i] = (kkey[i] & pmask) * D + 16 * kch[i];
+        voff[i] = (vch[i] << ps) + (16 * vgr[i] & pmask);
+    }
     u32x4 kraw[PER], vraw[PER];
-    int kpage[PER], vpage[PER], mpage = UNSEEN;   // pages of the next tile to load
-    auto look_up = [&](int t) {
+    // Table entries of the next tiles to load, and (vp, mp) those of the tiles
+    // in vraw and in mk, mv, the scales of a tile's group tid % NG; WIDE: the
+    // pages of tiles t, t + 1 and t + 2 in iteration t, and the entry of t + 3.
+    int kpage[PER], vpage[PER], mpage, vp[PER], mp;
+    int page0 = 0, page1 = 0, page2 = 0, ahead;
+    float mk, mv;
+    auto uniform = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+    auto look_up_k = [&](int t) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) kpage[i] = entry(tile(t) * KT + (kkey[i] & ~15));
+    };
+    auto look_up_v = [&](int t) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) vpage[i] = entry(tile(t) * KT + 16 * vgr[i]);
+    };
+    auto look_up_meta = [&](int t) { mpage = entry(tile(t) * KT + 16 * (tid % NG)); };
+    auto look_up = [&](int t) { ahead = entry(tile(t) * KT); };
+    // of the page's codes for this head, the tile's part
+    auto k_base = [&](int pg, int t) { return p.kc + ((((int64_t)(held(pg) ? pg : 0) * p.b.Hkv + u.head) << ps) + (tile(t) * KT & pmask)) * D; };
+    auto v_base = [&](int pg, int t) { return p.vc + ((((int64_t)(held(pg) ? pg : 0) * p.b.Hkv + u.head) << ps) * D + (tile(t) * KT & pmask)); };
+    auto load_k = [&](int t, int pg) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) kraw[i] = *reinterpret_cast<const u32x4 *>(k_base(WIDE ? pg : kpage[i], t) + (uint32_t)koff[i]);
+    };
+    auto load_v = [&](int t, int pg) {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            if (!mine(i)) continue;
-            kpage[i] = page_at(t * KT + (k_key(i) & ~15));
-            vpage[i] = page_at(t * KT + 16 * v_group(i));
-        }
-        if (tid < NG) mpage = page_at(t * KT + 16 * tid);
-    };
-    float mk = 0.0f, mv = 0.0f;   // the scales of group `tid`
-    int vp[PER], mp = UNSEEN;     // pages of the tile in kraw, vraw
-    auto load = [&](int t) {
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            if (!mine(i)) continue;
-            const int64_t ka = (int64_t)(kpage[i] < 0 ? 0 : kpage[i]) * p.b.Hkv + u.head;
-            kraw[i] = *reinterpret_cast<const u32x4 *>(p.kc + (ka << ps) * D + (int64_t)((t * KT + k_key(i)) & pmask) * D + 16 * k_chunk(i));
-            const int64_t va = (int64_t)(vpage[i] < 0 ? 0 : vpage[i]) * p.b.Hkv + u.head;
-            vraw[i] = *reinterpret_cast<const u32x4 *>(p.vc + (va << ps) * D + ((int64_t)v_chan(i) << ps) + ((t * KT + 16 * v_group(i)) & pmask));
-            vp[i] = vpage[i];
-        }
-        if (tid < NG) {
-            mp = mpage;
-            const int64_t a = (int64_t)(mp < 0 ? 0 : mp) * p.b.Hkv + u.head;
-            mk = p.ks[a];
-            mv = p.vs[a];
+            vraw[i] = *reinterpret_cast<const u32x4 *>(v_base(WIDE ? pg : vpage[i], t) + (uint32_t)voff[i]);
+            vp[i] = WIDE ? pg : vpage[i];
         }
     };
-    auto sees = [&](int r, int key) {
+    auto load_meta = [&](int pg) {
+        mp = WIDE ? pg : mpage;
+        const int64_t at = (int64_t)(held(mp) ? mp : 0) * p.b.Hkv + u.head;
+        mk = p.ks[at];
+        mv = p.vs[at];
+    };
+    auto row_sees = [&](int r, int key) {
         const int rp = sq.pos0 + (r0 + r) / G;
         return key >= from(rp) && key < upto(rp);
     };
-    // a tile that not every row of the workgroup sees whole
-    auto partial_tile = [&](int t) { return t * KT < lo_all || t * KT + KT > hi_all; };
-    auto store = [&](int t, int b) {
+    // unit `second` of the thread's two of each chunk (the lower half of a row's lanes store their even unit first, the upper
+    // their odd one: all banks each time)
+    auto store_k = [&](int b, int second) {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            if (!mine(i)) continue;
-            const int key = k_key(i), m = (key & ~31) | swap23(key & 31), c = k_chunk(i);
-            u32x4 x = kraw[i];
-            kbuf[b][k_at(m, 2 * c)] = __builtin_bit_cast(u32x4, widen(x[0], x[1]));
-            kbuf[b][k_at(m, 2 * c + 1)] = __builtin_bit_cast(u32x4, widen(x[2], x[3]));
-            x = vraw[i];
-            const int d = v_chan(i), g = v_group(i);
-            // values that no row sees are whatever memory holds: zeroed, as 0 * NaN is NaN
-            if (vp[i] < 0) {
-                x = u32x4{0, 0, 0, 0};
-            } else if (partial_tile(t)) {
-                const int k0 = t * KT + 16 * g;
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    x[w] &= byte_mask(k0 + 4 * w, lo_any, hi_any);
-                    const uint32_t nan = nan_bytes(x[w]);
-                    if (nan) {
-                        marked = 1;
-                        mark_nan<D>(marks, nan, d, k0 + 4 * w, rend - r0, sees);
-                        x[w] &= ~((nan >> 7) * 0xFFu);
-                    }
-                }
-            }
-            vbuf[b][v_at(d, 2 * g)] = __builtin_bit_cast(u32x4, widen(x[0], x[1]));
-            vbuf[b][v_at(d, 2 * g + 1)] = __builtin_bit_cast(u32x4, widen(x[2], x[3]));
+            const int m = (kkey[i] & ~31) | swap23(kkey[i] & 31), c = kch[i];
+            const bool odd = (c >= D / 32) != (second != 0);
+            const uint32_t w0 = odd ? kraw[i][2] : kraw[i][0], w1 = odd ? kraw[i][3] : kraw[i][1];
+            sh.k[b][k_at(m, 2 * c + odd)] = __builtin_bit_cast(u32x4, widen(w0, w1));
         }
-        if (tid < NG) {
-            // logits of a missing page are NaN; unseen groups are masked
-            meta[b][tid][0] = mp == MISSING ? __builtin_nanf("") : (mp == UNSEEN ? 0.0f : mk * scale);
-            meta[b][tid][1] = mp < 0 ? 1.0f : mv;
+    };
+    // Values of tile t that no row sees are whatever memory holds: zeroed, as
+    // 0 * NaN is NaN; only in a tile that not every row sees whole.
+    auto mask_v = [&](int t) {
+        const int key0 = tile(t) * KT;
+        if (key0 >= lo_all && key0 + KT <= hi_all) return;
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const int key = key0 + 16 * vgr[i] + 4 * w;
+                uint32_t x = vraw[i][w] & byte_mask(key, lo_any, hi_any);
+                const uint32_t nan = held(vp[i]) ? nan_bytes(x) : 0u;
+                if (nan) {
+                    sh.marked = 1;
+                    mark_nan<D>(sh.marks, nan, vch[i], key, rend - r0, row_sees);
+                    x &= ~((nan >> 7) * 0xFFu);
+                }
+                vraw[i][w] = x;
+            }
+    };
+    auto store_v = [&](int b, int second) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const uint32_t keep = held(vp[i]) ? ~0u : 0u;
+            sh.v[b][v_at(vch[i], 2 * vgr[i] + second)] = __builtin_bit_cast(u32x4, widen(vraw[i][2 * second] & keep, vraw[i][2 * second + 1] & keep));
+        }
+    };
+    // The factor of a group's logits (scale, log2 e, key scale) and the scale of
+    // its values: logits of a missing page are NaN, keys that no row sees are masked.
+    float tc = 0.0f, tv = 1.0f;   // WIDE: those of tile t in iteration t
+    auto store_meta = [&](int t) {
+        if constexpr (WIDE) {
+            tc = held(mp) ? mk * scale : __builtin_nanf("");
+            tv = held(mp) ? mv : 1.0f;
+        } else {   // (every thread stores its group's, the same ones)
+            const int key = tile(t) * KT + 16 * (tid % NG);
+            const bool is = held(mp), see = seen(key);
+            sh.meta[t & 3][tid % NG][0] = is ? mk * scale : (see ? __builtin_nanf("") : 0.0f);
+            sh.meta[t & 3][tid % NG][1] = is && see ? mv : 1.0f;
         }
     };
 
@@ -188,69 +240,140 @@ __global__ __launch_bounds__(THREADS, 2) void cache_prompt_kernel(CacheAttnParam
     // m: the reference of the exponentials; l: of this lane's keys.  A row that sees keys beyond the table's reach is NaN.
     float m = NEG_INF, l = (p.causal && pos + 1 < sq.all ? pos + 1 : sq.all) > sq.len ? __builtin_nanf("") : 0.0f;
 
-    for (int i = tid; i < ManyRows::ROWS * (D / 32); i += THREADS) marks[0][i] = 0;
-    if (tid == 0) marked = 0;
+    for (int i = tid; i < ManyRows::ROWS * (D / 32); i += THREADS) sh.marks[0][i] = 0;
+    if (tid == 0) sh.marked = 0;
+    // what the products of the first tile's predecessor read
+    for (int i = tid; i < D * (VU + 1); i += THREADS) sh.v[(beg + 1) & 1][i] = u32x4{0, 0, 0, 0};
     __syncthreads();
     if (beg < end) {
-        look_up(beg);
-        load(beg);
-        if (beg + 1 < end) look_up(beg + 1);
-        store(beg, 0);
-        if (beg + 1 < end) {
-            load(beg + 1);
-            if (beg + 2 < end) look_up(beg + 2);
+        if constexpr (WIDE) {
+            look_up(beg);
+            page0 = uniform(ahead);
+            look_up(beg + 1);
+            page1 = uniform(ahead);
+            look_up(beg + 2);
+            load_k(beg, page0);
+            load_v(beg, page0);
+            load_meta(page0);
+            store_k(beg & 1, 0);
+            store_k(beg & 1, 1);
+            mask_v(beg);
+            load_k(beg + 1, page1);
+        } else {
+            look_up_k(beg);
+            look_up_v(beg);
+            look_up_meta(beg);
+            load_k(beg, 0);
+            load_v(beg, 0);
+            load_meta(0);
+            look_up_k(beg + 1);
+            look_up_v(beg + 1);
+            look_up_meta(beg + 1);
+            store_k(beg & 1, 0);
+            store_k(beg & 1, 1);
+            store_meta(beg);
+            mask_v(beg);
+            load_k(beg + 1, 0);
+            load_meta(0);
+            look_up_k(beg + 2);
+            look_up_meta(beg + 2);
         }
-        __syncthreads();
     }
-    for (int t = beg; t < end; ++t) {
-        const int b = (t - beg) & 1;
-        if (t + 1 < end) {
-            store(t + 1, b ^ 1);
-            if (t + 2 < end) {
-                load(t + 2);
-                if (t + 3 < end) look_up(t + 3);
+    __syncthreads();
+    const bool behind = wave >= WAVES / 2;
+    if (behind) __syncthreads();
+
+    f32x16 s[NB];
+    bf16x8 pf[NG];
+    // the stores of iteration t and the loads of the next one's, in pieces
+    constexpr int PIECES = 9;
+    auto stage = [&](int t, int piece) {
+        switch (piece) {
+        case 0: store_v(t & 1, 0); break;
+        case 1: store_v(t & 1, 1); break;
+        case 2: store_k(t + 1 & 1, 0); break;
+        case 3: store_k(t + 1 & 1, 1); break;
+        case 4:
+            store_meta(WIDE ? t : t + 1);
+            if (WIDE) page2 = uniform(ahead);
+            break;
+        case 5: load_v(t + 1, page1); break;
+        case 6: load_k(t + 2, page2); break;
+        case 7: load_meta(page1); break;
+        default:
+            if constexpr (WIDE) {
+                page0 = page1;
+                page1 = page2;
+                look_up(t + 3);
+            } else {
+                look_up_v(t + 2), look_up_k(t + 3), look_up_meta(t + 3);
             }
         }
-        const int key0 = t * KT;
-        if (active && key0 < whi_any && key0 + KT > wlo_any) {
-            f32x16 s[NB];
+    };
+    // whether some row of the wave sees some key of the tile
+    auto visible = [&](int t) { return active && t * KT < whi_any && t * KT + KT > wlo_any; };
 #pragma unroll
-            for (int i = 0; i < NB; ++i) {
+    for (int g = 0; g < NG; ++g) pf[g] = __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
+    for (int t = beg; t <= end && beg < end; ++t) {
+        const bool now = t < end && visible(t);
+        // (Also for tiles that no row of the wave sees: their logits are left unused, their probabilities 0, and their values
+        // hold no NaN, as not every row sees them.)
+        {
+            // Operands come from LDS AHEAD products before they are used;
+            // neighbouring products are on different accumulators.
+            constexpr int OV = DB * NG, ALL = OV + NB * D / 16, EVERY = ALL / PIECES;
+            bf16x8 a[AHEAD];
+            auto operand = [&](int i) {
+                return __builtin_bit_cast(bf16x8, i < OV ? sh.v[t + 1 & 1][v_at(32 * (i % DB) + n, 2 * (i / DB) + half)]
+                                                         : sh.k[t & 1][k_at(32 * ((i - OV) % NB) + n, 2 * ((i - OV) / NB) + half)]);
+            };
+#pragma unroll
+            for (int i = 0; i < NB; ++i)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) s[i][e] = 0.0f;
-                const int r = 32 * i + n;
 #pragma unroll
-                for (int k = 0; k < D / 16; ++k) {
-                    const bf16x8 a = __builtin_bit_cast(bf16x8, kbuf[b][k_at(r, 2 * k + half)]);
-                    s[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[k], s[i], 0, 0, 0);
-                }
-            }
-            float c[NG], vs[NG];
+            for (int i = 0; i < AHEAD; ++i) a[i] = operand(i);
 #pragma unroll
-            for (int g = 0; g < NG; ++g) {
-                c[g] = meta[b][g][0];
-                vs[g] = meta[b][g][1];
+            for (int i = 0; i < ALL; ++i) {
+                if (i < OV) o[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i % AHEAD], pf[i / DB], o[i % DB], 0, 0, 0);
+                else s[(i - OV) % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i % AHEAD], qf[(i - OV) / NB], s[(i - OV) % NB], 0, 0, 0);
+                if (i + AHEAD < ALL) a[i % AHEAD] = operand(i + AHEAD);
+                if (i % EVERY == EVERY - 1 && i / EVERY < PIECES) stage(t, i / EVERY);
+                __builtin_amdgcn_sched_barrier(0x0006);   // (only vector and scalar arithmetic may move past)
             }
-            const bool partial = key0 < wlo_all || key0 + KT > whi_all;
+        }
+        __syncthreads();
+        if (now) {
+            const int key0 = t * KT;
+            constexpr int CG = WIDE ? 1 : NG;   // groups with factors of their own
+            float c[CG], vs[CG];
+#pragma unroll
+            for (int g = 0; g < CG; ++g) {
+                c[g] = WIDE ? tc : sh.meta[t & 3][g][0];
+                vs[g] = WIDE ? tv : sh.meta[t & 3][g][1];
+            }
             // logits of group g: s[g / 2][8 (g % 2) + j], key 16 g + 8 half + j
-            if (partial) {
+            if (key0 < wlo_all || key0 + KT > whi_all) {
 #pragma unroll
-                for (int g = 0; g < NG; ++g) {
+                for (int g = 0; g < NG; ++g)
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
                         const int key = key0 + 16 * g + 8 * half + j;
-                        const float x = s[g / 2][8 * (g & 1) + j] * c[g];
-                        s[g / 2][8 * (g & 1) + j] = key < lo || key >= hi ? NEG_INF : x;
+                        const float y = s[g / 2][8 * (g & 1) + j] * c[g % CG];
+                        s[g / 2][8 * (g & 1) + j] = key < lo || key >= hi ? NEG_INF : y;
                     }
-                    c[g] = 1.0f;
-                }
+#pragma unroll
+                for (int g = 0; g < CG; ++g) c[g] = 1.0f;
             }
             float mt = NEG_INF;
 #pragma unroll
-            for (int g = 0; g < NG; ++g) {
-                float mg = s[g / 2][8 * (g & 1)];
+            for (int g = 0; g < CG; ++g) {
+                float mg = NEG_INF;
 #pragma unroll
-                for (int j = 1; j < 8; ++j) mg = fmaxf(mg, s[g / 2][8 * (g & 1) + j]);
+                for (int j = 0; j < KT / 2 / CG; j += 2) {
+                    const int e = KT / 2 / CG * g + j;
+                    mg = fmaxf(fmaxf(mg, s[e / 16][e % 16]), s[e / 16][e % 16 + 1]);
+                }
                 mt = fmaxf(mt, mg * c[g]);
             }
             mt = fmaxf(mt, __shfl_xor(mt, 32, 64));
@@ -264,40 +387,45 @@ __global__ __launch_bounds__(THREADS, 2) void cache_prompt_kernel(CacheAttnParam
                     for (int e = 0; e < 16; ++e) o[i][e] *= alpha;
             }
             const float ms = m == NEG_INF ? 0.0f : m;   // (a row that has seen no key yet)
-            bf16x8 pf[NG];
-#pragma unroll
-            for (int g = 0; g < NG; ++g) {
-                float x[8], sum = 0.0f;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    x[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[g / 2][8 * (g & 1) + j], c[g], -ms));
-                    sum += x[j];
-                }
-                l += sum;
-                u32x4 w;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) w[e] = pack2(x[2 * e] * vs[g], x[2 * e + 1] * vs[g]);
-                pf[g] = __builtin_bit_cast(bf16x8, w);
-            }
-#pragma unroll
-            for (int i = 0; i < DB; ++i) {
-                const int d = 32 * i + n;
+            // probabilities of all groups: exp2(s c - ref), summed into l times `unit`, times vs in the operand
+            auto exponentials = [&](float ref, float unit, bool scaled) {
 #pragma unroll
                 for (int g = 0; g < NG; ++g) {
-                    const bf16x8 a = __builtin_bit_cast(bf16x8, vbuf[b][v_at(d, 2 * g + half)]);
-                    o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pf[g], o[i], 0, 0, 0);
+                    float y[8], sum = 0.0f;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        y[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[g / 2][8 * (g & 1) + j], c[g % CG], -ref));
+                        sum += y[j];
+                    }
+                    l = __builtin_fmaf(sum, unit, l);
+                    u32x4 w;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        w[e] = scaled ? pack2(y[2 * e], y[2 * e + 1]) : pack2(y[2 * e] * vs[g % CG], y[2 * e + 1] * vs[g % CG]);
+                    pf[g] = __builtin_bit_cast(bf16x8, w);
                 }
-            }
+            };
+            // One value scale for the tile goes into the exponent (a power of
+            // two, so that the sum has it divided out exactly), if it leaves
+            // the smallest probabilities that count (2^-60) far above fp32's.
+            if (WIDE && vs[0] > 0x1p-64f && vs[0] < 0x1p64f) exponentials(ms - __builtin_amdgcn_logf(vs[0]), 1.0f / vs[0], true);
+            else exponentials(ms, 1.0f, false);
         }
+        if (!now) {
+#pragma unroll
+            for (int g = 0; g < NG; ++g) pf[g] = __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
+        }
+        mask_v(t + 1);
         __syncthreads();
     }
+    if (!behind) __syncthreads();
     if (!active) return;
     l += __shfl_xor(l, 32, 64);
     if (w0 + n >= rend) return;
-    if (marked) {
+    if (sh.marked) {
 #pragma unroll
         for (int i = 0; i < DB; ++i) {
-            const uint32_t nan = marks[32 * wave + n][i] >> (4 * half);
+            const uint32_t nan = sh.marks[32 * wave + n][i] >> (4 * half);
 #pragma unroll
             for (int e = 0; e < 16; ++e) o[i][e] = nan >> (8 * (e >> 2) + (e & 3)) & 1u ? __builtin_nanf("") : o[i][e];
         }
@@ -309,11 +437,11 @@ __global__ __launch_bounds__(THREADS, 2) void cache_prompt_kernel(CacheAttnParam
         for (int i = 0; i < DB; ++i)
 #pragma unroll
             for (int a = 0; a < 4; ++a)
-                *reinterpret_cast<f32x4 *>(p.part + at * D + 32 * i + 8 * a + 4 * half) =
+                *reinterpret_cast<f32x4 *>(p.part[1] + at * D + 32 * i + 8 * a + 4 * half) =
                     f32x4{o[i][4 * a], o[i][4 * a + 1], o[i][4 * a + 2], o[i][4 * a + 3]};
         if (half == 0) {
-            p.part_ml[at * 2] = m;
-            p.part_ml[at * 2 + 1] = l;
+            p.part_ml[1][at * 2] = m;
+            p.part_ml[1][at * 2 + 1] = l;
         }
         return;
     }
@@ -328,17 +456,47 @@ __global__ __launch_bounds__(THREADS, 2) void cache_prompt_kernel(CacheAttnParam
     if (half == 0) p.lse[orow] = l == 0.0f ? NEG_INF : (m + __builtin_amdgcn_logf(l)) * LN2;
 }
 
+template <int D, int KT, bool WIDE>
+__global__ __launch_bounds__(THREADS, 2) void cache_prompt_kernel(CacheAttnParams p)
+{
+    __shared__ PromptShared<D, KT> sh;
+    cache_prompt<D, KT, WIDE>(p, (int)blockIdx.x, sh);
+}
+
+// Both forms side by side: a batch of chunks and single tokens.
+template <int D, int KT, int KF, bool WIDE>
+__global__ __launch_bounds__(THREADS, 2) void cache_mixed_kernel(CacheAttnParams p)
+{
+    constexpr size_t A = sizeof(PromptShared<D, KT>), B = sizeof(FewShared<D, WAVES>);
+    __shared__ __attribute__((aligned(16))) char sh[A > B ? A : B];
+    const int x = (int)blockIdx.x;
+    if (x < p.units[1]) cache_prompt<D, KT, WIDE>(p, x, *reinterpret_cast<PromptShared<D, KT> *>(sh));
+    else cache_few<D, KF, WAVES>(p, x - p.units[1], *reinterpret_cast<FewShared<D, WAVES> *>(sh));
+}
+
+template <int D, int KT, int KF, bool WIDE>
+hipError_t launch(const CacheAttnParams &p, hipStream_t s)
+{
+    if (p.units[0]) cache_mixed_kernel<D, KT, KF, WIDE><<<dim3((unsigned)(p.units[0] + p.units[1])), THREADS, 0, s>>>(p);
+    else cache_prompt_kernel<D, KT, WIDE><<<dim3((unsigned)p.units[1]), THREADS, 0, s>>>(p);
+    return hipGetLastError();
+}
+
+template <int D, int KT, int KF>
+hipError_t launch_any(const CacheAttnParams &p, hipStream_t s)
+{
+    return 1 << p.b.page_shift >= KT ? launch<D, KT, KF, true>(p, s) : launch<D, KT, KF, false>(p, s);
+}
+
 } // namespace
 
 hipError_t launch_cache_prompt(int D, const CacheAttnParams &p, hipStream_t s)
 {
-    const dim3 grid((unsigned)max_units<ManyRows>(p));
     switch (D) {
-    case 64: cache_prompt_kernel<64, 64><<<grid, THREADS, 0, s>>>(p); break;
-    case 128: cache_prompt_kernel<128, 64><<<grid, THREADS, 0, s>>>(p); break;
-    default: cache_prompt_kernel<256, 32><<<grid, THREADS, 0, s>>>(p); break;
+    case 64: return launch_any<64, 64, 64>(p, s);
+    case 128: return launch_any<128, 64, 64>(p, s);
+    default: return launch_any<256, 32, 32>(p, s);
     }
-    return hipGetLastError();
 }
 
 } // namespace lamp

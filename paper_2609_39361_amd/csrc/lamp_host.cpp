@@ -894,12 +894,13 @@ int lamp_get_sim_tables(int device, uint16_t *sim8, uint32_t *sim16)
 
 static bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
-// Rows of d channels with 16-byte loads: the pointer and every stride.
-static int check_rows(const char *name, const void *p, bool f32, const int64_t *strides, int n)
+// Rows of d channels with 16-byte loads: the pointer and every stride of more
+// than one index.
+static int check_rows(const char *name, const void *p, bool f32, const int64_t *strides, const int64_t *sizes, int n)
 {
     if (!p) return fail(LAMP_ERR_INVALID_ARG, "null pointer: %s", name);
     bool ok = aligned16(p);
-    for (int i = 0; i < n; ++i) ok = ok && strides[i] % (f32 ? 4 : 8) == 0;
+    for (int i = 0; i < n; ++i) ok = ok && (sizes[i] <= 1 || strides[i] % (f32 ? 4 : 8) == 0);
     if (!ok) return fail(LAMP_ERR_INVALID_ARG, "%s: rows are not aligned to 16 bytes", name);
     return LAMP_OK;
 }
@@ -950,8 +951,9 @@ int lamp_qk_norm_rope(const lamp_rows *in, const lamp_rows *out, int B, int N, i
         heads += in[i].heads;
         if (in[i].heads == 0) continue;
         const int64_t is[3] = {in[i].batch, in[i].token, in[i].head}, os[3] = {out[i].batch, out[i].token, out[i].head};
-        rc = check_rows(names[i], in[i].p, in_f32 != 0, is, 3);
-        if (!rc) rc = check_rows(names[i], out[i].p, false, os, 3);
+        const int64_t sizes[3] = {B, N, in[i].heads};
+        rc = check_rows(names[i], in[i].p, in_f32 != 0, is, sizes, 3);
+        if (!rc) rc = check_rows(names[i], out[i].p, false, os, sizes, 3);
         if (rc) return rc;
         p.in[i] = {in[i].p, in[i].batch, in[i].token, in[i].head};
         p.out[i] = {static_cast<uint16_t *>(out[i].p), out[i].batch, out[i].token, out[i].head};
@@ -1008,9 +1010,9 @@ int lamp_kv_append(const void *k, const void *v, int in_f32, int64_t k_token, in
     if (rc) return rc;
     if (k_gain && !aligned16(k_gain)) return fail(LAMP_ERR_INVALID_ARG, "gain not aligned to 16 bytes");
     if (batch->S == 0 || batch->T == 0) return LAMP_OK;
-    const int64_t ks[2] = {k_token, k_head}, vs[2] = {v_token, v_head};
-    rc = check_rows("k", k, in_f32 != 0, ks, 2);
-    if (!rc) rc = check_rows("v", v, in_f32 != 0, vs, 2);
+    const int64_t ks[2] = {k_token, k_head}, vs[2] = {v_token, v_head}, sizes[2] = {batch->T, cache->Hkv};
+    rc = check_rows("k", k, in_f32 != 0, ks, sizes, 2);
+    if (!rc) rc = check_rows("v", v, in_f32 != 0, vs, sizes, 2);
     if (rc) return rc;
     p.k = k;
     p.v = v;
@@ -1056,8 +1058,8 @@ int lamp_attn_cache(const uint16_t *q, int64_t q_token, int64_t q_head, int Hq, 
     if ((int64_t)batch->T * Hq > (int64_t)1 << 27 || Hq > 65536)
         return fail(LAMP_ERR_UNSUPPORTED, "T*Hq above 2^27 or Hq above 65536");
     if (batch->S == 0 || batch->T == 0) return LAMP_OK;
-    const int64_t qs[2] = {q_token, q_head};
-    rc = check_rows("q", q, false, qs, 2);
+    const int64_t qs[2] = {q_token, q_head}, sizes[2] = {batch->T, Hq};
+    rc = check_rows("q", q, false, qs, sizes, 2);
     if (rc) return rc;
     if (!o || !lse) return fail(LAMP_ERR_INVALID_ARG, "null pointer among o, lse");
     if (!aligned16(o)) return fail(LAMP_ERR_INVALID_ARG, "o not aligned to 16 bytes");
@@ -1076,6 +1078,7 @@ int lamp_attn_cache(const uint16_t *q, int64_t q_token, int64_t q_head, int Hq, 
     p.scale_log2 = (float)(scale * 1.4426950408889634);
     const size_t need = lamp::cache_attn_workspace(cache->d, batch->T, batch->S, Hq / cache->Hkv, cache->Hkv,
                                                    (int64_t)batch->width * cache->page);
+    void *base = nullptr;
     if (need > 0) {
         lamp_fwd_extra extra{};
         extra.workspace = workspace;
@@ -1083,12 +1086,10 @@ int lamp_attn_cache(const uint16_t *q, int64_t q_token, int64_t q_head, int Hq, 
         int dev = 0;
         rc = current_device(&dev);
         if (rc) return rc;
-        void *base = nullptr;
         rc = call_ws(dev, &extra, need, static_cast<hipStream_t>(stream), &base);
         if (rc) return rc;
-        p.part = static_cast<float *>(base);
     }
-    HIP_TRY(lamp::launch_cache_attn(cache->d, p, static_cast<hipStream_t>(stream)));
+    HIP_TRY(lamp::launch_cache_attn(cache->d, p, base, static_cast<hipStream_t>(stream)));
     return LAMP_OK;
 }
 

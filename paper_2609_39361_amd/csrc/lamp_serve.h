@@ -70,19 +70,24 @@ struct CacheAttnParams {
     const float *ks, *vs;
     uint16_t *o;              // [T][Hq][D] bf16
     float *lse;               // [T][Hq]
-    float *part;              // partial outputs of split row tiles: [slots][rows of a tile][D] (workspace)
-    float *part_ml;           // their running maxima and sums [slots][rows of a tile][2]
     int Hq, causal, window;
     float scale_log2;         // logit scale times log2(e)
-    int64_t rows_above, rows_upto;   // the launch takes the sequences with this many rows (new tokens times heads of a group)
-    int slots;                // partial outputs that the workspace holds
+    // By form of the kernel (lamp_cache_plan.h; 0: few rows a sequence, 1: many).
+    int rows_above[2], rows_upto[2];   // it takes the sequences with this many rows (new tokens times heads of a group)
+    int units[2];             // workgroups: no lengths give more
+    int slots[2];             // partial outputs of split row tiles that the workspace holds: likewise
+    int *counts;              // those that this call has (workspace)
+    void *info[2];            // [slots] PartInfo (workspace)
+    float *part[2];           // [slots][rows of a tile][D] (workspace)
+    float *part_ml[2];        // their running maxima and sums [slots][rows of a tile][2] (workspace)
 };
 
 // Bytes of workspace a call over sequences of at most `keys` keys needs.
 size_t cache_attn_workspace(int D, int64_t T, int64_t S, int G, int Hkv, int64_t keys);
-// p.part: that workspace (null where it needs none).
-hipError_t launch_cache_attn(int D, const CacheAttnParams &p, hipStream_t s);
-// The form for many rows a sequence (lamp_cache_prompt.hip), of launch_cache_attn.
+// ws: that workspace (null where it needs none).  Fills in p from units on.
+hipError_t launch_cache_attn(int D, CacheAttnParams &p, void *ws, hipStream_t s);
+// The kernel with the form for many rows (lamp_cache_prompt.hip), and, where
+// p.units[0] > 0, that for few beside it; of launch_cache_attn.
 hipError_t launch_cache_prompt(int D, const CacheAttnParams &p, hipStream_t s);
 
 } // namespace lamp

@@ -6,10 +6,10 @@ library must have been built (python -m paper_2609_39361_amd.build); there is
 no fallback path.
 """
 import collections
-import contextlib
 import ctypes
 import math
 import os
+import struct
 
 import torch
 
@@ -336,38 +336,28 @@ def attn_decode(q, k, v, causal=True, window=0, tk=64, delta=2.0 ** -8, tau=0.5,
 
 
 # --- serving: norms with rotation, the 8-bit paged cache, attention over it ----
+# A serving step makes these calls once a layer, so that the host's time counts:
+# each has one test of everything a call must be, and names what is wrong only
+# where that fails; the C structs are packed bytes.
 
-class Rows(ctypes.Structure):
-    """struct lamp_rows (include/lamp.h)."""
-    _fields_ = [("p", ctypes.c_void_p), ("batch", ctypes.c_int64), ("token", ctypes.c_int64), ("head", ctypes.c_int64),
-                ("heads", ctypes.c_int)]
-
-
-class _Cache(ctypes.Structure):
-    """struct lamp_cache (include/lamp.h)."""
-    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
-                ("pages", ctypes.c_int), ("Hkv", ctypes.c_int), ("page", ctypes.c_int), ("d", ctypes.c_int)]
-
-
-class _Batch(ctypes.Structure):
-    """struct lamp_batch (include/lamp.h)."""
-    _fields_ = [("table", ctypes.c_void_p), ("table_stride", ctypes.c_int64), ("kv_lens", ctypes.c_void_p),
-                ("q_start", ctypes.c_void_p), ("S", ctypes.c_int), ("T", ctypes.c_int), ("width", ctypes.c_int)]
-
+_ROWS3 = struct.Struct("@" + "Pqqqi0P" * 3)   # struct lamp_rows [3] (include/lamp.h)
+_CACHE = struct.Struct("@PPPPiiii")            # struct lamp_cache
+_BATCH = struct.Struct("@PqPPiii0P")           # struct lamp_batch
 
 # An 8-bit paged cache: codes k [pages,Hkv,page,d] and v [pages,Hkv,d,page] (float8_e4m3fn, V
 # transposed within its page), scales k_scale and v_scale [pages,Hkv] (fp32 powers of two)
 KVCache = collections.namedtuple("KVCache", "k v k_scale v_scale")
 
-_FLOATS = (torch.bfloat16, torch.float32)
+_BF16, _F32, _I32, _E4M3 = torch.bfloat16, torch.float32, torch.int32, torch.float8_e4m3fn
+_FLOATS = (_BF16, _F32)
 
 
 def kv_cache(pages, Hkv, d, page=64, device="cuda"):
     """An empty KVCache of `pages` pages of `page` tokens (zero codes and scales)."""
     z = dict(device=device)
-    return KVCache(torch.zeros((pages, Hkv, page, d), dtype=torch.uint8, **z).view(torch.float8_e4m3fn),
-                   torch.zeros((pages, Hkv, d, page), dtype=torch.uint8, **z).view(torch.float8_e4m3fn),
-                   torch.zeros((pages, Hkv), dtype=torch.float32, **z), torch.zeros((pages, Hkv), dtype=torch.float32, **z))
+    return KVCache(torch.zeros((pages, Hkv, page, d), dtype=torch.uint8, **z).view(_E4M3),
+                   torch.zeros((pages, Hkv, d, page), dtype=torch.uint8, **z).view(_E4M3),
+                   torch.zeros((pages, Hkv), dtype=_F32, **z), torch.zeros((pages, Hkv), dtype=_F32, **z))
 
 
 def rope_table(n, rot, base=1e6, device="cuda"):
@@ -378,35 +368,44 @@ def rope_table(n, rot, base=1e6, device="cuda"):
     return torch.cat([ang.cos(), ang.sin()], dim=-1).float()
 
 
-def _on(device):
-    """The device made current, if it is not."""
-    return contextlib.nullcontext() if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+def _call(dev, fn, *args):
+    """One library call on the current stream of CUDA device `dev` (an index)."""
+    if torch.cuda.current_device() == dev:
+        _check(fn(*args, torch._C._cuda_getCurrentRawStream(dev)))
+    else:
+        with torch.cuda.device(dev):
+            _check(fn(*args, torch._C._cuda_getCurrentRawStream(dev)))
 
 
-def _check_tensor(t, name, dtypes, device, shape=None):
-    """A CUDA tensor on `device` of one of `dtypes`, contiguous in its last dimension (`shape`: of that shape, dense)."""
-    if not isinstance(t, torch.Tensor) or t.dtype not in dtypes or t.device != device:
-        raise ValueError("%s must be a %s tensor on %s" % (name, " or ".join(str(x) for x in dtypes), device))
-    if shape is not None and (t.shape != shape or not t.is_contiguous()):
+def _must(t, name, dtypes, dev, shape=None):
+    """Refuses what is not a tensor of `dtypes` on CUDA device `dev`, contiguous in its last dimension (`shape`: of that
+    shape, dense)."""
+    if not isinstance(t, torch.Tensor) or t.dtype not in dtypes or t.get_device() != dev or dev < 0:
+        raise ValueError("%s must be a %s tensor on CUDA device %d" % (name, " or ".join(str(x) for x in dtypes), max(dev, 0)))
+    if shape is not None and (tuple(t.shape) != tuple(shape) or not t.is_contiguous()):
         raise ValueError("%s must be contiguous, of shape %s" % (name, tuple(shape)))
     if t.dim() and t.stride(-1) != 1 and t.shape[-1] > 1:
         raise ValueError("%s must be contiguous in its last dimension" % name)
 
 
-def _strides(t):
-    """Strides in elements; 0 where only one index exists."""
-    return tuple(s if n > 1 else 0 for s, n in zip(t.stride(), t.shape))
+def _gain(w, name, dev, d):
+    """(pointer, whether fp32) of a gain."""
+    if w is None:
+        return None, 0
+    if w.get_device() != dev or w.shape != (d,) or not w.is_contiguous() or w.dtype not in _FLOATS:
+        _must(w, name, _FLOATS, dev, (d,))
+    return w.data_ptr(), 1 if w.dtype is _F32 else 0
 
 
-def _check_norm_rope(dev, d, gains, rope):
-    for name, w in gains:
-        if w is not None:
-            _check_tensor(w, name, _FLOATS, dev, (d,))
-    if rope is not None:
-        _check_tensor(rope, "rope", (torch.float32,), dev)
-        if rope.dim() != 2 or not rope.is_contiguous():
-            raise ValueError("rope must be a contiguous [positions, rot] table")
-    return (None, 0, 0) if rope is None else (rope.data_ptr(), rope.shape[0], rope.shape[1])
+def _rope(rope, dev):
+    """(pointer, positions, rotated channels) of a table."""
+    if rope is None:
+        return None, 0, 0
+    if rope.dtype is not _F32 or rope.get_device() != dev or rope.dim() != 2 or not rope.is_contiguous():
+        _must(rope, "rope", (_F32,), dev)
+        raise ValueError("rope must be a contiguous [positions, rot] table")
+    n, rot = rope.shape
+    return rope.data_ptr(), n, rot
 
 
 def qk_norm_rope(q, k=None, v=None, q_weight=None, k_weight=None, rope=None, positions=None, eps=1e-6, out=None):
@@ -419,82 +418,100 @@ def qk_norm_rope(q, k=None, v=None, q_weight=None, k_weight=None, rope=None, pos
     `positions`: int32 [B,N] or [T]; default 0 .. N-1.  v is laid out (and rounded) with them.  `out`: the
     tensors to write into (None where the input is None), of the outputs' shapes with any strides; tokens
     may be written in place.  Returns (q, k, v), None for what was not given."""
-    ins = (q, k, v)
-    if not isinstance(q, torch.Tensor) or q.dim() not in (3, 4) or not q.is_cuda or q.dtype not in _FLOATS:
+    if not isinstance(q, torch.Tensor) or not q.is_cuda or q.dim() not in (3, 4) or q.dtype not in _FLOATS:
         raise ValueError("q must be a bf16 or fp32 CUDA tensor [B,N,Hq,d] or [T,Hq,d]")
-    dev, prompt, d = q.device, q.dim() == 4, q.shape[-1]
-    lead = q.shape[:-2]
-    B, N = lead if prompt else (1, lead[0])
-    for t, name in zip(ins, "qkv"):
-        if t is not None:
-            _check_tensor(t, name, (q.dtype,), dev)
-            if t.dim() != q.dim() or t.shape[:-2] != lead or t.shape[-1] != d:
-                raise ValueError("%s shape %s does not match q %s" % (name, tuple(t.shape), tuple(q.shape)))
+    dev, shape, dtype = q.get_device(), q.shape, q.dtype
+    if len(shape) == 4:
+        B, N, Hq, d = shape
+        prompt = True
+    else:
+        N, Hq, d = shape
+        B, prompt = 1, False
+    qw, q32 = _gain(q_weight, "q_weight", dev, d)
+    kw, k32 = _gain(k_weight, "k_weight", dev, d)
+    table, npos, rot = _rope(rope, dev)
+    if positions is not None:
+        if positions.dtype is not _I32 or positions.get_device() != dev or positions.shape != shape[:-2] \
+                or not positions.is_contiguous():
+            _must(positions, "positions", (_I32,), dev, shape[:-2])
+    rows_in, rows_out, outs = [], [], []
+    for i, t in enumerate((q, k, v)):
+        o = None if out is None else out[i]
+        if t is None:
+            if o is not None:
+                raise ValueError("out must hold one tensor for each input")
+            rows_in += (0, 0, 0, 0, 0)
+            rows_out += (0, 0, 0, 0, 0)
+            outs.append(None)
+            continue
+        if i:
+            if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.get_device() != dev:
+                _must(t, "qkv"[i], (dtype,), dev)
+            if t.dim() != len(shape) or t.shape[:-2] != shape[:-2] or t.shape[-1] != d:
+                raise ValueError("%s shape %s does not match q %s" % ("qkv"[i], tuple(t.shape), tuple(shape)))
+        if t.stride(-1) != 1:
+            _must(t, "qkv"[i], (dtype,), dev)
+        H = t.shape[-2]
+        want = (B, H, N, d) if prompt else (N, H, d)
+        if o is None:
+            if out is not None:
+                raise ValueError("out must hold one tensor for each input")
+            o = torch.empty(want, dtype=_BF16, device=q.device)
+        else:
+            _must(o, "out[%d]" % i, (_BF16,), dev)
+            if o.shape != want:
+                raise ValueError("out[%d] must be of shape %s" % (i, want))
+        outs.append(o)
+        if prompt:
+            b, n, h, _ = t.stride()
+            rows_in += (t.data_ptr(), b, n, h, H)
+            b, h, n, _ = o.stride()
+        else:
+            n, h, _ = t.stride()
+            rows_in += (t.data_ptr(), 0, n, h, H)
+            b, (n, h, _) = 0, o.stride()
+        rows_out += (o.data_ptr(), b, n, h, H)
     if k is not None and v is not None and k.shape != v.shape:
         raise ValueError("v shape %s differs from k %s" % (tuple(v.shape), tuple(k.shape)))
-    table, npos, rot = _check_norm_rope(dev, d, (("q_weight", q_weight), ("k_weight", k_weight)), rope)
-    if positions is not None:
-        _check_tensor(positions, "positions", (torch.int32,), dev, lead)
-    outs = []
-    for i, t in enumerate(ins):
-        o = None if out is None else out[i]
-        shape = None if t is None else ((B, t.shape[2], N, d) if prompt else tuple(t.shape))
-        if (t is None) != (o is None) and out is not None:
-            raise ValueError("out must hold one tensor for each input")
-        if o is not None:
-            _check_tensor(o, "out[%d]" % i, (torch.bfloat16,), dev)
-            if tuple(o.shape) != shape:
-                raise ValueError("out[%d] must be of shape %s" % (i, shape))
-        elif t is not None:
-            o = torch.empty(shape, dtype=torch.bfloat16, device=dev)
-        outs.append(o)
-    if B * N and q.shape[-2]:
-        ri, ro = (Rows * 3)(), (Rows * 3)()
-        for i, (t, o) in enumerate(zip(ins, outs)):
-            if t is not None:
-                st, so = _strides(t), _strides(o)
-                if prompt:
-                    ri[i] = (t.data_ptr(), st[0], st[1], st[2], t.shape[2])
-                    ro[i] = (o.data_ptr(), so[0], so[2], so[1], t.shape[2])
-                else:
-                    ri[i] = (t.data_ptr(), 0, st[0], st[1], t.shape[1])
-                    ro[i] = (o.data_ptr(), 0, so[0], so[1], t.shape[1])
-        f32 = torch.float32
-        with _on(dev):
-            _check(lib().lamp_qk_norm_rope(
-                ri, ro, B, N, d, int(q.dtype == f32), None if q_weight is None else q_weight.data_ptr(),
-                None if k_weight is None else k_weight.data_ptr(),
-                int(q_weight is not None and q_weight.dtype == f32) + 2 * int(k_weight is not None and k_weight.dtype == f32),
-                table, npos, rot, None if positions is None else positions.data_ptr(), float(eps), _stream(dev)))
+    if B * N and d:
+        _call(dev, lib().lamp_qk_norm_rope, _ROWS3.pack(*rows_in), _ROWS3.pack(*rows_out), B, N, d,
+              1 if dtype is _F32 else 0, qw, kw, q32 + 2 * k32, table, npos, rot,
+              None if positions is None else positions.data_ptr(), eps)
     return tuple(outs)
 
 
 def _paged(cache, block_table, kv_lens, q_start, T):
-    """(lamp_cache, lamp_batch) of a call, checked."""
+    """(lamp_cache, lamp_batch, device, Hkv, page, d, S, width) of a call, checked."""
     kc, vc, ks, vs = cache
     if not isinstance(kc, torch.Tensor) or kc.dim() != 4 or not kc.is_cuda:
         raise ValueError("cache.k must be a float8_e4m3fn CUDA tensor [pages,Hkv,page,d]")
-    dev = kc.device
+    dev = kc.get_device()
     pages, Hkv, page, d = kc.shape
-    fp8 = (torch.float8_e4m3fn,)
-    _check_tensor(kc, "cache.k", fp8, dev, kc.shape)
-    _check_tensor(vc, "cache.v", fp8, dev, (pages, Hkv, d, page))
-    _check_tensor(ks, "cache.k_scale", (torch.float32,), dev, (pages, Hkv))
-    _check_tensor(vs, "cache.v_scale", (torch.float32,), dev, (pages, Hkv))
-    i32 = (torch.int32,)
-    _check_tensor(block_table, "block_table", i32, dev)
-    if block_table.dim() != 2:
-        raise ValueError("block_table must be [S, pages of a sequence]")
+    if not (kc.dtype is _E4M3 and vc.dtype is _E4M3 and ks.dtype is _F32 and vs.dtype is _F32
+            and vc.get_device() == dev and ks.get_device() == dev and vs.get_device() == dev
+            and vc.shape == (pages, Hkv, d, page) and ks.shape == (pages, Hkv) and vs.shape == (pages, Hkv)
+            and kc.is_contiguous() and vc.is_contiguous() and ks.is_contiguous() and vs.is_contiguous()):
+        _must(kc, "cache.k", (_E4M3,), dev, kc.shape)
+        _must(vc, "cache.v", (_E4M3,), dev, (pages, Hkv, d, page))
+        _must(ks, "cache.k_scale", (_F32,), dev, (pages, Hkv))
+        _must(vs, "cache.v_scale", (_F32,), dev, (pages, Hkv))
+    if not isinstance(block_table, torch.Tensor) or block_table.dim() != 2:
+        raise ValueError("block_table must be an int32 tensor [S, pages of a sequence]")
     S, width = block_table.shape
-    _check_tensor(kv_lens, "kv_lens", i32, dev, (S,))
+    if not (block_table.dtype is _I32 and kv_lens.dtype is _I32 and block_table.get_device() == dev
+            and kv_lens.get_device() == dev and kv_lens.shape == (S,) and kv_lens.is_contiguous()
+            and (width < 2 or block_table.stride(1) == 1)):
+        _must(block_table, "block_table", (_I32,), dev)
+        _must(kv_lens, "kv_lens", (_I32,), dev, (S,))
     if q_start is not None:
-        _check_tensor(q_start, "q_start", i32, dev, (S + 1,))
+        if not (q_start.dtype is _I32 and q_start.get_device() == dev and q_start.shape == (S + 1,)
+                and q_start.is_contiguous()):
+            _must(q_start, "q_start", (_I32,), dev, (S + 1,))
     elif T != S:
         raise ValueError("without q_start there is one token for each of the %d sequences, not %d" % (S, T))
-    c = _Cache(kc.data_ptr(), vc.data_ptr(), ks.data_ptr(), vs.data_ptr(), pages, Hkv, page, d)
-    b = _Batch(block_table.data_ptr(), block_table.stride(0), kv_lens.data_ptr(),
-               None if q_start is None else q_start.data_ptr(), S, T, width)
-    return c, b, dev
+    return (_CACHE.pack(kc.data_ptr(), vc.data_ptr(), ks.data_ptr(), vs.data_ptr(), pages, Hkv, page, d),
+            _BATCH.pack(block_table.data_ptr(), block_table.stride(0), kv_lens.data_ptr(),
+                        0 if q_start is None else q_start.data_ptr(), S, T, width), dev, Hkv, page, d, S, width)
 
 
 def kv_append(k, v, cache, block_table, kv_lens, q_start=None, k_weight=None, rope=None, eps=1e-6):
@@ -508,18 +525,18 @@ def kv_append(k, v, cache, block_table, kv_lens, q_start=None, k_weight=None, ro
     is read on the device, so that a captured call follows lengths that change.  Returns the cache."""
     if not isinstance(k, torch.Tensor) or not isinstance(v, torch.Tensor) or k.dim() != 3 or k.shape != v.shape:
         raise ValueError("k and v [T,Hkv,d] expected")
-    c, b, dev = _paged(cache, block_table, kv_lens, q_start, k.shape[0])
-    _check_tensor(k, "k", _FLOATS, dev)
-    _check_tensor(v, "v", (k.dtype,), dev)
-    if k.shape[1:] != (c.Hkv, c.d):
-        raise ValueError("k of %d heads and d = %d, a cache of %d and %d" % (k.shape[1], k.shape[2], c.Hkv, c.d))
-    table, npos, rot = _check_norm_rope(dev, c.d, (("k_weight", k_weight),), rope)
-    f32 = torch.float32
-    with _on(dev):
-        _check(lib().lamp_kv_append(
-            k.data_ptr(), v.data_ptr(), int(k.dtype == f32), *_strides(k)[:2], *_strides(v)[:2],
-            ctypes.byref(c), ctypes.byref(b), None if k_weight is None else k_weight.data_ptr(),
-            int(k_weight is not None and k_weight.dtype == f32), table, npos, rot, float(eps), _stream(dev)))
+    T, H, dk = k.shape
+    c, b, dev, Hkv, _, d, _, _ = _paged(cache, block_table, kv_lens, q_start, T)
+    dtype = k.dtype
+    if not (dtype in _FLOATS and v.dtype is dtype and k.get_device() == dev and v.get_device() == dev
+            and k.stride(2) == 1 and v.stride(2) == 1):
+        _must(k, "k", _FLOATS, dev)
+        _must(v, "v", (dtype,), dev)
+    if H != Hkv or dk != d:
+        raise ValueError("k of %d heads and d = %d, a cache of %d and %d" % (H, dk, Hkv, d))
+    w, w32 = _gain(k_weight, "k_weight", dev, d)
+    _call(dev, lib().lamp_kv_append, k.data_ptr(), v.data_ptr(), 1 if dtype is _F32 else 0, *k.stride()[:2], *v.stride()[:2], c, b,
+          w, w32, *_rope(rope, dev), eps)
     return cache
 
 
@@ -540,30 +557,30 @@ def attn_cache(q, cache, block_table, kv_lens, q_start=None, causal=True, window
     tensor of attn_cache_workspace_size(...) bytes; by default one of torch's, on the current stream."""
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
         raise ValueError("q [T,Hq,d] expected")
-    T, Hq, d = q.shape
-    c, b, dev = _paged(cache, block_table, kv_lens, q_start, T)
-    _check_tensor(q, "q", (torch.bfloat16,), dev)
-    if d != c.d:
-        raise ValueError("q of d = %d, a cache of %d" % (d, c.d))
+    T, Hq, dq = q.shape
+    c, b, dev, Hkv, page, d, S, width = _paged(cache, block_table, kv_lens, q_start, T)
+    if q.dtype is not _BF16 or q.get_device() != dev or q.stride(2) != 1:
+        _must(q, "q", (_BF16,), dev)
+    if dq != d:
+        raise ValueError("q of d = %d, a cache of %d" % (dq, d))
     if out is None:
-        o = torch.empty((T, Hq, d), dtype=torch.bfloat16, device=dev)
-        lse = torch.empty((T, Hq), dtype=torch.float32, device=dev)
+        o, lse = q.new_empty((T, Hq, d)), torch.empty((T, Hq), dtype=_F32, device=q.device)
     else:
         o, lse = out
-        _check_out(o, "o", (T, Hq, d), torch.bfloat16, dev)
-        _check_out(lse, "lse", (T, Hq), torch.float32, dev)
+        _must(o, "o", (_BF16,), dev, (T, Hq, d))
+        _must(lse, "lse", (_F32,), dev, (T, Hq))
     L = lib()
     if workspace is None:
-        need = L.lamp_attn_cache_workspace_size(T, b.S, Hq, c.Hkv, d, c.page, b.width)
-        workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
-    elif workspace.device != dev or not workspace.is_contiguous():
+        need = L.lamp_attn_cache_workspace_size(T, S, Hq, Hkv, d, page, width)
+        if need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous tensor on the inputs' device")
-    with _on(dev):
-        _check(L.lamp_attn_cache(
-            q.data_ptr(), *_strides(q)[:2], Hq, ctypes.byref(c), ctypes.byref(b), int(causal), int(window),
-            d ** -0.5 if scale is None else float(scale), o.data_ptr(), lse.data_ptr(),
-            None if workspace is None else workspace.data_ptr(),
-            0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(dev)))
+    else:
+        need = workspace.numel() * workspace.element_size()
+    _call(dev, L.lamp_attn_cache, q.data_ptr(), *q.stride()[:2], Hq, c, b, 1 if causal else 0, window,
+          d ** -0.5 if scale is None else scale, o.data_ptr(), lse.data_ptr(),
+          None if workspace is None else workspace.data_ptr(), need)
     return o, lse
 
 

@@ -21,10 +21,7 @@ def _err():
 
 
 def _rows(q=(4096, 512, 128, 64, 4), k=(4096, 512, 128, 64, 2), v=(4096, 512, 128, 64, 2)):
-    r = (lamp.Rows * 3)()
-    for i, x in enumerate((q, k, v)):
-        r[i] = x
-    return r
+    return lamp._ROWS3.pack(*q, *k, *v)
 
 
 def _norm(rin=None, rout=None, B=1, N=3, d=64, f32=0, qw=4096, kw=4096, bits=0, rope=4096, npos=8, rot=64, pos=None, eps=1e-6):
@@ -57,20 +54,20 @@ def test_norm_rope_refusals():
 
 
 def _cache(k=4096, v=4096, ks=4096, vs=4096, pages=4, H=2, page=64, d=64):
-    return lamp._Cache(k, v, ks, vs, pages, H, page, d)
+    return lamp._CACHE.pack(k, v, ks, vs, pages, H, page, d)
 
 
 def _batch(table=4096, stride=4, kv=4096, st=4096, S=2, T=5, width=4):
-    return lamp._Batch(table, stride, kv, st, S, T, width)
+    return lamp._BATCH.pack(table, stride, kv, st, S, T, width)
 
 
 def _append(c=None, b=None, k=4096, v=4096, f32=0, strides=(128, 64, 128, 64), w=4096, rope=4096, npos=8, rot=64, eps=1e-6):
-    return lamp.lib().lamp_kv_append(P(k), P(v), f32, *strides, ctypes.byref(c or _cache()), ctypes.byref(b or _batch()), P(w), 0,
+    return lamp.lib().lamp_kv_append(P(k), P(v), f32, *strides, c or _cache(), b or _batch(), P(w), 0,
                                      P(rope), npos, rot, eps, None)
 
 
 def _attn(c=None, b=None, q=4096, strides=(256, 64), Hq=4, causal=1, window=0, scale=0.125, o=4096, lse=4096, ws=None, n=0):
-    return lamp.lib().lamp_attn_cache(P(q), *strides, Hq, ctypes.byref(c or _cache()), ctypes.byref(b or _batch()), causal, window,
+    return lamp.lib().lamp_attn_cache(P(q), *strides, Hq, c or _cache(), b or _batch(), causal, window,
                                       scale, P(o), P(lse), ws, n, None)
 
 
@@ -120,8 +117,8 @@ def test_attention_workspace_size():
     assert size(0, 1, 32, 8, 128, 64, 500) == 0 and size(1, 1, 3, 2, 128, 64, 500) == 0
     assert size(1, 1, 32, 8, 96, 64, 500) == 0 and size(1, 1, 32, 8, 128, 48, 500) == 0
     assert size(1, 1, 32, 8, 128, 256, 1 << 23) == 0
-    # bounded whatever the batch
-    assert size(1 << 20, 1 << 10, 64, 8, 256, 256, 1 << 12) <= 64 << 20
+    # bounded whatever the batch: at most 512 partial outputs of 256 rows and 1024 of 16, each of d + 2 numbers, and what names them
+    assert size(1 << 20, 1 << 10, 64, 8, 256, 256, 1 << 12) <= (512 * 256 + 1024 * 16) * 258 * 4 + 1536 * 32 + 8 * 256
 
 
 def test_binding_refuses_cpu_tensors():
