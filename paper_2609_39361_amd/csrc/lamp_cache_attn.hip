@@ -27,48 +27,90 @@ __global__ __launch_bounds__(256) void cache_few_kernel(CacheAttnParams p)
 
 // The pieces of the rows of split row tiles joined.  The workgroups of a row
 // tile's c partial outputs share its rows, the k-th those with row % c = k.
-// Few rows (many pieces): a workgroup's waves take the pieces in turn, a row
-// after another; many rows (few pieces): MANY_BY workgroups for each partial
-// output, a wave takes whole rows.  A lane holds D/64 channels.
+// Few rows (many pieces): a workgroup's waves take the pieces in turn, 16 at
+// once each, a row after another; a lane holds D/64 channels.  Many rows (few
+// pieces): MANY_BY workgroups for each partial output, 16 lanes a row.  Bound
+// by latency: the loads of a step do not wait for each other.
 constexpr int MANY_BY = 8;
 
+__device__ __forceinline__ float join_lse(float m, float sum)
+{
+    return sum == 0.0f ? NEG_INF : (m + __builtin_amdgcn_logf(sum)) * LN2;
+}
+
 template <int D>
-__global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnParams p)
+__device__ __forceinline__ void join_many(const CacheAttnParams &p, const PartInfo &i, int slot0, int by, int G)
+{
+    constexpr int C = D / 16;
+    const int lane = threadIdx.x & 15;
+    const float *part = p.part[1], *ml = p.part_ml[1];
+    for (int r = i.piece + i.pieces * (by * 16 + ((int)threadIdx.x >> 4)); r < i.rows; r += i.pieces * 16 * MANY_BY) {
+        const int64_t base = (int64_t)slot0 * ManyRows::ROWS + r;
+        float m = NEG_INF, sum = 0.0f, v[C] = {};
+        for (int c0 = 0; c0 < i.pieces; c0 += 4) {
+            float mc[4], lc[4];
+            f32x4 o[4][C / 4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {   // (beyond the last: read again, weight 0)
+                const int64_t at = base + (int64_t)(c0 + k < i.pieces ? c0 + k : c0) * ManyRows::ROWS;
+                mc[k] = ml[at * 2];
+                lc[k] = ml[at * 2 + 1];
+#pragma unroll
+                for (int e = 0; e < C / 4; ++e) o[k][e] = *reinterpret_cast<const f32x4 *>(part + at * D + C * lane + 4 * e);
+            }
+            float mn = m;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) mn = fmaxf(mn, mc[k]);
+            const float ms = mn == NEG_INF ? 0.0f : mn, f0 = __builtin_amdgcn_exp2f(m - ms);
+            m = mn;
+            sum *= f0;
+#pragma unroll
+            for (int e = 0; e < C; ++e) v[e] *= f0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (c0 + k < i.pieces) {
+                    const float f = __builtin_amdgcn_exp2f(mc[k] - ms);
+                    sum += lc[k] * f;
+#pragma unroll
+                    for (int e = 0; e < C; ++e) v[e] += o[k][e / 4][e % 4] * f;
+                }
+            }
+        }
+        const int gr = i.row0 + r, t = gr / G;
+        const int64_t orow = (int64_t)(i.token + t) * p.Hq + i.head * G + gr - t * G;
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+#pragma unroll
+        for (int e = 0; e < C; e += 4)
+            *reinterpret_cast<u32x2 *>(p.o + orow * D + C * lane + e) = u32x2{pack2(v[e] * inv, v[e + 1] * inv), pack2(v[e + 2] * inv, v[e + 3] * inv)};
+        if (lane == 0) p.lse[orow] = join_lse(m, sum);
+    }
+}
+
+template <int D>
+__device__ __forceinline__ void join_few(const CacheAttnParams &p, const PartInfo &i, int slot0, int G)
 {
     constexpr int C = D / 64;
     __shared__ float obuf[4 * D], lbuf[4];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), G = p.Hq / p.b.Hkv;
-    const bool many = (int)blockIdx.x >= p.slots[0];
-    const int form = many ? 1 : 0, x = many ? ((int)blockIdx.x - p.slots[0]) / MANY_BY : (int)blockIdx.x;
-    const int tile_rows = many ? ManyRows::ROWS : FewRows::ROWS;
-    if (x >= p.counts[form]) return;
-    const PartInfo i = static_cast<const PartInfo *>(p.info[form])[x];
-    // (whatever tables that break their rules leave here, nothing outside the arrays is touched)
-    const int slot0 = x - i.piece;
-    if (i.piece < 0 || i.pieces <= i.piece || slot0 < 0 || i.pieces > p.slots[form] - slot0 || i.head < 0 || i.head >= p.b.Hkv || i.token < 0
-        || i.row0 < 0 || i.rows < 0 || i.rows > tile_rows || i.token + (i.row0 + (int64_t)i.rows - 1) / G >= p.b.T)
-        return;
-    const float *part = p.part[form], *ml = p.part_ml[form];
-    const int share = many ? ((int)blockIdx.x - p.slots[0]) % MANY_BY * 4 + wave : 0, shares = many ? 4 * MANY_BY : 1;
-    const int first = many ? 0 : wave, step = many ? 1 : 4;   // the wave's pieces
-    for (int r = i.piece + i.pieces * share; r < i.rows; r += i.pieces * shares) {
-        const int64_t base = (int64_t)slot0 * tile_rows + r;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const float *part = p.part[0], *ml = p.part_ml[0];
+    for (int r = i.piece; r < i.rows; r += i.pieces) {
+        const int64_t base = (int64_t)slot0 * FewRows::ROWS + r;
         float mx = NEG_INF;
-        for (int c = lane; c < i.pieces; c += 64) mx = fmaxf(mx, ml[(base + (int64_t)c * tile_rows) * 2]);
+        for (int c = lane; c < i.pieces; c += 64) mx = fmaxf(mx, ml[(base + (int64_t)c * FewRows::ROWS) * 2]);
 #pragma unroll
         for (int k = 1; k < 64; k <<= 1) mx = fmaxf(mx, __shfl_xor(mx, k, 64));
         const float ms = mx == NEG_INF ? 0.0f : mx;
         float sum = 0.0f, v[C] = {};
         // rounds of 16 of the wave's pieces, whose weights 16 lanes work out
-        for (int c0 = first; c0 < i.pieces; c0 += 16 * step) {
-            const int c = c0 + (lane & 15) * step;
-            const int64_t at = (base + (int64_t)(c < i.pieces ? c : 0) * tile_rows) * 2;
+        for (int c0 = wave; c0 < i.pieces; c0 += 64) {
+            const int c = c0 + (lane & 15) * 4;
+            const int64_t at = (base + (int64_t)(c < i.pieces ? c : 0) * FewRows::ROWS) * 2;
             const float f = c < i.pieces ? __builtin_amdgcn_exp2f(ml[at] - ms) : 0.0f;
             const float fl = c < i.pieces ? ml[at + 1] * f : 0.0f;
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
-                if (c0 + j * step < i.pieces) {
-                    const float *o = part + (base + (int64_t)(c0 + j * step) * tile_rows) * D + C * lane;
+                if (c0 + 4 * j < i.pieces) {
+                    const float *o = part + (base + (int64_t)(c0 + 4 * j) * FewRows::ROWS) * D + C * lane;
                     const float fj = __builtin_bit_cast(float, lane_value(__builtin_bit_cast(int, f), j));
                     sum += __builtin_bit_cast(float, lane_value(__builtin_bit_cast(int, fl), j));
 #pragma unroll
@@ -76,32 +118,48 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnParams p)
                 }
             }
         }
-        if (!many) {
-            __syncthreads();   // (the row before has been read)
+        __syncthreads();   // (the row before has been read)
 #pragma unroll
-            for (int e = 0; e < C; ++e) obuf[wave * D + C * lane + e] = v[e];
-            if (lane == 0) lbuf[wave] = sum;
-            __syncthreads();
-            if (wave != 0) continue;
-            sum = lbuf[0] + lbuf[1] + lbuf[2] + lbuf[3];
-#pragma unroll
-            for (int e = 0; e < C; ++e) {
-                const int d = C * lane + e;
-                v[e] = obuf[d] + obuf[D + d] + obuf[2 * D + d] + obuf[3 * D + d];
-            }
-        }
+        for (int e = 0; e < C; ++e) obuf[wave * D + C * lane + e] = v[e];
+        if (lane == 0) lbuf[wave] = sum;
+        __syncthreads();
+        if (wave != 0) continue;
+        sum = lbuf[0] + lbuf[1] + lbuf[2] + lbuf[3];
         const int gr = i.row0 + r, t = gr / G;
         const int64_t orow = (int64_t)(i.token + t) * p.Hq + i.head * G + gr - t * G;
         const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
         uint16_t *o = p.o + orow * D + C * lane;
+#pragma unroll
+        for (int e = 0; e < C; ++e) {
+            const int d = C * lane + e;
+            v[e] = (obuf[d] + obuf[D + d] + obuf[2 * D + d] + obuf[3 * D + d]) * inv;
+        }
         if constexpr (C == 1) {
-            *o = (uint16_t)pack2(v[0] * inv, 0.0f);
+            *o = (uint16_t)pack2(v[0], 0.0f);
         } else {
 #pragma unroll
-            for (int e = 0; e < C; e += 2) *reinterpret_cast<uint32_t *>(o + e) = pack2(v[e] * inv, v[e + 1] * inv);
+            for (int e = 0; e < C; e += 2) *reinterpret_cast<uint32_t *>(o + e) = pack2(v[e], v[e + 1]);
         }
-        if (lane == 0) p.lse[orow] = sum == 0.0f ? NEG_INF : (mx + __builtin_amdgcn_logf(sum)) * LN2;
+        if (lane == 0) p.lse[orow] = join_lse(mx, sum);
     }
+}
+
+template <int D>
+__global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnParams p)
+{
+    const int G = p.Hq / p.b.Hkv, b = (int)blockIdx.x - p.slots[0];
+    const bool many = b >= 0;
+    const int form = many ? 1 : 0, x = many ? b / MANY_BY : (int)blockIdx.x;
+    const int count = p.counts[form];
+    const PartInfo i = static_cast<const PartInfo *>(p.info[form])[x];   // (of this call where x < count)
+    // (whatever tables that break their rules leave here, nothing outside the arrays is touched)
+    const int slot0 = x - i.piece;
+    if (x >= count || i.piece < 0 || i.pieces <= i.piece || slot0 < 0 || i.pieces > p.slots[form] - slot0 || i.head < 0 || i.head >= p.b.Hkv
+        || i.token < 0 || i.row0 < 0 || i.rows < 0 || i.rows > (many ? ManyRows::ROWS : FewRows::ROWS)
+        || i.token + (i.row0 + (int64_t)i.rows - 1) / G >= p.b.T)
+        return;
+    if (many) join_many<D>(p, i, slot0, b % MANY_BY, G);
+    else join_few<D>(p, i, slot0, G);
 }
 
 template <int D, int KT>

@@ -41,15 +41,19 @@ constexpr int WAVES = 8, THREADS = 64 * WAVES;
 // and o is rescaled a few times a row instead of at every tile.
 constexpr float LAZY = 8.0f;
 
-constexpr int AHEAD = 6;   // operands in flight from LDS
-
 __device__ __forceinline__ int swap23(int m)
 {
     return (m & ~12) | ((m & 4) << 1) | ((m & 8) >> 1);
 }
 
+// Operands of the queries that are read from LDS: at d = 256 registers hold
+// half of them beside o.
+template <int D>
+constexpr int Q_LDS = D > 128 ? D / 32 : 0;
+
 template <int D, int KT>
 struct PromptShared {
+    u32x4 q[WAVES][Q_LDS<D> ? Q_LDS<D> : 1][Q_LDS<D> ? 64 : 1];
     u32x4 k[2][KT * (D / 8 + 1)];
     u32x4 v[2][D * (KT / 8 + 1)];
     float meta[4][KT / 16][2];                        // logit factor (scale, log2 e, key scale) and value scale of each group of 16 keys
@@ -98,7 +102,9 @@ __device__ __forceinline__ void cache_prompt(const CacheAttnParams &p, int x, Pr
     const int wpmin = sq.pos0 + w0 / G, wpmax = sq.pos0 + wlast / G;
     const int whi_any = upto(wpmax), wlo_any = from(wpmin), whi_all = upto(wpmin), wlo_all = from(wpmax);
 
-    bf16x8 qf[D / 16];
+    constexpr int QR = D / 16 - Q_LDS<D>;       // operands in registers
+    constexpr int AHEAD = D > 128 ? 4 : 8;      // operands in flight from LDS (4 beside d = 256's o: with 6 of them registers spill)
+    bf16x8 qf[QR];
     {
         const uint16_t *q = p.q + (int64_t)(sq.a + tok) * p.q_st + (int64_t)qh * p.q_sh + 8 * half;
 #pragma unroll
@@ -106,7 +112,8 @@ __device__ __forceinline__ void cache_prompt(const CacheAttnParams &p, int x, Pr
             u32x4 w = *reinterpret_cast<const u32x4 *>(q + 16 * k);
             // a negative scale as a negated query: factors of logits stay non-negative
             if (p.scale_log2 < 0.0f) w ^= 0x80008000u;
-            qf[k] = __builtin_bit_cast(bf16x8, w);
+            if (k < QR) qf[k] = __builtin_bit_cast(bf16x8, w);
+            else sh.q[wave][k - QR][lane] = w;
         }
     }
     const float scale = fabsf(p.scale_log2);
@@ -320,29 +327,36 @@ __device__ __forceinline__ void cache_prompt(const CacheAttnParams &p, int x, Pr
         // hold no NaN, as not every row sees them.)
         {
             // Operands come from LDS AHEAD products before they are used;
-            // neighbouring products are on different accumulators.
+            // neighbouring products are on different accumulators.  The phase
+            // has priority: its few instructions keep the matrix cores busy
+            // (8K prompt: 558 us with it, 580 without, 608 the other way round).
+            __builtin_amdgcn_s_setprio(1);
             constexpr int OV = DB * NG, ALL = OV + NB * D / 16, EVERY = ALL / PIECES;
-            bf16x8 a[AHEAD];
-            auto operand = [&](int i) {
-                return __builtin_bit_cast(bf16x8, i < OV ? sh.v[t + 1 & 1][v_at(32 * (i % DB) + n, 2 * (i / DB) + half)]
-                                                         : sh.k[t & 1][k_at(32 * ((i - OV) % NB) + n, 2 * ((i - OV) / NB) + half)]);
+            bf16x8 a[AHEAD], q[AHEAD];
+            auto read = [&](int i) {
+                const int k = (i - OV) / NB;
+                a[i % AHEAD] = __builtin_bit_cast(bf16x8, i < OV ? sh.v[t + 1 & 1][v_at(32 * (i % DB) + n, 2 * (i / DB) + half)]
+                                                                 : sh.k[t & 1][k_at(32 * ((i - OV) % NB) + n, 2 * k + half)]);
+                if (i >= OV && k >= QR) q[i % AHEAD] = __builtin_bit_cast(bf16x8, sh.q[wave][k - QR][lane]);
             };
 #pragma unroll
             for (int i = 0; i < NB; ++i)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) s[i][e] = 0.0f;
 #pragma unroll
-            for (int i = 0; i < AHEAD; ++i) a[i] = operand(i);
+            for (int i = 0; i < AHEAD; ++i) read(i);
 #pragma unroll
             for (int i = 0; i < ALL; ++i) {
-                if (i < OV) o[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i % AHEAD], pf[i / DB], o[i % DB], 0, 0, 0);
-                else s[(i - OV) % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i % AHEAD], qf[(i - OV) / NB], s[(i - OV) % NB], 0, 0, 0);
-                if (i + AHEAD < ALL) a[i % AHEAD] = operand(i + AHEAD);
+                const int k = (i - OV) / NB, at = i % AHEAD;
+                if (i < OV) o[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[at], pf[i / DB], o[i % DB], 0, 0, 0);
+                else s[(i - OV) % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[at], k < QR ? qf[k < QR ? k : 0] : q[at], s[(i - OV) % NB], 0, 0, 0);
+                if (i + AHEAD < ALL) read(i + AHEAD);
                 if (i % EVERY == EVERY - 1 && i / EVERY < PIECES) stage(t, i / EVERY);
                 __builtin_amdgcn_sched_barrier(0x0006);   // (only vector and scalar arithmetic may move past)
             }
         }
         __syncthreads();
+        __builtin_amdgcn_s_setprio(0);
         if (now) {
             const int key0 = t * KT;
             constexpr int CG = WIDE ? 1 : NG;   // groups with factors of their own
