@@ -222,17 +222,21 @@ struct PageWork {
 };
 
 // Sequence whose range of the non-decreasing starts f(0..S-1) holds x: the
-// last s with f(s) <= x.
+// last s with f(s) <= x, by the whole wave, 64 places at once (each round is
+// one load's latency).
 template <class F>
 __device__ __forceinline__ int last_at_most(int S, int64_t x, F f)
 {
-    int lo = 0, hi = S - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (f(mid) <= x) lo = mid;
-        else hi = mid - 1;
+    const int lane = threadIdx.x & 63;
+    int lo = 0, n = S;
+    for (;;) {
+        const int step = (n + 63) / 64;
+        const int at = lo + lane * step;
+        const uint64_t below = __ballot(lane == 0 || (lane * step < n && f(at) <= x));
+        lo += (63 - __builtin_clzll(below)) * step;
+        if (step == 1) return lo;
+        n = S - lo < step ? S - lo : step;
     }
-    return lo;
 }
 
 // Work of workgroup x.  By token: token x's page, if x is the first new token
@@ -266,19 +270,36 @@ __device__ PageWork page_work(const PagedBatch &b, int by_token, int x)
     return {pg, (int)(f - lo), (int)(end - f), (int)(a + (f - p0)), (int)f};
 }
 
+// Byte c of four words (4 codes of consecutive channels of 4 tokens) as the
+// words of 4 tokens of each channel.
+__device__ __forceinline__ void transpose4(uint32_t *w)
+{
+    const uint32_t a = __builtin_amdgcn_perm(w[1], w[0], 0x05010400u), b = __builtin_amdgcn_perm(w[1], w[0], 0x07030602u);
+    const uint32_t c = __builtin_amdgcn_perm(w[3], w[2], 0x05010400u), d = __builtin_amdgcn_perm(w[3], w[2], 0x07030602u);
+    w[0] = __builtin_amdgcn_perm(c, a, 0x05040100u);
+    w[1] = __builtin_amdgcn_perm(c, a, 0x07060302u);
+    w[2] = __builtin_amdgcn_perm(d, b, 0x05040100u);
+    w[3] = __builtin_amdgcn_perm(d, b, 0x07060302u);
+}
+
 // One workgroup writes the new keys (blockIdx.z 0) or values (1) of one page
 // and head: their largest magnitude, the page's scale (a power of two, so that
-// growing it keeps the codes already there), then the codes.  Values go
-// through an LDS tile that transposes them.  Bound by HBM for prompts (each
-// input read twice, the second time from the L2), by latency for single tokens.
-constexpr int VT = 64, VT_STRIDE = VT + 4;   // slots of the transposing tile, bytes of one of its rows
+// growing it keeps the codes already there), then the codes.  The finished
+// numbers stay in registers between the two (those of 64 tokens; longer pages
+// read the rest again).  Values go through an LDS tile row by row and come out
+// as 16 tokens of 4 channels a thread, transposed by byte permutes.  Bound by
+// HBM for prompts, by latency for single tokens.
+constexpr int VT = 64;       // slots of the transposing tile
 
-template <int D, bool F32>
+// LONG: pages of more than 64 tokens.
+template <int D, bool F32, bool LONG>
 __global__ __launch_bounds__(256) void kv_append_kernel(AppendParams p)
 {
     constexpr int LPR = D / 16, RPB = 256 / LPR;   // rows of one pass
+    constexpr int KEEP = D / 64;                   // rows of a thread in a page of 64
+    constexpr int STRIDE = D + 16;                 // bytes of a row of the tile
     __shared__ float red[4];
-    __shared__ uint32_t tile[D * VT_STRIDE / 4];
+    __shared__ u32x4 tile[VT * STRIDE / 16];
     const PageWork w = page_work(p.b, p.by_token, (int)blockIdx.x);
     if (w.count == 0) return;   // (the whole workgroup)
     const int tid = (int)threadIdx.x, head = (int)blockIdx.y, page = 1 << p.b.page_shift;
@@ -311,23 +332,32 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendParams p)
         }
         norm_rotate<D>(x, x + 8, normed, wa, wb, p.eps, ch.rotated, cs, sn);
     };
-    float m = 0.0f;
-    for (int i = tid / LPR; i < w.count; i += RPB) {
-        float x[16];
-        row(i, x);
+    float m = 0.0f, kept[KEEP][16];
+    auto widest = [&](const float *x) {
 #pragma unroll
         for (int c = 0; c < 16; ++c) m = finite(x[c]) ? fmaxf(m, fabsf(x[c])) : m;
+    };
+    const int i0 = tid / LPR;
+#pragma unroll
+    for (int k = 0; k < KEEP; ++k)
+        if (i0 + k * RPB < w.count) row(i0 + k * RPB, kept[k]);
+#pragma unroll
+    for (int k = 0; k < KEEP; ++k)
+        if (i0 + k * RPB < w.count) widest(kept[k]);
+    for (int i = i0 + KEEP * RPB; LONG && i < w.count; i += RPB) {
+        float x[16];
+        row(i, x);
+        widest(x);
     }
 #pragma unroll
     for (int k = 1; k < 64; k <<= 1) m = fmaxf(m, __shfl_xor(m, k, 64));
     if ((tid & 63) == 0) red[tid >> 6] = m;
-    __syncthreads();
-    m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
     float *scale = (is_v ? p.vs : p.ks) + w.page * p.b.Hkv + head;
     uint8_t *codes = (is_v ? p.vc : p.kc) + (w.page * p.b.Hkv + head) * (int64_t)page * D;
-    const float need = scale_for(m), old = *scale;
-    const float now = w.first > 0 && old > need ? old : need, inv = inv_pow2(now);
-    __syncthreads();   // every thread has the old scale
+    const float old = w.first > 0 ? *scale : 0.0f;
+    __syncthreads();   // (and every thread has the old scale)
+    m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    const float need = scale_for(m), now = w.first > 0 && old > need ? old : need, inv = inv_pow2(now);
     if (w.first > 0 && old < now) {
         // the codes of the slots before, under the new scale (in 16-byte units)
         const float ratio = old * inv;
@@ -356,43 +386,54 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendParams p)
         }
     }
     if (tid == 0) *scale = now;
-    if (!is_v) {
-        for (int i = tid / LPR; i < w.count; i += RPB) {
+    // the codes of row i: to the cache (keys) or to the tile of slots from t0 (values)
+    auto write = [&](int i, const float *x, int t0) {
+        uint8_t *c = is_v ? reinterpret_cast<uint8_t *>(tile) + (w.first + i - t0) * STRIDE : codes + (int64_t)(w.first + i) * D;
+        *reinterpret_cast<u32x2 *>(c + ch.c0) = u32x2{encode4(x, inv), encode4(x + 4, inv)};
+        *reinterpret_cast<u32x2 *>(c + ch.c1) = u32x2{encode4(x + 8, inv), encode4(x + 12, inv)};
+    };
+    // rows [a, e)
+    auto write_rows = [&](int a, int e, int t0) {
+#pragma unroll
+        for (int k = 0; k < KEEP; ++k)
+            if (i0 + k * RPB >= a && i0 + k * RPB < e) write(i0 + k * RPB, kept[k], t0);
+        for (int i = i0 + KEEP * RPB; LONG && i < e; i += RPB) {
+            if (i < a) continue;
             float x[16];
             row(i, x);
-            uint8_t *c = codes + (int64_t)(w.first + i) * D;
-            *reinterpret_cast<u32x2 *>(c + ch.c0) = u32x2{encode4(x, inv), encode4(x + 4, inv)};
-            *reinterpret_cast<u32x2 *>(c + ch.c1) = u32x2{encode4(x + 8, inv), encode4(x + 12, inv)};
+            write(i, x, t0);
         }
+    };
+    if (!is_v) {
+        write_rows(0, w.count, 0);
         return;
     }
-    uint8_t *tb = reinterpret_cast<uint8_t *>(tile);
     const int last = w.first + w.count;
     for (int t0 = w.first / VT * VT; t0 < last; t0 += VT) {
-        const int a = w.first > t0 ? w.first - t0 : 0, e = last - t0 < VT ? last - t0 : VT;   // slots [a, e) of this tile
+        const int a = w.first > t0 ? w.first : t0, e = last - t0 < VT ? last : t0 + VT;   // slots of this tile
         __syncthreads();   // the tile is free (and the rescaled codes are written)
-        for (int i = a + tid / LPR; i < e; i += RPB) {
-            float x[16];
-            row(t0 + i - w.first, x);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const uint32_t c = encode4(x + 4 * k, inv);
-                const int d = (k < 2 ? ch.c0 : ch.c1) + 4 * (k & 1);
-#pragma unroll
-                for (int q = 0; q < 4; ++q) tb[(d + q) * VT_STRIDE + i] = (uint8_t)(c >> (8 * q));
-            }
-        }
+        write_rows(a - w.first, e - w.first, t0);
         __syncthreads();
-        // words of 4 slots; single bytes where a word holds other slots
-        const int u0 = a / 4, un = (e + 3) / 4 - u0;
-        for (int u = tid; u < D * un; u += 256) {
-            const int d = u / un, s0 = (u0 + (u - d * un)) * 4;
-            uint8_t *c = codes + (int64_t)d * page + t0 + s0;
-            if (s0 >= a && s0 + 4 <= e) {
-                *reinterpret_cast<uint32_t *>(c) = tile[(d * VT_STRIDE + s0) / 4];
-            } else {
-                for (int q = 0; q < 4; ++q)
-                    if (s0 + q >= a && s0 + q < e) c[q] = tb[d * VT_STRIDE + s0 + q];
+        const int u0 = (a - t0) / 16, un = (e - t0 + 15) / 16 - u0;   // units of 16 slots
+        for (int u = tid; u < D / 4 * un; u += 256) {
+            const int c4 = u % (D / 4), s0 = (u0 + u / (D / 4)) * 16;
+            if (t0 + s0 >= a && t0 + s0 + 16 <= e) {
+                uint32_t x[4][4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x[i][j] = reinterpret_cast<const uint32_t *>(tile)[(s0 + 4 * i + j) * (STRIDE / 4) + c4];
+                    transpose4(x[i]);
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    *reinterpret_cast<u32x4 *>(codes + (int64_t)(4 * c4 + j) * page + t0 + s0) = u32x4{x[0][j], x[1][j], x[2][j], x[3][j]};
+            } else {   // a unit that holds other slots too
+                for (int s = t0 + s0 > a ? t0 + s0 : a; s < t0 + s0 + 16 && s < e; ++s) {
+                    const uint32_t x = reinterpret_cast<const uint32_t *>(tile)[(s - t0) * (STRIDE / 4) + c4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) codes[(int64_t)(4 * c4 + j) * page + s] = (uint8_t)(x >> (8 * j));
+                }
             }
         }
     }
@@ -419,6 +460,17 @@ hipError_t launch_norm_rope(int D, bool f32, const NormRopeParams &params, hipSt
     return hipGetLastError();
 }
 
+template <int D>
+static hipError_t launch_append(bool f32, const AppendParams &p, dim3 grid, hipStream_t s)
+{
+    if (1 << p.b.page_shift <= 64) {
+        f32 ? kv_append_kernel<D, true, false><<<grid, 256, 0, s>>>(p) : kv_append_kernel<D, false, false><<<grid, 256, 0, s>>>(p);
+    } else {
+        f32 ? kv_append_kernel<D, true, true><<<grid, 256, 0, s>>>(p) : kv_append_kernel<D, false, true><<<grid, 256, 0, s>>>(p);
+    }
+    return hipGetLastError();
+}
+
 hipError_t launch_kv_append(int D, bool f32, const AppendParams &params, hipStream_t s)
 {
     AppendParams p = params;
@@ -427,11 +479,10 @@ hipError_t launch_kv_append(int D, bool f32, const AppendParams &params, hipStre
     p.by_token = p.b.T <= slots;
     const dim3 grid((unsigned)(p.by_token ? p.b.T : slots), (unsigned)p.b.Hkv, 2);
     switch (D) {
-    case 64: f32 ? kv_append_kernel<64, true><<<grid, 256, 0, s>>>(p) : kv_append_kernel<64, false><<<grid, 256, 0, s>>>(p); break;
-    case 128: f32 ? kv_append_kernel<128, true><<<grid, 256, 0, s>>>(p) : kv_append_kernel<128, false><<<grid, 256, 0, s>>>(p); break;
-    default: f32 ? kv_append_kernel<256, true><<<grid, 256, 0, s>>>(p) : kv_append_kernel<256, false><<<grid, 256, 0, s>>>(p); break;
+    case 64: return launch_append<64>(f32, p, grid, s);
+    case 128: return launch_append<128>(f32, p, grid, s);
+    default: return launch_append<256>(f32, p, grid, s);
     }
-    return hipGetLastError();
 }
 
 } // namespace lamp
