@@ -90,49 +90,68 @@ template <int D>
 __device__ __forceinline__ void join_few(const CacheAttnParams &p, const PartInfo &i, int slot0, int G)
 {
     constexpr int C = D / 64;
-    __shared__ float obuf[4 * D], lbuf[4];
+    __shared__ float obuf[4 * D], mbuf[4], lbuf[4];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const float *part = p.part[0], *ml = p.part_ml[0];
     for (int r = i.piece; r < i.rows; r += i.pieces) {
         const int64_t base = (int64_t)slot0 * FewRows::ROWS + r;
-        float mx = NEG_INF;
-        for (int c = lane; c < i.pieces; c += 64) mx = fmaxf(mx, ml[(base + (int64_t)c * FewRows::ROWS) * 2]);
-#pragma unroll
-        for (int k = 1; k < 64; k <<= 1) mx = fmaxf(mx, __shfl_xor(mx, k, 64));
-        const float ms = mx == NEG_INF ? 0.0f : mx;
-        float sum = 0.0f, v[C] = {};
-        // rounds of 16 of the wave's pieces, whose weights 16 lanes work out
+        float m = NEG_INF, sum = 0.0f, v[C] = {};
         for (int c0 = wave; c0 < i.pieces; c0 += 64) {
+            // lane k % 16 has the maximum and sum of the round's piece k (beyond the last: none)
             const int c = c0 + (lane & 15) * 4;
-            const int64_t at = (base + (int64_t)(c < i.pieces ? c : 0) * FewRows::ROWS) * 2;
-            const float f = c < i.pieces ? __builtin_amdgcn_exp2f(ml[at] - ms) : 0.0f;
-            const float fl = c < i.pieces ? ml[at + 1] * f : 0.0f;
+            const int64_t at = (base + (int64_t)(c < i.pieces ? c : c0) * FewRows::ROWS) * 2;
+            const float mc = c < i.pieces ? ml[at] : NEG_INF, lc = ml[at + 1];
+            float o[16][C];
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+#pragma unroll
+                for (int e = 0; e < C; ++e)
+                    o[j][e] = part[(base + (int64_t)(c0 + 4 * j < i.pieces ? c0 + 4 * j : c0) * FewRows::ROWS) * D + C * lane + e];
+            float mn = mc;
+#pragma unroll
+            for (int k = 1; k < 16; k <<= 1) mn = fmaxf(mn, __shfl_xor(mn, k, 64));
+            mn = fmaxf(mn, m);
+            const float ms = mn == NEG_INF ? 0.0f : mn, f0 = __builtin_amdgcn_exp2f(m - ms);
+            const float f = __builtin_amdgcn_exp2f(mc - ms), fl = c < i.pieces ? lc * f : 0.0f;
+            m = mn;
+            sum *= f0;
+#pragma unroll
+            for (int e = 0; e < C; ++e) v[e] *= f0;
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
                 if (c0 + 4 * j < i.pieces) {
-                    const float *o = part + (base + (int64_t)(c0 + 4 * j) * FewRows::ROWS) * D + C * lane;
                     const float fj = __builtin_bit_cast(float, lane_value(__builtin_bit_cast(int, f), j));
                     sum += __builtin_bit_cast(float, lane_value(__builtin_bit_cast(int, fl), j));
 #pragma unroll
-                    for (int e = 0; e < C; ++e) v[e] += o[e] * fj;
+                    for (int e = 0; e < C; ++e) v[e] += o[j][e] * fj;
                 }
             }
         }
         __syncthreads();   // (the row before has been read)
 #pragma unroll
         for (int e = 0; e < C; ++e) obuf[wave * D + C * lane + e] = v[e];
-        if (lane == 0) lbuf[wave] = sum;
+        if (lane == 0) mbuf[wave] = m, lbuf[wave] = sum;
         __syncthreads();
         if (wave != 0) continue;
-        sum = lbuf[0] + lbuf[1] + lbuf[2] + lbuf[3];
+        m = fmaxf(fmaxf(mbuf[0], mbuf[1]), fmaxf(mbuf[2], mbuf[3]));
+        const float ms = m == NEG_INF ? 0.0f : m;
+        float f[4];
+        sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            f[w] = __builtin_amdgcn_exp2f(mbuf[w] - ms);
+            sum += lbuf[w] * f[w];
+        }
         const int gr = i.row0 + r, t = gr / G;
         const int64_t orow = (int64_t)(i.token + t) * p.Hq + i.head * G + gr - t * G;
         const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
         uint16_t *o = p.o + orow * D + C * lane;
 #pragma unroll
         for (int e = 0; e < C; ++e) {
-            const int d = C * lane + e;
-            v[e] = (obuf[d] + obuf[D + d] + obuf[2 * D + d] + obuf[3 * D + d]) * inv;
+            v[e] = 0.0f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) v[e] += obuf[w * D + C * lane + e] * f[w];
+            v[e] *= inv;
         }
         if constexpr (C == 1) {
             *o = (uint16_t)pack2(v[0], 0.0f);
@@ -140,7 +159,7 @@ __device__ __forceinline__ void join_few(const CacheAttnParams &p, const PartInf
 #pragma unroll
             for (int e = 0; e < C; e += 2) *reinterpret_cast<uint32_t *>(o + e) = pack2(v[e], v[e + 1]);
         }
-        if (lane == 0) p.lse[orow] = join_lse(mx, sum);
+        if (lane == 0) p.lse[orow] = join_lse(m, sum);
     }
 }
 
