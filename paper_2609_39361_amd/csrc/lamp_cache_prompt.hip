@@ -20,13 +20,14 @@
 // A wave alternates between a phase for the matrix cores (o += V^T P^T of the
 // tile before, then S^T of this one, with the widening and storing of its share
 // of the next tile between the products) and one for the vector unit (the
-// softmax of this tile).  A barrier ends every phase and the upper four waves,
-// which share the four SIMDs with the lower four, run one phase behind: while
-// one wave of a SIMD multiplies, the other exponentiates.  With phases numbered
-// so that the lower half multiplies for tile t in phase 2 t and the upper in
-// 2 t + 1, K of tile t + 1 and V of tile t are stored in phases 2 t and 2 t + 1
-// and read in 2 t + 2 and 2 t + 3; K of t - 1 and V of t - 2, whose buffers they
-// take, were last read in phase 2 t - 1: two buffers of each do.
+// softmax of this tile).  There is one barrier a tile, which the lower four
+// waves meet after the softmax and the upper four, which share the four SIMDs
+// with them, after the products: between two barriers the lower half multiplies
+// for tile t and then exponentiates, the upper exponentiates for tile t - 1 and
+// then multiplies for t, so that the two waves of a SIMD are at different units.
+// The products of tile t read K of tile t and V of t - 1 and store K of t + 1 and
+// V of t, in buffers whose former tiles were read before the last barrier: two
+// of each do.
 #include <hip/hip_runtime.h>
 
 #include "lamp_cache_few.h"
@@ -288,7 +289,6 @@ __device__ __forceinline__ void cache_prompt(const CacheAttnParams &p, int x, Pr
     }
     __syncthreads();
     const bool behind = wave >= WAVES / 2;
-    if (behind) __syncthreads();
 
     f32x16 s[NB];
     bf16x8 pf[NG];
@@ -355,8 +355,8 @@ __device__ __forceinline__ void cache_prompt(const CacheAttnParams &p, int x, Pr
                 __builtin_amdgcn_sched_barrier(0x0006);   // (only vector and scalar arithmetic may move past)
             }
         }
-        __syncthreads();
         __builtin_amdgcn_s_setprio(0);
+        if (behind) __syncthreads();
         if (now) {
             const int key0 = t * KT;
             constexpr int CG = WIDE ? 1 : NG;   // groups with factors of their own
@@ -422,7 +422,7 @@ __device__ __forceinline__ void cache_prompt(const CacheAttnParams &p, int x, Pr
             // One value scale for the tile goes into the exponent (a power of
             // two, so that the sum has it divided out exactly), if it leaves
             // the smallest probabilities that count (2^-60) far above fp32's.
-            if (WIDE && vs[0] > 0x1p-64f && vs[0] < 0x1p64f) exponentials(ms - __builtin_amdgcn_logf(vs[0]), 1.0f / vs[0], true);
+            if (WIDE && vs[0] > 0x1p-64f && vs[0] < 0x1p64f) exponentials(ms - __builtin_amdgcn_logf(vs[0]), __builtin_amdgcn_rcpf(vs[0]), true);
             else exponentials(ms, 1.0f, false);
         }
         if (!now) {
@@ -430,9 +430,8 @@ __device__ __forceinline__ void cache_prompt(const CacheAttnParams &p, int x, Pr
             for (int g = 0; g < NG; ++g) pf[g] = __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
         }
         mask_v(t + 1);
-        __syncthreads();
+        if (!behind) __syncthreads();
     }
-    if (!behind) __syncthreads();
     if (!active) return;
     l += __shfl_xor(l, 32, 64);
     if (w0 + n >= rend) return;
