@@ -476,7 +476,7 @@ def qk_norm_rope(q, k=None, v=None, q_weight=None, k_weight=None, rope=None, pos
     if B * N and d:
         _call(dev, lib().lamp_qk_norm_rope, _ROWS3.pack(*rows_in), _ROWS3.pack(*rows_out), B, N, d,
               1 if dtype is _F32 else 0, qw, kw, q32 + 2 * k32, table, npos, rot,
-              None if positions is None else positions.data_ptr(), eps)
+              None if positions is None else positions.data_ptr(), float(eps))
     return tuple(outs)
 
 
@@ -536,7 +536,7 @@ def kv_append(k, v, cache, block_table, kv_lens, q_start=None, k_weight=None, ro
         raise ValueError("k of %d heads and d = %d, a cache of %d and %d" % (H, dk, Hkv, d))
     w, w32 = _gain(k_weight, "k_weight", dev, d)
     _call(dev, lib().lamp_kv_append, k.data_ptr(), v.data_ptr(), 1 if dtype is _F32 else 0, *k.stride()[:2], *v.stride()[:2], c, b,
-          w, w32, *_rope(rope, dev), eps)
+          w, w32, *_rope(rope, dev), float(eps))
     return cache
 
 
@@ -578,8 +578,8 @@ def attn_cache(q, cache, block_table, kv_lens, q_start=None, causal=True, window
         raise ValueError("workspace must be a contiguous tensor on the inputs' device")
     else:
         need = workspace.numel() * workspace.element_size()
-    _call(dev, L.lamp_attn_cache, q.data_ptr(), *q.stride()[:2], Hq, c, b, 1 if causal else 0, window,
-          d ** -0.5 if scale is None else scale, o.data_ptr(), lse.data_ptr(),
+    _call(dev, L.lamp_attn_cache, q.data_ptr(), *q.stride()[:2], Hq, c, b, 1 if causal else 0, int(window),
+          d ** -0.5 if scale is None else float(scale), o.data_ptr(), lse.data_ptr(),
           None if workspace is None else workspace.data_ptr(), need)
     return o, lse
 
