@@ -99,54 +99,108 @@ __device__ __forceinline__ int lane_value(int v, int lane)
     return __builtin_amdgcn_readlane(v, lane);
 }
 
-// Unit x of form F (by every wave, the same in each).  The workgroup of unit 0
-// also writes how many partial outputs the form has.
+// What is known of a sequence (a lane's) to find a unit in it.
+struct Share {
+    int tiles, c, units, slots;   // row tiles, pieces of each, and theirs of all kv heads
+};
+
 template <class F>
+__device__ __forceinline__ Share share_of(const CacheAttnParams &p, const SeqPlan &r, int chunk)
+{
+    const int c = (r.kt + chunk - 1) / chunk, pieces = c < 1 ? 1 : c, units = r.tiles * p.b.Hkv * pieces;
+    return {r.tiles, pieces, units, pieces > 1 ? units : 0};
+}
+
+// Key tiles of a piece.
+template <class F>
+__device__ __forceinline__ int chunk_of(const CacheAttnParams &p, float total)
+{
+    // (rounded up by more than the sum's fp32 rounding, so that the bound of the units holds)
+    const float want = total * (float)p.b.Hkv * (1.0001f / F::TARGET);
+    return want < F::MIN_TILES ? F::MIN_TILES : (want < 1e8f ? (int)want + 1 : 100000000);
+}
+
+// Unit x, if it is one of this wave's 64 sequences from s0, before which there
+// are `units` units and `slots` partial outputs; ui, si: inclusive sums of the
+// lanes' shares.  (Tables that break their rules may count past the bounds:
+// such units are left out.)
+template <class F>
+__device__ __forceinline__ bool unit_among(const CacheAttnParams &p, const Share &h, int s0, int units, int slots, int ui, int si, int x,
+                                           Unit &found)
+{
+    const uint64_t hit = __ballot(x >= units + ui - h.units && x < units + ui);
+    if (!hit) return false;
+    const int l = __builtin_ctzll(hit);
+    const int c = lane_value(h.c, l), local = x - (units + lane_value(ui - h.units, l)), pair = local / c;
+    const int slot = slots + lane_value(si - h.slots, l) + local, tiles = lane_value(h.tiles, l);
+    if (local < 0 || pair >= tiles * p.b.Hkv || (c > 1 && (slot < 0 || slot >= p.slots[F::FORM]))) return false;
+    // (causal: the last row tiles see most keys, and start first)
+    found = {s0 + l, tiles - 1 - pair / p.b.Hkv, pair % p.b.Hkv, local - pair * c, c, slot};
+    return true;
+}
+
+// Unit x of form F, the same in each of the workgroup's WAVES waves; the
+// workgroup of unit 0 also writes how many partial outputs the form has.  Up to
+// 64 sequences every wave works by itself; more are shared among the waves.
+template <class F, int WAVES>
 __device__ Unit find_unit(const CacheAttnParams &p, int G, int x)
 {
     const int lane = threadIdx.x & 63;
-    SeqPlan first;   // of the first 64 sequences
-    float total = 0.0f;
-    for (int s = lane; s < p.b.S; s += 64) {
-        const SeqPlan r = seq_plan<F>(p, s, G);
-        if (s == lane) first = r;
-        total += (float)r.tiles * (float)r.kt;
-    }
-    total = __builtin_bit_cast(float, lane_value(__builtin_bit_cast(int, wave_scan(total)), 63)) * (float)p.b.Hkv;
-    // (rounded up by more than the sum's fp32 rounding, so that the bound of the units holds)
-    const float want = total * (1.0001f / F::TARGET);
-    const int chunk = want < F::MIN_TILES ? F::MIN_TILES : (want < 1e8f ? (int)want + 1 : 100000000);
-    int units = 0, slots = 0;   // of the sequences before this round of 64
     Unit found = {-1, 0, 0, 0, 0, 0};
-    for (int s0 = 0; s0 < p.b.S; s0 += 64) {
-        const int s = s0 + lane;
-        int tiles = 0, c = 1;
-        if (s < p.b.S) {
-            const SeqPlan r = s0 == 0 ? first : seq_plan<F>(p, s, G);
-            tiles = r.tiles;
-            c = (r.kt + chunk - 1) / chunk;
-            c = c < 1 ? 1 : c;
+    int units = 0, slots = 0;
+    if (p.b.S <= 64) {
+        SeqPlan r = {};
+        if (lane < p.b.S) r = seq_plan<F>(p, lane, G);
+        const float total = wave_scan((float)r.tiles * (float)r.kt);
+        const int chunk = chunk_of<F>(p, __builtin_bit_cast(float, lane_value(__builtin_bit_cast(int, total), 63)));
+        const Share h = share_of<F>(p, r, chunk);
+        const int ui = wave_scan(h.units), si = wave_scan(h.slots);
+        unit_among<F>(p, h, 0, 0, 0, ui, si, x, found);
+        slots = lane_value(si, 63);
+    } else {
+        __shared__ float totals[WAVES];
+        __shared__ int sums[2][WAVES][2];
+        __shared__ Unit shared;
+        const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+        SeqPlan first = {};   // of the first round
+        float total = 0.0f;
+        for (int s = threadIdx.x; s < p.b.S; s += 64 * WAVES) {
+            const SeqPlan r = seq_plan<F>(p, s, G);
+            if (s == (int)threadIdx.x) first = r;
+            total += (float)r.tiles * (float)r.kt;
         }
-        const int pairs = tiles * p.b.Hkv, u = pairs * c, sl = c > 1 ? u : 0;
-        const int ui = wave_scan(u), si = wave_scan(sl);
-        const uint64_t hit = __ballot(x >= units + ui - u && x < units + ui);
-        if (hit) {
-            const int l = __builtin_ctzll(hit);
-            const int cs = lane_value(c, l), local = x - (units + lane_value(ui - u, l)), pair = local / cs;
-            const int slot = slots + lane_value(si - sl, l) + local;
-            // (tables that break their rules may count past the bounds: such units are left out)
-            if (local >= 0 && pair < lane_value(pairs, l) && (cs == 1 || (slot >= 0 && slot < p.slots[F::FORM]))) {
-                found.s = s0 + l;
-                found.pieces = cs;
-                found.piece = local - pair * cs;
-                found.head = pair % p.b.Hkv;
-                found.tile = lane_value(tiles, l) - 1 - pair / p.b.Hkv;   // (causal: the last row tiles see most keys, and start first)
-                found.slot = slot;
+        total = wave_scan(total);
+        if (lane == 63) totals[wave] = total;
+        if (threadIdx.x == 0) shared = found;
+        __syncthreads();
+        total = 0.0f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) total += totals[w];
+        const int chunk = chunk_of<F>(p, total);
+        for (int s0 = 0, round = 0; s0 < p.b.S; s0 += 64 * WAVES, round ^= 1) {
+            const int s = s0 + (int)threadIdx.x;
+            SeqPlan r = {};
+            if (s < p.b.S) r = s0 == 0 ? first : seq_plan<F>(p, s, G);
+            const Share h = share_of<F>(p, r, chunk);
+            const int ui = wave_scan(h.units), si = wave_scan(h.slots);
+            if (lane == 63) {
+                sums[round][wave][0] = ui;
+                sums[round][wave][1] = si;
             }
-            if (x != 0) return found;
+            __syncthreads();   // (two sets of sums: a round's are read before the next but one writes them)
+            int before[2] = {units, slots};
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) {
+                if (w < wave) before[0] += sums[round][w][0], before[1] += sums[round][w][1];
+                units += sums[round][w][0];
+                slots += sums[round][w][1];
+            }
+            if (unit_among<F>(p, h, s0 + 64 * wave, before[0], before[1], ui, si, x, found) && lane == 0) shared = found;
+            if (x != 0 && x < units) break;   // (of the whole workgroup)
         }
-        units += lane_value(ui, 63);
-        slots += lane_value(si, 63);
+        __syncthreads();
+        auto same = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+        found = {same(shared.s), same(shared.tile), same(shared.head), same(shared.piece), same(shared.pieces), same(shared.slot)};
     }
     if (x == 0 && p.slots[F::FORM] && threadIdx.x == 0) p.counts[F::FORM] = slots;
     return found;

@@ -77,7 +77,7 @@ __device__ __forceinline__ void cache_prompt(const CacheAttnParams &p, int x, Pr
     constexpr int PER = (CH + THREADS - 1) / THREADS;   // chunks of K of a thread, and of V
 
     const int G = p.Hq / p.b.Hkv;
-    const Unit u = find_unit<ManyRows>(p, G, x);
+    const Unit u = find_unit<ManyRows, WAVES>(p, G, x);
     if (u.s < 0) return;
     const SeqPlan sq = seq_plan<ManyRows>(p, u.s, G);
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
