@@ -263,6 +263,142 @@ def test_attention_long(L, lens, Hq, H, d):
     _run_attn(L, *_attn_case(L, lens, Hq, H, d, 64, seed=4), 64, Hq)
 
 
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("page", [16, 32, 64, 128, 256])
+@pytest.mark.parametrize("window", [0, 70])
+def test_attention_both_forms_every_page(L, d, page, window):
+    """Chunks of many rows beside single tokens, lengths around the pages' and the tiles' ends."""
+    lens = [(70, 150), (page - 1, 1), (2 * page, 1), (31, 64), (0, 129)]
+    _run_attn(L, *_attn_case(L, lens, 4, 2, d, page, seed=d + page), page, 4, window=window)
+
+
+def test_attention_many_sequences_of_many_rows(L):
+    """More sequences than a wave has lanes, more than a workgroup has threads, in both forms."""
+    lens = [(i % 50, 17 + i % 9) for i in range(70)] + [(i % 70, 1) for i in range(60)]
+    _run_attn(L, *_attn_case(L, lens, 6, 1, 64, 16, seed=20), 16, 6)
+    lens = [(i % 5, 1 + i % 2) for i in range(600)]
+    _run_attn(L, *_attn_case(L, lens, 2, 1, 64, 16, seed=21), 16, 2)
+
+
+@pytest.mark.parametrize("scale", [-0.1, 0.0, 3.0])
+@pytest.mark.parametrize("lens", [[(200, 1), (30, 4)], [(100, 180)]])
+def test_attention_scales(L, lens, scale):
+    """Logits of either sign, none, and so large that the softmax is one key."""
+    for page in (16, 64):
+        _run_attn(L, *_attn_case(L, lens, 4, 2, 128, page, seed=22), page, 4, scale=scale)
+
+
+@pytest.mark.parametrize("d,page", [(128, 64), (64, 16), (256, 64)])
+def test_attention_value_scales_far_apart(L, d, page):
+    """Pages whose values lie 2^140 apart; a page of scale 0."""
+    q, parts, table, kv, starts = _attn_case(L, [(250, 1), (60, 200), (3, 90)], 4, 2, d, page, seed=23)
+    for s in range(3):
+        for j in range(table.shape[1]):
+            if int(table[s, j]) >= 0:
+                parts[3][int(table[s, j])] = [2.0 ** 70, 2.0 ** -70, 1.0, 0.0, 2.0 ** -100][(s + j) % 5]
+    _run_attn(L, q, parts, table, kv, starts, page, 4)
+
+
+def test_attention_logits_that_keep_growing(L):
+    """Keys whose logits rise and fall by hundreds along the sequence: the running maximum moves in most tiles."""
+    for lens, page in (([(600, 1)], 64), ([(100, 500)], 64), ([(100, 500)], 16)):
+        q, parts, table, kv, starts = _attn_case(L, lens, 2, 1, 128, page, seed=24)
+        for j in range(-(-kv[0] // page)):
+            parts[2][int(table[0, j])] = 2.0 ** (-8 + (j * page) // 64)
+        _run_attn(L, q, parts, table, kv, starts, page, 2)
+
+
+def test_attention_shared_pages_and_no_table(L):
+    """Two sequences that share the pages of a prefix; tables of no columns; no sequences."""
+    q, parts, table, kv, starts = _attn_case(L, [(100, 40), (100, 40)], 4, 2, 128, 32, seed=25)
+    table[1, :3] = table[0, :3]
+    _run_attn(L, q, parts, table, kv, starts, 32, 4)
+    cache, qd = _device_cache(L, parts), q.cuda()
+    none = torch.empty(2, 0, dtype=torch.int32, device="cuda")
+    o, lse = L.attn_cache(qd, cache, none, _i32([0, 5]), _i32(starts))
+    assert not o[:40].any() and bool((lse[:40] == -math.inf).all())        # a length of 0
+    assert not o[40:75].any() and torch.isnan(o[75:]).all()               # 5 keys, none in the table: the last 5 rows see them
+    for t in L.attn_cache(qd[:0], cache, none[:0], _i32([]), _i32([0])):
+        assert t.shape[0] == 0
+    before = [t.clone() for t in cache]
+    new = torch.randn(80, 2, 128, dtype=torch.bfloat16, device="cuda")
+    L.kv_append(new, new, cache, none, _i32([0, 5]), _i32(starts))
+    L.kv_append(new[:0], new[:0], cache, none[:0], _i32([]))
+    for a, b in zip(before, cache):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+def test_attention_tables_that_break_their_rules(L):
+    """Starts that decrease, overlap or pass T, negative lengths, wild table entries of the other sequences: the rows that
+    belong to the first sequence alone, and its pages, are right (the kernels bound every index they take from the tables)."""
+    Hq, H, d, page = 4, 2, 64, 16
+    q, parts, table, kv, starts = _attn_case(L, [(40, 30), (0, 20), (9, 50)], Hq, H, d, page, seed=26)
+    ref = R.Cache(*parts)
+    o, lse, ob, lb = R.attention(q, ref, table, kv, starts, page)
+    wild = table.clone()
+    wild[1] = torch.tensor([-(2 ** 31), 2 ** 31 - 1, 12345678, -5, 99][:wild.shape[1]] + [7] * max(0, wild.shape[1] - 5), dtype=torch.int32)
+    for s1, kv1 in (([0, 30, 50, 100], [70, -7, 59]), ([0, 30, 20, 100], [70, 20, 59]), ([0, 30, 5000, 100], [70, 20, 59])):
+        got = L.attn_cache(q.cuda(), _device_cache(L, parts), wild.cuda(), _i32(kv1), _i32(s1))
+        n = min([30] + s1[1:])   # (rows from 20 on are the third sequence's too where it starts there)
+        R.near(got[0][:n], o[:n], ob[:n], "o")
+        R.near(got[1][:n], lse[:n], lb[:n], "lse")
+        cache = _device_cache(L, parts)
+        new = torch.randn(100, 2, H, d, generator=_gen(27)).to(torch.bfloat16)
+        nd = new.cuda()
+        L.kv_append(nd[:, 0], nd[:, 1], cache, wild.cuda(), _i32(kv1), _i32(s1))
+        want = R.Cache(*parts)
+        R.append(want, new[:, 0], new[:, 1], table[:1], kv[:1], starts[:2], page)
+        for j in range(5):
+            g = int(table[0, j])
+            assert torch.equal(cache.k[g].cpu().float().double().nan_to_num(7e9), want.k[g].nan_to_num(7e9))
+            assert torch.equal(cache.v[g].cpu().float().double().nan_to_num(7e9), want.v[g].nan_to_num(7e9))
+
+
+def test_binding_refuses(L):
+    """Wrong types, shapes, strides and devices of every argument, before anything is launched."""
+    q = torch.zeros(3, 4, 64, dtype=torch.bfloat16, device="cuda")
+    k = torch.zeros(3, 2, 64, dtype=torch.bfloat16, device="cuda")
+    w, rope = torch.ones(64, device="cuda"), L.rope_table(8, 64)
+    pos = torch.zeros(3, dtype=torch.int32, device="cuda")
+    bad = [dict(q=q.cpu()), dict(q=q.half()), dict(q=q[0]), dict(k=k.float()), dict(k=k[:2]), dict(v=k[:, :1]), dict(q=q.transpose(1, 2)),
+           dict(q_weight=w.half()), dict(q_weight=w[:32]), dict(k_weight=w.cpu()), dict(rope=rope.double()), dict(rope=rope[0]),
+           dict(rope=rope[:, ::2]), dict(positions=pos.long()), dict(positions=pos[:2]), dict(out=(q, None, None)),
+           dict(out=(q.float(), k, k)), dict(out=(q[:2], k, k))]
+    for kw in bad:
+        with pytest.raises(ValueError):
+            L.qk_norm_rope(**{**dict(q=q, k=k, v=k, q_weight=w, k_weight=w, rope=rope, positions=pos), **kw})
+    wide = torch.zeros(3, 4, 65, dtype=torch.bfloat16, device="cuda")[..., :64]
+    for kw in (dict(q=wide), dict(q=q, eps=-1.0), dict(q=q, rope=L.rope_table(8, 24))):
+        with pytest.raises(L.LampError):
+            L.qk_norm_rope(**kw)
+    cache = L.kv_cache(6, 2, 64, 16)
+    table, kv = torch.zeros(3, 2, dtype=torch.int32, device="cuda"), _i32([1, 1, 1])
+    st = _i32([0, 1, 2, 3])
+    parts = [dict(cache=cache._replace(k=cache.k.view(torch.uint8))), dict(cache=cache._replace(v=cache.k)), dict(cache=cache._replace(k_scale=cache.k_scale[:3])),
+             dict(cache=cache._replace(v_scale=cache.v_scale.double())), dict(block_table=table.long()), dict(block_table=table[0]),
+             dict(block_table=table.t()), dict(kv_lens=kv.long()), dict(kv_lens=kv[:2]), dict(q_start=st[:3]), dict(q_start=st.float()),
+             dict(kv_lens=kv.cpu())]
+    base = dict(cache=cache, block_table=table, kv_lens=kv, q_start=st)
+    for kw in parts + [dict(k=k.half()), dict(v=k.float()), dict(k=k[:, :1], v=k[:, :1]), dict(k=k[0], v=k[0]), dict(k=q, v=q), dict(k_weight=w.half())]:
+        with pytest.raises(ValueError):
+            L.kv_append(**{**dict(k=k, v=k), **base, **kw})
+    for kw in parts + [dict(q=q.float()), dict(q=q[0]), dict(q=q.cpu()), dict(out=(q, w)), dict(out=(q.float(), torch.zeros(3, 4, device="cuda"))),
+                       dict(workspace=torch.zeros(9)), dict(q=torch.zeros(3, 4, 128, dtype=torch.bfloat16, device="cuda"))]:
+        with pytest.raises(ValueError):
+            L.attn_cache(**{**dict(q=q), **base, **kw})
+    with pytest.raises(ValueError):
+        L.attn_cache(q[:2], cache, table, kv)      # without q_start: one token for each sequence
+    for kw in (dict(window=-1), dict(causal=False, window=3), dict(scale=math.nan)):
+        with pytest.raises(L.LampError):
+            L.attn_cache(q, **base, **kw)
+    with pytest.raises(L.LampError):
+        L.attn_cache(torch.zeros(3, 3, 64, dtype=torch.bfloat16, device="cuda"), **base)
+    long = torch.zeros(3, 40, dtype=torch.int32, device="cuda")
+    with pytest.raises(L.LampError):               # a workspace that is too small
+        L.attn_cache(q, cache, long, kv, st, workspace=torch.zeros(512, dtype=torch.uint8, device="cuda"))
+    torch.cuda.synchronize()
+
+
 def test_attention_rows_that_see_nothing_and_rows_of_no_sequence(L):
     """kv_lens below the new tokens (negative positions), length 0, and rows behind the last sequence."""
     Hq, H, d, page = 4, 2, 128, 16
