@@ -29,12 +29,11 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
 SOURCES = ["lamp_kernels.hip", "lamp_fwd.hip", "lamp_fwd16.hip", "lamp_fwd16_sr.hip", "lamp_decode.hip", "lamp_rates.hip",
-           "lamp_noalloc.hip", "lamp_serve.hip", "lamp_cache_attn.hip", "lamp_cache_prompt.hip",
-           "lamp_host.cpp"]
-# parts of lamp_fwd16.hip and lamp_fwd16_sr.hip that this build compiles as units
-# of their own, side by side (-DLAMP_SPLIT_UNITS; without it those include them)
-SPLIT_UNITS = ["lamp_fwd16_d64.hip", "lamp_fwd16_d256.hip", "lamp_fwd16_sim.hip", "lamp_fwd16_sr_d64.hip",
-               "lamp_fwd16_sr_d256.hip"]
+           "lamp_noalloc.hip", "lamp_host.cpp"]
+# parts of lamp_fwd16.hip, lamp_fwd16_sr.hip and lamp_kernels.hip (the serving operators) that this build
+# compiles as units of their own, side by side (-DLAMP_SPLIT_UNITS; without it those include them)
+SPLIT_UNITS = ["lamp_cache_prompt.hip", "lamp_cache_attn.hip", "lamp_serve.hip", "lamp_fwd16_d64.hip",
+               "lamp_fwd16_d256.hip", "lamp_fwd16_sim.hip", "lamp_fwd16_sr_d64.hip", "lamp_fwd16_sr_d256.hip"]
 
 DPP_VGPR_WAITS = 2
 DPP_EXEC_WAITS = 5

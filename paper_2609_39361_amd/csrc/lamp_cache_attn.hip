@@ -182,7 +182,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnParams p)
 }
 
 template <int D, int KT>
-hipError_t launch(const CacheAttnParams &p, hipStream_t s)
+hipError_t launch_forms(const CacheAttnParams &p, hipStream_t s)
 {
     if (p.units[1]) {
         const hipError_t e = launch_cache_prompt(D, p, s);
@@ -288,9 +288,9 @@ hipError_t launch_cache_attn(int D, CacheAttnParams &p, void *ws, hipStream_t s)
         p.part[f] = reinterpret_cast<float *>(base + l.part[f]);
     }
     switch (D) {
-    case 64: return launch<64, 64>(p, s);
-    case 128: return launch<128, 64>(p, s);
-    default: return launch<256, 32>(p, s);
+    case 64: return launch_forms<64, 64>(p, s);
+    case 128: return launch_forms<128, 64>(p, s);
+    default: return launch_forms<256, 32>(p, s);
     }
 }
 

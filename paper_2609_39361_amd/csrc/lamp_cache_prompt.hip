@@ -488,7 +488,7 @@ __global__ __launch_bounds__(THREADS, 2) void cache_mixed_kernel(CacheAttnParams
 }
 
 template <int D, int KT, int KF, bool WIDE>
-hipError_t launch(const CacheAttnParams &p, hipStream_t s)
+hipError_t launch_prompt(const CacheAttnParams &p, hipStream_t s)
 {
     if (p.units[0]) cache_mixed_kernel<D, KT, KF, WIDE><<<dim3((unsigned)(p.units[0] + p.units[1])), THREADS, 0, s>>>(p);
     else cache_prompt_kernel<D, KT, WIDE><<<dim3((unsigned)p.units[1]), THREADS, 0, s>>>(p);
@@ -496,9 +496,9 @@ hipError_t launch(const CacheAttnParams &p, hipStream_t s)
 }
 
 template <int D, int KT, int KF>
-hipError_t launch_any(const CacheAttnParams &p, hipStream_t s)
+hipError_t launch_prompt_of(const CacheAttnParams &p, hipStream_t s)
 {
-    return 1 << p.b.page_shift >= KT ? launch<D, KT, KF, true>(p, s) : launch<D, KT, KF, false>(p, s);
+    return 1 << p.b.page_shift >= KT ? launch_prompt<D, KT, KF, true>(p, s) : launch_prompt<D, KT, KF, false>(p, s);
 }
 
 } // namespace
@@ -506,9 +506,9 @@ hipError_t launch_any(const CacheAttnParams &p, hipStream_t s)
 hipError_t launch_cache_prompt(int D, const CacheAttnParams &p, hipStream_t s)
 {
     switch (D) {
-    case 64: return launch_any<64, 64, 64>(p, s);
-    case 128: return launch_any<128, 64, 64>(p, s);
-    default: return launch_any<256, 32, 32>(p, s);
+    case 64: return launch_prompt_of<64, 64, 64>(p, s);
+    case 128: return launch_prompt_of<128, 64, 64>(p, s);
+    default: return launch_prompt_of<256, 32, 32>(p, s);
     }
 }
 

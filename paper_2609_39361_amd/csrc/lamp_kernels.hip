@@ -470,3 +470,11 @@ hipError_t launch_selftest_exp_doc(const double *x, double *y, size_t n, hipStre
 }
 
 } // namespace lamp
+
+// The serving operators: units of their own in the library's build
+// (LAMP_SPLIT_UNITS).
+#ifndef LAMP_SPLIT_UNITS
+#include "lamp_serve.hip"
+#include "lamp_cache_attn.hip"
+#include "lamp_cache_prompt.hip"
+#endif
