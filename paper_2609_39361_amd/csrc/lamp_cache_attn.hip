@@ -41,17 +41,17 @@ __device__ __forceinline__ float join_lse(float m, float sum)
 template <int D>
 __device__ __forceinline__ void join_many(const CacheAttnParams &p, const PartInfo &i, int slot0, int by, int G)
 {
-    constexpr int C = D / 16;
+    constexpr int C = D / 16, AT = 4;   // pieces at once
     const int lane = threadIdx.x & 15;
     const float *part = p.part[1], *ml = p.part_ml[1];
     for (int r = i.piece + i.pieces * (by * 16 + ((int)threadIdx.x >> 4)); r < i.rows; r += i.pieces * 16 * MANY_BY) {
         const int64_t base = (int64_t)slot0 * ManyRows::ROWS + r;
         float m = NEG_INF, sum = 0.0f, v[C] = {};
-        for (int c0 = 0; c0 < i.pieces; c0 += 4) {
-            float mc[4], lc[4];
-            f32x4 o[4][C / 4];
+        for (int c0 = 0; c0 < i.pieces; c0 += AT) {
+            float mc[AT], lc[AT];
+            f32x4 o[AT][C / 4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {   // (beyond the last: read again, weight 0)
+            for (int k = 0; k < AT; ++k) {   // (beyond the last: read again, weight 0)
                 const int64_t at = base + (int64_t)(c0 + k < i.pieces ? c0 + k : c0) * ManyRows::ROWS;
                 mc[k] = ml[at * 2];
                 lc[k] = ml[at * 2 + 1];
@@ -60,14 +60,14 @@ __device__ __forceinline__ void join_many(const CacheAttnParams &p, const PartIn
             }
             float mn = m;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) mn = fmaxf(mn, mc[k]);
+            for (int k = 0; k < AT; ++k) mn = fmaxf(mn, mc[k]);
             const float ms = mn == NEG_INF ? 0.0f : mn, f0 = __builtin_amdgcn_exp2f(m - ms);
             m = mn;
             sum *= f0;
 #pragma unroll
             for (int e = 0; e < C; ++e) v[e] *= f0;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
+            for (int k = 0; k < AT; ++k) {
                 if (c0 + k < i.pieces) {
                     const float f = __builtin_amdgcn_exp2f(mc[k] - ms);
                     sum += lc[k] * f;
@@ -168,7 +168,8 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnParams p)
 {
     const int G = p.Hq / p.b.Hkv, b = (int)blockIdx.x - p.slots[0];
     const bool many = b >= 0;
-    const int form = many ? 1 : 0, x = many ? b / MANY_BY : (int)blockIdx.x;
+    // (a row tile's workgroups lie slots apart: neighbours are on different XCDs)
+    const int form = many ? 1 : 0, x = many ? b % p.slots[1] : (int)blockIdx.x;
     const int count = p.counts[form];
     const PartInfo i = static_cast<const PartInfo *>(p.info[form])[x];   // (of this call where x < count)
     // (whatever tables that break their rules leave here, nothing outside the arrays is touched)
@@ -177,7 +178,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnParams p)
         || i.token < 0 || i.row0 < 0 || i.rows < 0 || i.rows > (many ? ManyRows::ROWS : FewRows::ROWS)
         || i.token + (i.row0 + (int64_t)i.rows - 1) / G >= p.b.T)
         return;
-    if (many) join_many<D>(p, i, slot0, b % MANY_BY, G);
+    if (many) join_many<D>(p, i, slot0, b / p.slots[1], G);
     else join_few<D>(p, i, slot0, G);
 }
 

@@ -39,7 +39,7 @@ __device__ __forceinline__ void cache_few(const CacheAttnParams &p, int x, FewSh
     float *obuf = sh.o, *ml = sh.ml;
 
     const int G = p.Hq / p.b.Hkv;
-    const Unit u = find_unit<FewRows, WAVES>(p, G, x);
+    const Unit u = find_unit<FewRowsOf<WAVES>, WAVES>(p, G, x);
     if (u.s < 0) return;
     const SeqPlan sq = seq_plan<FewRows>(p, u.s, G);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), n = lane & 15, g = lane >> 4;

@@ -26,9 +26,11 @@ constexpr int TILE = 64;       // keys of the plan's tiles
 // The two forms of the attention.  ROWS: query rows of a workgroup (row = token
 // * G + head of the group); TARGET: workgroups that fill the 256 CUs; MIN_TILES:
 // least key tiles of a piece.
-struct FewRows {       // single tokens and short chunks (lamp_cache_few.h)
-    static constexpr int ROWS = 16, TARGET = 512, MIN_TILES = 4, FORM = 0;
+template <int WAVES>
+struct FewRowsOf {     // single tokens and short chunks (lamp_cache_few.h): 8 waves fill a CU's registers, a tile for each wave
+    static constexpr int ROWS = 16, TARGET = 2048 / WAVES, MIN_TILES = WAVES, FORM = 0;
 };
+using FewRows = FewRowsOf<4>;
 struct ManyRows {      // prompts (lamp_cache_prompt.hip)
     static constexpr int ROWS = 256, TARGET = 256, MIN_TILES = 8, FORM = 1;
 };
