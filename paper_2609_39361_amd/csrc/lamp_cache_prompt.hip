@@ -255,18 +255,17 @@ __device__ __forceinline__ void cache_prompt(const CacheAttnParams &p, int x, Pr
     __syncthreads();
     if (beg < end) {
         if constexpr (WIDE) {
-            look_up(beg);
-            page0 = uniform(ahead);
-            look_up(beg + 1);
-            page1 = uniform(ahead);
+            const int first = entry(tile(beg) * KT), second = entry(tile(beg + 1) * KT);
             look_up(beg + 2);
+            page0 = uniform(first);
+            page1 = uniform(second);
             load_k(beg, page0);
             load_v(beg, page0);
             load_meta(page0);
             store_k(beg & 1, 0);
             store_k(beg & 1, 1);
-            mask_v(beg);
             load_k(beg + 1, page1);
+            mask_v(beg);
         } else {
             look_up_k(beg);
             look_up_v(beg);
@@ -280,11 +279,11 @@ __device__ __forceinline__ void cache_prompt(const CacheAttnParams &p, int x, Pr
             store_k(beg & 1, 0);
             store_k(beg & 1, 1);
             store_meta(beg);
-            mask_v(beg);
             load_k(beg + 1, 0);
             load_meta(0);
             look_up_k(beg + 2);
             look_up_meta(beg + 2);
+            mask_v(beg);
         }
     }
     __syncthreads();
