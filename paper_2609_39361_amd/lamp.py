@@ -368,13 +368,18 @@ def rope_table(n, rot, base=1e6, device="cuda"):
     return torch.cat([ang.cos(), ang.sin()], dim=-1).float()
 
 
+_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+
+
 def _call(dev, fn, *args):
     """One library call on the current stream of CUDA device `dev` (an index)."""
-    if torch.cuda.current_device() == dev:
-        _check(fn(*args, torch._C._cuda_getCurrentRawStream(dev)))
+    if _current_device() == dev:
+        rc = fn(*args, _raw_stream(dev))
     else:
         with torch.cuda.device(dev):
-            _check(fn(*args, torch._C._cuda_getCurrentRawStream(dev)))
+            rc = fn(*args, _raw_stream(dev))
+    if rc:
+        _check(rc)
 
 
 def _must(t, name, dtypes, dev, shape=None):
@@ -456,7 +461,7 @@ def qk_norm_rope(q, k=None, v=None, q_weight=None, k_weight=None, rope=None, pos
         if o is None:
             if out is not None:
                 raise ValueError("out must hold one tensor for each input")
-            o = torch.empty(want, dtype=_BF16, device=q.device)
+            o = q.new_empty(want, dtype=_BF16)
         else:
             _must(o, "out[%d]" % i, (_BF16,), dev)
             if o.shape != want:
@@ -564,7 +569,7 @@ def attn_cache(q, cache, block_table, kv_lens, q_start=None, causal=True, window
     if dq != d:
         raise ValueError("q of d = %d, a cache of %d" % (dq, d))
     if out is None:
-        o, lse = q.new_empty((T, Hq, d)), torch.empty((T, Hq), dtype=_F32, device=q.device)
+        o, lse = q.new_empty((T, Hq, d)), q.new_empty((T, Hq), dtype=_F32)
     else:
         o, lse = out
         _must(o, "o", (_BF16,), dev, (T, Hq, d))
@@ -573,7 +578,7 @@ def attn_cache(q, cache, block_table, kv_lens, q_start=None, causal=True, window
     if workspace is None:
         need = L.lamp_attn_cache_workspace_size(T, S, Hq, Hkv, d, page, width)
         if need:
-            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+            workspace = q.new_empty(need, dtype=torch.uint8)
     elif workspace.get_device() != dev or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous tensor on the inputs' device")
     else:
