@@ -407,7 +407,7 @@ typedef struct lamp_cache {
  * (j+1)*page); entries that no call reads or writes may hold anything.  Tokens
  * from q_start[S] on belong to no sequence: nothing is written for them.
  * All DEVICE memory; values that break these rules give wrong results, never an
- * access outside the arrays.  Built: T up to 2^23, S*Hkv up to 2^22, width*page
+ * access outside the arrays.  Built: T up to 2^23, S*Hkv up to 2^20, width*page
  * up to 2^30, T*Hq up to 2^27.  S = 0 or T = 0 returns LAMP_OK.
  */
 typedef struct lamp_batch {

@@ -31,6 +31,72 @@ __global__ __launch_bounds__(256, 2) void cache_few_kernel(CacheAttnParams p)
     cache_few<D, KT, 4>(p, (int)blockIdx.x, sh);
 }
 
+// The plan of many sequences, a workgroup for each form: key tiles of a piece
+// from the sum over all sequences, then what lies before each.  A thread takes
+// consecutive sequences, in three passes over their lengths (bound by these
+// loads' latency).
+template <class F>
+__device__ void plan_form(const CacheAttnParams &p)
+{
+    constexpr int THREADS = 1024, WAVES = THREADS / 64;
+    __shared__ float totals[WAVES];
+    __shared__ Before sums[WAVES];
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), G = p.Hq / p.b.Hkv;
+    const int each = (p.b.S + THREADS - 1) / THREADS;
+    const int s0 = tid * each < p.b.S ? tid * each : p.b.S, s1 = p.b.S - s0 < each ? p.b.S : s0 + each;
+    float total = 0.0f;
+#pragma unroll 4
+    for (int s = s0; s < s1; ++s) {
+        const SeqPlan r = seq_plan<F>(p, s, G);
+        total += (float)r.tiles * (float)r.kt;
+    }
+    total = wave_scan(total);
+    if (lane == 63) totals[wave] = total;
+    __syncthreads();
+    total = 0.0f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) total += totals[w];
+    const int chunk = chunk_of<F>(p, total);
+    Before at = {0, 0};
+#pragma unroll 4
+    for (int s = s0; s < s1; ++s) {
+        const Share h = share_of<F>(p, seq_plan<F>(p, s, G), chunk);
+        at.units += h.units;
+        at.slots += h.slots;
+    }
+    const Before own = at;
+    at = {wave_scan(at.units), wave_scan(at.slots)};
+    if (lane == 63) sums[wave] = at;
+    __syncthreads();
+    at = {at.units - own.units, at.slots - own.slots};
+    int slots = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        if (w < wave) at.units += sums[w].units, at.slots += sums[w].slots;
+        slots += sums[w].slots;
+    }
+    if (tid == 0) {
+        p.counts[F::FORM] = slots;
+        p.counts[2 + F::FORM] = chunk;
+    }
+    Before *before = static_cast<Before *>(p.before[F::FORM]);
+#pragma unroll 4
+    for (int s = s0; s < s1; ++s) {
+        const Share h = share_of<F>(p, seq_plan<F>(p, s, G), chunk);
+        before[s] = at;
+        at.units += h.units;
+        at.slots += h.slots;
+    }
+}
+
+__global__ __launch_bounds__(1024) void cache_plan_kernel(CacheAttnParams p)
+{
+    if (p.units[blockIdx.x] == 0) return;
+    if (blockIdx.x == 1) plan_form<ManyRows>(p);
+    else if (p.units[1]) plan_form<FewRowsOf<8>>(p);   // (of the kernel with both forms)
+    else plan_form<FewRowsOf<4>>(p);
+}
+
 // The pieces of the rows of split row tiles joined.  The workgroups of a row
 // tile's c partial outputs share its rows, the k-th those with row % c = k.
 // Few rows (many pieces): a workgroup's waves take the pieces in turn, 16 at
@@ -87,7 +153,8 @@ __device__ __forceinline__ void join_many(const CacheAttnParams &p, const PartIn
         const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
 #pragma unroll
         for (int e = 0; e < C; e += 4)
-            *reinterpret_cast<u32x2 *>(p.o + orow * D + C * lane + e) = u32x2{pack2(v[e] * inv, v[e + 1] * inv), pack2(v[e + 2] * inv, v[e + 3] * inv)};
+            *reinterpret_cast<u32x2 *>(p.o + orow * D + C * lane + e) =
+                u32x2{pack2(v[e] * inv, v[e + 1] * inv), pack2(v[e + 2] * inv, v[e + 3] * inv)};
         if (lane == 0) p.lse[orow] = join_lse(m, sum);
     }
 }
@@ -191,6 +258,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnParams p)
 template <int D, int KT>
 hipError_t launch_forms(const CacheAttnParams &p, hipStream_t s)
 {
+    if (p.b.S > PLAN_ALONE) cache_plan_kernel<<<dim3(2), 1024, 0, s>>>(p);
     if (p.units[1]) {
         const hipError_t e = launch_cache_prompt(D, p, s);
         if (e != hipSuccess) return e;
@@ -250,12 +318,12 @@ Bounds bounds(int64_t T, int64_t S, int G, int Hkv, int64_t keys)
     return b;
 }
 
-// The workspace: counts, infos, running maxima and sums, partial outputs.
+// The workspace: counts, the plan, infos, running maxima and sums, partial outputs.
 struct Layout {
-    size_t info[2], ml[2], part[2], total;
+    size_t before[2], info[2], ml[2], part[2], total;
 };
 
-Layout layout(const Bounds &b, int D)
+Layout layout(const Bounds &b, int D, int64_t S)
 {
     Layout l = {};
     size_t at = 256;
@@ -265,10 +333,12 @@ Layout layout(const Bounds &b, int D)
         at += align256(bytes);
         return here;
     };
+    const bool plan = S > PLAN_ALONE;
+    for (int f = 0; f < 2; ++f) l.before[f] = take(plan && b.units[f] ? S * sizeof(Before) : 0);
     for (int f = 0; f < 2; ++f) l.info[f] = take(b.slots[f] * sizeof(PartInfo));
     for (int f = 0; f < 2; ++f) l.ml[f] = take(rows[f] * 2 * sizeof(float));
     for (int f = 0; f < 2; ++f) l.part[f] = take(rows[f] * D * sizeof(float));
-    l.total = b.slots[0] + b.slots[1] ? at : 0;
+    l.total = plan || b.slots[0] + b.slots[1] ? at : 0;
     return l;
 }
 
@@ -276,13 +346,13 @@ Layout layout(const Bounds &b, int D)
 
 size_t cache_attn_workspace(int D, int64_t T, int64_t S, int G, int Hkv, int64_t keys)
 {
-    return layout(bounds(T, S, G, Hkv, keys), D).total;
+    return layout(bounds(T, S, G, Hkv, keys), D, S).total;
 }
 
 hipError_t launch_cache_attn(int D, CacheAttnParams &p, void *ws, hipStream_t s)
 {
     const Bounds b = bounds(p.b.T, p.b.S, p.Hq / p.b.Hkv, p.b.Hkv, (int64_t)p.b.width << p.b.page_shift);
-    const Layout l = layout(b, D);
+    const Layout l = layout(b, D, p.b.S);
     char *base = static_cast<char *>(ws);
     p.counts = reinterpret_cast<int *>(base);
     for (int f = 0; f < 2; ++f) {
@@ -290,6 +360,7 @@ hipError_t launch_cache_attn(int D, CacheAttnParams &p, void *ws, hipStream_t s)
         p.rows_upto[f] = b.upto[f];
         p.units[f] = b.units[f];
         p.slots[f] = b.slots[f];
+        p.before[f] = base + l.before[f];
         p.info[f] = base + l.info[f];
         p.part_ml[f] = reinterpret_cast<float *>(base + l.ml[f]);
         p.part[f] = reinterpret_cast<float *>(base + l.part[f]);

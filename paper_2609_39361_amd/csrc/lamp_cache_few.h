@@ -22,9 +22,9 @@ namespace {
 // tile's are requested as soon as this tile's have been used.  Bound by HBM
 // (32 x 8192 keys, d = 128: 5.6 TB/s where a large copy reaches 5.1), for one
 // sequence by the latencies of lengths, table and codes, one after another
-// (20011 keys, 41 MB: 13 us, about 6 of them before and after the stream).
-// Tiles of 64 keys (32 at d = 256, for registers): tiles of 32 take 5 to 20 %
-// longer; three workgroups a CU instead of two spill and take 64 % longer.
+// (20011 keys, 41 MB: 13 us; 37 tokens' whole call: 6).  Tiles of 64 keys (32 at
+// d = 256, for registers): 32 x 8192 keys 104 us, with tiles of 32 110; three
+// workgroups a CU instead of two spill (169).
 template <int D, int WAVES>
 struct FewShared {
     float o[WAVES * 16 * (D + 4)];
@@ -44,7 +44,7 @@ __device__ __forceinline__ void cache_few(const CacheAttnParams &p, int x, FewSh
     float *obuf = sh.o, *ml = sh.ml;
 
     const int G = p.Hq / p.b.Hkv;
-    const Unit u = find_unit<FewRowsOf<WAVES>, WAVES>(p, G, x);
+    const Unit u = find_unit<FewRowsOf<WAVES>>(p, G, x);
     if (u.s < 0) return;
     const SeqPlan sq = seq_plan<FewRows>(p, u.s, G);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), n = lane & 15, g = lane >> 4;

@@ -7,6 +7,7 @@
 
 #include <type_traits>
 
+#include "lamp_search.h"
 #include "lamp_serve.h"
 
 namespace lamp {
@@ -37,9 +38,13 @@ struct ManyRows {      // prompts (lamp_cache_prompt.hip)
 
 // The key range of one sequence is cut in pieces when its row tiles alone do
 // not fill the device: with `total` the key tiles of all (sequence, row tile,
-// kv head) triples of a form, pieces hold about total / TARGET tiles.  Every
-// workgroup works the plan out for itself from the lengths (no planning launch,
-// and a captured graph follows lengths that change).
+// kv head) triples of a form, pieces hold about total / TARGET tiles.  Up to
+// PLAN_ALONE sequences every wave works the plan out for itself from the lengths
+// (one load a lane, no launch more); for more, a launch of its own leaves it in
+// the workspace (cache_plan_kernel).  Either way the lengths are read on the
+// device, and a captured graph follows them.
+constexpr int PLAN_ALONE = 256;
+
 struct Unit {
     int s;           // sequence (-1: none)
     int tile, head;  // row tile, kv head
@@ -101,6 +106,11 @@ __device__ __forceinline__ int lane_value(int v, int lane)
     return __builtin_amdgcn_readlane(v, lane);
 }
 
+// Units and partial outputs of the sequences before one (workspace).
+struct Before {
+    int units, slots;
+};
+
 // What is known of a sequence (a lane's) to find a unit in it.
 struct Share {
     int tiles, c, units, slots;   // row tiles, pieces of each, and theirs of all kv heads
@@ -122,90 +132,70 @@ __device__ __forceinline__ int chunk_of(const CacheAttnParams &p, float total)
     return want < F::MIN_TILES ? F::MIN_TILES : (want < 1e8f ? (int)want + 1 : 100000000);
 }
 
-// Unit x, if it is one of this wave's 64 sequences from s0, before which there
-// are `units` units and `slots` partial outputs; ui, si: inclusive sums of the
-// lanes' shares.  (Tables that break their rules may count past the bounds:
-// such units are left out.)
+// Unit `local` of sequence s, whose partial outputs start at `slots`.  (Tables
+// that break their rules may count past the bounds: such units are left out.)
 template <class F>
-__device__ __forceinline__ bool unit_among(const CacheAttnParams &p, const Share &h, int s0, int units, int slots, int ui, int si, int x,
-                                           Unit &found)
+__device__ __forceinline__ Unit unit_of(const CacheAttnParams &p, int s, int tiles, int c, int local, int slots)
 {
-    const uint64_t hit = __ballot(x >= units + ui - h.units && x < units + ui);
-    if (!hit) return false;
-    const int l = __builtin_ctzll(hit);
-    const int c = lane_value(h.c, l), local = x - (units + lane_value(ui - h.units, l)), pair = local / c;
-    const int slot = slots + lane_value(si - h.slots, l) + local, tiles = lane_value(h.tiles, l);
-    if (local < 0 || pair >= tiles * p.b.Hkv || (c > 1 && (slot < 0 || slot >= p.slots[F::FORM]))) return false;
+    const int pair = local / c, slot = slots + local;
+    if (local < 0 || pair >= tiles * p.b.Hkv || (c > 1 && (slot < 0 || slot >= p.slots[F::FORM]))) return {-1, 0, 0, 0, 0, 0};
     // (causal: the last row tiles see most keys, and start first)
-    found = {s0 + l, tiles - 1 - pair / p.b.Hkv, pair % p.b.Hkv, local - pair * c, c, slot};
-    return true;
+    return {s, tiles - 1 - pair / p.b.Hkv, pair % p.b.Hkv, local - pair * c, c, slot};
 }
 
-// Unit x of form F, the same in each of the workgroup's WAVES waves; the
-// workgroup of unit 0 also writes how many partial outputs the form has.  Up to
-// 64 sequences every wave works by itself; more are shared among the waves.
-template <class F, int WAVES>
-__device__ Unit find_unit(const CacheAttnParams &p, int G, int x)
+// Unit x, by a wave that plans for itself: lane l has the EACH sequences from
+// EACH l.
+template <class F, int EACH>
+__device__ __forceinline__ Unit plan_alone(const CacheAttnParams &p, int G, int x)
 {
     const int lane = threadIdx.x & 63;
-    Unit found = {-1, 0, 0, 0, 0, 0};
-    int units = 0, slots = 0;
-    if (p.b.S <= 64) {
-        SeqPlan r = {};
-        if (lane < p.b.S) r = seq_plan<F>(p, lane, G);
-        const float total = wave_scan((float)r.tiles * (float)r.kt);
-        const int chunk = chunk_of<F>(p, __builtin_bit_cast(float, lane_value(__builtin_bit_cast(int, total), 63)));
-        const Share h = share_of<F>(p, r, chunk);
-        const int ui = wave_scan(h.units), si = wave_scan(h.slots);
-        unit_among<F>(p, h, 0, 0, 0, ui, si, x, found);
-        slots = lane_value(si, 63);
-    } else {
-        __shared__ float totals[WAVES];
-        __shared__ int sums[2][WAVES][2];
-        __shared__ Unit shared;
-        const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-        SeqPlan first = {};   // of the first round
-        float total = 0.0f;
-        for (int s = threadIdx.x; s < p.b.S; s += 64 * WAVES) {
-            const SeqPlan r = seq_plan<F>(p, s, G);
-            if (s == (int)threadIdx.x) first = r;
-            total += (float)r.tiles * (float)r.kt;
-        }
-        total = wave_scan(total);
-        if (lane == 63) totals[wave] = total;
-        if (threadIdx.x == 0) shared = found;
-        __syncthreads();
-        total = 0.0f;
+    SeqPlan r[EACH];
+    float total = 0.0f;
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) total += totals[w];
-        const int chunk = chunk_of<F>(p, total);
-        for (int s0 = 0, round = 0; s0 < p.b.S; s0 += 64 * WAVES, round ^= 1) {
-            const int s = s0 + (int)threadIdx.x;
-            SeqPlan r = {};
-            if (s < p.b.S) r = s0 == 0 ? first : seq_plan<F>(p, s, G);
-            const Share h = share_of<F>(p, r, chunk);
-            const int ui = wave_scan(h.units), si = wave_scan(h.slots);
-            if (lane == 63) {
-                sums[round][wave][0] = ui;
-                sums[round][wave][1] = si;
-            }
-            __syncthreads();   // (two sets of sums: a round's are read before the next but one writes them)
-            int before[2] = {units, slots};
-#pragma unroll
-            for (int w = 0; w < WAVES; ++w) {
-                if (w < wave) before[0] += sums[round][w][0], before[1] += sums[round][w][1];
-                units += sums[round][w][0];
-                slots += sums[round][w][1];
-            }
-            if (unit_among<F>(p, h, s0 + 64 * wave, before[0], before[1], ui, si, x, found) && lane == 0) shared = found;
-            if (x != 0 && x < units) break;   // (of the whole workgroup)
-        }
-        __syncthreads();
-        auto same = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
-        found = {same(shared.s), same(shared.tile), same(shared.head), same(shared.piece), same(shared.pieces), same(shared.slot)};
+    for (int i = 0; i < EACH; ++i) {
+        const int s = EACH * lane + i;
+        r[i] = s < p.b.S ? seq_plan<F>(p, s, G) : SeqPlan{};
+        total += (float)r[i].tiles * (float)r[i].kt;
     }
-    if (x == 0 && p.slots[F::FORM] && threadIdx.x == 0) p.counts[F::FORM] = slots;
-    return found;
+    total = wave_scan(total);
+    const int chunk = chunk_of<F>(p, __builtin_bit_cast(float, lane_value(__builtin_bit_cast(int, total), 63)));
+    Share h[EACH];
+    int units = 0, slots = 0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        h[i] = share_of<F>(p, r[i], chunk);
+        units += h[i].units;
+        slots += h[i].slots;
+    }
+    const int ui = wave_scan(units), si = wave_scan(slots);
+    if (x == 0 && p.slots[F::FORM] && threadIdx.x == 0) p.counts[F::FORM] = lane_value(si, 63);
+    const uint64_t hit = __ballot(x >= ui - units && x < ui);
+    if (!hit) return {-1, 0, 0, 0, 0, 0};
+    const int l = __builtin_ctzll(hit);
+    int local = x - lane_value(ui - units, l), before = lane_value(si - slots, l), i = 0;
+    Share at = {lane_value(h[0].tiles, l), lane_value(h[0].c, l), lane_value(h[0].units, l), lane_value(h[0].slots, l)};
+#pragma unroll
+    for (int k = 1; k < EACH; ++k) {
+        if (i == k - 1 && local >= at.units) {
+            local -= at.units;
+            before += at.slots;
+            at = {lane_value(h[k].tiles, l), lane_value(h[k].c, l), lane_value(h[k].units, l), lane_value(h[k].slots, l)};
+            i = k;
+        }
+    }
+    return unit_of<F>(p, EACH * l + i, at.tiles, at.c, local, before);
+}
+
+// Unit x of form F, the same in each of the workgroup's waves.
+template <class F>
+__device__ Unit find_unit(const CacheAttnParams &p, int G, int x)
+{
+    if (p.b.S <= 64) return plan_alone<F, 1>(p, G, x);
+    if (p.b.S <= PLAN_ALONE) return plan_alone<F, PLAN_ALONE / 64>(p, G, x);
+    const Before *before = static_cast<const Before *>(p.before[F::FORM]);
+    const int s = last_at_most(p.b.S, x, [&](int i) { return (int64_t)before[i].units; });
+    const Share h = share_of<F>(p, seq_plan<F>(p, s, G), p.counts[2 + F::FORM]);
+    return unit_of<F>(p, s, h.tiles, h.c, x - before[s].units, before[s].slots);
 }
 
 // What cache_join_kernel needs to know of a partial output; each unit writes its own.

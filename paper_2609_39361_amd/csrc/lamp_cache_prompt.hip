@@ -29,13 +29,14 @@
 // V of t, in buffers whose former tiles were read before the last barrier: two
 // of each do.
 //
-// An 8K prompt (32/8 heads, d = 128) takes 538 us, 1.02 PFLOP/s, where a large
-// bf16 product of the library reaches 1.28.  A tile of 64 keys takes a SIMD's two
-// waves about 4200 cycles: 2050 of products, 2500 of vector instructions (1024 of
-// them exponentials), which share the issue slots, and the rest at the phases'
-// ends.  Both waves in the same phase: 608 us; no priority for the products: 580;
-// operands read one product ahead: 710.  For d = 256 half of the queries' operands
-// come from LDS as well (registers hold o and the other half).
+// Bound by the issue of products and vector instructions together.  An 8K prompt
+// (32/8 heads, d = 128) takes 540 us, 1.02 PFLOP/s, where a large bf16 product
+// reaches 1.28: by its counters a tile of 64 keys takes a SIMD's two waves 4260
+// cycles, the matrix cores being busy for 2050 of them and the vector unit for
+// 2340 (no LDS bank conflicts).  Both waves in the same phase: 589 us instead of
+// 557; 64 rows a wave, one wave a SIMD: registers spill, 8 times as long.  For
+// d = 256 half of the queries' operands come from LDS as well (registers hold o
+// and the other half).
 #include <hip/hip_runtime.h>
 
 #include "lamp_cache_few.h"
@@ -45,9 +46,9 @@ namespace {
 
 constexpr int WAVES = 8, THREADS = 64 * WAVES;
 
-// The running maximum is raised only when a logit passes it by 2^LAZY (in
-// units of log2): probabilities stay below 2^LAZY, far inside fp32 and bf16,
-// and o is rescaled a few times a row instead of at every tile.
+// The running maximum is raised only when a logit (times log2 e) passes it by
+// LAZY: probabilities stay below 2^LAZY, far inside fp32 and bf16, and o is
+// rescaled a few times a row instead of at every tile.
 constexpr float LAZY = 8.0f;
 
 __device__ __forceinline__ int swap23(int m)
@@ -65,7 +66,7 @@ struct PromptShared {
     u32x4 q[WAVES][Q_LDS<D> ? Q_LDS<D> : 1][Q_LDS<D> ? 64 : 1];
     u32x4 k[2][KT * (D / 8 + 1)];
     u32x4 v[2][D * (KT / 8 + 1)];
-    float meta[4][KT / 16][2];                        // logit factor (scale, log2 e, key scale) and value scale of each group of 16 keys
+    float meta[4][KT / 16][2];                        // of each 16 keys: logit factor (scale, log2 e, key scale), value scale
     uint32_t marks[ManyRows::ROWS][D / 32];           // rows and channels that see NaN values (mark_nan)
     int marked;
 };
@@ -85,7 +86,7 @@ __device__ __forceinline__ void cache_prompt(const CacheAttnParams &p, int x, Pr
     constexpr int PER = (CH + THREADS - 1) / THREADS;   // chunks of K of a thread, and of V
 
     const int G = p.Hq / p.b.Hkv;
-    const Unit u = find_unit<ManyRows, WAVES>(p, G, x);
+    const Unit u = find_unit<ManyRows>(p, G, x);
     if (u.s < 0) return;
     const SeqPlan sq = seq_plan<ManyRows>(p, u.s, G);
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -93,7 +94,7 @@ __device__ __forceinline__ void cache_prompt(const CacheAttnParams &p, int x, Pr
     const int rows = sq.n * G, r0 = u.tile * ManyRows::ROWS;
     const int rend = r0 + ManyRows::ROWS < rows ? r0 + ManyRows::ROWS : rows;
     write_info<ManyRows>(p, u, sq.a, r0, rend - r0);
-    // keys that rows from ra to rb (inclusive) see: some of them [lo, hi), all of them [lo_all, hi_all)
+    // keys that a position sees; those that some row sees, that every row sees
     auto upto = [&](int pos) { return p.causal ? (pos + 1 < sq.len ? pos + 1 : sq.len) : sq.len; };
     auto from = [&](int pos) { return p.window > 0 && pos - p.window + 1 > 0 ? pos - p.window + 1 : 0; };
     const int pmin = sq.pos0 + r0 / G, pmax = sq.pos0 + (rend - 1) / G;
@@ -112,7 +113,7 @@ __device__ __forceinline__ void cache_prompt(const CacheAttnParams &p, int x, Pr
     const int whi_any = upto(wpmax), wlo_any = from(wpmin), whi_all = upto(wpmin), wlo_all = from(wpmax);
 
     constexpr int QR = D / 16 - Q_LDS<D>;       // operands in registers
-    constexpr int AHEAD = D > 128 ? 4 : 8;      // operands in flight from LDS (4 beside d = 256's o: with 6 of them registers spill)
+    constexpr int AHEAD = 2;                    // operands in flight from LDS (8K prompt: with one 564 us, two 540, eight 543)
     bf16x8 qf[QR];
     {
         const uint16_t *q = p.q + (int64_t)(sq.a + tok) * p.q_st + (int64_t)qh * p.q_sh + 8 * half;
@@ -172,8 +173,9 @@ __device__ __forceinline__ void cache_prompt(const CacheAttnParams &p, int x, Pr
     auto look_up_meta = [&](int t) { mpage = entry(tile(t) * KT + 16 * (tid % NG)); };
     auto look_up = [&](int t) { ahead = entry(tile(t) * KT); };
     // of the page's codes for this head, the tile's part
-    auto k_base = [&](int pg, int t) { return p.kc + ((((int64_t)(held(pg) ? pg : 0) * p.b.Hkv + u.head) << ps) + (tile(t) * KT & pmask)) * D; };
-    auto v_base = [&](int pg, int t) { return p.vc + ((((int64_t)(held(pg) ? pg : 0) * p.b.Hkv + u.head) << ps) * D + (tile(t) * KT & pmask)); };
+    auto page_row = [&](int pg) { return ((int64_t)(held(pg) ? pg : 0) * p.b.Hkv + u.head) << ps; };
+    auto k_base = [&](int pg, int t) { return p.kc + (page_row(pg) + (tile(t) * KT & pmask)) * D; };
+    auto v_base = [&](int pg, int t) { return p.vc + (page_row(pg) * D + (tile(t) * KT & pmask)); };
     auto load_k = [&](int t, int pg) {
 #pragma unroll
         for (int i = 0; i < PER; ++i) kraw[i] = *reinterpret_cast<const u32x4 *>(k_base(WIDE ? pg : kpage[i], t) + (uint32_t)koff[i]);
@@ -230,7 +232,8 @@ __device__ __forceinline__ void cache_prompt(const CacheAttnParams &p, int x, Pr
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const uint32_t keep = held(vp[i]) ? ~0u : 0u;
-            sh.v[b][v_at(vch[i], 2 * vgr[i] + second)] = __builtin_bit_cast(u32x4, widen(vraw[i][2 * second] & keep, vraw[i][2 * second + 1] & keep));
+            const bf16x8 x = widen(vraw[i][2 * second] & keep, vraw[i][2 * second + 1] & keep);
+            sh.v[b][v_at(vch[i], 2 * vgr[i] + second)] = __builtin_bit_cast(u32x4, x);
         }
     };
     // The factor of a group's logits (scale, log2 e, key scale) and the scale of
@@ -336,7 +339,7 @@ __device__ __forceinline__ void cache_prompt(const CacheAttnParams &p, int x, Pr
             // Operands come from LDS AHEAD products before they are used;
             // neighbouring products are on different accumulators.  The phase
             // has priority: its few instructions keep the matrix cores busy
-            // (8K prompt: 558 us with it, 580 without, 608 the other way round).
+            // (8K prompt: 557 us with it, 587 without, 608 the other way round).
             __builtin_amdgcn_s_setprio(1);
             constexpr int OV = DB * NG, ALL = OV + NB * D / 16, EVERY = ALL / PIECES;
             bf16x8 a[AHEAD], q[AHEAD];
@@ -354,9 +357,9 @@ __device__ __forceinline__ void cache_prompt(const CacheAttnParams &p, int x, Pr
             for (int i = 0; i < AHEAD; ++i) read(i);
 #pragma unroll
             for (int i = 0; i < ALL; ++i) {
-                const int k = (i - OV) / NB, at = i % AHEAD;
+                const int k = (i - OV) / NB, at = i % AHEAD, b = (i - OV) % NB;
                 if (i < OV) o[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[at], pf[i / DB], o[i % DB], 0, 0, 0);
-                else s[(i - OV) % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[at], k < QR ? qf[k < QR ? k : 0] : q[at], s[(i - OV) % NB], 0, 0, 0);
+                else s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[at], k < QR ? qf[k < QR ? k : 0] : q[at], s[b], 0, 0, 0);
                 if (i + AHEAD < ALL) read(i + AHEAD);
                 if (i % EVERY == EVERY - 1 && i / EVERY < PIECES) stage(t, i / EVERY);
                 __builtin_amdgcn_sched_barrier(0x0006);   // (only vector and scalar arithmetic may move past)
@@ -429,8 +432,10 @@ __device__ __forceinline__ void cache_prompt(const CacheAttnParams &p, int x, Pr
             // One value scale for the tile goes into the exponent (a power of
             // two, so that the sum has it divided out exactly), if it leaves
             // the smallest probabilities that count (2^-60) far above fp32's.
-            if (WIDE && vs[0] > 0x1p-64f && vs[0] < 0x1p64f) exponentials(ms - __builtin_amdgcn_logf(vs[0]), __builtin_amdgcn_rcpf(vs[0]), true);
-            else exponentials(ms, 1.0f, false);
+            if (WIDE && vs[0] > 0x1p-64f && vs[0] < 0x1p64f)
+                exponentials(ms - __builtin_amdgcn_logf(vs[0]), __builtin_amdgcn_rcpf(vs[0]), true);
+            else
+                exponentials(ms, 1.0f, false);
         }
         if (!now) {
 #pragma unroll

@@ -993,8 +993,8 @@ static int check_paged(const lamp_cache *c, const lamp_batch *n, lamp::PagedBatc
     if (!n->q_start && n->T != n->S) return fail(LAMP_ERR_INVALID_ARG, "without q_start T=%d must equal S=%d", n->T, n->S);
     if (n->S > 0 && n->T > 0 && ((!n->table && n->width > 0) || !n->kv_lens))
         return fail(LAMP_ERR_INVALID_ARG, "null pointer in the batch");
-    if (n->T > 1 << 23 || (int64_t)n->S * c->Hkv > 1 << 22 || ((int64_t)n->width << ps) > (int64_t)1 << 30)
-        return fail(LAMP_ERR_UNSUPPORTED, "T above 2^23, S*Hkv above 2^22 or width*page above 2^30");
+    if (n->T > 1 << 23 || (int64_t)n->S * c->Hkv > 1 << 20 || ((int64_t)n->width << ps) > (int64_t)1 << 30)
+        return fail(LAMP_ERR_UNSUPPORTED, "T above 2^23, S*Hkv above 2^20 or width*page above 2^30");
     *b = {n->table, n->kv_lens, n->q_start, n->table_stride, n->S, n->T, n->width, c->pages, ps, c->Hkv};
     return LAMP_OK;
 }
@@ -1039,7 +1039,7 @@ size_t lamp_attn_cache_workspace_size(int T, int S, int Hq, int Hkv, int d, int 
     if (T <= 0 || S <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv || width <= 0) return 0;
     if ((d != 64 && d != 128 && d != 256) || page < 16 || page > 256 || (page & (page - 1))) return 0;
     if ((int64_t)width * page > (int64_t)1 << 30) return 0;
-    if (T > 1 << 23 || (int64_t)S * Hkv > 1 << 22 || (int64_t)T * Hq > (int64_t)1 << 27) return 0;
+    if (T > 1 << 23 || (int64_t)S * Hkv > 1 << 20 || (int64_t)T * Hq > (int64_t)1 << 27) return 0;
     return lamp::cache_attn_workspace(d, T, S, Hq / Hkv, Hkv, (int64_t)width * page);
 }
 
@@ -1054,7 +1054,8 @@ int lamp_attn_cache(const uint16_t *q, int64_t q_token, int64_t q_head, int Hq, 
     if (causal != 0 && causal != 1) return fail(LAMP_ERR_INVALID_ARG, "causal must be 0 or 1");
     if (window < 0) return fail(LAMP_ERR_INVALID_ARG, "window must be >= 0");
     if (window > 0 && !causal) return fail(LAMP_ERR_INVALID_ARG, "a sliding window requires causal=1");
-    if (!std::isfinite(scale)) return fail(LAMP_ERR_INVALID_ARG, "scale must be finite");
+    const float scale_log2 = (float)(scale * 1.4426950408889634);
+    if (!std::isfinite(scale_log2)) return fail(LAMP_ERR_INVALID_ARG, "scale must be finite in fp32");
     if ((int64_t)batch->T * Hq > (int64_t)1 << 27 || Hq > 65536)
         return fail(LAMP_ERR_UNSUPPORTED, "T*Hq above 2^27 or Hq above 65536");
     if (batch->S == 0 || batch->T == 0) return LAMP_OK;
@@ -1075,7 +1076,7 @@ int lamp_attn_cache(const uint16_t *q, int64_t q_token, int64_t q_head, int Hq, 
     p.Hq = Hq;
     p.causal = causal;
     p.window = window < 1 << 30 ? window : 1 << 30;   // (no key lies farther back)
-    p.scale_log2 = (float)(scale * 1.4426950408889634);
+    p.scale_log2 = scale_log2;
     const size_t need = lamp::cache_attn_workspace(cache->d, batch->T, batch->S, Hq / cache->Hkv, cache->Hkv,
                                                    (int64_t)batch->width * cache->page);
     void *base = nullptr;

@@ -57,7 +57,9 @@ struct AppendParams {
     const float *rope;        // [npos][rot], or null
     int npos, rot, w_f32;
     float eps;
-    int by_token;             // (set by the launcher) a workgroup for every token (the first new one of its page does the work), not for every page slot
+    // (set by the launcher) a workgroup for every token (the first new one of its
+    // page does the work), not for every page that could receive tokens
+    int by_token;
 };
 
 hipError_t launch_kv_append(int D, bool f32, const AppendParams &p, hipStream_t s);
@@ -76,7 +78,8 @@ struct CacheAttnParams {
     int rows_above[2], rows_upto[2];   // it takes the sequences with this many rows (new tokens times heads of a group)
     int units[2];             // workgroups: no lengths give more
     int slots[2];             // partial outputs of split row tiles that the workspace holds: likewise
-    int *counts;              // those that this call has (workspace)
+    int *counts;              // those that this call has, by form, then the plan's tiles of a piece (workspace)
+    void *before[2];          // [S] Before: the plan of more than PLAN_ALONE sequences (workspace)
     void *info[2];            // [slots] PartInfo (workspace)
     float *part[2];           // [slots][rows of a tile][D] (workspace)
     float *part_ml[2];        // their running maxima and sums [slots][rows of a tile][2] (workspace)

@@ -13,6 +13,7 @@
 #include <hip/hip_runtime.h>
 
 #include "lamp_device.h"
+#include "lamp_search.h"
 #include "lamp_serve.h"
 
 namespace lamp {
@@ -186,7 +187,7 @@ __device__ __forceinline__ float scale_for(float amax)
     return __builtin_bit_cast(float, (uint32_t)((e < -100 ? -100 : e) + 127) << 23);
 }
 
-// 1/s of a power of two 2^e, -100 <= e <= 119.
+// 1/s of a power of two 2^e, -100 <= e <= 120.
 __device__ __forceinline__ float inv_pow2(float s)
 {
     return __builtin_bit_cast(float, (254u << 23) - __builtin_bit_cast(uint32_t, s));
@@ -222,24 +223,6 @@ struct PageWork {
     int64_t page;
     int first, count, tok, pos;
 };
-
-// Sequence whose range of the non-decreasing starts f(0..S-1) holds x: the
-// last s with f(s) <= x, by the whole wave, 64 places at once (each round is
-// one load's latency).
-template <class F>
-__device__ __forceinline__ int last_at_most(int S, int64_t x, F f)
-{
-    const int lane = threadIdx.x & 63;
-    int lo = 0, n = S;
-    for (;;) {
-        const int step = (n + 63) / 64;
-        const int at = lo + lane * step;
-        const uint64_t below = __ballot(lane == 0 || (lane * step < n && f(at) <= x));
-        lo += (63 - __builtin_clzll(below)) * step;
-        if (step == 1) return lo;
-        n = S - lo < step ? S - lo : step;
-    }
-}
 
 // Work of workgroup x.  By token: token x's page, if x is the first new token
 // in it.  By slot: sequence s owns the slots from floor(start_s / page) + 2 s,

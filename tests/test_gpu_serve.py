@@ -280,6 +280,75 @@ def test_attention_many_sequences_of_many_rows(L):
     _run_attn(L, *_attn_case(L, lens, 2, 1, 64, 16, seed=21), 16, 2)
 
 
+def test_attention_more_sequences_than_the_plan_has_threads(L):
+    """Sequences of 0 to 2 new tokens and some of many among 2100, cut in pieces and not, tokens of none behind them."""
+    lens = [(i % 37, (i + 1) % 3) for i in range(2100)]
+    lens[5], lens[1030], lens[2099] = (700, 3), (900, 70), (0, 90)
+    q, parts, table, kv, starts = _attn_case(L, lens, 2, 1, 64, 16, seed=30, trailing=5)
+    o, lse = torch.full((starts[-1] + 5, 2, 64), 7.0, dtype=torch.bfloat16, device="cuda"), torch.full((starts[-1] + 5, 2), 7.0, device="cuda")
+    ref, rl, ob, lb = R.attention(q[:starts[-1]], R.Cache(*parts), table, kv, starts, 16)
+    L.attn_cache(q.cuda(), _device_cache(L, parts), table.cuda(), _i32(kv), _i32(starts), out=(o, lse))
+    R.near(o[:-5], ref, ob, "o")
+    R.near(lse[:-5], rl, lb, "lse")
+    assert bool((o[-5:] == 7).all()) and bool((lse[-5:] == 7).all())
+
+
+@pytest.mark.parametrize("more", [90, 400])
+def test_attention_tables_of_many_sequences_that_break_their_rules(L, more):
+    """As test_attention_tables_that_break_their_rules, with many sequences behind the first."""
+    lens = [(40, 30)] + [(9, 1)] * more
+    q, parts, table, kv, starts = _attn_case(L, lens, 4, 2, 64, 16, seed=31)
+    o, lse, ob, lb = R.attention(q, R.Cache(*parts), table, kv, starts, 16)
+    wild = table.clone()
+    wild[1:] = torch.tensor([-(2 ** 31), 2 ** 31 - 1, 12345678, -5, 99, 7], dtype=torch.int32)
+    st = _i32(starts)
+    for s in (st.flip(0), torch.where(torch.arange(more + 2, device="cuda") % 2 == 0, st, 2 ** 31 - 1), torch.full_like(st, -(2 ** 31))):
+        s = s.to(torch.int32)
+        s[0], s[1] = 0, 30
+        for kv1 in (_i32([70] + [2 ** 31 - 1] * more), _i32([70] + [-5] * more)):
+            s[2:] = s[2:].clamp(min=30)   # (rows from 30 on may be several sequences')
+            got = L.attn_cache(q.cuda(), _device_cache(L, parts), wild.cuda(), kv1, s)
+            R.near(got[0][:30], o[:30], ob[:30], "o")
+            R.near(got[1][:30], lse[:30], lb[:30], "lse")
+
+
+@pytest.mark.parametrize("S", [80, 300])
+def test_captured_plan_follows_the_lengths(L, S):
+    """Many sequences, short and in pieces, captured once and replayed with other lengths and starts, eager work between."""
+    T = 2 * S
+    lens = [(900, 2)] * S
+    q, parts, table, _, _ = _attn_case(L, lens, 4, 1, 64, 16, seed=32, poison=False)
+    c, td, qd = _device_cache(L, parts), table.cuda(), q.cuda()
+    steps = []
+    for i in range(4):
+        n = [(7 * s + i) % 3 for s in range(S)]
+        n[i] += 20
+        kv = [min(902, (s * 53 * (i + 1)) % 880 + n[s]) for s in range(S)]
+        st = [0]
+        for x in n:
+            st.append(min(T, st[-1] + x))
+        steps.append((_i32(kv), _i32(st)))
+    kv, st = steps[0][0].clone(), steps[0][1].clone()
+    out = (torch.zeros((T, 4, 64), dtype=torch.bfloat16, device="cuda"), torch.zeros((T, 4), device="cuda"))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        L.attn_cache(qd, c, td, kv, st, out=out)   # loads the code
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        L.attn_cache(qd, c, td, kv, st, out=out)
+    for i, (a, b) in enumerate(steps + steps[:2]):
+        kv.copy_(a)
+        st.copy_(b)
+        graph.replay()
+        n = int(b[-1])
+        want = L.attn_cache(qd, c, td, a, b)
+        assert torch.equal(out[0][:n], want[0][:n]) and torch.equal(out[1][:n], want[1][:n]), "replay %d" % i
+        torch.randn(1000, 1000, device="cuda").sum().item()
+
+
 @pytest.mark.parametrize("scale", [-0.1, 0.0, 3.0])
 @pytest.mark.parametrize("lens", [[(200, 1), (30, 4)], [(100, 180)]])
 def test_attention_scales(L, lens, scale):

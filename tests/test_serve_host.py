@@ -87,6 +87,7 @@ def test_cache_and_batch_refusals(call):
     assert call(b=_batch(table=0)) == INVALID and call(b=_batch(kv=0)) == INVALID
     assert call(b=_batch(T=(1 << 23) + 1)) == UNSUPPORTED
     assert call(b=_batch(S=1 << 22)) == UNSUPPORTED
+    assert call(b=_batch(S=(1 << 19) + 1)) == UNSUPPORTED and "S*Hkv" in _err()   # (2 heads)
     assert call(b=_batch(width=(1 << 24) + 1)) == UNSUPPORTED
     assert call(b=_batch(S=0, st=0, T=0)) == OK and call(b=_batch(T=0)) == OK
 
@@ -105,6 +106,7 @@ def test_attention_refusals():
     assert _attn(causal=2) == INVALID and _attn(window=-1) == INVALID
     assert _attn(causal=0, window=4) == INVALID and "window" in _err()
     assert _attn(scale=math.inf) == INVALID and _attn(scale=math.nan) == INVALID
+    assert _attn(scale=1e39) == INVALID and _attn(scale=-3e38) == INVALID   # (times log2 e, in fp32)
     assert _attn(q=0) == INVALID and _attn(o=0) == INVALID and _attn(lse=0) == INVALID and _attn(o=4104) == INVALID
     assert _attn(strides=(250, 64)) == INVALID and "q: rows" in _err()
     assert _attn(b=_batch(T=1 << 22), Hq=64) == UNSUPPORTED
@@ -117,8 +119,11 @@ def test_attention_workspace_size():
     assert size(0, 1, 32, 8, 128, 64, 500) == 0 and size(1, 1, 3, 2, 128, 64, 500) == 0
     assert size(1, 1, 32, 8, 96, 64, 500) == 0 and size(1, 1, 32, 8, 128, 48, 500) == 0
     assert size(1, 1, 32, 8, 128, 256, 1 << 23) == 0
-    # bounded whatever the batch: at most 512 partial outputs of 256 rows and 1024 of 16, each of d + 2 numbers, and what names them
-    assert size(1 << 20, 1 << 10, 64, 8, 256, 256, 1 << 12) <= (512 * 256 + 1024 * 16) * 258 * 4 + 1536 * 32 + 8 * 256
+    # more than 256 sequences: where each starts in the plan (8 bytes a sequence; one form here), each part from a multiple of 256
+    assert size(256, 256, 32, 8, 128, 64, 1) == 0
+    assert size(257, 257, 32, 8, 128, 64, 1) == 256 + 256 * math.ceil(257 * 8 / 256)
+    # bounded whatever the batch: at most 512 partial outputs of 256 rows and 1024 of 16, each of d + 2 numbers, what names them, and the plan
+    assert size(1 << 20, 1 << 10, 64, 8, 256, 256, 1 << 12) <= (512 * 256 + 1024 * 16) * 258 * 4 + 1536 * 32 + 8 * 256 + 2 * 8 * 1024
 
 
 def test_binding_refuses_cpu_tensors():
