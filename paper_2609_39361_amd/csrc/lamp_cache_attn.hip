@@ -56,11 +56,11 @@ __device__ void plan_form(const CacheAttnParams &p)
     total = 0.0f;
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) total += totals[w];
-    const int chunk = chunk_of<F>(p, total);
+    const float piece = piece_of<F>(p, total);
     Before at = {0, 0};
 #pragma unroll 4
     for (int s = s0; s < s1; ++s) {
-        const Share h = share_of<F>(p, seq_plan<F>(p, s, G), chunk);
+        const Share h = share_of<F>(p, seq_plan<F>(p, s, G), piece);
         at.units += h.units;
         at.slots += h.slots;
     }
@@ -77,12 +77,12 @@ __device__ void plan_form(const CacheAttnParams &p)
     }
     if (tid == 0) {
         p.counts[F::FORM] = slots;
-        p.counts[2 + F::FORM] = chunk;
+        p.piece[F::FORM] = piece;
     }
     Before *before = static_cast<Before *>(p.before[F::FORM]);
 #pragma unroll 4
     for (int s = s0; s < s1; ++s) {
-        const Share h = share_of<F>(p, seq_plan<F>(p, s, G), chunk);
+        const Share h = share_of<F>(p, seq_plan<F>(p, s, G), piece);
         before[s] = at;
         at.units += h.units;
         at.slots += h.slots;
@@ -284,18 +284,20 @@ struct Bounds {
     int above[2], upto[2], units[2], slots[2];
 };
 
-// A sequence of kt key tiles and `pairs` row tiles times heads is cut in
-// c = ceil(kt / chunk) < 1 + kt / chunk pieces, and sum(pairs kt) / chunk <=
-// TARGET: below sum(pairs) + TARGET units, and at most kt / MIN_TILES + 1 a
-// pair.  Where c >= 2, c < 2 kt / chunk: below 2 TARGET partial outputs.
-// Sequences no longer than one piece need none.
+// A sequence of kt key tiles and `pairs` row tiles times heads is cut in at most
+// c = kt / piece + 0.01 pieces, and sum(pairs kt) / piece <= TARGET: below
+// sum(pairs) + TARGET units, and at most kt / MIN_TILES a pair (or one).  Where
+// c >= 2, sum(pairs) is below TARGET / 1.99: below TARGET + TARGET / 128 partial
+// outputs.  (Both with room for the rounding of the fp32 sums.)  Where no pair
+// can have two pieces there are none.
 template <class F>
 void bound(Bounds &b, int64_t pairs, int64_t keys)
 {
-    const int64_t most = ((keys + TILE - 1) / TILE + F::MIN_TILES - 1) / F::MIN_TILES;   // pieces of a pair
+    const int64_t most = (keys + TILE - 1) / TILE / F::MIN_TILES;   // pieces of a pair
     const int64_t a = pairs + F::TARGET, c = pairs * (most > 1 ? most : 1), units = a < c ? a : c;
+    const int64_t parts = F::TARGET + F::TARGET / 128;
     b.units[F::FORM] = (int)units;
-    b.slots[F::FORM] = most <= 1 ? 0 : (int)(units < 2 * F::TARGET ? units : 2 * F::TARGET);
+    b.slots[F::FORM] = most <= 1 ? 0 : (int)(units < parts ? units : parts);
 }
 
 Bounds bounds(int64_t T, int64_t S, int G, int Hkv, int64_t keys)
@@ -355,6 +357,7 @@ hipError_t launch_cache_attn(int D, CacheAttnParams &p, void *ws, hipStream_t s)
     const Layout l = layout(b, D, p.b.S);
     char *base = static_cast<char *>(ws);
     p.counts = reinterpret_cast<int *>(base);
+    p.piece = reinterpret_cast<float *>(base) + 2;
     for (int f = 0; f < 2; ++f) {
         p.rows_above[f] = b.above[f];
         p.rows_upto[f] = b.upto[f];

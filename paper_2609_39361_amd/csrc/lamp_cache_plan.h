@@ -32,8 +32,8 @@ struct FewRowsOf {     // single tokens and short chunks (lamp_cache_few.h): 8 w
     static constexpr int ROWS = 16, TARGET = 2048 / WAVES, MIN_TILES = WAVES, FORM = 0;
 };
 using FewRows = FewRowsOf<4>;
-struct ManyRows {      // prompts (lamp_cache_prompt.hip)
-    static constexpr int ROWS = 256, TARGET = 256, MIN_TILES = 8, FORM = 1;
+struct ManyRows {      // prompts (lamp_cache_prompt.hip; 32 row tiles' window of 1024: 31 us with pieces of 5 tiles at least, 37 of 8)
+    static constexpr int ROWS = 256, TARGET = 256, MIN_TILES = 5, FORM = 1;
 };
 
 // The key range of one sequence is cut in pieces when its row tiles alone do
@@ -116,20 +116,23 @@ struct Share {
     int tiles, c, units, slots;   // row tiles, pieces of each, and theirs of all kv heads
 };
 
+// `each`: key tiles of a piece.  Pieces are no shorter than that (but for a
+// hundredth of a piece), so that where the row tiles alone do not fill the
+// device, their pieces fill it once and not a little more.  (With pieces no
+// longer than that, 80 row tiles' 6640 keys took 119 us instead of 86, and nine
+// single tokens' 8000 48 instead of 41.)
 template <class F>
-__device__ __forceinline__ Share share_of(const CacheAttnParams &p, const SeqPlan &r, int chunk)
+__device__ __forceinline__ Share share_of(const CacheAttnParams &p, const SeqPlan &r, float each)
 {
-    const int c = (r.kt + chunk - 1) / chunk, pieces = c < 1 ? 1 : c, units = r.tiles * p.b.Hkv * pieces;
+    const int c = (int)((float)r.kt * (1.0f / each) + 0.01f), pieces = c < 1 ? 1 : c, units = r.tiles * p.b.Hkv * pieces;
     return {r.tiles, pieces, units, pieces > 1 ? units : 0};
 }
 
 // Key tiles of a piece.
 template <class F>
-__device__ __forceinline__ int chunk_of(const CacheAttnParams &p, float total)
+__device__ __forceinline__ float piece_of(const CacheAttnParams &p, float total)
 {
-    // (rounded up by more than the sum's fp32 rounding, so that the bound of the units holds)
-    const float want = total * (float)p.b.Hkv * (1.0001f / F::TARGET);
-    return want < F::MIN_TILES ? F::MIN_TILES : (want < 1e8f ? (int)want + 1 : 100000000);
+    return fmaxf(total * (float)p.b.Hkv * (1.0f / F::TARGET), (float)F::MIN_TILES);
 }
 
 // Unit `local` of sequence s, whose partial outputs start at `slots`.  (Tables
@@ -158,12 +161,12 @@ __device__ __forceinline__ Unit plan_alone(const CacheAttnParams &p, int G, int 
         total += (float)r[i].tiles * (float)r[i].kt;
     }
     total = wave_scan(total);
-    const int chunk = chunk_of<F>(p, __builtin_bit_cast(float, lane_value(__builtin_bit_cast(int, total), 63)));
+    const float each = piece_of<F>(p, __builtin_bit_cast(float, lane_value(__builtin_bit_cast(int, total), 63)));
     Share h[EACH];
     int units = 0, slots = 0;
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
-        h[i] = share_of<F>(p, r[i], chunk);
+        h[i] = share_of<F>(p, r[i], each);
         units += h[i].units;
         slots += h[i].slots;
     }
@@ -194,7 +197,7 @@ __device__ Unit find_unit(const CacheAttnParams &p, int G, int x)
     if (p.b.S <= PLAN_ALONE) return plan_alone<F, PLAN_ALONE / 64>(p, G, x);
     const Before *before = static_cast<const Before *>(p.before[F::FORM]);
     const int s = last_at_most(p.b.S, x, [&](int i) { return (int64_t)before[i].units; });
-    const Share h = share_of<F>(p, seq_plan<F>(p, s, G), p.counts[2 + F::FORM]);
+    const Share h = share_of<F>(p, seq_plan<F>(p, s, G), p.piece[F::FORM]);
     return unit_of<F>(p, s, h.tiles, h.c, x - before[s].units, before[s].slots);
 }
 

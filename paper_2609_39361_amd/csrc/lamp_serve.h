@@ -78,8 +78,9 @@ struct CacheAttnParams {
     int rows_above[2], rows_upto[2];   // it takes the sequences with this many rows (new tokens times heads of a group)
     int units[2];             // workgroups: no lengths give more
     int slots[2];             // partial outputs of split row tiles that the workspace holds: likewise
-    int *counts;              // those that this call has, by form, then the plan's tiles of a piece (workspace)
-    void *before[2];          // [S] Before: the plan of more than PLAN_ALONE sequences (workspace)
+    int *counts;              // those that this call has (workspace)
+    float *piece;             // the plan of more than PLAN_ALONE sequences: key tiles of a piece (workspace)
+    void *before[2];          // and [S] Before (workspace)
     void *info[2];            // [slots] PartInfo (workspace)
     float *part[2];           // [slots][rows of a tile][D] (workspace)
     float *part_ml[2];        // their running maxima and sums [slots][rows of a tile][2] (workspace)
