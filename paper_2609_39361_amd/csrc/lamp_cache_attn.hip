@@ -39,28 +39,30 @@ template <class F>
 __device__ void plan_form(const CacheAttnParams &p)
 {
     constexpr int THREADS = 1024, WAVES = THREADS / 64;
-    __shared__ float totals[WAVES];
+    __shared__ Work works[WAVES];
     __shared__ Before sums[WAVES];
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), G = p.Hq / p.b.Hkv;
     const int each = (p.b.S + THREADS - 1) / THREADS;
     const int s0 = tid * each < p.b.S ? tid * each : p.b.S, s1 = p.b.S - s0 < each ? p.b.S : s0 + each;
-    float total = 0.0f;
+    Work work = {};
 #pragma unroll 4
-    for (int s = s0; s < s1; ++s) {
-        const SeqPlan r = seq_plan<F>(p, s, G);
-        total += (float)r.tiles * (float)r.kt;
-    }
-    total = wave_scan(total);
-    if (lane == 63) totals[wave] = total;
+    for (int s = s0; s < s1; ++s) add(work, seq_plan<F>(p, s, G));
+    work = wave_work(work);
+    if (lane == 0) works[wave] = work;
     __syncthreads();
-    total = 0.0f;
+    work = {};
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) total += totals[w];
-    const float piece = piece_of<F>(p, total);
+    for (int w = 0; w < WAVES; ++w) {
+        work.tiles += works[w].tiles;
+        work.most += works[w].most;
+        work.mean += works[w].mean;
+        work.longest = fmaxf(work.longest, works[w].longest);
+    }
+    const Split split = split_of<F>(p, work);
     Before at = {0, 0};
 #pragma unroll 4
     for (int s = s0; s < s1; ++s) {
-        const Share h = share_of<F>(p, seq_plan<F>(p, s, G), piece);
+        const Share h = share_of<F>(p, seq_plan<F>(p, s, G), split);
         at.units += h.units;
         at.slots += h.slots;
     }
@@ -77,12 +79,12 @@ __device__ void plan_form(const CacheAttnParams &p)
     }
     if (tid == 0) {
         p.counts[F::FORM] = slots;
-        p.piece[F::FORM] = piece;
+        static_cast<Split *>(p.split)[F::FORM] = split;
     }
     Before *before = static_cast<Before *>(p.before[F::FORM]);
 #pragma unroll 4
     for (int s = s0; s < s1; ++s) {
-        const Share h = share_of<F>(p, seq_plan<F>(p, s, G), piece);
+        const Share h = share_of<F>(p, seq_plan<F>(p, s, G), split);
         before[s] = at;
         at.units += h.units;
         at.slots += h.slots;
@@ -285,17 +287,16 @@ struct Bounds {
 };
 
 // A sequence of kt key tiles and `pairs` row tiles times heads is cut in at most
-// c = kt / piece + 0.01 pieces, and sum(pairs kt) / piece <= TARGET: below
-// sum(pairs) + TARGET units, and at most kt / MIN_TILES a pair (or one).  Where
-// c >= 2, sum(pairs) is below TARGET / 1.99: below TARGET + TARGET / 128 partial
-// outputs.  (Both with room for the rounding of the fp32 sums.)  Where no pair
-// can have two pieces there are none.
+// kt / each + 0.01 pieces, or two where kt / each > 1.01, and sum(pairs kt) / each
+// <= TARGET: below sum(pairs) + TARGET units, and at most kt / MIN_TILES a pair
+// (or one).  Where there are two or more they are below 2 kt / each: below
+// 2 TARGET partial outputs.  Where no pair can have two there are none.
 template <class F>
 void bound(Bounds &b, int64_t pairs, int64_t keys)
 {
     const int64_t most = (keys + TILE - 1) / TILE / F::MIN_TILES;   // pieces of a pair
     const int64_t a = pairs + F::TARGET, c = pairs * (most > 1 ? most : 1), units = a < c ? a : c;
-    const int64_t parts = F::TARGET + F::TARGET / 128;
+    const int64_t parts = 2 * F::TARGET;
     b.units[F::FORM] = (int)units;
     b.slots[F::FORM] = most <= 1 ? 0 : (int)(units < parts ? units : parts);
 }
@@ -357,7 +358,7 @@ hipError_t launch_cache_attn(int D, CacheAttnParams &p, void *ws, hipStream_t s)
     const Layout l = layout(b, D, p.b.S);
     char *base = static_cast<char *>(ws);
     p.counts = reinterpret_cast<int *>(base);
-    p.piece = reinterpret_cast<float *>(base) + 2;
+    p.split = base + 16;
     for (int f = 0; f < 2; ++f) {
         p.rows_above[f] = b.above[f];
         p.rows_upto[f] = b.upto[f];

@@ -63,8 +63,8 @@ __device__ __forceinline__ void cache_few(const CacheAttnParams &p, int x, FewSh
     const int hi = upto(pos), lo = from(pos);
     const int hi_any = upto(pmax), lo_any = from(pmin), hi_all = upto(pmin), lo_all = from(pmax);
     const int t0 = lo_any / KT, t1 = hi_any > lo_any ? (hi_any + KT - 1) / KT : t0;
-    const int beg = t0 + (int)((int64_t)(t1 - t0) * u.piece / u.pieces);
-    const int end = t0 + (int)((int64_t)(t1 - t0) * (u.piece + 1) / u.pieces);
+    const int beg = __builtin_amdgcn_readfirstlane(t0 + (int)((int64_t)(t1 - t0) * u.piece / u.pieces));
+    const int end = __builtin_amdgcn_readfirstlane(t0 + (int)((int64_t)(t1 - t0) * (u.piece + 1) / u.pieces));
 
     bf16x8 qf[D / 32];
     {

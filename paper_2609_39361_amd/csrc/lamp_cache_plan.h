@@ -58,7 +58,11 @@ struct SeqPlan {
     int pos0;        // position of the first new token
     int tiles;       // row tiles
     int kt;          // key tiles that a row tile visits at most
+    float mean;      // and on average
 };
+
+// Row tiles whose mean is this part of the longest at least count as even.
+constexpr float EVEN = 0.75f;
 
 template <class F>
 __device__ __forceinline__ SeqPlan seq_plan(const CacheAttnParams &p, int s, int G)
@@ -79,18 +83,19 @@ __device__ __forceinline__ SeqPlan seq_plan(const CacheAttnParams &p, int s, int
         const int span = (p.window + F::ROWS - 1 + TILE - 1) / TILE + 1;
         if (span < r.kt) r.kt = span;
     }
+    r.mean = p.causal ? fminf((float)r.kt, ((float)r.len - 0.5f * (float)r.n) * (1.0f / TILE)) : (float)r.kt;
     return r;
 }
 
-// Inclusive sum over the wave's lanes.
-template <class T>
-__device__ __forceinline__ T wave_scan(T v)
+// Inclusive sum over the wave's lanes; and maximum, of numbers >= 0.
+template <class T, class OP>
+__device__ __forceinline__ T wave_scan_by(T v, OP op)
 {
     const T zero = 0;
     auto step = [&](auto ctrl, auto rows) {
         const int x = __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, zero), __builtin_bit_cast(int, v), decltype(ctrl)::value,
                                                   decltype(rows)::value, 0xf, false);
-        v += __builtin_bit_cast(T, x);
+        v = op(v, __builtin_bit_cast(T, x));
     };
     step(std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xf>{});   // row_shr:1
     step(std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xf>{});   // row_shr:2
@@ -99,6 +104,17 @@ __device__ __forceinline__ T wave_scan(T v)
     step(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});   // row_bcast:15
     step(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});   // row_bcast:31
     return v;
+}
+
+template <class T>
+__device__ __forceinline__ T wave_scan(T v)
+{
+    return wave_scan_by(v, [](T a, T b) { return a + b; });
+}
+
+__device__ __forceinline__ float wave_scan_max(float v)
+{
+    return wave_scan_by(v, [](float a, float b) { return fmaxf(a, b); });
 }
 
 __device__ __forceinline__ int lane_value(int v, int lane)
@@ -116,23 +132,51 @@ struct Share {
     int tiles, c, units, slots;   // row tiles, pieces of each, and theirs of all kv heads
 };
 
-// `each`: key tiles of a piece.  Pieces are no shorter than that (but for a
-// hundredth of a piece), so that where the row tiles alone do not fill the
-// device, their pieces fill it once and not a little more.  (With pieces no
-// longer than that, 80 row tiles' 6640 keys took 119 us instead of 86, and nine
-// single tokens' 8000 48 instead of 41.)
+// How row tiles are cut: those of kt key tiles in kt / each pieces, rounded down,
+// but in `least` where that is above 1, and no shorter than `tiles`.
+struct Split {
+    float each;
+    int least, tiles;
+};
+
 template <class F>
-__device__ __forceinline__ Share share_of(const CacheAttnParams &p, const SeqPlan &r, float each)
+__device__ __forceinline__ Share share_of(const CacheAttnParams &p, const SeqPlan &r, Split split)
 {
-    const int c = (int)((float)r.kt * (1.0f / each) + 0.01f), pieces = c < 1 ? 1 : c, units = r.tiles * p.b.Hkv * pieces;
+    const float x = (float)r.kt * (1.0f / split.each) + 0.01f;   // (an even share stays one under the sums' rounding)
+    const int c = x > 1.02f && x < 2.0f ? split.least : (int)x, most = r.kt / split.tiles, fit = c < most ? c : most;
+    const int pieces = fit < 1 ? 1 : fit, units = r.tiles * p.b.Hkv * pieces;
     return {r.tiles, pieces, units, pieces > 1 ? units : 0};
 }
 
-// Key tiles of a piece.
-template <class F>
-__device__ __forceinline__ float piece_of(const CacheAttnParams &p, float total)
+// Sums over a form's row tiles (of one head): their number, the key tiles they
+// visit at most and on average; and the most that one visits.
+struct Work {
+    float tiles, most, mean, longest;
+};
+
+__device__ __forceinline__ void add(Work &w, const SeqPlan &r)
 {
-    return fmaxf(total * (float)p.b.Hkv * (1.0f / F::TARGET), (float)F::MIN_TILES);
+    const float t = (float)r.tiles;
+    w.tiles += t;
+    w.most += t * (float)r.kt;
+    w.mean += t * r.mean;
+    w.longest = fmaxf(w.longest, r.tiles ? (float)r.kt : 0.0f);
+}
+
+// An even share of the work is `each` key tiles.  Pieces are no shorter, so that
+// they fill the device once and not a little more: 80 row tiles of 6640 keys
+// take 86 us, with pieces no longer than the share 119; nine single tokens of
+// 8000 keys 41 instead of 48.  But where prompts' row tiles visit unlike numbers
+// of keys, those longer than the share are cut in two (prompts of 300 to 1300
+// tokens together: 100 us instead of 123).  Beside single tokens, whose units
+// fill the rest of the device, pieces are of 8 tiles at least (512 tokens after
+// 1000 keys beside 15 single tokens: 71 us, of 5 tiles 76).
+template <class F>
+__device__ __forceinline__ Split split_of(const CacheAttnParams &p, const Work &w)
+{
+    const int tiles = F::FORM && p.units[0] ? 8 : F::MIN_TILES;
+    const float each = fmaxf(w.most * (float)p.b.Hkv * (1.0f / F::TARGET), (float)tiles);
+    return {each, F::FORM && w.mean < EVEN * w.tiles * w.longest ? 2 : 1, tiles};
 }
 
 // Unit `local` of sequence s, whose partial outputs start at `slots`.  (Tables
@@ -146,6 +190,14 @@ __device__ __forceinline__ Unit unit_of(const CacheAttnParams &p, int s, int til
     return {s, tiles - 1 - pair / p.b.Hkv, pair % p.b.Hkv, local - pair * c, c, slot};
 }
 
+// Of the wave's lanes together.
+__device__ __forceinline__ Work wave_work(Work w)
+{
+    auto last = [](float v) { return __builtin_bit_cast(float, lane_value(__builtin_bit_cast(int, v), 63)); };
+    w = {wave_scan(w.tiles), wave_scan(w.most), wave_scan(w.mean), wave_scan_max(w.longest)};
+    return {last(w.tiles), last(w.most), last(w.mean), last(w.longest)};
+}
+
 // Unit x, by a wave that plans for itself: lane l has the EACH sequences from
 // EACH l.
 template <class F, int EACH>
@@ -153,20 +205,19 @@ __device__ __forceinline__ Unit plan_alone(const CacheAttnParams &p, int G, int 
 {
     const int lane = threadIdx.x & 63;
     SeqPlan r[EACH];
-    float total = 0.0f;
+    Work w = {};
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
         const int s = EACH * lane + i;
         r[i] = s < p.b.S ? seq_plan<F>(p, s, G) : SeqPlan{};
-        total += (float)r[i].tiles * (float)r[i].kt;
+        add(w, r[i]);
     }
-    total = wave_scan(total);
-    const float each = piece_of<F>(p, __builtin_bit_cast(float, lane_value(__builtin_bit_cast(int, total), 63)));
+    const Split split = split_of<F>(p, wave_work(w));
     Share h[EACH];
     int units = 0, slots = 0;
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
-        h[i] = share_of<F>(p, r[i], each);
+        h[i] = share_of<F>(p, r[i], split);
         units += h[i].units;
         slots += h[i].slots;
     }
@@ -189,16 +240,33 @@ __device__ __forceinline__ Unit plan_alone(const CacheAttnParams &p, int G, int 
     return unit_of<F>(p, EACH * l + i, at.tiles, at.c, local, before);
 }
 
-// Unit x of form F, the same in each of the workgroup's waves.
 template <class F>
-__device__ Unit find_unit(const CacheAttnParams &p, int G, int x)
+__device__ __forceinline__ Unit unit_at(const CacheAttnParams &p, int G, int x)
 {
+    if (p.b.S == 1) {
+        const SeqPlan r = seq_plan<F>(p, 0, G);
+        Work w = {};
+        add(w, r);
+        const Share h = share_of<F>(p, r, split_of<F>(p, w));
+        if (x == 0 && p.slots[F::FORM] && threadIdx.x == 0) p.counts[F::FORM] = h.slots;
+        return unit_of<F>(p, 0, h.tiles, h.c, x, 0);
+    }
     if (p.b.S <= 64) return plan_alone<F, 1>(p, G, x);
     if (p.b.S <= PLAN_ALONE) return plan_alone<F, PLAN_ALONE / 64>(p, G, x);
     const Before *before = static_cast<const Before *>(p.before[F::FORM]);
     const int s = last_at_most(p.b.S, x, [&](int i) { return (int64_t)before[i].units; });
-    const Share h = share_of<F>(p, seq_plan<F>(p, s, G), p.piece[F::FORM]);
+    const Share h = share_of<F>(p, seq_plan<F>(p, s, G), static_cast<const Split *>(p.split)[F::FORM]);
     return unit_of<F>(p, s, h.tiles, h.c, x - before[s].units, before[s].slots);
+}
+
+// Unit x of form F, the same in each of the workgroup's waves (in scalar
+// registers, whatever it was worked out in).
+template <class F>
+__device__ __forceinline__ Unit find_unit(const CacheAttnParams &p, int G, int x)
+{
+    const Unit u = unit_at<F>(p, G, x);
+    auto same = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+    return {same(u.s), same(u.tile), same(u.head), same(u.piece), same(u.pieces), same(u.slot)};
 }
 
 // What cache_join_kernel needs to know of a partial output; each unit writes its own.

@@ -100,8 +100,8 @@ __device__ __forceinline__ void cache_prompt(const CacheAttnParams &p, int x, Pr
     const int pmin = sq.pos0 + r0 / G, pmax = sq.pos0 + (rend - 1) / G;
     const int hi_any = upto(pmax), lo_any = from(pmin), hi_all = upto(pmin), lo_all = from(pmax);
     const int t0 = lo_any / KT, t1 = hi_any > lo_any ? (hi_any + KT - 1) / KT : t0;
-    const int beg = t0 + (int)((int64_t)(t1 - t0) * u.piece / u.pieces);
-    const int end = t0 + (int)((int64_t)(t1 - t0) * (u.piece + 1) / u.pieces);
+    const int beg = __builtin_amdgcn_readfirstlane(t0 + (int)((int64_t)(t1 - t0) * u.piece / u.pieces));
+    const int end = __builtin_amdgcn_readfirstlane(t0 + (int)((int64_t)(t1 - t0) * (u.piece + 1) / u.pieces));
 
     // this wave's rows (missing ones repeat the last and are not written)
     const int w0 = r0 + 32 * wave, wlast = w0 + 31 < rend ? w0 + 31 : rend - 1;
@@ -113,7 +113,8 @@ __device__ __forceinline__ void cache_prompt(const CacheAttnParams &p, int x, Pr
     const int whi_any = upto(wpmax), wlo_any = from(wpmin), whi_all = upto(wpmin), wlo_all = from(wpmax);
 
     constexpr int QR = D / 16 - Q_LDS<D>;       // operands in registers
-    constexpr int AHEAD = 2;                    // operands in flight from LDS (8K prompt: with one 564 us, two 540, eight 543)
+    // operands in flight from LDS (8K prompt, d = 128: with one 564 us, two 540, eight 543; d = 256, 8K: two 446, four 427)
+    constexpr int AHEAD = D > 128 ? 4 : 2;
     bf16x8 qf[QR];
     {
         const uint16_t *q = p.q + (int64_t)(sq.a + tok) * p.q_st + (int64_t)qh * p.q_sh + 8 * half;

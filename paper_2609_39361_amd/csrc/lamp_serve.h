@@ -79,7 +79,7 @@ struct CacheAttnParams {
     int units[2];             // workgroups: no lengths give more
     int slots[2];             // partial outputs of split row tiles that the workspace holds: likewise
     int *counts;              // those that this call has (workspace)
-    float *piece;             // the plan of more than PLAN_ALONE sequences: key tiles of a piece (workspace)
+    void *split;              // the plan of more than PLAN_ALONE sequences: Split of each form (workspace)
     void *before[2];          // and [S] Before (workspace)
     void *info[2];            // [slots] PartInfo (workspace)
     float *part[2];           // [slots][rows of a tile][D] (workspace)

@@ -122,8 +122,8 @@ def test_attention_workspace_size():
     # more than 256 sequences: where each starts in the plan (8 bytes a sequence; one form here), each part from a multiple of 256
     assert size(256, 256, 32, 8, 128, 64, 1) == 0
     assert size(257, 257, 32, 8, 128, 64, 1) == 256 + 256 * math.ceil(257 * 8 / 256)
-    # bounded whatever the batch: at most 258 partial outputs of 256 rows and 516 of 16, each of d + 2 numbers, what names them, and the plan
-    assert size(1 << 20, 1 << 10, 64, 8, 256, 256, 1 << 12) <= (258 * 256 + 516 * 16) * 258 * 4 + 774 * 32 + 8 * 256 + 2 * 8 * 1024
+    # bounded whatever the batch: at most 512 partial outputs of 256 rows and 1024 of 16, each of d + 2 numbers, what names them, and the plan
+    assert size(1 << 20, 1 << 10, 64, 8, 256, 256, 1 << 12) <= (512 * 256 + 1024 * 16) * 258 * 4 + 1536 * 32 + 8 * 256 + 2 * 8 * 1024
 
 
 def test_binding_refuses_cpu_tensors():
