@@ -371,7 +371,7 @@ typedef struct lamp_rows {
  *
  * in[0..2] / out[0..2]: queries, keys, values; heads = 0 (both) leaves one
  * out.  Values are copied (rounded to bf16).  in_f32: the inputs are fp32
- * (else bf16); outputs are bf16.  Outputs may have any strides, e.g. in
+ * (else bf16); outputs are bf16.  Outputs may have any strides but 0, e.g. in
  * [B][N][H][d] and out [B][H][N][d], what lamp_attn_fwd reads; an output may
  * be its own input (same pointer, strides and type), not overlap one otherwise.
  * gain_f32: bit 0, the gain of the queries is fp32 (else bf16), bit 1, that of

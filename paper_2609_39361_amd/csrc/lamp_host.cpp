@@ -955,6 +955,8 @@ int lamp_qk_norm_rope(const lamp_rows *in, const lamp_rows *out, int B, int N, i
         rc = check_rows(names[i], in[i].p, in_f32 != 0, is, sizes, 3);
         if (!rc) rc = check_rows(names[i], out[i].p, false, os, sizes, 3);
         if (rc) return rc;
+        for (int k = 0; k < 3; ++k)
+            if (sizes[k] > 1 && os[k] == 0) return fail(LAMP_ERR_INVALID_ARG, "%s: output rows share memory (a stride of 0)", names[i]);
         p.in[i] = {in[i].p, in[i].batch, in[i].token, in[i].head};
         p.out[i] = {static_cast<uint16_t *>(out[i].p), out[i].batch, out[i].token, out[i].head};
     }

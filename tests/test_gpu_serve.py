@@ -280,6 +280,12 @@ def test_attention_many_sequences_of_many_rows(L):
     _run_attn(L, *_attn_case(L, lens, 2, 1, 64, 16, seed=21), 16, 2)
 
 
+@pytest.mark.parametrize("lens,window", [([(0, 1100)], 0), ([(0, 1100), (300, 20), (700, 1)], 0), ([(0, 900), (0, 200)], 0), ([(900, 300)], 400)])
+def test_attention_row_tiles_of_unlike_lengths(L, lens, window):
+    """Between half and all of the workgroups that fill the device: row tiles cut in two, or not, alone and beside tokens."""
+    _run_attn(L, *_attn_case(L, lens, 32, 8, 64, 64, seed=33), 64, 32, window=window)
+
+
 def test_attention_more_sequences_than_the_plan_has_threads(L):
     """Sequences of 0 to 2 new tokens and some of many among 2100, cut in pieces and not, tokens of none behind them."""
     lens = [(i % 37, (i + 1) % 3) for i in range(2100)]

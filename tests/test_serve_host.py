@@ -45,6 +45,8 @@ def test_norm_rope_refusals():
     assert _norm(rin=_rows(q=(4104, 512, 128, 64, 4))) == INVALID and "q: rows" in _err()
     assert _norm(rin=_rows(k=(4096, 512, 132, 64, 2))) == INVALID and "k: rows" in _err()
     assert _norm(rout=_rows(v=(4096, 512, 128, 60, 2))) == INVALID and "v: rows" in _err()
+    assert _norm(rout=_rows(q=(4096, 512, 128, 0, 4))) == INVALID and "share" in _err()
+    assert _norm(rout=_rows(k=(4096, 512, 0, 64, 2))) == INVALID and "share" in _err()
     assert _norm(rin=_rows(k=(4096, 512, 128, 64, 3))) == INVALID and "heads" in _err()
     assert _norm(B=1 << 13, N=1 << 13) == UNSUPPORTED
     # nothing to do
