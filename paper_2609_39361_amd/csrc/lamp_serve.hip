@@ -233,11 +233,24 @@ __device__ PageWork page_work(const PagedBatch &b, int by_token, int x)
     const PageWork none = {0, 0, 0, 0, 0};
     auto start = [&](int s) { return b.q_start ? b.q_start[s] : s; };
     const int ps = b.page_shift, page = 1 << ps;
-    const int s = by_token ? last_at_most(b.S, x, [&](int i) { return (int64_t)start(i); })
-                           : last_at_most(b.S, x, [&](int i) { return (int64_t)(start(i) >> ps) + 2 * (int64_t)i; });
-    int a = start(s), e = start(s + 1);
+    auto first = [&](int a, int i) { return by_token ? (int64_t)a : (int64_t)(a >> ps) + 2 * (int64_t)i; };
+    int s, a, e, keys;
+    if (b.S > 1 && b.S <= 64) {   // (a lane for each sequence: one load's latency)
+        const int i = (int)(threadIdx.x & 63) < b.S ? (int)(threadIdx.x & 63) : b.S - 1;
+        const int ai = start(i), ei = start(i + 1), ki = b.kv_lens[i];
+        s = 63 - __builtin_clzll(__ballot(i == 0 || first(ai, i) <= x));
+        s = s < b.S ? s : b.S - 1;   // (the lanes behind the last sequence repeat it)
+        a = __builtin_amdgcn_readlane(ai, s);
+        e = __builtin_amdgcn_readlane(ei, s);
+        keys = __builtin_amdgcn_readlane(ki, s);
+    } else {
+        s = b.S == 1 ? 0 : last_at_most(b.S, x, [&](int i) { return first(start(i), i); });
+        a = start(s);
+        e = start(s + 1);
+        keys = b.kv_lens[s];
+    }
     if (a < 0 || e > b.T || e <= a) return none;
-    const int64_t len = b.kv_lens[s], p0 = len - (e - a);   // position of the first new token
+    const int64_t len = keys, p0 = len - (e - a);           // position of the first new token
     const int64_t q0 = p0 > 0 ? p0 : 0;                       // first position that exists
     int64_t idx;
     if (by_token) {
