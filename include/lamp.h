@@ -454,8 +454,10 @@ int lamp_kv_append(const void *k, const void *v, int in_f32, int64_t k_token, in
  * softmax is in fp32; probabilities times the values' scale are rounded to
  * bf16 for the product with the values, which is summed in fp32.
  * A row that sees no key has o = 0 and lse = -infinity; one that sees a key of
- * a missing page (or beyond the table) is NaN.  A NaN or an infinity, of a key,
- * a value or a query, reaches only rows that see it.
+ * a missing page (or beyond the table) is NaN.  A row that sees keys, all with
+ * logits of -infinity (an infinite query), has o = NaN and lse = -infinity; a
+ * logit of +infinity makes both NaN.  A NaN or an infinity, of a key, a value
+ * or a query, reaches only rows that see it.
  *
  * workspace: at least lamp_attn_cache_workspace_size(...) bytes, 256-byte
  * aligned, or NULL: the library's per-device workspace, as for lamp_attn_fwd.

@@ -107,11 +107,6 @@ __global__ __launch_bounds__(1024) void cache_plan_kernel(CacheAttnParams p)
 // by latency: the loads of a step do not wait for each other.
 constexpr int MANY_BY = 8;
 
-__device__ __forceinline__ float join_lse(float m, float sum)
-{
-    return sum == 0.0f ? NEG_INF : (m + __builtin_amdgcn_logf(sum)) * LN2;
-}
-
 template <int D>
 __device__ __forceinline__ void join_many(const CacheAttnParams &p, const PartInfo &i, int slot0, int by, int G)
 {
@@ -152,12 +147,12 @@ __device__ __forceinline__ void join_many(const CacheAttnParams &p, const PartIn
         }
         const int gr = i.row0 + r, t = gr / G;
         const int64_t orow = (int64_t)(i.token + t) * p.Hq + i.head * G + gr - t * G;
-        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        const float inv = finish(m, sum);
 #pragma unroll
         for (int e = 0; e < C; e += 4)
             *reinterpret_cast<u32x2 *>(p.o + orow * D + C * lane + e) =
                 u32x2{pack2(v[e] * inv, v[e + 1] * inv), pack2(v[e + 2] * inv, v[e + 3] * inv)};
-        if (lane == 0) p.lse[orow] = join_lse(m, sum);
+        if (lane == 0) p.lse[orow] = finish_lse(m, sum);
     }
 }
 
@@ -219,7 +214,7 @@ __device__ __forceinline__ void join_few(const CacheAttnParams &p, const PartInf
         }
         const int gr = i.row0 + r, t = gr / G;
         const int64_t orow = (int64_t)(i.token + t) * p.Hq + i.head * G + gr - t * G;
-        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        const float inv = finish(m, sum);
         uint16_t *o = p.o + orow * D + C * lane;
 #pragma unroll
         for (int e = 0; e < C; ++e) {
@@ -234,7 +229,7 @@ __device__ __forceinline__ void join_few(const CacheAttnParams &p, const PartInf
 #pragma unroll
             for (int e = 0; e < C; e += 2) *reinterpret_cast<uint32_t *>(o + e) = pack2(v[e], v[e + 1]);
         }
-        if (lane == 0) p.lse[orow] = join_lse(m, sum);
+        if (lane == 0) p.lse[orow] = finish_lse(m, sum);
     }
 }
 

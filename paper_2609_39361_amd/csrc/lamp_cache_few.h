@@ -129,7 +129,7 @@ __device__ __forceinline__ void cache_few(const CacheAttnParams &p, int x, FewSh
 #pragma unroll
     for (int i = 0; i < DT; ++i) o[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     // l: of this lane's keys.  A row that sees keys beyond the table's reach is NaN.
-    float m = NEG_INF, l = (p.causal && pos + 1 < sq.all ? pos + 1 : sq.all) > sq.len ? __builtin_nanf("") : 0.0f;
+    float m = hi > lo ? LOWEST : NEG_INF, l = (p.causal && pos + 1 < sq.all ? pos + 1 : sq.all) > sq.len ? __builtin_nanf("") : 0.0f;
 
     int t = beg + wave;
     if (t < end) {
@@ -275,9 +275,9 @@ __device__ __forceinline__ void cache_few(const CacheAttnParams &p, int x, FewSh
         } else {
             const int gr = r0 + r, i = gr / G;
             const int64_t orow = (int64_t)(sq.a + i) * p.Hq + u.head * G + gr - i * G;
-            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+            const float inv = finish(mx, sum);
             *reinterpret_cast<u32x2 *>(p.o + orow * D + d) = u32x2{pack2(v[0] * inv, v[1] * inv), pack2(v[2] * inv, v[3] * inv)};
-            if (d == 0) p.lse[orow] = sum == 0.0f ? NEG_INF : (mx + __builtin_amdgcn_logf(sum)) * LN2;
+            if (d == 0) p.lse[orow] = finish_lse(mx, sum);
         }
     }
 }

@@ -22,6 +22,9 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr float NEG_INF = -__builtin_inff();
 constexpr float LN2 = 0.6931471805599453f;
+// Where the running maximum of a row that sees keys starts: below every finite
+// logit, so that -infinity is left to the rows that see none.
+constexpr float LOWEST = -3.4028234663852886e38f;
 constexpr int TILE = 64;       // keys of the plan's tiles
 
 // The two forms of the attention.  ROWS: query rows of a workgroup (row = token
@@ -282,6 +285,19 @@ __device__ __forceinline__ void write_info(const CacheAttnParams &p, const Unit 
         PartInfo *i = static_cast<PartInfo *>(p.info[F::FORM]) + u.slot;
         *i = {token, row0, rows, u.head, u.piece, u.pieces, {0, 0}};
     }
+}
+
+// The factor that finishes o, and lse, from a row's maximum m and sum l of
+// exponentials (l == 0: the row saw no key, and is 0, or only logits of
+// -infinity, and is 0/0).
+__device__ __forceinline__ float finish(float m, float l)
+{
+    return l != 0.0f ? 1.0f / l : (m == NEG_INF ? 0.0f : __builtin_nanf(""));
+}
+
+__device__ __forceinline__ float finish_lse(float m, float l)
+{
+    return l == 0.0f ? NEG_INF : (m + __builtin_amdgcn_logf(l)) * LN2;
 }
 
 __device__ __forceinline__ uint32_t pack2(float a, float b)

@@ -258,7 +258,7 @@ __device__ __forceinline__ void cache_prompt(const CacheAttnParams &p, int x, Pr
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[i][e] = 0.0f;
     // m: the reference of the exponentials; l: of this lane's keys.  A row that sees keys beyond the table's reach is NaN.
-    float m = NEG_INF, l = (p.causal && pos + 1 < sq.all ? pos + 1 : sq.all) > sq.len ? __builtin_nanf("") : 0.0f;
+    float m = hi > lo ? LOWEST : NEG_INF, l = (p.causal && pos + 1 < sq.all ? pos + 1 : sq.all) > sq.len ? __builtin_nanf("") : 0.0f;
 
     for (int i = tid; i < ManyRows::ROWS * (D / 32); i += THREADS) sh.marks[0][i] = 0;
     if (tid == 0) sh.marked = 0;
@@ -472,14 +472,14 @@ __device__ __forceinline__ void cache_prompt(const CacheAttnParams &p, int x, Pr
         return;
     }
     const int64_t orow = (int64_t)(sq.a + tok) * p.Hq + qh;
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    const float inv = finish(m, l);
 #pragma unroll
     for (int i = 0; i < DB; ++i)
 #pragma unroll
         for (int a = 0; a < 4; ++a)
             *reinterpret_cast<u32x2 *>(p.o + orow * D + 32 * i + 8 * a + 4 * half) =
                 u32x2{pack2(o[i][4 * a] * inv, o[i][4 * a + 1] * inv), pack2(o[i][4 * a + 2] * inv, o[i][4 * a + 3] * inv)};
-    if (half == 0) p.lse[orow] = l == 0.0f ? NEG_INF : (m + __builtin_amdgcn_logf(l)) * LN2;
+    if (half == 0) p.lse[orow] = finish_lse(m, l);
 }
 
 template <int D, int KT, bool WIDE>

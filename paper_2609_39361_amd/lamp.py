@@ -558,7 +558,8 @@ def attn_cache(q, cache, block_table, kv_lens, q_start=None, causal=True, window
     block_table, kv_lens and q_start as for kv_append: prompts, chunks and single tokens of any lengths in
     one call.  The token at position p sees the sequence's keys j <= p (causal) with j > p - window
     (window > 0).  `scale` of the logits: default 1/sqrt(d).  A row that sees no key has o = 0 and
-    lse = -inf; tokens behind q_start[S] are left as they are in `out` = (o, lse).  `workspace`: a device
+    lse = -inf (one whose logits are all -inf: o = NaN); tokens behind q_start[S] are left as they are in
+    `out` = (o, lse).  `workspace`: a device
     tensor of attn_cache_workspace_size(...) bytes; by default one of torch's, on the current stream."""
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
         raise ValueError("q [T,Hq,d] expected")

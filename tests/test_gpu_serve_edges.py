@@ -1,0 +1,50 @@
+"""The serving operators on the GPU where their definitions have no finite
+value, or where the host's plan of a batch changes, against plain 64-bit
+arithmetic (serveref.py)."""
+import math
+
+import pytest
+import torch
+
+import serveref as R
+from test_gpu_serve import L, NAN_CODES, _attn_case, _device_cache, _gen, _i32, _run_attn, _same_cache  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+# (cached, new) lengths, Hq, Hkv, d, page, window, scale: each form alone, in pieces, both beside each other
+INFINITE = [
+    ([(40, 1), (0, 1)], 4, 1, 128, 64, 0, None),
+    ([(30, 5)], 4, 2, 64, 16, 0, -0.2),
+    ([(3000, 1)], 8, 2, 128, 64, 0, None),
+    ([(2500, 3)], 4, 1, 256, 32, 900, None),
+    ([(100, 200)], 4, 2, 128, 64, 0, None),
+    ([(50, 150)], 2, 1, 256, 16, 70, -0.2),
+    ([(4000, 300)], 4, 1, 64, 64, 0, None),
+    ([(700, 150), (30, 1), (900, 4)], 4, 2, 128, 32, 0, None),
+]
+
+
+@pytest.mark.parametrize("i", range(len(INFINITE)))
+def test_attention_of_infinite_logits(L, i):  # noqa: F811
+    """Rows whose logits are all -infinity have no softmax (0/0): o is NaN and lse -infinity, unlike rows that see no
+    key (o = 0).  Logits of +infinity: NaN.  Neither reaches another row."""
+    lens, Hq, H, d, page, window, scale = INFINITE[i]
+    q, parts, table, kv, starts = _attn_case(L, lens, Hq, H, d, page, seed=40 + i)
+    parts[0].view(torch.uint8)[..., 0] = 0x38          # every key's channel 0 is 1
+    T, sign = starts[-1], -1.0 if scale and scale < 0 else 1.0
+    rows = torch.arange(T * Hq).view(T, Hq)
+    low, high = rows % 5 == 1, rows % 5 == 3            # (each in every row tile)
+    clean = q.clone()
+    clean[low | high] = 0.0
+    q[..., 0][low] = -math.inf * sign
+    q[..., 0][high] = math.inf * sign
+    kw = dict(window=window, scale=scale)
+    o, lse, ob, lb = R.attention(clean, R.Cache(*parts), table, kv, starts, page, True, window, scale)
+    got = [t.cpu() for t in L.attn_cache(q.cuda(), _device_cache(L, parts), table.cuda(), _i32(kv), _i32(starts), **kw)]
+    rest = ~(low | high)
+    R.near(got[0][rest], o[rest], ob[rest], "o")
+    R.near(got[1][rest], lse[rest], lb[rest], "lse")
+    assert torch.isnan(got[0][high]).all() and torch.isnan(got[1][high]).all()
+    assert torch.isnan(got[0][low]).all(), "rows of -infinity: o"
+    assert bool((got[1][low] == -math.inf).all()), "rows of -infinity: lse"
