@@ -410,6 +410,8 @@ def _rope(rope, dev):
         _must(rope, "rope", (_F32,), dev)
         raise ValueError("rope must be a contiguous [positions, rot] table")
     n, rot = rope.shape
+    if n == 0 or rot == 0:   # (its address is null: "not rotated")
+        raise ValueError("rope must have rows and channels, not shape %s" % ((n, rot),))
     return rope.data_ptr(), n, rot
 
 

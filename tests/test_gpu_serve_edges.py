@@ -48,3 +48,14 @@ def test_attention_of_infinite_logits(L, i):  # noqa: F811
     assert torch.isnan(got[0][high]).all() and torch.isnan(got[1][high]).all()
     assert torch.isnan(got[0][low]).all(), "rows of -infinity: o"
     assert bool((got[1][low] == -math.inf).all()), "rows of -infinity: lse"
+
+
+def test_empty_rope_tables_are_refused(L):  # noqa: F811
+    """By every entry point that takes one (they came back unrotated)."""
+    k = torch.zeros(3, 2, 64, dtype=torch.bfloat16, device="cuda")
+    cache, table = L.kv_cache(6, 2, 64, 16), torch.zeros(3, 2, dtype=torch.int32, device="cuda")
+    for rope in (L.rope_table(0, 64), L.rope_table(4, 64)[:0], L.rope_table(4, 64)[:, :0].contiguous()):
+        with pytest.raises(ValueError):
+            L.qk_norm_rope(k, rope=rope)
+        with pytest.raises(ValueError):
+            L.kv_append(k, k, cache, table, _i32([1, 1, 1]), rope=rope)
