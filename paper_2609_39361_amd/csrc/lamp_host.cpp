@@ -1038,7 +1038,7 @@ int lamp_kv_append(const void *k, const void *v, int in_f32, int64_t k_token, in
 
 size_t lamp_attn_cache_workspace_size(int T, int S, int Hq, int Hkv, int d, int page, int width)
 {
-    if (T <= 0 || S <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv || width <= 0) return 0;
+    if (T <= 0 || S <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv || width < 0) return 0;
     if ((d != 64 && d != 128 && d != 256) || page < 16 || page > 256 || (page & (page - 1))) return 0;
     if ((int64_t)width * page > (int64_t)1 << 30) return 0;
     if (T > 1 << 23 || (int64_t)S * Hkv > 1 << 20 || (int64_t)T * Hq > (int64_t)1 << 27) return 0;

@@ -59,3 +59,33 @@ def test_empty_rope_tables_are_refused(L):  # noqa: F811
             L.qk_norm_rope(k, rope=rope)
         with pytest.raises(ValueError):
             L.kv_append(k, k, cache, table, _i32([1, 1, 1]), rope=rope)
+
+
+def test_tables_without_columns_of_many_sequences(L):  # noqa: F811
+    """Planned by a launch of its own, in the caller's workspace: the size it is told is what the call needs; captured and
+    replayed with other lengths."""
+    S, Hq, d, page = 300, 4, 64, 16
+    cache, none = L.kv_cache(2, 1, d, page), torch.empty(S, 0, dtype=torch.int32, device="cuda")
+    q = torch.randn(S, Hq, d, generator=_gen(50)).to(torch.bfloat16).cuda()
+    need = L.attn_cache_workspace_size(S, S, Hq, 1, d, page, 0)
+    kv = _i32([0] * S)
+    with pytest.raises(L.LampError):
+        L.attn_cache(q, cache, none, kv, workspace=torch.zeros(need - 1, dtype=torch.uint8, device="cuda"))
+    ws = torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda")
+    out = (torch.full((S, Hq, d), 7.0, dtype=torch.bfloat16, device="cuda"), torch.full((S, Hq), 7.0, device="cuda"))
+
+    def check(lens):
+        seen = torch.tensor(lens) > 0   # (a key that the table does not hold)
+        assert torch.isnan(out[0].cpu()[seen]).all() and torch.isnan(out[1].cpu()[seen]).all()
+        assert not out[0].cpu()[~seen].any() and bool((out[1].cpu()[~seen] == -math.inf).all())
+    L.attn_cache(q, cache, none, kv, out=out, workspace=ws)
+    check([0] * S)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        L.attn_cache(q, cache, none, kv, out=out)
+    for i in range(3):
+        lens = [(s + i) % 3 for s in range(S)]
+        kv.copy_(_i32(lens))
+        graph.replay()
+        check(lens)
+        torch.randn(1000, 1000, device="cuda").sum().item()

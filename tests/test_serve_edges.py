@@ -18,3 +18,11 @@ def test_an_empty_rope_table_is_refused(shape):
     with pytest.raises(ValueError, match="rope"):
         lamp._rope(torch.ones(4, 64)[:shape[0], :shape[1]].contiguous(), -1)
     assert lamp._rope(None, -1) == (None, 0, 0)
+
+
+def test_workspace_size_of_tables_without_columns():
+    """attn_cache accepts them, so the size says what such a call needs: the plan of more than 256 sequences."""
+    size = lamp.attn_cache_workspace_size
+    assert size(256, 256, 4, 1, 64, 16, 0) == 0 and size(3, 2, 4, 1, 64, 16, 0) == 0
+    assert size(300, 300, 4, 1, 64, 16, 0) == size(300, 300, 4, 1, 64, 16, 1) > 0
+    assert size(300, 300, 4, 1, 64, 16, -1) == 0
