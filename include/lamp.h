@@ -378,7 +378,8 @@ typedef struct lamp_rows {
  * the keys.  rope: [npos][rot] fp32, the row of a position holds rot/2 cosines,
  * then rot/2 sines; rot a positive multiple of 16, at most d.  positions: int32
  * [B][N], or NULL: token n is at position n.  A token whose position lies
- * outside the table has NaN in its rotated channels.
+ * outside the table has NaN in its rotated channels.  eps: 0 or a positive
+ * number within fp32's range.
  * Built: d in {64, 128, 256}, B*N up to 2^25.  B = 0 or N = 0 returns LAMP_OK.
  */
 int lamp_qk_norm_rope(const lamp_rows *in, const lamp_rows *out, int B, int N, int d, int in_f32,

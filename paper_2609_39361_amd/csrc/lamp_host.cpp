@@ -2,6 +2,7 @@
 // argument validation, per-device tables and workspace, kernel launches.
 #include <hip/hip_runtime.h>
 
+#include <cfloat>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -917,7 +918,9 @@ static int check_rope(const float *rope, int npos, int rot, int d)
 
 static int check_eps(double eps)
 {
-    if (!(eps >= 0.0) || std::isinf(eps)) return fail(LAMP_ERR_INVALID_ARG, "eps must be finite and >= 0");
+    // (the kernels hold it in fp32)
+    if (!(eps >= 0.0 && eps <= (double)FLT_MAX) || (eps > 0.0 && (float)eps == 0.0f))
+        return fail(LAMP_ERR_INVALID_ARG, "eps must be 0 or a positive number in fp32's range");
     return LAMP_OK;
 }
 

@@ -1,5 +1,6 @@
 """The serving operators' binding and argument checks at their edges, on the
 CPU (nothing is launched)."""
+import ctypes
 import os
 
 import pytest
@@ -26,3 +27,15 @@ def test_workspace_size_of_tables_without_columns():
     assert size(256, 256, 4, 1, 64, 16, 0) == 0 and size(3, 2, 4, 1, 64, 16, 0) == 0
     assert size(300, 300, 4, 1, 64, 16, 0) == size(300, 300, 4, 1, 64, 16, 1) > 0
     assert size(300, 300, 4, 1, 64, 16, -1) == 0
+
+
+@pytest.mark.parametrize("eps,ok", [(1e39, False), (1e308, False), (1e-50, False), (0.0, True), (1e-45, True), (3.4e38, True)])
+def test_eps_is_an_fp32_number(eps, ok):
+    """The kernels hold it in fp32: one that is infinite there would make every row 0, one that vanishes zero rows NaN.
+    (No tokens: the checks alone.)"""
+    rows, L, P = lamp._ROWS3.pack(*(4096, 512, 128, 64, 2) * 3), lamp.lib(), ctypes.c_void_p
+    rc = [L.lamp_qk_norm_rope(rows, rows, 1, 0, 64, 0, None, None, 0, None, 0, 0, None, eps, None),
+          L.lamp_kv_append(None, None, 0, 128, 64, 128, 64, lamp._CACHE.pack(4096, 4096, 4096, 4096, 4, 2, 64, 64),
+                           lamp._BATCH.pack(4096, 4, 4096, 4096, 2, 0, 4), P(4096), 0, None, 0, 0, eps, None)]
+    assert rc == ([0, 0] if ok else [1, 1])
+    assert ok or "eps" in L.lamp_last_error().decode()
