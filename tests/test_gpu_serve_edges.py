@@ -89,3 +89,16 @@ def test_tables_without_columns_of_many_sequences(L):  # noqa: F811
         graph.replay()
         check(lens)
         torch.randn(1000, 1000, device="cuda").sum().item()
+
+
+def test_attention_windows_beyond_32_bits(L):  # noqa: F811
+    """A window that no C int holds is one that hides nothing, not its low 32 bits."""
+    q, parts, table, kv, starts = _attn_case(L, [(90, 4), (20, 1)], 4, 2, 64, 16, seed=51)
+    args = (q.cuda(), _device_cache(L, parts), table.cuda(), _i32(kv), _i32(starts))
+    want = L.attn_cache(*args)
+    for window in (2 ** 31, 2 ** 32 + 3, 2 ** 40, 2 ** 64 + 1):
+        for a, b in zip(L.attn_cache(*args, window=window), want):
+            assert torch.equal(a, b), window
+    for window in (-2 ** 32 + 3, -2 ** 31 - 1):
+        with pytest.raises(L.LampError):
+            L.attn_cache(*args, window=window)
