@@ -586,6 +586,8 @@ def attn_cache(q, cache, block_table, kv_lens, q_start=None, causal=True, window
         raise ValueError("workspace must be a contiguous tensor on the inputs' device")
     else:
         need = workspace.numel() * workspace.element_size()
+        if not need and L.lamp_attn_cache_workspace_size(T, S, Hq, Hkv, d, page, width):   # (its address is null)
+            raise ValueError("workspace is empty")
     window = max(-1, min(int(window), 0x7FFFFFFF))   # (no key lies farther back; ctypes would take the low 32 bits)
     _call(dev, L.lamp_attn_cache, q.data_ptr(), *q.stride()[:2], Hq, c, b, 1 if causal else 0, window,
           d ** -0.5 if scale is None else float(scale), o.data_ptr(), lse.data_ptr(),

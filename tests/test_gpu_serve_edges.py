@@ -102,3 +102,18 @@ def test_attention_windows_beyond_32_bits(L):  # noqa: F811
     for window in (-2 ** 32 + 3, -2 ** 31 - 1):
         with pytest.raises(L.LampError):
             L.attn_cache(*args, window=window)
+
+
+def test_an_empty_workspace_is_no_workspace(L):  # noqa: F811
+    """One without bytes is refused where the call needs some (its address is null, which the library takes as its own
+    shared workspace) and taken where it needs none."""
+    q, parts, table, kv, starts = _attn_case(L, [(2000, 1), (20, 1)], 4, 2, 64, 16, seed=52)
+    args = (q.cuda(), _device_cache(L, parts), table.cuda(), _i32(kv), _i32(starts))
+    assert L.attn_cache_workspace_size(2, 2, 4, 2, 64, 16, table.shape[1]) > 0
+    none = torch.empty(0, dtype=torch.uint8, device="cuda")
+    with pytest.raises(ValueError):
+        L.attn_cache(*args, workspace=none)
+    short = (args[0], args[1], args[2][:, :8], _i32([100, 21]), args[4])
+    assert L.attn_cache_workspace_size(2, 2, 4, 2, 64, 16, 8) == 0
+    for a, b in zip(L.attn_cache(*short, workspace=none), L.attn_cache(*short)):
+        assert torch.equal(a, b)
