@@ -368,7 +368,9 @@ def rope_table(n, rot, base=1e6, device="cuda"):
     return torch.cat([ang.cos(), ang.sin()], dim=-1).float()
 
 
-_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+# (the calls behind torch's public ones, without the objects those make; a torch built without a GPU has none)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _call(dev, fn, *args):

@@ -2,12 +2,15 @@
 CPU (nothing is launched)."""
 import ctypes
 import os
+import subprocess
+import sys
 
 import pytest
 import torch
 
 from paper_2609_39361_amd import lamp
 
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 pytestmark = pytest.mark.skipif(not os.path.exists(lamp.LIB_PATH), reason="liblamp.so not built")
 
 
@@ -39,3 +42,21 @@ def test_eps_is_an_fp32_number(eps, ok):
                            lamp._BATCH.pack(4096, 4, 4096, 4096, 2, 0, 4), P(4096), 0, None, 0, 0, eps, None)]
     assert rc == ([0, 0] if ok else [1, 1])
     assert ok or "eps" in L.lamp_last_error().decode()
+
+
+def test_the_binding_imports_with_a_torch_without_a_gpu_build():
+    """Whose torch._C has none of the calls behind the current stream and device; with one, the public calls do."""
+    code = """
+import torch
+for name in ("_cuda_getCurrentRawStream", "_cuda_getDevice"):
+    if hasattr(torch._C, name):
+        delattr(torch._C, name)
+from paper_2609_39361_amd import lamp
+assert lamp.rope_table(4, 16, device="cpu").shape == (4, 16)
+assert lamp._current_device is torch.cuda.current_device
+class Stream:
+    cuda_stream = 7
+torch.cuda.current_stream = lambda dev: Stream
+assert lamp._raw_stream(0) == 7
+"""
+    subprocess.run([sys.executable, "-c", code], check=True, cwd=ROOT)
