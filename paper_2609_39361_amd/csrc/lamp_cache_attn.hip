@@ -15,8 +15,9 @@
 // Two forms, for sequences of few rows (lamp_cache_few.h; bound by HBM: 32
 // single tokens over 8K keys, 32/8 heads, d = 128: 537 MB in 95 us, 5.6 TB/s) and
 // of many (lamp_cache_prompt.hip; bound by the matrix cores and the vector unit:
-// an 8K prompt 538 us, 1.02 PFLOP/s), in one launch where a batch holds both;
-// then, where a sequence may have been cut in pieces, a launch that joins them.
+// an 8K prompt 538 us, 1.02 PFLOP/s), in one launch where a batch holds both, or
+// in two where sequences are short on average (CHUNK); then, where a sequence may
+// have been cut in pieces, a launch that joins them.
 #include <hip/hip_runtime.h>
 
 #include "lamp_cache_few.h"
@@ -95,7 +96,7 @@ __global__ __launch_bounds__(1024) void cache_plan_kernel(CacheAttnParams p)
 {
     if (p.units[blockIdx.x] == 0) return;
     if (blockIdx.x == 1) plan_form<ManyRows>(p);
-    else if (p.units[1]) plan_form<FewRowsOf<8>>(p);   // (of the kernel with both forms)
+    else if (p.units[1] && !p.apart) plan_form<FewRowsOf<8>>(p);   // (of the kernel with both forms)
     else plan_form<FewRowsOf<4>>(p);
 }
 
@@ -256,11 +257,10 @@ template <int D, int KT>
 hipError_t launch_forms(const CacheAttnParams &p, hipStream_t s)
 {
     if (p.b.S > PLAN_ALONE) cache_plan_kernel<<<dim3(2), 1024, 0, s>>>(p);
+    if (!p.units[1] || p.apart) cache_few_kernel<D, KT><<<dim3((unsigned)p.units[0]), 256, 0, s>>>(p);
     if (p.units[1]) {
         const hipError_t e = launch_cache_prompt(D, p, s);
         if (e != hipSuccess) return e;
-    } else {
-        cache_few_kernel<D, KT><<<dim3((unsigned)p.units[0]), 256, 0, s>>>(p);
     }
     const int joins = p.slots[0] + MANY_BY * p.slots[1];
     if (joins) cache_join_kernel<D><<<dim3((unsigned)joins), 256, 0, s>>>(p);
@@ -274,11 +274,30 @@ size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 // in it and 243 in the other, 64 rows 227 and 240, 128 rows 428 and 258).
 constexpr int FEW = 64;
 
+// Batches of 16 rows a sequence or fewer on average (single tokens, a few drafted
+// ones, a chunk beside many of them) take the form for few rows: in the kernel of
+// both forms short sequences leave half of its 8 waves idle (200 sequences of up
+// to 8 tokens and 500 keys: 23 us, 51 in it).  But an average bounds no sequence,
+// and a long chunk among them costs up to 2.5 times what it does in the other
+// form.  So that follows in a launch of its own where the longest sequence there
+// can be, if every other has a token, could cost far more than a launch: its rows
+// times the table's keys, the kv heads and d are CHUNK at least.  Beside 127
+// single tokens over 20 to 30000 keys (32/8 heads, d = 128) a chunk of 385 tokens:
+// 436 us instead of 728, of 100 314 instead of 396, of 50 (1.4 CHUNK) 295 instead
+// of 311.  Where no sequence is long after all, that launch ends at once (128
+// sequences of 4 tokens over 8000 keys: 377 us instead of 368; 1000 of 4 over 1000
+// 442 instead of 423; 32 of 4 over 300, in a table of 32768, 16 instead of 14).
+// Below CHUNK it rather loses (97 tokens beside 31 single ones, all over 8000 keys,
+// 0.8 CHUNK: 137 us instead of 116; 512 of one head beside 63, 1.05 CHUNK: 234 and
+// 232).
+constexpr int64_t CHUNK = (int64_t)1 << 32;
+
 // Bounds of a call from what the host knows: no sequence has more than T G
 // rows, and they have T G / S on average.  Either form is right for any
 // sequence: which takes which is a matter of time only.
 struct Bounds {
     int above[2], upto[2], units[2], slots[2];
+    bool apart;   // both forms, in launches of their own
 };
 
 // A sequence of kt key tiles and `pairs` row tiles times heads is cut in at most
@@ -296,12 +315,15 @@ void bound(Bounds &b, int64_t pairs, int64_t keys)
     b.slots[F::FORM] = most <= 1 ? 0 : (int)(units < parts ? units : parts);
 }
 
-Bounds bounds(int64_t T, int64_t S, int G, int Hkv, int64_t keys)
+Bounds bounds(int D, int64_t T, int64_t S, int G, int Hkv, int64_t keys)
 {
     Bounds b = {};
     const int64_t rows = T * G;
-    const bool few = rows <= FEW || rows <= FewRows::ROWS * S;   // (short sequences, whatever q_start says)
+    const int64_t longest = (T - S + 1) * G;                     // (rows of one sequence, if every other has a token)
+    const bool brief = rows <= FewRows::ROWS * S;
+    const bool few = rows <= FEW || (brief && (longest <= FEW || longest * keys * Hkv * D < CHUNK));
     const bool both = !few && S > 1;
+    b.apart = both && brief;
     const int64_t limit = few ? rows : (both ? FEW : 0);         // rows up to which a sequence is among the few
     if (few || both) {
         const int64_t most = rows / FewRows::ROWS + S, each = S * ((limit + FewRows::ROWS - 1) / FewRows::ROWS);
@@ -311,7 +333,8 @@ Bounds bounds(int64_t T, int64_t S, int G, int Hkv, int64_t keys)
     if (!few) {
         b.above[1] = (int)limit;
         b.upto[1] = (int)rows;
-        bound<ManyRows>(b, (rows / ManyRows::ROWS + S) * Hkv, keys);
+        const int64_t longer = rows / (limit + 1);   // sequences of more than `limit` rows at most
+        bound<ManyRows>(b, (rows / ManyRows::ROWS + (longer < S ? longer : S)) * Hkv, keys);
     }
     return b;
 }
@@ -344,14 +367,15 @@ Layout layout(const Bounds &b, int D, int64_t S)
 
 size_t cache_attn_workspace(int D, int64_t T, int64_t S, int G, int Hkv, int64_t keys)
 {
-    return layout(bounds(T, S, G, Hkv, keys), D, S).total;
+    return layout(bounds(D, T, S, G, Hkv, keys), D, S).total;
 }
 
 hipError_t launch_cache_attn(int D, CacheAttnParams &p, void *ws, hipStream_t s)
 {
-    const Bounds b = bounds(p.b.T, p.b.S, p.Hq / p.b.Hkv, p.b.Hkv, (int64_t)p.b.width << p.b.page_shift);
+    const Bounds b = bounds(D, p.b.T, p.b.S, p.Hq / p.b.Hkv, p.b.Hkv, (int64_t)p.b.width << p.b.page_shift);
     const Layout l = layout(b, D, p.b.S);
     char *base = static_cast<char *>(ws);
+    p.apart = b.apart;
     p.counts = reinterpret_cast<int *>(base);
     p.split = base + 16;
     for (int f = 0; f < 2; ++f) {

@@ -171,13 +171,14 @@ __device__ __forceinline__ void add(Work &w, const SeqPlan &r)
 // take 86 us, with pieces no longer than the share 119; nine single tokens of
 // 8000 keys 41 instead of 48.  But where prompts' row tiles visit unlike numbers
 // of keys, those longer than the share are cut in two (prompts of 300 to 1300
-// tokens together: 100 us instead of 123).  Beside single tokens, whose units
-// fill the rest of the device, pieces are of 8 tiles at least (512 tokens after
-// 1000 keys beside 15 single tokens: 71 us, of 5 tiles 76).
+// tokens together: 100 us instead of 123).  In the launch of both forms pieces
+// are of 8 tiles at least, as if single tokens' units, which that launch is for,
+// filled the rest of the device (512 tokens after 1000 keys beside 15 single
+// tokens: 71 us, of 5 tiles 76).
 template <class F>
 __device__ __forceinline__ Split split_of(const CacheAttnParams &p, const Work &w)
 {
-    const int tiles = F::FORM && p.units[0] ? 8 : F::MIN_TILES;
+    const int tiles = F::FORM && p.units[0] && !p.apart ? 8 : F::MIN_TILES;
     const float each = fmaxf(w.most * (float)p.b.Hkv * (1.0f / F::TARGET), (float)tiles);
     return {each, F::FORM && w.mean < EVEN * w.tiles * w.longest ? 2 : 1, tiles};
 }

@@ -503,7 +503,7 @@ __global__ __launch_bounds__(THREADS, 2) void cache_mixed_kernel(CacheAttnParams
 template <int D, int KT, int KF, bool WIDE>
 hipError_t launch_prompt(const CacheAttnParams &p, hipStream_t s)
 {
-    if (p.units[0]) cache_mixed_kernel<D, KT, KF, WIDE><<<dim3((unsigned)(p.units[0] + p.units[1])), THREADS, 0, s>>>(p);
+    if (p.units[0] && !p.apart) cache_mixed_kernel<D, KT, KF, WIDE><<<dim3((unsigned)(p.units[0] + p.units[1])), THREADS, 0, s>>>(p);
     else cache_prompt_kernel<D, KT, WIDE><<<dim3((unsigned)p.units[1]), THREADS, 0, s>>>(p);
     return hipGetLastError();
 }

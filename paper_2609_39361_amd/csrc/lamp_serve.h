@@ -78,6 +78,7 @@ struct CacheAttnParams {
     int rows_above[2], rows_upto[2];   // it takes the sequences with this many rows (new tokens times heads of a group)
     int units[2];             // workgroups: no lengths give more
     int slots[2];             // partial outputs of split row tiles that the workspace holds: likewise
+    int apart;                // both forms, in launches of their own
     int *counts;              // those that this call has (workspace)
     void *split;              // the plan of more than PLAN_ALONE sequences: Split of each form (workspace)
     void *before[2];          // and [S] Before (workspace)
@@ -91,7 +92,7 @@ size_t cache_attn_workspace(int D, int64_t T, int64_t S, int G, int Hkv, int64_t
 // ws: that workspace (null where it needs none).  Fills in p from units on.
 hipError_t launch_cache_attn(int D, CacheAttnParams &p, void *ws, hipStream_t s);
 // The kernel with the form for many rows (lamp_cache_prompt.hip), and, where
-// p.units[0] > 0, that for few beside it; of launch_cache_attn.
+// p.units[0] > 0 and not p.apart, that for few beside it; of launch_cache_attn.
 hipError_t launch_cache_prompt(int D, const CacheAttnParams &p, hipStream_t s);
 
 } // namespace lamp

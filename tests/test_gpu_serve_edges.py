@@ -117,3 +117,41 @@ def test_an_empty_workspace_is_no_workspace(L):  # noqa: F811
     assert L.attn_cache_workspace_size(2, 2, 4, 2, 64, 16, 8) == 0
     for a, b in zip(L.attn_cache(*short, workspace=none), L.attn_cache(*short)):
         assert torch.equal(a, b)
+
+
+def _wide(table, width):
+    """The table in one of `width` columns, of which the others hold -1."""
+    wide = torch.full((table.shape[0], width), -1, dtype=torch.int32)
+    wide[:, :table.shape[1]] = table
+    return wide
+
+
+# lengths, Hq, Hkv, d, page, columns: a chunk among sequences so short that they have 16 rows or fewer on average, in a table of
+# so many keys that it takes the form for many rows in a launch of its own; planned by each wave and by a launch
+CHUNKS = [
+    ([(i * 37 % 500, 1) for i in range(60)] + [(900, 150), (0, 1)], 4, 1, 128, 64, 900),
+    ([(300, 120)] + [(i * 41 % 300, 1) for i in range(150)], 8, 2, 64, 16, 9000),
+    ([(i * 29 % 200, 1 + i % 2) for i in range(280)] + [(1500, 90), (0, 200)], 8, 2, 128, 32, 2000),
+    ([(5, 0), (2000, 100)] + [(i * 31 % 400, 1) for i in range(64)], 4, 2, 256, 128, 400),
+    ([(i % 9, 1 + i % 3) for i in range(90)] + [(3, 1)], 8, 2, 64, 16, 9000),     # (no long one after all)
+]
+
+
+def _chunk_case(L, i, seed):  # noqa: F811
+    lens, Hq, H, d, page, width = CHUNKS[i]
+    q, parts, table, kv, starts = _attn_case(L, lens, Hq, H, d, page, seed=seed)
+    G, S, T = Hq // H, len(lens), starts[-1]
+    assert T * G <= 16 * S and 64 < (T - S + 1) * G
+    assert (T - S + 1) * G * width * page * H * d >= 1 << 32   # (the host's rule)
+    return q, parts, _wide(table, width), kv, starts, page, Hq
+
+
+@pytest.mark.parametrize("window", [0, 100])
+@pytest.mark.parametrize("i", range(len(CHUNKS)))
+def test_attention_of_a_chunk_among_many_tokens(L, i, window):  # noqa: F811
+    """Each sequence in the form it takes, and bit-equal repeats."""
+    q, parts, table, kv, starts, page, Hq = _chunk_case(L, i, 60 + i)
+    got = _run_attn(L, q, parts, table, kv, starts, page, Hq, window=window)
+    again = L.attn_cache(q.cuda(), _device_cache(L, parts), table.cuda(), _i32(kv), _i32(starts), window=window)
+    for a, b in zip(got, again):
+        assert torch.equal(a, b)

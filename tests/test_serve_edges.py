@@ -60,3 +60,17 @@ torch.cuda.current_stream = lambda dev: Stream
 assert lamp._raw_stream(0) == 7
 """
     subprocess.run([sys.executable, "-c", code], check=True, cwd=ROOT)
+
+
+def test_workspace_size_of_a_chunk_among_many_tokens():
+    """A long chunk beside many single tokens is held by the form for many rows, whose partial outputs the workspace has,
+    though the batch has few rows a sequence on average; single tokens and short tables need none of them."""
+    size = lamp.attn_cache_workspace_size
+    few = 1024 * 16 * 130 * 4 + 2048 * 40   # (1024 partial outputs of 16 rows, d + 2 numbers each, and what names them)
+    for S, chunk, Hq in ((128, 385, 32), (64, 961, 8), (300, 400, 32)):
+        rows = (S - 1 + chunk) * (Hq // 8)
+        units = (rows // 256 + min(S, rows // 65)) * 8 + 256   # (more than 64 rows each; 256 fill the device)
+        assert size(S - 1 + chunk, S, Hq, 8, 128, 64, 470) > min(units, 512) * 256 * 130 * 4
+        assert size(S, S, Hq, 8, 128, 64, 470) < few           # (one token each)
+        assert size(S - 1 + chunk, S, Hq, 8, 128, 64, 8) < few
+    assert size(4 * 32, 32, 32, 8, 128, 64, 16) < few          # (four tokens each)
