@@ -371,15 +371,17 @@ typedef struct lamp_rows {
  *
  * in[0..2] / out[0..2]: queries, keys, values; heads = 0 (both) leaves one
  * out.  Values are copied (rounded to bf16).  in_f32: the inputs are fp32
- * (else bf16); outputs are bf16.  Outputs may have any strides but 0, e.g. in
- * [B][N][H][d] and out [B][H][N][d], what lamp_attn_fwd reads; an output may
- * be its own input (same pointer, strides and type), not overlap one otherwise.
+ * (else bf16); outputs are bf16.  Outputs may have any strides under which no
+ * two rows share memory (0 is refused), e.g. in [B][N][H][d] and out
+ * [B][H][N][d], what lamp_attn_fwd reads; an output may be its own input (same
+ * pointer, strides and type), not overlap one otherwise.
  * gain_f32: bit 0, the gain of the queries is fp32 (else bf16), bit 1, that of
  * the keys.  rope: [npos][rot] fp32, the row of a position holds rot/2 cosines,
  * then rot/2 sines; rot a positive multiple of 16, at most d.  positions: int32
  * [B][N], or NULL: token n is at position n.  A token whose position lies
  * outside the table has NaN in its rotated channels.  eps: 0 or a positive
- * number within fp32's range.
+ * number within fp32's range.  The mean of squares is fp32 too: a row whose sum
+ * of squares passes 2^128 comes out 0.
  * Built: d in {64, 128, 256}, B*N up to 2^25.  B = 0 or N = 0 returns LAMP_OK.
  */
 int lamp_qk_norm_rope(const lamp_rows *in, const lamp_rows *out, int B, int N, int d, int in_f32,
@@ -436,7 +438,7 @@ typedef struct lamp_batch {
  *
  * Tokens whose table entry is missing (outside [0, pages), or beyond width) or
  * whose position is negative are dropped.  No page may receive tokens of two
- * sequences in one call.
+ * sequences, or of two places of a table, in one call.
  */
 int lamp_kv_append(const void *k, const void *v, int in_f32, int64_t k_token, int64_t k_head, int64_t v_token,
                    int64_t v_head, const lamp_cache *cache, const lamp_batch *batch, const void *k_gain, int gain_f32,
@@ -448,7 +450,7 @@ int lamp_kv_append(const void *k, const void *v, int in_f32, int64_t k_token, in
  * tokens in one call.
  *
  * q [T][Hq][d] bf16 (strides q_token, q_head); o [T][Hq][d] bf16 and lse
- * [T][Hq] fp32 (natural log), dense.  Query head h reads kv head h / (Hq/Hkv).
+ * [T][Hq] fp32 (natural log), dense, overlapping nothing else.  Query head h reads kv head h / (Hq/Hkv).
  * The token at position p sees keys j < kv_lens[s] with j <= p (causal) and
  * j > p - window (window > 0; requires causal).  Logits are scale * q.k.
  * Products of bf16 queries and 8-bit keys are exact and summed in fp32; the

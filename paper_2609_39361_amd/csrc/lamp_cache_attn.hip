@@ -13,9 +13,9 @@
 // products would run at a sixteenth of the rate); l sums the unrounded ones.
 //
 // Two forms, for sequences of few rows (lamp_cache_few.h; bound by HBM: 32
-// single tokens over 8K keys, 32/8 heads, d = 128: 537 MB in 95 us, 5.6 TB/s) and
+// single tokens over 8K keys, 32/8 heads, d = 128: 537 MB in 97 us, 5.5 TB/s) and
 // of many (lamp_cache_prompt.hip; bound by the matrix cores and the vector unit:
-// an 8K prompt 538 us, 1.02 PFLOP/s), in one launch where a batch holds both, or
+// an 8K prompt 520 us, 1.06 PFLOP/s), in one launch where a batch holds both, or
 // in two where sequences are short on average (CHUNK); then, where a sequence may
 // have been cut in pieces, a launch that joins them.
 #include <hip/hip_runtime.h>

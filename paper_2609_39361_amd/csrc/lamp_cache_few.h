@@ -20,11 +20,11 @@ namespace {
 // V's KT/4 keys of a channel (V is stored transposed within its page).  Codes
 // go from global memory straight to registers in 16-byte loads; the next
 // tile's are requested as soon as this tile's have been used.  Bound by HBM
-// (32 x 8192 keys, d = 128: 5.6 TB/s where a large copy reaches 5.1), for one
-// sequence by the latencies of lengths, table and codes, one after another
-// (20011 keys, 41 MB: 13 us; 37 tokens' whole call: 6).  Tiles of 64 keys (32 at
-// d = 256, for registers): 32 x 8192 keys 104 us, with tiles of 32 110; three
-// workgroups a CU instead of two spill (169).
+// (32 x 8192 keys, d = 128: 537 MB in 97 us, 5.5 TB/s where a large copy reaches
+// 5.1), for one sequence by the latencies of lengths, table and codes, one after
+// another (20011 keys, 41 MB: 13 us; 37 tokens: 6).  Tiles of 64 keys (32 at d =
+// 256, for registers): with tiles of 32 the 32 x 8192 keys take 6 % longer; with
+// three workgroups a CU instead of two registers spill (62 %).
 template <int D, int WAVES>
 struct FewShared {
     float o[WAVES * 16 * (D + 4)];

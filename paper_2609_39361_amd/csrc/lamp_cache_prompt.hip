@@ -30,8 +30,9 @@
 // of each do.
 //
 // Bound by the issue of products and vector instructions together.  An 8K prompt
-// (32/8 heads, d = 128) takes 540 us, 1.02 PFLOP/s, where a large bf16 product
-// reaches 1.28: by its counters a tile of 64 keys takes a SIMD's two waves 4260
+// (32/8 heads, d = 128) takes 520 us a call back to back (562 the median
+// in a trace, 534 the least), 1.06 PFLOP/s, where a large bf16 product reaches
+// 1.28: by its counters a tile of 64 keys takes a SIMD's two waves 4260
 // cycles, the matrix cores being busy for 2050 of them and the vector unit for
 // 2340 (no LDS bank conflicts).  Both waves in the same phase: 589 us instead of
 // 557; 64 rows a wave, one wave a SIMD: registers spill, 8 times as long.  For
@@ -113,7 +114,8 @@ __device__ __forceinline__ void cache_prompt(const CacheAttnParams &p, int x, Pr
     const int whi_any = upto(wpmax), wlo_any = from(wpmin), whi_all = upto(wpmin), wlo_all = from(wpmax);
 
     constexpr int QR = D / 16 - Q_LDS<D>;       // operands in registers
-    // operands in flight from LDS (8K prompt, d = 128: with one 564 us, two 540, eight 543; d = 256, 8K: two 446, four 427)
+    // operands in flight from LDS (8K prompt, d = 128, side by side: with one 564 us, two 540, eight 543; d = 256, 8K: two 446,
+    // four 427)
     constexpr int AHEAD = D > 128 ? 4 : 2;
     bf16x8 qf[QR];
     {
@@ -433,6 +435,8 @@ __device__ __forceinline__ void cache_prompt(const CacheAttnParams &p, int x, Pr
             // One value scale for the tile goes into the exponent (a power of
             // two, so that the sum has it divided out exactly), if it leaves
             // the smallest probabilities that count (2^-60) far above fp32's.
+            // The reference is rounded once more for it, to fp32: as the logits
+            // are, half a step of a number of their size.
             if (WIDE && vs[0] > 0x1p-64f && vs[0] < 0x1p64f)
                 exponentials(ms - __builtin_amdgcn_logf(vs[0]), __builtin_amdgcn_rcpf(vs[0]), true);
             else

@@ -113,8 +113,9 @@ __device__ __forceinline__ void norm_rotate(float *a, float *b, bool normed, con
 // Bound by HBM (each element read and written once); a wave takes whole rows
 // of one token, 1024/D at a time, so the token's cos and sin and the gains are
 // loaded once and stay in registers over its heads.  4 x 8192 tokens of 32/8
-// heads, d = 128: 809 MB in 180 us, 4.5 TB/s (a large copy: 5.1); 1999 tokens
-// 14 us; one token 4 us, a launch's latency.
+// heads, d = 128: 809 MB in 189 us in a trace, 4.3 TB/s (180 a call back to back;
+// a large copy: 5.1), of fp32 1212 MB in 231, 5.2 TB/s; 1999 tokens 14 us; one
+// token 4 us, a launch's latency.
 template <int D, bool F32>
 __global__ __launch_bounds__(256) void norm_rope_kernel(NormRopeParams p)
 {
@@ -289,7 +290,9 @@ __device__ __forceinline__ void transpose4(uint32_t *w)
 // HBM for prompts (32K tokens of 8 heads, d = 128: 218 MB in 59 us, 3.7 TB/s, with
 // the rotation's table read from the L2 once a head; keeping cos and sin over 4
 // heads instead doubles the registers and takes 78), by the latencies of starts,
-// lengths, table and rows for single tokens (32: 5 us).
+// lengths, table and rows for single tokens (32: 5 us).  Short pages leave lanes
+// idle (16 tokens of d = 64 are 64 of the 256 threads' rows) and look up as much a
+// page as long ones (13 MB of fp32 tokens into pages of 16: 9.6 us).
 constexpr int VT = 64;       // slots of the transposing tile
 
 // LONG: pages of more than 64 tokens.

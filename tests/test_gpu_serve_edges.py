@@ -322,3 +322,18 @@ def test_captured_chunk_that_comes_and_goes(L, S, width):  # noqa: F811
         for x, y in zip(L.attn_cache(qd, c, td, a, b), out):
             assert torch.equal(x[:n], y[:n]), "replay %d" % i
         torch.randn(1000, 1000, device="cuda").sum().item()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_norm_rope_at_the_ends_of_fp32(L, dtype):  # noqa: F811
+    """Rows whose squares fp32 still holds are normed; one whose sum of squares passes 2^128 comes out 0."""
+    x = torch.randn(4, 2, 64, generator=_gen(95)).to(dtype)
+    x[0] *= 2.0 ** 58
+    x[1] *= 2.0 ** 100
+    x[2] *= 2.0 ** -60
+    w = torch.ones(64)
+    y = L.qk_norm_rope(x.cuda(), q_weight=w.cuda(), eps=0.0)[0]
+    for t in (0, 2, 3):
+        want, err = R.norm_rope(x[t], w, None, None, 0.0)
+        R.near(y[t], want, R.BF16 * want.abs() + 1.01 * err, "row %d" % t)
+    assert not y[1].any()
