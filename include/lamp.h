@@ -455,7 +455,8 @@ int lamp_kv_append(const void *k, const void *v, int in_f32, int64_t k_token, in
  * j > p - window (window > 0; requires causal).  Logits are scale * q.k.
  * Products of bf16 queries and 8-bit keys are exact and summed in fp32; the
  * softmax is in fp32; probabilities times the values' scale are rounded to
- * bf16 for the product with the values, which is summed in fp32.
+ * bf16 for the product with the values, which is summed in fp32 and divided by
+ * the sum at the end (values up to 2^88 cannot overflow it).
  * A row that sees no key has o = 0 and lse = -infinity; one that sees a key of
  * a missing page (or beyond the table) is NaN.  A row that sees keys, all with
  * logits of -infinity (an infinite query), has o = NaN and lse = -infinity; a
