@@ -281,7 +281,7 @@ def prepare(case, seed):
     hkv, d = case["Hkv"], case["d"]
     if op == "bounds":
         st["bounds"] = torch.zeros((st["k"].shape[0], hkv, 2, d), device="cuda", dtype=torch.int8)
-        return dict(st, case=case)
+        return dict(st, tokens=total, case=case)
     hq = case["Hq"]
     st["q"] = (1.5 * randn(total, hq, d) / gain.repeat_interleave(hq // hkv, 1)[:, :, 0]).to(torch.bfloat16)
     if op == "select":
@@ -451,7 +451,7 @@ def _own_run(st):
         return lens, q_start, positions, pool.state, st["table"], pool.ring
     cache = lamp.KVCache(st["k"], st["v"], st["k_scale"], st["v_scale"])
     if c["op"] == "bounds":
-        return lamp.kv_bounds(cache, st["bounds"], st["table"], st["kv_lens"], q_start=st["q_start"])
+        return lamp.kv_bounds(cache, st["bounds"], st["table"], st["kv_lens"], st["tokens"], q_start=st["q_start"])
     if c["op"] == "select":
         return lamp.select_pages(st["q"], cache, st["bounds"], st["table"], st["kv_lens"], c["budget"], q_start=st["q_start"],
                                  first=c["first"], last=c["last"])
