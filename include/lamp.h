@@ -475,6 +475,106 @@ int lamp_attn_cache(const uint16_t *q, int64_t q_token, int64_t q_head, int Hq, 
 size_t lamp_attn_cache_workspace_size(int T, int S, int Hq, int Hkv, int d, int page, int width);
 
 /*
+ * Long contexts and changing batches, over the same cache: planning a step on the
+ * device (lamp_kv_advance), attention over pages that a cheap score selects
+ * (lamp_kv_bounds, lamp_select_pages, lamp_attn_pages), and attention of sequences
+ * that share a prefix (lamp_attn_shared).  Asynchronous and capturable as above.
+ */
+
+/*
+ * lamp_kv_advance -- the next step of S sequences: sequence s has lens[s] keys and
+ * adds add[s] >= 0 tokens, or (add[s] < 0) leaves.  Into a batch (lamp_batch) for
+ * the calls above go
+ *   kv_lens[s] = lens[s] + add[s] (0 where it leaves),  q_start [S+1],
+ *   positions [T]: of each new token (0 behind the last),
+ * and into the table the pages of the places
+ * [ceil(lens/page), ceil((lens+add)/page)), others being left as they are.
+ *
+ * Free pages are in a ring: ring [pages], state[0] its first free entry, state[1] how
+ * many there are.  Pages are taken from its front, by sequence and place; those of
+ * the sequences that leave are put behind its end in the same order and can be
+ * taken from the next call on.  The first prefix_lens[s] / page places (rounded
+ * down; prefix_lens NULL: none) are not the sequence's own and do not go back.
+ * state_out: [0], [1] as state, [2] the pages that the step needs, [3] 0, or why
+ * it was not admitted: 1 too few free pages, 2 a sequence longer than width * page,
+ * 4 more than T new tokens.  A step that is not admitted adds no token
+ * (kv_lens = lens, q_start = 0, no page is taken); sequences leave all the same.
+ * 8 (in any case) more pages would go back than the ring has room for, and none does.
+ *
+ * kv_lens may be lens, and state_out state; no other two arrays may overlap.  page:
+ * 16, 32, 64, 128 or 256; S up to 2^20, T up to 2^23, width*page up to 2^30.
+ * Values that break these rules give wrong results, never an access outside the
+ * arrays.
+ */
+int lamp_kv_advance(const int32_t *lens, const int32_t *add, const int32_t *prefix_lens, int32_t *table,
+                    int64_t table_stride, int S, int width, int page, int T, int32_t *ring, int pages,
+                    const int32_t *state, int32_t *kv_lens, int32_t *q_start, int32_t *positions, int32_t *state_out,
+                    void *stream);
+
+/*
+ * lamp_kv_bounds -- for each page that holds new tokens of the batch (after
+ * lamp_kv_append), each head and channel: the range of the code values of the keys
+ * there, in units of 4, rounded outward: bounds int8 [pages][Hkv][2][d], [0] the
+ * largest, [1] the smallest.  So no key's channel is above 4 k_scale bounds[0] or below
+ * 4 k_scale bounds[1].  NaN codes take no part; a channel without a number has 0
+ * and 0.  The values of the cache are not read.  Other pages keep theirs.  bounds
+ * 16-byte aligned.
+ */
+int lamp_kv_bounds(const lamp_cache *cache, const lamp_batch *batch, int8_t *bounds, void *stream);
+
+/*
+ * lamp_select_pages -- for each new token and kv head the `budget` places of the
+ * sequence's table row whose pages have the largest scores.
+ *
+ * The queries of the token's Hq/Hkv heads of the group are rounded to integers
+ * q' = q / 2^e (to nearest even), e >= -100 the smallest with |q'| <= 127 for all of
+ * them (what is not finite counts as 0).  A page's score is
+ *   k_scale * max over the heads of sum_c max(q'_c bounds[0]_c, q'_c bounds[1]_c),
+ * an integer times a power of two, exact in fp32: in units of 2^(e+2) an upper
+ * bound of q.k for the rounded query.  Places are those of the keys that the token
+ * sees, [0, p/page] at position p, and within the table.  The first `first` and the
+ * last `last` of them are taken always, then those of the largest score, ties to the
+ * lower place; places without a page come after all others.  places int32
+ * [T][Hkv][budget]: ascending, -1 behind the last.  budget >= first + last.
+ * Nothing is written for tokens from q_start[S] on.
+ *
+ * workspace: lamp_select_pages_workspace_size(...) bytes, as for lamp_attn_cache.
+ * budget up to 2^20, T*Hkv*width up to 2^32; other limits as for lamp_attn_cache.
+ */
+int lamp_select_pages(const uint16_t *q, int64_t q_token, int64_t q_head, int Hq, const lamp_cache *cache,
+                      const lamp_batch *batch, const int8_t *bounds, int budget, int first, int last,
+                      int32_t *places, void *workspace, size_t workspace_bytes, void *stream);
+size_t lamp_select_pages_workspace_size(int T, int Hkv, int width, int budget);
+
+/*
+ * lamp_attn_pages -- lamp_attn_cache (causal) where each token and kv head sees only
+ * the keys of the places in its list, places int32 [T][Hkv][budget]: any order,
+ * each place at most once; entries outside [0, width) and places behind the
+ * token's position hold no keys.  Edges as for lamp_attn_cache: a row without keys
+ * has o = 0 and lse = -infinity, one with a listed place without a page is NaN.
+ * T*Hq*ceil(budget/1024) up to 2^24; other limits as for lamp_attn_cache.
+ */
+int lamp_attn_pages(const uint16_t *q, int64_t q_token, int64_t q_head, int Hq, const lamp_cache *cache,
+                    const lamp_batch *batch, const int32_t *places, int budget, double scale, uint16_t *o, float *lse,
+                    void *workspace, size_t workspace_bytes, void *stream);
+size_t lamp_attn_pages_workspace_size(int T, int Hq, int Hkv, int d, int page, int budget);
+
+/*
+ * lamp_attn_shared -- lamp_attn_cache (causal, no window) where sequences share
+ * prefixes: the sequences [group_start[g], group_start[g+1]) of group g hold the
+ * same first prefix_lens[s] keys (the same number for all of a group; rounded down
+ * to whole pages), which are read once for the group, through the table row of its
+ * first sequence.  group_start int32 [groups+1], non-decreasing, from 0 to S;
+ * prefix_lens int32 [S], at most the keys before the sequence's new tokens (0: none).
+ * The same results as lamp_attn_cache's but for the order of fp32 sums.
+ * T*Hq up to 2^23; other limits as for lamp_attn_cache.
+ */
+int lamp_attn_shared(const uint16_t *q, int64_t q_token, int64_t q_head, int Hq, const lamp_cache *cache,
+                     const lamp_batch *batch, const int32_t *prefix_lens, const int32_t *group_start, int groups,
+                     double scale, uint16_t *o, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+size_t lamp_attn_shared_workspace_size(int T, int S, int groups, int Hq, int Hkv, int d, int page, int width);
+
+/*
  * lamp_attn_logits8 -- the 8-bit logits alone (Alg. 1, first accumulation;
  * Sec. 4.1 recursive FMA summation rounded to e4m3 after every step).
  * Writes the e4m3 codes of rows [row0, row0 + nrows) of every (b, h):

@@ -32,8 +32,9 @@ SOURCES = ["lamp_kernels.hip", "lamp_fwd.hip", "lamp_fwd16.hip", "lamp_fwd16_sr.
            "lamp_noalloc.hip", "lamp_host.cpp"]
 # parts of lamp_fwd16.hip, lamp_fwd16_sr.hip and lamp_kernels.hip (the serving operators) that this build
 # compiles as units of their own, side by side (-DLAMP_SPLIT_UNITS; without it those include them)
-SPLIT_UNITS = ["lamp_cache_prompt.hip", "lamp_cache_attn.hip", "lamp_serve.hip", "lamp_fwd16_d64.hip",
-               "lamp_fwd16_d256.hip", "lamp_fwd16_sim.hip", "lamp_fwd16_sr_d64.hip", "lamp_fwd16_sr_d256.hip"]
+SPLIT_UNITS = ["lamp_cache_shared.hip", "lamp_cache_prompt.hip", "lamp_cache_attn.hip", "lamp_cache_pages.hip", "lamp_serve.hip",
+               "lamp_pages.hip", "lamp_advance.hip", "lamp_fwd16_d64.hip", "lamp_fwd16_d256.hip", "lamp_fwd16_sim.hip",
+               "lamp_fwd16_sr_d64.hip", "lamp_fwd16_sr_d256.hip"]
 
 DPP_VGPR_WAITS = 2
 DPP_EXEC_WAITS = 5

@@ -32,9 +32,20 @@ struct FewShared {
     uint32_t marks[FewRows::ROWS][D / 32];   // rows and channels that see NaN values (mark_nan)
 };
 
-template <int D, int KT, int WAVES>
-__device__ __forceinline__ void cache_few(const CacheAttnParams &p, int x, FewShared<D, WAVES> &sh)
+// Over selected pages (attn_pages): the entries of a piece's part of the token's
+// list, as (page, position of its first key).
+template <int D, int WAVES>
+struct PagesShared : FewShared<D, WAVES> {
+    int page[PAGES_LISTED], key[PAGES_LISTED];
+    int listed, seen;   // entries up to the last that counts, and how many do
+};
+
+// PAGES: the keys are those of a list of pages; key numbers of tiles, page_at and
+// the loads go through the list, those of masks are positions.
+template <int D, int KT, int WAVES, class P, class SH>
+__device__ __forceinline__ void cache_few(const P &p, int x, SH &sh)
 {
+    constexpr bool PAGES = std::is_same_v<P, PagesAttnParams>;
     constexpr int NT = KT / 16;        // K operands of a tile
     constexpr int KPL = KT / 4;        // keys of a lane
     constexpr int KW = D / 16;         // words of a lane's channels of one key
@@ -47,24 +58,25 @@ __device__ __forceinline__ void cache_few(const CacheAttnParams &p, int x, FewSh
     const Unit u = find_unit<FewRowsOf<WAVES>>(p, G, x);
     if (u.s < 0) return;
     const SeqPlan sq = seq_plan<FewRows>(p, u.s, G);
+    if (PAGES && sq.n == 0) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
     if (threadIdx.x < FewRows::ROWS * (D / 32)) sh.marks[0][threadIdx.x] = 0;
     __syncthreads();
     const int rows = sq.n * G;
     const int r0 = u.tile * FewRows::ROWS, rlast = (r0 + FewRows::ROWS < rows ? r0 + FewRows::ROWS : rows) - 1;
-    write_info<FewRows>(p, u, sq.a, r0, rlast + 1 - r0);
+    write_info<FewRows>(p, u, sq, r0, rlast + 1 - r0);
     const int row = r0 + n < rows ? r0 + n : rlast;   // (missing rows repeat the last, and are not written)
     const int tok = row / G, qh = u.head * G + row - tok * G;
     const int pos = sq.pos0 + tok;                    // may be negative: sees nothing
     const int pmin = sq.pos0 + r0 / G, pmax = sq.pos0 + rlast / G;
     // keys that a position sees: this row's, those that some row sees, that every row sees
-    auto upto = [&](int x) { return p.causal ? (x + 1 < sq.len ? x + 1 : sq.len) : sq.len; };
-    auto from = [&](int x) { return p.window > 0 && x - p.window + 1 > 0 ? x - p.window + 1 : 0; };
+    auto upto = [&](int x) { return sq.causal ? (x + 1 < sq.len ? x + 1 : sq.len) : sq.len; };
+    auto from = [&](int x) { return p.window > 0 && x - p.window + 1 > 0 ? x - p.window + 1 : sq.lo; };
     const int hi = upto(pos), lo = from(pos);
     const int hi_any = upto(pmax), lo_any = from(pmin), hi_all = upto(pmin), lo_all = from(pmax);
     const int t0 = lo_any / KT, t1 = hi_any > lo_any ? (hi_any + KT - 1) / KT : t0;
-    const int beg = __builtin_amdgcn_readfirstlane(t0 + (int)((int64_t)(t1 - t0) * u.piece / u.pieces));
-    const int end = __builtin_amdgcn_readfirstlane(t0 + (int)((int64_t)(t1 - t0) * (u.piece + 1) / u.pieces));
+    int beg = __builtin_amdgcn_readfirstlane(t0 + (int)((int64_t)(t1 - t0) * u.piece / u.pieces));
+    int end = __builtin_amdgcn_readfirstlane(t0 + (int)((int64_t)(t1 - t0) * (u.piece + 1) / u.pieces));
 
     bf16x8 qf[D / 32];
     {
@@ -73,15 +85,40 @@ __device__ __forceinline__ void cache_few(const CacheAttnParams &p, int x, FewSh
         for (int k = 0; k < D / 32; ++k) qf[k] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(q + 8 * k));
     }
 
-    const int *table = p.b.table + u.s * p.b.table_stride;
+    const int *table = p.b.table + sq.row * p.b.table_stride;
     const int ps = p.b.page_shift, pmask = (1 << ps) - 1;
+    if constexpr (PAGES) {
+        if (threadIdx.x == 0) sh.listed = sh.seen = 0;
+        __syncthreads();
+        const int e0 = u.piece * p.per, many = p.budget - e0 < p.per ? p.budget - e0 : p.per;
+        const int *list = p.places + ((int64_t)sq.a * p.b.Hkv + u.head) * p.budget + e0;
+        for (int i = (int)threadIdx.x; i < many; i += 64 * WAVES) {
+            const int place = list[i];
+            const bool is = place >= 0 && place < p.b.width && place << ps < hi_any;
+            sh.page[i] = is ? table[place] : INT_MIN;
+            sh.key[i] = is ? place << ps : INT_MAX / 2;
+            if (is) atomicMax(&sh.listed, i + 1), sh.seen = 1;
+        }
+        __syncthreads();
+        beg = 0;
+        end = __builtin_amdgcn_readfirstlane(((sh.listed << ps) + KT - 1) / KT);
+    }
     // page of the KPL keys from `key` (a page holds them whole): as the table has it (not looked at before its first use, a tile
     // on), or UNSEEN by every row
     constexpr int UNSEEN = INT_MIN;
     auto page_at = [&](int key) {
         int pg = UNSEEN;
-        if (key < hi_any && key + KPL > lo_any) pg = table[key >> ps];
+        if constexpr (PAGES) {
+            if (key >> ps < sh.listed) pg = sh.page[key >> ps];
+        } else if (key < hi_any && key + KPL > lo_any) {
+            pg = table[key >> ps];
+        }
         return pg;
+    };
+    // position of the first of the KPL keys from `key`
+    auto position = [&](int key) {
+        if constexpr (PAGES) return key >> ps < sh.listed ? sh.key[key >> ps] + (key & pmask) : INT_MAX / 2;
+        else return key;
     };
     auto held = [&](int pg) { return pg >= 0 && pg < p.b.pages; };   // (otherwise UNSEEN or missing)
     const int kgrp = ((n >> 2) * KPL);   // the lane's key group as a row of K, its first key in the tile
@@ -129,7 +166,9 @@ __device__ __forceinline__ void cache_few(const CacheAttnParams &p, int x, FewSh
 #pragma unroll
     for (int i = 0; i < DT; ++i) o[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     // l: of this lane's keys.  A row that sees keys beyond the table's reach is NaN.
-    float m = hi > lo ? LOWEST : NEG_INF, l = (p.causal && pos + 1 < sq.all ? pos + 1 : sq.all) > sq.len ? __builtin_nanf("") : 0.0f;
+    bool some_key = hi > lo;
+    if constexpr (PAGES) some_key = sh.seen != 0;
+    float m = some_key ? LOWEST : NEG_INF, l = !PAGES && (sq.causal && pos + 1 < sq.all ? pos + 1 : sq.all) > sq.len ? __builtin_nanf("") : 0.0f;
 
     int t = beg + wave;
     if (t < end) {
@@ -153,8 +192,9 @@ __device__ __forceinline__ void cache_few(const CacheAttnParams &p, int x, FewSh
                 acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(kreg[i][2 * k], kreg[i][2 * k + 1]), qf[k], acc[i], 0, 0, 0);
         }
         if (next < end) load_k(next);
-        const int key0 = t * KT + g * KPL;   // the lane's keys: key0 + 4 i + e
-        const bool partial = t * KT < lo_all || t * KT + KT > hi_all || __ballot(bad) != 0;   // (of the whole wave)
+        const int key0 = position(t * KT + g * KPL);   // the lane's keys: key0 + 4 i + e
+        const bool partial = PAGES ? __ballot(bad || key0 + KPL > hi_all) != 0
+                                   : t * KT < lo_all || t * KT + KT > hi_all || __ballot(bad) != 0;   // (of the whole wave)
         float x[KPL];
 #pragma unroll
         for (int i = 0; i < NT; ++i)
@@ -265,8 +305,8 @@ __device__ __forceinline__ void cache_few(const CacheAttnParams &p, int x, FewSh
         const uint32_t nan = sh.marks[r][d >> 5] >> (d & 31);
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = nan >> e & 1u ? __builtin_nanf("") : v[e];
-        if (u.pieces > 1) {
-            const int64_t at_row = (int64_t)u.slot * FewRows::ROWS + r;
+        if (joined(p, sq, u.pieces)) {
+            const int64_t at_row = PAGES ? ((int64_t)u.piece * p.b.T + sq.a) * p.Hq + u.head * G + r0 + r : (int64_t)u.slot * FewRows::ROWS + r;
             *reinterpret_cast<f32x4 *>(p.part[0] + at_row * D + d) = v;
             if (d == 0) {
                 p.part_ml[0][at_row * 2] = mx;

@@ -62,6 +62,8 @@ struct SeqPlan {
     int tiles;       // row tiles
     int kt;          // key tiles that a row tile visits at most
     float mean;      // and on average
+    int row;         // of the table
+    int lo, causal;  // first key of the range; whether a row sees none behind its own position
 };
 
 // Row tiles whose mean is this part of the longest at least count as even.
@@ -71,6 +73,9 @@ template <class F>
 __device__ __forceinline__ SeqPlan seq_plan(const CacheAttnParams &p, int s, int G)
 {
     SeqPlan r;
+    r.row = s;
+    r.lo = 0;
+    r.causal = p.causal;
     r.a = p.b.q_start ? p.b.q_start[s] : s;
     const int e = p.b.q_start ? p.b.q_start[s + 1] : s + 1;
     const int len = p.b.kv_lens[s] > 0 ? p.b.kv_lens[s] : 0;
@@ -88,6 +93,86 @@ __device__ __forceinline__ SeqPlan seq_plan(const CacheAttnParams &p, int s, int
     }
     r.mean = p.causal ? fminf((float)r.kt, ((float)r.len - 0.5f * (float)r.n) * (1.0f / TILE)) : (float)r.kt;
     return r;
+}
+
+// Groups of sequences with a shared prefix (lamp_cache_shared.hip): what is
+// planned is each group's new tokens over the prefix, then each sequence's over
+// the keys behind it.
+__device__ __forceinline__ int prefix_of(const SharedAttnParams &p, int s)
+{
+    const int page = 1 << p.b.page_shift, reach = p.b.width << p.b.page_shift;
+    int n = s >= 0 && s < p.b.S ? p.prefix_lens[s] : 0;
+    n = n > 0 ? n & ~(page - 1) : 0;   // (whole pages)
+    return n < reach ? n : reach;
+}
+
+template <class F>
+__device__ __forceinline__ SeqPlan seq_plan(const SharedAttnParams &p, int v, int G)
+{
+    SeqPlan r;
+    const bool group = v < p.groups;
+    const int s = group ? p.group_start[v] : v - p.groups, s1 = group ? p.group_start[v + 1] : s + 1;
+    const bool is = s >= 0 && s1 <= p.b.S && s < s1;
+    r.row = is ? s : 0;
+    r.a = !is ? 0 : (p.b.q_start ? p.b.q_start[s] : s);
+    const int e = !is ? 0 : (p.b.q_start ? p.b.q_start[s1] : s1);
+    const int prefix = prefix_of(p, r.row);
+    r.n = r.a >= 0 && e <= p.b.T && e > r.a ? e - r.a : 0;
+    const int reach = p.b.width << p.b.page_shift;   // (at most 2^30)
+    r.causal = !group;
+    if (group) {
+        r.lo = 0;
+        r.pos0 = 0;
+        r.all = r.len = prefix;
+        if (prefix == 0) r.n = 0;
+    } else {
+        const int len = p.b.kv_lens[r.row] > 0 ? p.b.kv_lens[r.row] : 0;
+        r.lo = prefix;
+        r.pos0 = len - r.n;
+        r.all = len;
+        r.len = len < reach ? len : reach;
+    }
+    const int rows = r.n * G;                        // (at most 2^27)
+    r.tiles = rows > p.rows_above[F::FORM] && rows <= p.rows_upto[F::FORM] ? (rows + F::ROWS - 1) / F::ROWS : 0;
+    const int keys = r.len > r.lo ? r.len - r.lo : 0;
+    r.kt = (keys + TILE - 1) / TILE;
+    r.mean = r.causal ? fmaxf(0.0f, fminf((float)r.kt, ((float)keys - 0.5f * (float)r.n) * (1.0f / TILE))) : (float)r.kt;
+    return r;
+}
+
+// A token and its list of pages: planned from the sizes alone.
+constexpr int PAGES_LISTED = 1024;   // entries of a piece
+
+template <class F>
+__device__ __forceinline__ SeqPlan seq_plan(const PagesAttnParams &p, int t, int)
+{
+    SeqPlan r = {};
+    int s = t, e = t + 1, a = t;
+    if (p.b.q_start) {
+        s = last_at_most(p.b.S, t, [&](int i) { return (int64_t)p.b.q_start[i]; });
+        a = p.b.q_start[s];
+        e = p.b.q_start[s + 1];
+    }
+    const int len = p.b.kv_lens[s] > 0 ? p.b.kv_lens[s] : 0, reach = p.b.width << p.b.page_shift;
+    r.row = s;
+    r.a = t;
+    r.n = a >= 0 && a <= t && t < e && e <= p.b.T;
+    r.causal = 1;
+    r.pos0 = len - (e - t);
+    r.all = len;
+    r.len = len < reach ? len : reach;
+    return r;
+}
+
+// What a plan goes over, and whether a sequence's units of `pieces` pieces leave
+// partial outputs to be joined.
+__device__ __forceinline__ int planned(const CacheAttnParams &p) { return p.b.S; }
+__device__ __forceinline__ int planned(const SharedAttnParams &p) { return p.b.S + p.groups; }
+__device__ __forceinline__ bool joined(const CacheAttnParams &, const SeqPlan &, int pieces) { return pieces > 1; }
+__device__ __forceinline__ bool joined(const PagesAttnParams &, const SeqPlan &, int pieces) { return pieces > 1; }
+__device__ __forceinline__ bool joined(const SharedAttnParams &, const SeqPlan &r, int pieces)
+{
+    return pieces > 1 || r.lo > 0 || !r.causal;
 }
 
 // Inclusive sum over the wave's lanes; and maximum, of numbers >= 0.
@@ -142,13 +227,13 @@ struct Split {
     int least, tiles;
 };
 
-template <class F>
-__device__ __forceinline__ Share share_of(const CacheAttnParams &p, const SeqPlan &r, Split split)
+template <class F, class P>
+__device__ __forceinline__ Share share_of(const P &p, const SeqPlan &r, Split split)
 {
     const float x = (float)r.kt * (1.0f / split.each) + 0.01f;   // (an even share stays one under the sums' rounding)
     const int c = x > 1.02f && x < 2.0f ? split.least : (int)x, most = r.kt / split.tiles, fit = c < most ? c : most;
     const int pieces = fit < 1 ? 1 : fit, units = r.tiles * p.b.Hkv * pieces;
-    return {r.tiles, pieces, units, pieces > 1 ? units : 0};
+    return {r.tiles, pieces, units, joined(p, r, pieces) ? units : 0};
 }
 
 // Sums over a form's row tiles (of one head): their number, the key tiles they
@@ -185,11 +270,12 @@ __device__ __forceinline__ Split split_of(const CacheAttnParams &p, const Work &
 
 // Unit `local` of sequence s, whose partial outputs start at `slots`.  (Tables
 // that break their rules may count past the bounds: such units are left out.)
-template <class F>
-__device__ __forceinline__ Unit unit_of(const CacheAttnParams &p, int s, int tiles, int c, int local, int slots)
+template <class F, class P>
+__device__ __forceinline__ Unit unit_of(const P &p, int s, int tiles, int c, int local, int slots)
 {
+    constexpr bool ANY = !std::is_same_v<P, CacheAttnParams>;   // (one piece may have a partial output too)
     const int pair = local / c, slot = slots + local;
-    if (local < 0 || pair >= tiles * p.b.Hkv || (c > 1 && (slot < 0 || slot >= p.slots[F::FORM]))) return {-1, 0, 0, 0, 0, 0};
+    if (local < 0 || pair >= tiles * p.b.Hkv || ((ANY || c > 1) && (slot < 0 || slot >= p.slots[F::FORM]))) return {-1, 0, 0, 0, 0, 0};
     // (causal: the last row tiles see most keys, and start first)
     return {s, tiles - 1 - pair / p.b.Hkv, pair % p.b.Hkv, local - pair * c, c, slot};
 }
@@ -204,8 +290,8 @@ __device__ __forceinline__ Work wave_work(Work w)
 
 // Unit x, by a wave that plans for itself: lane l has the EACH sequences from
 // EACH l.
-template <class F, int EACH>
-__device__ __forceinline__ Unit plan_alone(const CacheAttnParams &p, int G, int x)
+template <class F, int EACH, class P>
+__device__ __forceinline__ Unit plan_alone(const P &p, int G, int x)
 {
     const int lane = threadIdx.x & 63;
     SeqPlan r[EACH];
@@ -213,7 +299,7 @@ __device__ __forceinline__ Unit plan_alone(const CacheAttnParams &p, int G, int 
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
         const int s = EACH * lane + i;
-        r[i] = s < p.b.S ? seq_plan<F>(p, s, G) : SeqPlan{};
+        r[i] = s < planned(p) ? seq_plan<F>(p, s, G) : SeqPlan{};
         add(w, r[i]);
     }
     const Split split = split_of<F>(p, wave_work(w));
@@ -244,10 +330,71 @@ __device__ __forceinline__ Unit plan_alone(const CacheAttnParams &p, int G, int 
     return unit_of<F>(p, EACH * l + i, at.tiles, at.c, local, before);
 }
 
-template <class F>
-__device__ __forceinline__ Unit unit_at(const CacheAttnParams &p, int G, int x)
+// The plan of many sequences, a workgroup for each form: key tiles of a piece
+// from the sum over all sequences, then what lies before each.  A thread takes
+// consecutive sequences, in three passes over their lengths (bound by these
+// loads' latency).
+template <class F, class P>
+__device__ void plan_form(const P &p)
 {
-    if (p.b.S == 1) {
+    constexpr int THREADS = 1024, WAVES = THREADS / 64;
+    __shared__ Work works[WAVES];
+    __shared__ Before sums[WAVES];
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), G = p.Hq / p.b.Hkv;
+    const int S = planned(p), each = (S + THREADS - 1) / THREADS;
+    const int s0 = tid * each < S ? tid * each : S, s1 = S - s0 < each ? S : s0 + each;
+    Work work = {};
+#pragma unroll 4
+    for (int s = s0; s < s1; ++s) add(work, seq_plan<F>(p, s, G));
+    work = wave_work(work);
+    if (lane == 0) works[wave] = work;
+    __syncthreads();
+    work = {};
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        work.tiles += works[w].tiles;
+        work.most += works[w].most;
+        work.mean += works[w].mean;
+        work.longest = fmaxf(work.longest, works[w].longest);
+    }
+    const Split split = split_of<F>(p, work);
+    Before at = {0, 0};
+#pragma unroll 4
+    for (int s = s0; s < s1; ++s) {
+        const Share h = share_of<F>(p, seq_plan<F>(p, s, G), split);
+        at.units += h.units;
+        at.slots += h.slots;
+    }
+    const Before own = at;
+    at = {wave_scan(at.units), wave_scan(at.slots)};
+    if (lane == 63) sums[wave] = at;
+    __syncthreads();
+    at = {at.units - own.units, at.slots - own.slots};
+    int slots = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        if (w < wave) at.units += sums[w].units, at.slots += sums[w].slots;
+        slots += sums[w].slots;
+    }
+    if (tid == 0) {
+        p.counts[F::FORM] = slots;
+        static_cast<Split *>(p.split)[F::FORM] = split;
+    }
+    Before *before = static_cast<Before *>(p.before[F::FORM]);
+#pragma unroll 4
+    for (int s = s0; s < s1; ++s) {
+        const Share h = share_of<F>(p, seq_plan<F>(p, s, G), split);
+        before[s] = at;
+        at.units += h.units;
+        at.slots += h.slots;
+    }
+}
+
+template <class F, class P>
+__device__ __forceinline__ Unit unit_at(const P &p, int G, int x)
+{
+    const int S = planned(p);
+    if (S == 1) {
         const SeqPlan r = seq_plan<F>(p, 0, G);
         Work w = {};
         add(w, r);
@@ -255,23 +402,33 @@ __device__ __forceinline__ Unit unit_at(const CacheAttnParams &p, int G, int x)
         if (x == 0 && p.slots[F::FORM] && threadIdx.x == 0) p.counts[F::FORM] = h.slots;
         return unit_of<F>(p, 0, h.tiles, h.c, x, 0);
     }
-    if (p.b.S <= 64) return plan_alone<F, 1>(p, G, x);
-    if (p.b.S <= PLAN_ALONE) return plan_alone<F, PLAN_ALONE / 64>(p, G, x);
+    if (S <= 64) return plan_alone<F, 1>(p, G, x);
+    if (S <= PLAN_ALONE) return plan_alone<F, PLAN_ALONE / 64>(p, G, x);
     const Before *before = static_cast<const Before *>(p.before[F::FORM]);
-    const int s = last_at_most(p.b.S, x, [&](int i) { return (int64_t)before[i].units; });
+    const int s = last_at_most(S, x, [&](int i) { return (int64_t)before[i].units; });
     const Share h = share_of<F>(p, seq_plan<F>(p, s, G), static_cast<const Split *>(p.split)[F::FORM]);
     return unit_of<F>(p, s, h.tiles, h.c, x - before[s].units, before[s].slots);
 }
 
 // Unit x of form F, the same in each of the workgroup's waves (in scalar
 // registers, whatever it was worked out in).
-template <class F>
-__device__ __forceinline__ Unit find_unit(const CacheAttnParams &p, int G, int x)
+template <class F, class P>
+__device__ __forceinline__ Unit find_unit(const P &p, int G, int x)
 {
     const Unit u = unit_at<F>(p, G, x);
     auto same = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
     return {same(u.s), same(u.tile), same(u.head), same(u.piece), same(u.pieces), same(u.slot)};
 }
+
+template <class F>
+__device__ __forceinline__ Unit find_unit(const PagesAttnParams &p, int G, int x)
+{
+    const int tiles = (G + F::ROWS - 1) / F::ROWS, piece = x % p.pieces, y = x / p.pieces, z = y / tiles;
+    return {z / p.b.Hkv, y - z * tiles, z % p.b.Hkv, piece, p.pieces, 0};
+}
+
+template <class F>
+__device__ __forceinline__ void write_info(const PagesAttnParams &, const Unit &, const SeqPlan &, int, int) {}
 
 // What cache_join_kernel needs to know of a partial output; each unit writes its own.
 struct PartInfo {
@@ -280,11 +437,34 @@ struct PartInfo {
 };
 
 template <class F>
-__device__ __forceinline__ void write_info(const CacheAttnParams &p, const Unit &u, int token, int row0, int rows)
+__device__ __forceinline__ void write_info(const CacheAttnParams &p, const Unit &u, const SeqPlan &sq, int row0, int rows)
 {
     if (u.pieces > 1 && threadIdx.x == 0) {
         PartInfo *i = static_cast<PartInfo *>(p.info[F::FORM]) + u.slot;
-        *i = {token, row0, rows, u.head, u.piece, u.pieces, {0, 0}};
+        *i = {sq.a, row0, rows, u.head, u.piece, u.pieces, {0, 0}};
+    }
+}
+
+// Where a row's partial outputs of one of its two ranges lie, for the join of
+// attn_shared: the first one's row among all, and 2 pieces + form (0: none).
+struct RowInfo {
+    int at, pieces2;
+};
+
+// Of the first piece's unit, for its rows: [0][T][Hq] the prefix, [1][T][Hq] the
+// keys behind it.
+template <class F>
+__device__ __forceinline__ void write_info(const SharedAttnParams &p, const Unit &u, const SeqPlan &sq, int row0, int rows)
+{
+    if (u.piece != 0) return;
+    const int G = p.Hq / p.b.Hkv, base = F::FORM ? p.slots[0] * FewRows::ROWS + u.slot * F::ROWS : u.slot * F::ROWS;
+    const bool part = joined(p, sq, u.pieces);
+    RowInfo *info = static_cast<RowInfo *>(p.rows);
+    for (int r = (int)threadIdx.x; r < rows; r += (int)blockDim.x) {
+        const int gr = row0 + r, t = gr / G;
+        const int64_t row = (int64_t)(sq.a + t) * p.Hq + u.head * G + gr - t * G;
+        info[(sq.causal ? (int64_t)p.b.T * p.Hq : 0) + row] = part ? RowInfo{base + r, 2 * u.pieces + F::FORM} : RowInfo{0, 0};
+        if (sq.causal && sq.lo == 0) info[row] = RowInfo{0, 0};
     }
 }
 
@@ -348,6 +528,62 @@ __device__ __forceinline__ void mark_nan(uint32_t (*marks)[D / 32], uint32_t nan
         for (int r = 0; r < rows; ++r)
             if (sees(r, k)) atomicOr(&marks[r][d >> 5], 1u << (d & 31));
     }
+}
+
+// A row's partial outputs joined by a wave and written (attn_shared, attn_pages):
+// n0 of them from row at0 of `part` on, step0 rows apart, then n1 from at1.  A lane
+// holds D/64 channels, and for each 64 partial outputs the maximum and sum of one.
+// Bound by latency: 8 rows are requested at once.
+template <int D>
+__device__ __forceinline__ void join_row(const float *part, const float *ml, int64_t at0, int64_t step0, int n0, int64_t at1,
+                                         int64_t step1, int n1, uint16_t *o, float *lse)
+{
+    constexpr int C = D / 64, AT = 8;
+    const int lane = threadIdx.x & 63, n = n0 + n1;
+    auto row_of = [&](int k) { return k < n0 ? at0 + k * step0 : at1 + (k - n0) * step1; };
+    float m = NEG_INF, sum = 0.0f, v[C] = {};
+    for (int c0 = 0; c0 < n; c0 += 64) {
+        const int mine = c0 + lane, here = n - c0 < 64 ? n - c0 : 64;
+        const int64_t at = row_of(mine < n ? mine : c0) * 2;
+        const float mc = mine < n ? ml[at] : NEG_INF, lc = ml[at + 1];
+        float mn = mc;
+#pragma unroll
+        for (int k = 1; k < 64; k <<= 1) mn = fmaxf(mn, __shfl_xor(mn, k, 64));
+        mn = fmaxf(mn, m);
+        const float ms = mn == NEG_INF ? 0.0f : mn, f0 = __builtin_amdgcn_exp2f(m - ms);
+        const float f = __builtin_amdgcn_exp2f(mc - ms);
+        float l = mine < n ? lc * f : 0.0f;
+#pragma unroll
+        for (int k = 1; k < 64; k <<= 1) l += __shfl_xor(l, k, 64);
+        m = mn;
+        sum = sum * f0 + l;
+#pragma unroll
+        for (int e = 0; e < C; ++e) v[e] *= f0;
+        for (int k0 = 0; k0 < here; k0 += AT) {
+            float x[AT][C];
+#pragma unroll
+            for (int j = 0; j < AT; ++j) {   // (beyond the last: read again, not added)
+                const float *r = part + row_of(c0 + (k0 + j < here ? k0 + j : k0)) * D + C * lane;
+#pragma unroll
+                for (int e = 0; e < C; ++e) x[j][e] = r[e];
+            }
+#pragma unroll
+            for (int j = 0; j < AT; ++j) {
+                if (k0 + j >= here) break;
+                const float fj = __builtin_bit_cast(float, lane_value(__builtin_bit_cast(int, f), k0 + j));
+#pragma unroll
+                for (int e = 0; e < C; ++e) v[e] += x[j][e] * fj;
+            }
+        }
+    }
+    const float inv = finish(m, sum);
+    if constexpr (C == 1) {
+        o[lane] = (uint16_t)pack2(v[0] * inv, 0.0f);
+    } else {
+#pragma unroll
+        for (int e = 0; e < C; e += 2) *reinterpret_cast<uint32_t *>(o + C * lane + e) = pack2(v[e] * inv, v[e + 1] * inv);
+    }
+    if (lane == 0) *lse = finish_lse(m, sum);
 }
 
 } // namespace

@@ -1048,54 +1048,209 @@ size_t lamp_attn_cache_workspace_size(int T, int S, int Hq, int Hkv, int d, int 
     return lamp::cache_attn_workspace(d, T, S, Hq / Hkv, Hkv, (int64_t)width * page);
 }
 
-int lamp_attn_cache(const uint16_t *q, int64_t q_token, int64_t q_head, int Hq, const lamp_cache *cache,
-                    const lamp_batch *batch, int causal, int window, double scale, uint16_t *o, float *lse,
-                    void *workspace, size_t workspace_bytes, void *stream)
+// The queries of an attention over the cache and its outputs; *p is filled in.
+static int check_attn(const uint16_t *q, int64_t q_token, int64_t q_head, int Hq, const lamp_cache *cache,
+                      const lamp_batch *batch, double scale, uint16_t *o, float *lse, int64_t most_rows, lamp::CacheAttnParams *p)
 {
-    lamp::CacheAttnParams p{};
-    int rc = check_paged(cache, batch, &p.b);
+    int rc = check_paged(cache, batch, &p->b);
     if (rc) return rc;
     if (Hq <= 0 || Hq % cache->Hkv) return fail(LAMP_ERR_INVALID_ARG, "Hq=%d is not a multiple of Hkv=%d", Hq, cache->Hkv);
-    if (causal != 0 && causal != 1) return fail(LAMP_ERR_INVALID_ARG, "causal must be 0 or 1");
-    if (window < 0) return fail(LAMP_ERR_INVALID_ARG, "window must be >= 0");
-    if (window > 0 && !causal) return fail(LAMP_ERR_INVALID_ARG, "a sliding window requires causal=1");
     const float scale_log2 = (float)(scale * 1.4426950408889634);
     if (!std::isfinite(scale_log2)) return fail(LAMP_ERR_INVALID_ARG, "scale must be finite in fp32");
-    if ((int64_t)batch->T * Hq > (int64_t)1 << 27 || Hq > 65536)
-        return fail(LAMP_ERR_UNSUPPORTED, "T*Hq above 2^27 or Hq above 65536");
+    if ((int64_t)batch->T * Hq > most_rows || Hq > 65536)
+        return fail(LAMP_ERR_UNSUPPORTED, "T*Hq above %lld or Hq above 65536", (long long)most_rows);
     if (batch->S == 0 || batch->T == 0) return LAMP_OK;
     const int64_t qs[2] = {q_token, q_head}, sizes[2] = {batch->T, Hq};
     rc = check_rows("q", q, false, qs, sizes, 2);
     if (rc) return rc;
     if (!o || !lse) return fail(LAMP_ERR_INVALID_ARG, "null pointer among o, lse");
     if (!aligned16(o)) return fail(LAMP_ERR_INVALID_ARG, "o not aligned to 16 bytes");
-    p.q = q;
-    p.q_st = q_token;
-    p.q_sh = q_head;
-    p.kc = cache->k;
-    p.vc = cache->v;
-    p.ks = cache->k_scale;
-    p.vs = cache->v_scale;
-    p.o = o;
-    p.lse = lse;
-    p.Hq = Hq;
+    p->q = q;
+    p->q_st = q_token;
+    p->q_sh = q_head;
+    p->kc = cache->k;
+    p->vc = cache->v;
+    p->ks = cache->k_scale;
+    p->vs = cache->v_scale;
+    p->o = o;
+    p->lse = lse;
+    p->Hq = Hq;
+    p->causal = 1;
+    p->scale_log2 = scale_log2;
+    return LAMP_OK;
+}
+
+// The workspace of a serving call that needs `need` bytes: the caller's or the library's.
+static int serve_ws(size_t need, void *workspace, size_t workspace_bytes, void *stream, void **base)
+{
+    *base = nullptr;
+    if (need == 0) return LAMP_OK;
+    lamp_fwd_extra extra{};
+    extra.workspace = workspace;
+    extra.workspace_bytes = workspace_bytes;
+    int dev = 0;
+    const int rc = workspace ? LAMP_OK : current_device(&dev);   // (the library's is the device's)
+    return rc ? rc : call_ws(dev, &extra, need, static_cast<hipStream_t>(stream), base);
+}
+
+int lamp_attn_cache(const uint16_t *q, int64_t q_token, int64_t q_head, int Hq, const lamp_cache *cache,
+                    const lamp_batch *batch, int causal, int window, double scale, uint16_t *o, float *lse,
+                    void *workspace, size_t workspace_bytes, void *stream)
+{
+    lamp::CacheAttnParams p{};
+    if (causal != 0 && causal != 1) return fail(LAMP_ERR_INVALID_ARG, "causal must be 0 or 1");
+    if (window < 0) return fail(LAMP_ERR_INVALID_ARG, "window must be >= 0");
+    if (window > 0 && !causal) return fail(LAMP_ERR_INVALID_ARG, "a sliding window requires causal=1");
+    int rc = check_attn(q, q_token, q_head, Hq, cache, batch, scale, o, lse, (int64_t)1 << 27, &p);
+    if (rc || batch->S == 0 || batch->T == 0) return rc;
     p.causal = causal;
     p.window = window < 1 << 30 ? window : 1 << 30;   // (no key lies farther back)
-    p.scale_log2 = scale_log2;
     const size_t need = lamp::cache_attn_workspace(cache->d, batch->T, batch->S, Hq / cache->Hkv, cache->Hkv,
                                                    (int64_t)batch->width * cache->page);
     void *base = nullptr;
-    if (need > 0) {
-        lamp_fwd_extra extra{};
-        extra.workspace = workspace;
-        extra.workspace_bytes = workspace_bytes;
-        int dev = 0;
-        rc = current_device(&dev);
-        if (rc) return rc;
-        rc = call_ws(dev, &extra, need, static_cast<hipStream_t>(stream), &base);
-        if (rc) return rc;
-    }
+    rc = serve_ws(need, workspace, workspace_bytes, stream, &base);
+    if (rc) return rc;
     HIP_TRY(lamp::launch_cache_attn(cache->d, p, base, static_cast<hipStream_t>(stream)));
+    return LAMP_OK;
+}
+
+// --- long contexts and changing batches ---------------------------------------
+
+static bool built_page(int page) { return page >= 16 && page <= 256 && !(page & (page - 1)); }
+
+int lamp_kv_advance(const int32_t *lens, const int32_t *add, const int32_t *prefix_lens, int32_t *table,
+                    int64_t table_stride, int S, int width, int page, int T, int32_t *ring, int pages,
+                    const int32_t *state, int32_t *kv_lens, int32_t *q_start, int32_t *positions, int32_t *state_out,
+                    void *stream)
+{
+    if (S < 0 || width < 0 || T < 0 || pages <= 0)
+        return fail(LAMP_ERR_INVALID_ARG, "invalid sizes (S=%d width=%d T=%d pages=%d)", S, width, T, pages);
+    if (!built_page(page)) return fail(LAMP_ERR_UNSUPPORTED, "page of %d tokens not built (16, 32, 64, 128, 256)", page);
+    if (S > 1 << 20 || T > 1 << 23 || (int64_t)width * page > (int64_t)1 << 30)
+        return fail(LAMP_ERR_UNSUPPORTED, "S above 2^20, T above 2^23 or width*page above 2^30");
+    if (!ring || !state || !q_start || !state_out || (S > 0 && (!lens || !add || !kv_lens || (width > 0 && !table))) || (T > 0 && !positions))
+        return fail(LAMP_ERR_INVALID_ARG, "null pointer among the step's arrays");
+    int ps = 4;
+    while (1 << ps != page) ++ps;
+    const lamp::AdvanceParams p = {lens, add, prefix_lens, table, table_stride, ring, state, kv_lens, q_start, positions, state_out,
+                                   S, T, width, pages, ps};
+    HIP_TRY(lamp::launch_advance(p, static_cast<hipStream_t>(stream)));
+    return LAMP_OK;
+}
+
+int lamp_kv_bounds(const lamp_cache *cache, const lamp_batch *batch, int8_t *bounds, void *stream)
+{
+    lamp::BoundsParams p{};
+    const int rc = check_paged(cache, batch, &p.b);
+    if (rc) return rc;
+    if (batch->S == 0 || batch->T == 0) return LAMP_OK;
+    if (!bounds || !aligned16(bounds)) return fail(LAMP_ERR_INVALID_ARG, "bounds null or not aligned to 16 bytes");
+    p.kc = cache->k;
+    p.bounds = bounds;
+    HIP_TRY(lamp::launch_kv_bounds(cache->d, p, static_cast<hipStream_t>(stream)));
+    return LAMP_OK;
+}
+
+size_t lamp_select_pages_workspace_size(int T, int Hkv, int width, int budget)
+{
+    if (T <= 0 || Hkv <= 0 || width <= 0 || budget <= 0 || width <= budget) return 0;
+    if (T > 1 << 23 || (int64_t)T * Hkv > (int64_t)1 << 27 || (int64_t)T * Hkv * width > (int64_t)1 << 32) return 0;
+    return lamp::select_workspace(T, Hkv, width);
+}
+
+int lamp_select_pages(const uint16_t *q, int64_t q_token, int64_t q_head, int Hq, const lamp_cache *cache,
+                      const lamp_batch *batch, const int8_t *bounds, int budget, int first, int last,
+                      int32_t *places, void *workspace, size_t workspace_bytes, void *stream)
+{
+    lamp::SelectParams p{};
+    int rc = check_paged(cache, batch, &p.b);
+    if (rc) return rc;
+    if (Hq <= 0 || Hq % cache->Hkv) return fail(LAMP_ERR_INVALID_ARG, "Hq=%d is not a multiple of Hkv=%d", Hq, cache->Hkv);
+    if (first < 0 || last < 0 || budget <= 0 || (int64_t)first + last > budget)
+        return fail(LAMP_ERR_INVALID_ARG, "budget=%d must be positive and at least first=%d + last=%d", budget, first, last);
+    if ((int64_t)batch->T * Hq > (int64_t)1 << 27 || Hq > 65536 || budget > 1 << 20
+        || (int64_t)batch->T * cache->Hkv * batch->width > (int64_t)1 << 32)
+        return fail(LAMP_ERR_UNSUPPORTED, "T*Hq above 2^27, Hq above 65536, budget above 2^20 or T*Hkv*width above 2^32");
+    if (batch->S == 0 || batch->T == 0) return LAMP_OK;
+    const int64_t qs[2] = {q_token, q_head}, sizes[2] = {batch->T, Hq};
+    rc = check_rows("q", q, false, qs, sizes, 2);
+    if (rc) return rc;
+    if (!bounds || !aligned16(bounds)) return fail(LAMP_ERR_INVALID_ARG, "bounds null or not aligned to 16 bytes");
+    if (!places) return fail(LAMP_ERR_INVALID_ARG, "null pointer: places");
+    p.q = q;
+    p.q_st = q_token;
+    p.q_sh = q_head;
+    p.bounds = bounds;
+    p.ks = cache->k_scale;
+    p.places = places;
+    p.Hq = Hq;
+    p.budget = budget;
+    p.first = first;
+    p.last = last;
+    void *base = nullptr;
+    rc = serve_ws(lamp_select_pages_workspace_size(batch->T, cache->Hkv, batch->width, budget), workspace, workspace_bytes, stream, &base);
+    if (rc) return rc;
+    HIP_TRY(lamp::launch_select(cache->d, p, base, static_cast<hipStream_t>(stream)));
+    return LAMP_OK;
+}
+
+// (lists of more than 1024 entries are cut in any case)
+static bool too_many_lists(int64_t T, int64_t Hq, int64_t budget) { return T * Hq * ((budget + 1023) / 1024) > (int64_t)1 << 24; }
+
+size_t lamp_attn_pages_workspace_size(int T, int Hq, int Hkv, int d, int page, int budget)
+{
+    if (T <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv || budget <= 0 || budget > 1 << 20) return 0;
+    if ((d != 64 && d != 128 && d != 256) || !built_page(page) || too_many_lists(T, Hq, budget)) return 0;
+    return lamp::pages_attn_workspace(d, T, Hq / Hkv, Hkv, page, budget);
+}
+
+int lamp_attn_pages(const uint16_t *q, int64_t q_token, int64_t q_head, int Hq, const lamp_cache *cache,
+                    const lamp_batch *batch, const int32_t *places, int budget, double scale, uint16_t *o, float *lse,
+                    void *workspace, size_t workspace_bytes, void *stream)
+{
+    lamp::PagesAttnParams p{};
+    int rc = check_attn(q, q_token, q_head, Hq, cache, batch, scale, o, lse, (int64_t)1 << 24, &p);
+    if (rc) return rc;
+    if (budget <= 0) return fail(LAMP_ERR_INVALID_ARG, "budget=%d must be positive", budget);
+    if (budget > 1 << 20 || too_many_lists(batch->T, Hq, budget))
+        return fail(LAMP_ERR_UNSUPPORTED, "budget above 2^20 or T*Hq*ceil(budget/1024) above 2^24");
+    if (batch->S == 0 || batch->T == 0) return LAMP_OK;
+    if (!places) return fail(LAMP_ERR_INVALID_ARG, "null pointer: places");
+    p.places = places;
+    p.budget = budget;
+    void *base = nullptr;
+    rc = serve_ws(lamp_attn_pages_workspace_size(batch->T, Hq, cache->Hkv, cache->d, cache->page, budget), workspace, workspace_bytes,
+                  stream, &base);
+    if (rc) return rc;
+    HIP_TRY(lamp::launch_pages_attn(cache->d, p, base, static_cast<hipStream_t>(stream)));
+    return LAMP_OK;
+}
+
+size_t lamp_attn_shared_workspace_size(int T, int S, int groups, int Hq, int Hkv, int d, int page, int width)
+{
+    if (T <= 0 || S <= 0 || groups <= 0 || groups > S || Hq <= 0 || Hkv <= 0 || Hq % Hkv || width < 0) return 0;
+    if ((d != 64 && d != 128 && d != 256) || !built_page(page) || (int64_t)width * page > (int64_t)1 << 30) return 0;
+    if (T > 1 << 23 || (int64_t)S * Hkv > 1 << 20 || (int64_t)T * Hq > (int64_t)1 << 23) return 0;
+    return lamp::shared_attn_workspace(d, T, S, groups, Hq / Hkv, Hkv, (int64_t)width * page);
+}
+
+int lamp_attn_shared(const uint16_t *q, int64_t q_token, int64_t q_head, int Hq, const lamp_cache *cache,
+                     const lamp_batch *batch, const int32_t *prefix_lens, const int32_t *group_start, int groups,
+                     double scale, uint16_t *o, float *lse, void *workspace, size_t workspace_bytes, void *stream)
+{
+    lamp::SharedAttnParams p{};
+    int rc = check_attn(q, q_token, q_head, Hq, cache, batch, scale, o, lse, (int64_t)1 << 23, &p);
+    if (rc || batch->S == 0 || batch->T == 0) return rc;
+    if (groups <= 0 || groups > batch->S) return fail(LAMP_ERR_INVALID_ARG, "groups=%d of %d sequences", groups, batch->S);
+    if (!prefix_lens || !group_start) return fail(LAMP_ERR_INVALID_ARG, "null pointer among prefix_lens, group_start");
+    p.prefix_lens = prefix_lens;
+    p.group_start = group_start;
+    p.groups = groups;
+    void *base = nullptr;
+    rc = serve_ws(lamp_attn_shared_workspace_size(batch->T, batch->S, groups, Hq, cache->Hkv, cache->d, cache->page, batch->width),
+                  workspace, workspace_bytes, stream, &base);
+    if (rc) return rc;
+    HIP_TRY(lamp::launch_shared_attn(cache->d, p, base, static_cast<hipStream_t>(stream)));
     return LAMP_OK;
 }
 

@@ -477,4 +477,8 @@ hipError_t launch_selftest_exp_doc(const double *x, double *y, size_t n, hipStre
 #include "lamp_serve.hip"
 #include "lamp_cache_attn.hip"
 #include "lamp_cache_prompt.hip"
+#include "lamp_cache_shared.hip"
+#include "lamp_cache_pages.hip"
+#include "lamp_pages.hip"
+#include "lamp_advance.hip"
 #endif

@@ -87,12 +87,71 @@ struct CacheAttnParams {
     float *part_ml[2];        // their running maxima and sums [slots][rows of a tile][2] (workspace)
 };
 
+// Groups of sequences with a shared prefix (lamp_cache_shared.hip): causal, no window.
+struct SharedAttnParams : CacheAttnParams {
+    const int *prefix_lens;   // [S]
+    const int *group_start;   // [groups + 1], of sequences
+    int groups;
+    void *rows;               // RowInfo [2][T][Hq] (workspace)
+};
+
+// Attention over the pages of each token's and kv head's list (lamp_cache_pages.hip):
+// causal, no window.
+struct PagesAttnParams : CacheAttnParams {
+    const int *places;        // [T][Hkv][budget] of the sequence's table row
+    int budget;
+    int pieces, per;          // a list's parts, of `per` entries (set by the launcher)
+};
+
 // Bytes of workspace a call over sequences of at most `keys` keys needs.
 size_t cache_attn_workspace(int D, int64_t T, int64_t S, int G, int Hkv, int64_t keys);
 // ws: that workspace (null where it needs none).  Fills in p from units on.
 hipError_t launch_cache_attn(int D, CacheAttnParams &p, void *ws, hipStream_t s);
+size_t shared_attn_workspace(int D, int64_t T, int64_t S, int64_t groups, int G, int Hkv, int64_t keys);
+hipError_t launch_shared_attn(int D, SharedAttnParams &p, void *ws, hipStream_t s);
+size_t pages_attn_workspace(int D, int64_t T, int G, int Hkv, int64_t page, int64_t budget);
+hipError_t launch_pages_attn(int D, PagesAttnParams &p, void *ws, hipStream_t s);
 // The kernel with the form for many rows (lamp_cache_prompt.hip), and, where
 // p.units[0] > 0 and not p.apart, that for few beside it; of launch_cache_attn.
 hipError_t launch_cache_prompt(int D, const CacheAttnParams &p, hipStream_t s);
+
+// The range of each channel over a page's keys (lamp_pages.hip).
+struct BoundsParams {
+    PagedBatch b;
+    const uint8_t *kc;        // codes [pages][Hkv][page][D]
+    int8_t *bounds;           // [pages][Hkv][2][D]
+    int by_token;             // (set by the launcher)
+};
+
+hipError_t launch_kv_bounds(int D, const BoundsParams &p, hipStream_t s);
+
+struct SelectParams {
+    PagedBatch b;
+    const uint16_t *q;        // [T][Hq][D] bf16
+    int64_t q_st, q_sh;
+    const int8_t *bounds;     // [pages][Hkv][2][D]
+    const float *ks;          // [pages][Hkv]
+    int *places;              // [T][Hkv][budget]
+    int Hq, budget, first, last;
+    uint32_t *scores;         // [T][Hkv][width] (workspace)
+    int heads_shift;          // log2 of the heads of a group, rounded up, 16 at most (set by the launcher)
+    int chunk;                // places of a workgroup (set by the launcher)
+};
+
+size_t select_workspace(int64_t T, int Hkv, int64_t width);
+hipError_t launch_select(int D, SelectParams &p, void *ws, hipStream_t s);
+
+// A step of a batch (lamp_advance.hip).
+struct AdvanceParams {
+    const int *lens, *add, *prefix_lens;   // [S]; prefix_lens may be null
+    int *table;
+    int64_t table_stride;
+    int *ring;                             // [pages]
+    const int *state;                      // [4]: first free entry, free entries, -, -
+    int *kv_lens, *q_start, *positions, *state_out;   // [S], [S + 1], [T], [4]
+    int S, T, width, pages, page_shift;
+};
+
+hipError_t launch_advance(const AdvanceParams &p, hipStream_t s);
 
 } // namespace lamp

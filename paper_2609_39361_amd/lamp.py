@@ -82,6 +82,22 @@ def lib():
         L.lamp_attn_cache.restype = i32
         L.lamp_attn_cache_workspace_size.argtypes = [i32] * 7
         L.lamp_attn_cache_workspace_size.restype = sz
+        L.lamp_kv_advance.argtypes = [P, P, P, P, i64, i32, i32, i32, i32, P, i32, P, P, P, P, P, P]
+        L.lamp_kv_advance.restype = i32
+        L.lamp_kv_bounds.argtypes = [P, P, P, P]
+        L.lamp_kv_bounds.restype = i32
+        L.lamp_select_pages.argtypes = [P, i64, i64, i32, P, P, P, i32, i32, i32, P, P, sz, P]
+        L.lamp_select_pages.restype = i32
+        L.lamp_select_pages_workspace_size.argtypes = [i32] * 4
+        L.lamp_select_pages_workspace_size.restype = sz
+        L.lamp_attn_pages.argtypes = [P, i64, i64, i32, P, P, P, i32, f64, P, P, P, sz, P]
+        L.lamp_attn_pages.restype = i32
+        L.lamp_attn_pages_workspace_size.argtypes = [i32] * 6
+        L.lamp_attn_pages_workspace_size.restype = sz
+        L.lamp_attn_shared.argtypes = [P, i64, i64, i32, P, P, P, P, i32, f64, P, P, P, sz, P]
+        L.lamp_attn_shared.restype = i32
+        L.lamp_attn_shared_workspace_size.argtypes = [i32] * 8
+        L.lamp_attn_shared_workspace_size.restype = sz
         L.lamp_get_sim_tables.argtypes = [i32, P, P]
         L.lamp_get_sim_tables.restype = i32
         L.lamp_attn_fwd_workspace_size.argtypes = [i32] * 8
@@ -594,6 +610,209 @@ def attn_cache(q, cache, block_table, kv_lens, q_start=None, causal=True, window
     _call(dev, L.lamp_attn_cache, q.data_ptr(), *q.stride()[:2], Hq, c, b, 1 if causal else 0, window,
           d ** -0.5 if scale is None else float(scale), o.data_ptr(), lse.data_ptr(),
           None if workspace is None else workspace.data_ptr(), need)
+    return o, lse
+
+
+# --- serving long contexts and changing batches ---------------------------------
+
+# Free pages of a cache: ring int32 [pages]; state int32 [4]: the ring's first free entry, how many there are,
+# the pages that the last step needed, and why it was not admitted (0: it was; include/lamp.h)
+KVPool = collections.namedtuple("KVPool", "ring state")
+
+
+def kv_pool(pages, device="cuda"):
+    """A KVPool in which the pages 0 .. pages-1 are free."""
+    return KVPool(torch.arange(pages, dtype=_I32, device=device), torch.tensor([0, pages, 0, 0], dtype=_I32, device=device))
+
+
+def kv_advance(pool, block_table, kv_lens, add, page, tokens, prefix_lens=None, out=None):
+    """The next step of a batch, planned on the device: sequence s, of kv_lens[s] keys, adds add[s] tokens (int32 [S];
+    negative: it leaves, and its pages go back to the pool).  Pages of `page` tokens for the new ones are taken from the
+    pool and entered in block_table (int32 [S,width], in place).  Returns (kv_lens [S], q_start [S+1], positions [tokens],
+    pool) as kv_append, qk_norm_rope and the attentions take them: the lengths with the new tokens, and 0 as the position
+    of tokens behind the last.
+
+    prefix_lens (int32 [S]): the first prefix_lens[s] // page places hold pages that the sequence shares; they do not go
+    back.  A step with too few free pages, a sequence longer than the table or more than `tokens` new tokens adds no
+    token; pool.state[3] says why.  `out` = (kv_lens, q_start, positions, state): tensors to write into, of which kv_lens
+    and state may be the inputs, so that a captured call goes on from step to step."""
+    ring, state = pool
+    if not isinstance(block_table, torch.Tensor) or block_table.dim() != 2 or not block_table.is_cuda:
+        raise ValueError("block_table must be an int32 CUDA tensor [S, pages of a sequence]")
+    dev = block_table.get_device()
+    S, width = block_table.shape
+    _must(block_table, "block_table", (_I32,), dev)
+    if S > 1 and block_table.stride(0) < width:   # (written to)
+        raise ValueError("rows of block_table share memory")
+    _must(ring, "pool.ring", (_I32,), dev, (ring.numel(),))
+    _must(state, "pool.state", (_I32,), dev, (4,))
+    _must(kv_lens, "kv_lens", (_I32,), dev, (S,))
+    _must(add, "add", (_I32,), dev, (S,))
+    if prefix_lens is not None:
+        _must(prefix_lens, "prefix_lens", (_I32,), dev, (S,))
+    tokens = int(tokens)
+    if tokens < 0:
+        raise ValueError("tokens must not be negative")
+    if out is None:
+        lens, q_start = kv_lens.new_empty(S), kv_lens.new_empty(S + 1)
+        positions, new_state = kv_lens.new_empty(tokens), kv_lens.new_empty(4)
+    else:
+        lens, q_start, positions, new_state = out
+        for t, name, n in ((lens, "kv_lens", S), (q_start, "q_start", S + 1), (positions, "positions", tokens),
+                           (new_state, "state", 4)):
+            _must(t, "out: " + name, (_I32,), dev, (n,))
+    _call(dev, lib().lamp_kv_advance, kv_lens.data_ptr(), add.data_ptr(),
+          None if prefix_lens is None else prefix_lens.data_ptr(), block_table.data_ptr(), block_table.stride(0), S, width,
+          int(page), tokens, ring.data_ptr(), ring.numel(), state.data_ptr(), lens.data_ptr(), q_start.data_ptr(),
+          positions.data_ptr(), new_state.data_ptr())
+    return lens, q_start, positions, KVPool(ring, new_state)
+
+
+def kv_page_bounds(cache):
+    """Bounds of an empty KVCache's pages, for kv_bounds: int8 [pages,Hkv,2,d]."""
+    pages, Hkv, _, d = cache.k.shape
+    return torch.zeros((pages, Hkv, 2, d), dtype=torch.int8, device=cache.k.device)
+
+
+def _bounds(bounds, dev, shape):
+    if not isinstance(bounds, torch.Tensor) or bounds.dtype is not torch.int8 or bounds.get_device() != dev \
+            or bounds.shape != shape or not bounds.is_contiguous():
+        _must(bounds, "bounds", (torch.int8,), dev, shape)
+    return bounds.data_ptr()
+
+
+def kv_bounds(cache, bounds, block_table, kv_lens, tokens, q_start=None):
+    """Bring `bounds` (of kv_page_bounds) up to date for the pages that a batch of `tokens` new tokens went to, after
+    kv_append with the same block_table, kv_lens and q_start: the range of each channel over a page's keys in units of 4
+    code values, bounds[:,:,0] the largest (rounded up), bounds[:,:,1] the smallest (rounded down).  Returns bounds."""
+    c, b, dev, Hkv, _, d, _, _ = _paged(cache, block_table, kv_lens, q_start, int(tokens))
+    _call(dev, lib().lamp_kv_bounds, c, b, _bounds(bounds, dev, (cache.k.shape[0], Hkv, 2, d)))
+    return bounds
+
+
+def _tokens(q):
+    if not isinstance(q, torch.Tensor) or q.dim() != 3:
+        raise ValueError("q [T,Hq,d] expected")
+    return q.shape[0]
+
+
+def _queries(q, dev, d):
+    """(pointer, token stride, head stride, heads) of q [T,Hq,d], checked."""
+    if q.dtype is not _BF16 or q.get_device() != dev or q.stride(2) != 1:
+        _must(q, "q", (_BF16,), dev)
+    if q.shape[2] != d:
+        raise ValueError("q of d = %d, a cache of %d" % (q.shape[2], d))
+    return q.data_ptr(), q.stride(0), q.stride(1), q.shape[1]
+
+
+def _workspace(workspace, need, like, dev):
+    """(pointer, bytes, the tensor) of a call's workspace: the caller's, or one of torch's of `need` bytes."""
+    if workspace is None:
+        if not need:
+            return None, 0, None
+        workspace = like.new_empty(need, dtype=torch.uint8)
+        return workspace.data_ptr(), need, workspace
+    if workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on the inputs' device")
+    have = workspace.numel() * workspace.element_size()
+    if not have and need:   # (its address is null)
+        raise ValueError("workspace is empty")
+    return workspace.data_ptr(), have, workspace
+
+
+def _attn_out(q, out, dev):
+    T, Hq, d = q.shape
+    if out is None:
+        return q.new_empty((T, Hq, d)), q.new_empty((T, Hq), dtype=_F32)
+    o, lse = out
+    _must(o, "o", (_BF16,), dev, (T, Hq, d))
+    _must(lse, "lse", (_F32,), dev, (T, Hq))
+    return o, lse
+
+
+def select_pages_workspace_size(T, Hkv, width, budget):
+    """Bytes of workspace one select_pages call needs (0: none)."""
+    return int(lib().lamp_select_pages_workspace_size(T, Hkv, width, budget))
+
+
+def select_pages(q, cache, bounds, block_table, kv_lens, budget, q_start=None, first=1, last=2, out=None, workspace=None):
+    """For each new token and kv head the `budget` places of its sequence's block_table row whose pages could hold the
+    largest logits: int32 [T,Hkv,budget], ascending, -1 behind the last.  q [T,Hq,d] as for attn_cache, bounds as
+    kv_bounds keeps them.
+
+    A page's score is an upper bound, over the heads that share the kv head, of q.k for its keys, with q rounded to 8
+    bits: an exact number, so that the same places are selected everywhere (include/lamp.h).  The first `first` and the
+    last `last` places in the token's sight are taken always; ties go to the lower place.  Rows of tokens behind
+    q_start[S] are left as they are in `out`.  `workspace` as for attn_cache."""
+    T = _tokens(q)
+    c, b, dev, Hkv, _, d, _, width = _paged(cache, block_table, kv_lens, q_start, T)
+    rows = _queries(q, dev, d)
+    ranges = _bounds(bounds, dev, (cache.k.shape[0], Hkv, 2, d))
+    budget = int(budget)
+    if budget <= 0:
+        raise ValueError("budget must be positive")
+    if out is None:
+        out = kv_lens.new_empty((T, Hkv, budget))
+    else:
+        _must(out, "out", (_I32,), dev, (T, Hkv, budget))
+    L = lib()
+    ws, size, keep = _workspace(workspace, L.lamp_select_pages_workspace_size(T, Hkv, width, budget), q, dev)
+    _call(dev, L.lamp_select_pages, *rows, c, b, ranges, budget, int(first), int(last), out.data_ptr(), ws, size)
+    return out
+
+
+def attn_pages_workspace_size(T, Hq, Hkv, d, page, budget):
+    """Bytes of workspace one attn_pages call needs (0: none)."""
+    return int(lib().lamp_attn_pages_workspace_size(T, Hq, Hkv, d, page, budget))
+
+
+def attn_pages(q, cache, block_table, kv_lens, places, q_start=None, scale=None, out=None, workspace=None):
+    """attn_cache (causal) where each new token and kv head sees only the keys of the places in its list: places int32
+    [T,Hkv,budget], of select_pages or any others, each at most once; what is not a place of the table holds no keys.
+    Returns (o bf16 [T,Hq,d], lse fp32 [T,Hq])."""
+    T = _tokens(q)
+    c, b, dev, Hkv, page, d, _, _ = _paged(cache, block_table, kv_lens, q_start, T)
+    rows = _queries(q, dev, d)
+    if not isinstance(places, torch.Tensor) or places.dim() != 3 or places.shape[0] != T or places.shape[1] != Hkv \
+            or places.shape[2] == 0:
+        raise ValueError("places int32 [T,Hkv,budget] expected")
+    if places.dtype is not _I32 or places.get_device() != dev or not places.is_contiguous():
+        _must(places, "places", (_I32,), dev, places.shape)
+    budget = places.shape[2]
+    o, lse = _attn_out(q, out, dev)
+    L = lib()
+    ws, size, keep = _workspace(workspace, L.lamp_attn_pages_workspace_size(T, rows[3], Hkv, d, page, budget), q, dev)
+    _call(dev, L.lamp_attn_pages, *rows, c, b, places.data_ptr(), budget, d ** -0.5 if scale is None else float(scale),
+          o.data_ptr(), lse.data_ptr(), ws, size)
+    return o, lse
+
+
+def attn_shared_workspace_size(T, S, groups, Hq, Hkv, d, page, width):
+    """Bytes of workspace one attn_shared call needs."""
+    return int(lib().lamp_attn_shared_workspace_size(T, S, groups, Hq, Hkv, d, page, width))
+
+
+def attn_shared(q, cache, block_table, kv_lens, prefix_lens, group_start, q_start=None, scale=None, out=None,
+                workspace=None):
+    """attn_cache (causal) for sequences that share prefixes, each read once for all of its sequences: (o, lse).
+
+    The sequences group_start[g] .. group_start[g+1]-1 (int32 [groups+1], from 0 to S) hold the same first prefix_lens[s]
+    keys (int32 [S], the same for all of a group, rounded down to whole pages; 0: none), which all lie before their new
+    tokens and are read through the table row of the group's first sequence.  The other arguments, and what comes out, as
+    for attn_cache."""
+    T = _tokens(q)
+    c, b, dev, Hkv, page, d, S, width = _paged(cache, block_table, kv_lens, q_start, T)
+    rows = _queries(q, dev, d)
+    _must(prefix_lens, "prefix_lens", (_I32,), dev, (S,))
+    if not isinstance(group_start, torch.Tensor) or group_start.dim() != 1 or group_start.shape[0] < 2:
+        raise ValueError("group_start int32 [groups + 1] expected")
+    _must(group_start, "group_start", (_I32,), dev, group_start.shape)
+    groups = group_start.shape[0] - 1
+    o, lse = _attn_out(q, out, dev)
+    L = lib()
+    ws, size, keep = _workspace(workspace, L.lamp_attn_shared_workspace_size(T, S, groups, rows[3], Hkv, d, page, width), q, dev)
+    _call(dev, L.lamp_attn_shared, *rows, c, b, prefix_lens.data_ptr(), group_start.data_ptr(), groups,
+          d ** -0.5 if scale is None else float(scale), o.data_ptr(), lse.data_ptr(), ws, size)
     return o, lse
 
 
