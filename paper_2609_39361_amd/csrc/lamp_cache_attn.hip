@@ -32,6 +32,66 @@ __global__ __launch_bounds__(256, 2) void cache_few_kernel(CacheAttnParams p)
     cache_few<D, KT, 4>(p, (int)blockIdx.x, sh);
 }
 
+// The plan of many sequences, a workgroup for each form: key tiles of a piece
+// from the sum over all sequences, then what lies before each.  A thread takes
+// consecutive sequences, in three passes over their lengths (bound by these
+// loads' latency).
+template <class F>
+__device__ void plan_form(const CacheAttnParams &p)
+{
+    constexpr int THREADS = 1024, WAVES = THREADS / 64;
+    __shared__ Work works[WAVES];
+    __shared__ Before sums[WAVES];
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), G = p.Hq / p.b.Hkv;
+    const int each = (p.b.S + THREADS - 1) / THREADS;
+    const int s0 = tid * each < p.b.S ? tid * each : p.b.S, s1 = p.b.S - s0 < each ? p.b.S : s0 + each;
+    Work work = {};
+#pragma unroll 4
+    for (int s = s0; s < s1; ++s) add(work, seq_plan<F>(p, s, G));
+    work = wave_work(work);
+    if (lane == 0) works[wave] = work;
+    __syncthreads();
+    work = {};
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        work.tiles += works[w].tiles;
+        work.most += works[w].most;
+        work.mean += works[w].mean;
+        work.longest = fmaxf(work.longest, works[w].longest);
+    }
+    const Split split = split_of<F>(p, work);
+    Before at = {0, 0};
+#pragma unroll 4
+    for (int s = s0; s < s1; ++s) {
+        const Share h = share_of<F>(p, seq_plan<F>(p, s, G), split);
+        at.units += h.units;
+        at.slots += h.slots;
+    }
+    const Before own = at;
+    at = {wave_scan(at.units), wave_scan(at.slots)};
+    if (lane == 63) sums[wave] = at;
+    __syncthreads();
+    at = {at.units - own.units, at.slots - own.slots};
+    int slots = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        if (w < wave) at.units += sums[w].units, at.slots += sums[w].slots;
+        slots += sums[w].slots;
+    }
+    if (tid == 0) {
+        p.counts[F::FORM] = slots;
+        static_cast<Split *>(p.split)[F::FORM] = split;
+    }
+    Before *before = static_cast<Before *>(p.before[F::FORM]);
+#pragma unroll 4
+    for (int s = s0; s < s1; ++s) {
+        const Share h = share_of<F>(p, seq_plan<F>(p, s, G), split);
+        before[s] = at;
+        at.units += h.units;
+        at.slots += h.slots;
+    }
+}
+
 __global__ __launch_bounds__(1024) void cache_plan_kernel(CacheAttnParams p)
 {
     if (p.units[blockIdx.x] == 0) return;

@@ -55,9 +55,10 @@ __device__ __forceinline__ void cache_few(const P &p, int x, SH &sh)
     float *obuf = sh.o, *ml = sh.ml;
 
     const int G = p.Hq / p.b.Hkv;
-    const Unit u = find_unit<FewRowsOf<WAVES>>(p, G, x);
+    Unit u;
+    SeqPlan sq;
+    locate<FewRowsOf<WAVES>>(p, G, x, u, sq);
     if (u.s < 0) return;
-    const SeqPlan sq = seq_plan<FewRows>(p, u.s, G);
     if (PAGES && sq.n == 0) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
     if (threadIdx.x < FewRows::ROWS * (D / 32)) sh.marks[0][threadIdx.x] = 0;

@@ -86,9 +86,10 @@ __device__ __forceinline__ void cache_prompt(const P &p, int x, PromptShared<D, 
     constexpr int PER = (CH + THREADS - 1) / THREADS;   // chunks of K of a thread, and of V
 
     const int G = p.Hq / p.b.Hkv;
-    const Unit u = find_unit<ManyRows>(p, G, x);
+    Unit u;
+    SeqPlan sq;
+    locate<ManyRows>(p, G, x, u, sq);
     if (u.s < 0) return;
-    const SeqPlan sq = seq_plan<ManyRows>(p, u.s, G);
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 31, half = lane >> 5;
     const int rows = sq.n * G, r0 = u.tile * ManyRows::ROWS;

@@ -39,6 +39,10 @@ struct ManyRows {      // prompts (lamp_cache_prompt.hip; 32 row tiles' window o
     static constexpr int ROWS = 256, TARGET = 256, MIN_TILES = 5, FORM = 1;
 };
 
+struct PrefixRows {    // a group's rows over their shared prefix (lamp_cache_prefix.h): 8 waves fill a CU's registers
+    static constexpr int ROWS = 32, TARGET = 256, MIN_TILES = 8, FORM = 2;
+};
+
 // The key range of one sequence is cut in pieces when its row tiles alone do
 // not fill the device: with `total` the key tiles of all (sequence, row tile,
 // kv head) triples of a form, pieces hold about total / TARGET tiles.  Up to
@@ -98,45 +102,33 @@ __device__ __forceinline__ SeqPlan seq_plan(const CacheAttnParams &p, int s, int
 // Groups of sequences with a shared prefix (lamp_cache_shared.hip): what is
 // planned is each group's new tokens over the prefix, then each sequence's over
 // the keys behind it.
-__device__ __forceinline__ int prefix_of(const SharedAttnParams &p, int s)
-{
-    const int page = 1 << p.b.page_shift, reach = p.b.width << p.b.page_shift;
-    int n = s >= 0 && s < p.b.S ? p.prefix_lens[s] : 0;
-    n = n > 0 ? n & ~(page - 1) : 0;   // (whole pages)
-    return n < reach ? n : reach;
-}
-
+// (Without branches: the loads of several sequences do not wait for each other.)
 template <class F>
 __device__ __forceinline__ SeqPlan seq_plan(const SharedAttnParams &p, int v, int G)
 {
     SeqPlan r;
-    const bool group = v < p.groups;
-    const int s = group ? p.group_start[v] : v - p.groups, s1 = group ? p.group_start[v + 1] : s + 1;
+    const bool group = F::FORM == 2 || v < p.groups;
+    const int at = group ? v : 0, g0 = p.group_start[at], g1 = p.group_start[at + 1];
+    const int s = group ? g0 : v - p.groups, s1 = group ? g1 : s + 1;
     const bool is = s >= 0 && s1 <= p.b.S && s < s1;
-    r.row = is ? s : 0;
-    r.a = !is ? 0 : (p.b.q_start ? p.b.q_start[s] : s);
-    const int e = !is ? 0 : (p.b.q_start ? p.b.q_start[s1] : s1);
-    const int prefix = prefix_of(p, r.row);
-    r.n = r.a >= 0 && e <= p.b.T && e > r.a ? e - r.a : 0;
-    const int reach = p.b.width << p.b.page_shift;   // (at most 2^30)
+    const int i = is ? s : 0, i1 = is ? s1 : 0;
+    const int a = p.b.q_start ? p.b.q_start[i] : i, e = p.b.q_start ? p.b.q_start[i1] : i1;
+    const int keys = p.b.kv_lens[i], said = p.prefix_lens[i], page = 1 << p.b.page_shift, reach = p.b.width << p.b.page_shift;   // (at most 2^30)
+    const int whole = said > 0 ? said & ~(page - 1) : 0, prefix = whole < reach ? whole : reach, len = keys > 0 ? keys : 0;
+    r.row = i;
+    r.a = a;
+    r.n = is && a >= 0 && e <= p.b.T && e > a && (!group || prefix > 0) ? e - a : 0;
     r.causal = !group;
-    if (group) {
-        r.lo = 0;
-        r.pos0 = 0;
-        r.all = r.len = prefix;
-        if (prefix == 0) r.n = 0;
-    } else {
-        const int len = p.b.kv_lens[r.row] > 0 ? p.b.kv_lens[r.row] : 0;
-        r.lo = prefix;
-        r.pos0 = len - r.n;
-        r.all = len;
-        r.len = len < reach ? len : reach;
-    }
+    r.lo = group ? 0 : prefix;
+    r.pos0 = group ? 0 : len - r.n;
+    r.all = group ? prefix : len;
+    r.len = r.all < reach ? r.all : reach;
     const int rows = r.n * G;                        // (at most 2^27)
-    r.tiles = rows > p.rows_above[F::FORM] && rows <= p.rows_upto[F::FORM] ? (rows + F::ROWS - 1) / F::ROWS : 0;
-    const int keys = r.len > r.lo ? r.len - r.lo : 0;
-    r.kt = (keys + TILE - 1) / TILE;
-    r.mean = r.causal ? fmaxf(0.0f, fminf((float)r.kt, ((float)keys - 0.5f * (float)r.n) * (1.0f / TILE))) : (float)r.kt;
+    const int above = group ? p.group_above[F::FORM] : p.rows_above[F::FORM], upto = group ? p.group_upto[F::FORM] : p.rows_upto[F::FORM];
+    r.tiles = rows > above && rows <= upto ? (rows + F::ROWS - 1) / F::ROWS : 0;
+    const int span = r.len > r.lo ? r.len - r.lo : 0;
+    r.kt = (span + TILE - 1) / TILE;
+    r.mean = r.causal ? fmaxf(0.0f, fminf((float)r.kt, ((float)span - 0.5f * (float)r.n) * (1.0f / TILE))) : (float)r.kt;
     return r;
 }
 
@@ -164,10 +156,10 @@ __device__ __forceinline__ SeqPlan seq_plan(const PagesAttnParams &p, int t, int
     return r;
 }
 
-// What a plan goes over, and whether a sequence's units of `pieces` pieces leave
-// partial outputs to be joined.
-__device__ __forceinline__ int planned(const CacheAttnParams &p) { return p.b.S; }
-__device__ __forceinline__ int planned(const SharedAttnParams &p) { return p.b.S + p.groups; }
+// What a plan of attn_shared goes over; and whether a sequence's units of `pieces`
+// pieces leave partial outputs to be joined.
+template <class F>
+__device__ __forceinline__ int planned(const SharedAttnParams &p) { return F::FORM == 2 ? p.groups : p.b.S + p.groups; }
 __device__ __forceinline__ bool joined(const CacheAttnParams &, const SeqPlan &, int pieces) { return pieces > 1; }
 __device__ __forceinline__ bool joined(const PagesAttnParams &, const SeqPlan &, int pieces) { return pieces > 1; }
 __device__ __forceinline__ bool joined(const SharedAttnParams &, const SeqPlan &r, int pieces)
@@ -263,9 +255,9 @@ __device__ __forceinline__ void add(Work &w, const SeqPlan &r)
 template <class F>
 __device__ __forceinline__ Split split_of(const CacheAttnParams &p, const Work &w)
 {
-    const int tiles = F::FORM && p.units[0] && !p.apart ? 8 : F::MIN_TILES;
+    const int tiles = F::FORM == 1 && p.units[0] && !p.apart ? 8 : F::MIN_TILES;
     const float each = fmaxf(w.most * (float)p.b.Hkv * (1.0f / F::TARGET), (float)tiles);
-    return {each, F::FORM && w.mean < EVEN * w.tiles * w.longest ? 2 : 1, tiles};
+    return {each, F::FORM == 1 && w.mean < EVEN * w.tiles * w.longest ? 2 : 1, tiles};
 }
 
 // Unit `local` of sequence s, whose partial outputs start at `slots`.  (Tables
@@ -290,8 +282,8 @@ __device__ __forceinline__ Work wave_work(Work w)
 
 // Unit x, by a wave that plans for itself: lane l has the EACH sequences from
 // EACH l.
-template <class F, int EACH, class P>
-__device__ __forceinline__ Unit plan_alone(const P &p, int G, int x)
+template <class F, int EACH>
+__device__ __forceinline__ Unit plan_alone(const CacheAttnParams &p, int G, int x)
 {
     const int lane = threadIdx.x & 63;
     SeqPlan r[EACH];
@@ -299,7 +291,7 @@ __device__ __forceinline__ Unit plan_alone(const P &p, int G, int x)
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
         const int s = EACH * lane + i;
-        r[i] = s < planned(p) ? seq_plan<F>(p, s, G) : SeqPlan{};
+        r[i] = s < p.b.S ? seq_plan<F>(p, s, G) : SeqPlan{};
         add(w, r[i]);
     }
     const Split split = split_of<F>(p, wave_work(w));
@@ -330,71 +322,10 @@ __device__ __forceinline__ Unit plan_alone(const P &p, int G, int x)
     return unit_of<F>(p, EACH * l + i, at.tiles, at.c, local, before);
 }
 
-// The plan of many sequences, a workgroup for each form: key tiles of a piece
-// from the sum over all sequences, then what lies before each.  A thread takes
-// consecutive sequences, in three passes over their lengths (bound by these
-// loads' latency).
-template <class F, class P>
-__device__ void plan_form(const P &p)
+template <class F>
+__device__ __forceinline__ Unit unit_at(const CacheAttnParams &p, int G, int x)
 {
-    constexpr int THREADS = 1024, WAVES = THREADS / 64;
-    __shared__ Work works[WAVES];
-    __shared__ Before sums[WAVES];
-    const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), G = p.Hq / p.b.Hkv;
-    const int S = planned(p), each = (S + THREADS - 1) / THREADS;
-    const int s0 = tid * each < S ? tid * each : S, s1 = S - s0 < each ? S : s0 + each;
-    Work work = {};
-#pragma unroll 4
-    for (int s = s0; s < s1; ++s) add(work, seq_plan<F>(p, s, G));
-    work = wave_work(work);
-    if (lane == 0) works[wave] = work;
-    __syncthreads();
-    work = {};
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
-        work.tiles += works[w].tiles;
-        work.most += works[w].most;
-        work.mean += works[w].mean;
-        work.longest = fmaxf(work.longest, works[w].longest);
-    }
-    const Split split = split_of<F>(p, work);
-    Before at = {0, 0};
-#pragma unroll 4
-    for (int s = s0; s < s1; ++s) {
-        const Share h = share_of<F>(p, seq_plan<F>(p, s, G), split);
-        at.units += h.units;
-        at.slots += h.slots;
-    }
-    const Before own = at;
-    at = {wave_scan(at.units), wave_scan(at.slots)};
-    if (lane == 63) sums[wave] = at;
-    __syncthreads();
-    at = {at.units - own.units, at.slots - own.slots};
-    int slots = 0;
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
-        if (w < wave) at.units += sums[w].units, at.slots += sums[w].slots;
-        slots += sums[w].slots;
-    }
-    if (tid == 0) {
-        p.counts[F::FORM] = slots;
-        static_cast<Split *>(p.split)[F::FORM] = split;
-    }
-    Before *before = static_cast<Before *>(p.before[F::FORM]);
-#pragma unroll 4
-    for (int s = s0; s < s1; ++s) {
-        const Share h = share_of<F>(p, seq_plan<F>(p, s, G), split);
-        before[s] = at;
-        at.units += h.units;
-        at.slots += h.slots;
-    }
-}
-
-template <class F, class P>
-__device__ __forceinline__ Unit unit_at(const P &p, int G, int x)
-{
-    const int S = planned(p);
-    if (S == 1) {
+    if (p.b.S == 1) {
         const SeqPlan r = seq_plan<F>(p, 0, G);
         Work w = {};
         add(w, r);
@@ -402,18 +333,18 @@ __device__ __forceinline__ Unit unit_at(const P &p, int G, int x)
         if (x == 0 && p.slots[F::FORM] && threadIdx.x == 0) p.counts[F::FORM] = h.slots;
         return unit_of<F>(p, 0, h.tiles, h.c, x, 0);
     }
-    if (S <= 64) return plan_alone<F, 1>(p, G, x);
-    if (S <= PLAN_ALONE) return plan_alone<F, PLAN_ALONE / 64>(p, G, x);
+    if (p.b.S <= 64) return plan_alone<F, 1>(p, G, x);
+    if (p.b.S <= PLAN_ALONE) return plan_alone<F, PLAN_ALONE / 64>(p, G, x);
     const Before *before = static_cast<const Before *>(p.before[F::FORM]);
-    const int s = last_at_most(S, x, [&](int i) { return (int64_t)before[i].units; });
+    const int s = last_at_most(p.b.S, x, [&](int i) { return (int64_t)before[i].units; });
     const Share h = share_of<F>(p, seq_plan<F>(p, s, G), static_cast<const Split *>(p.split)[F::FORM]);
     return unit_of<F>(p, s, h.tiles, h.c, x - before[s].units, before[s].slots);
 }
 
 // Unit x of form F, the same in each of the workgroup's waves (in scalar
 // registers, whatever it was worked out in).
-template <class F, class P>
-__device__ __forceinline__ Unit find_unit(const P &p, int G, int x)
+template <class F>
+__device__ __forceinline__ Unit find_unit(const CacheAttnParams &p, int G, int x)
 {
     const Unit u = unit_at<F>(p, G, x);
     auto same = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
@@ -425,6 +356,87 @@ __device__ __forceinline__ Unit find_unit(const PagesAttnParams &p, int G, int x
 {
     const int tiles = (G + F::ROWS - 1) / F::ROWS, piece = x % p.pieces, y = x / p.pieces, z = y / tiles;
     return {z / p.b.Hkv, y - z * tiles, z % p.b.Hkv, piece, p.pieces, 0};
+}
+
+// Unit x and its sequence's plan.
+template <class F, class P>
+__device__ __forceinline__ void locate(const P &p, int G, int x, Unit &u, SeqPlan &sq)
+{
+    u = find_unit<F>(p, G, x);
+    if (u.s >= 0) sq = seq_plan<F>(p, u.s, G);
+}
+
+// What attn_shared's plan of more than SHARED_ALONE groups and sequences leaves for
+// each of them and form (workspace): where its units and partial outputs begin, its
+// row tiles and pieces of each, and what a unit needs to know of it.
+struct SeqInfo {
+    int units, slots, tiles, c;
+    int row, a, n, all, len, pos0, lo, causal;
+};
+constexpr int SHARED_ALONE = 128;
+
+// Unit x and its sequence's plan, by a wave that plans for itself: lane l has the EACH
+// groups and sequences from EACH l, and the plan comes from the lane that has it.
+template <class F, int EACH>
+__device__ __forceinline__ void locate_alone(const SharedAttnParams &p, int G, int x, int many, Unit &u, SeqPlan &sq)
+{
+    const int lane = threadIdx.x & 63;
+    SeqPlan r[EACH];
+    Work w = {};
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const int v = EACH * lane + i;
+        r[i] = seq_plan<F>(p, v < many ? v : many - 1, G);
+        if (v >= many) r[i].tiles = 0;
+        add(w, r[i]);
+    }
+    const Split split = split_of<F>(p, wave_work(w));
+    Share h[EACH];
+    int units = 0, slots = 0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        h[i] = share_of<F>(p, r[i], split);
+        units += h[i].units;
+        slots += h[i].slots;
+    }
+    const int ui = wave_scan(units), si = wave_scan(slots);
+    const uint64_t hit = __ballot(x >= ui - units && x < ui);
+    if (!hit) return;
+    // in each lane as if it were the one
+    int local = x - (ui - units), before = si - slots, k = 0;
+#pragma unroll
+    for (int i = 1; i < EACH; ++i) {
+        if (k == i - 1 && local >= h[i - 1].units) {
+            local -= h[i - 1].units;
+            before += h[i - 1].slots;
+            h[0] = h[i];
+            r[0] = r[i];
+            k = i;
+        }
+    }
+    const int l = __builtin_ctzll(hit);
+    auto of = [&](int v) { return lane_value(v, l); };
+    u = unit_of<F>(p, of(EACH * lane + k), of(h[0].tiles), of(h[0].c), of(local), of(before));
+    sq = {of(r[0].a), of(r[0].n), of(r[0].all), of(r[0].len), of(r[0].pos0), 0, 0, 0.0f, of(r[0].row), of(r[0].lo), of(r[0].causal)};
+}
+
+// Or from the plan of a launch of its own, which has a place for every unit.
+template <class F>
+__device__ __forceinline__ void locate(const SharedAttnParams &p, int G, int x, Unit &u, SeqPlan &sq)
+{
+    const int many = planned<F>(p);
+    u = {-1, 0, 0, 0, 0, 0};
+    if (p.b.S + p.groups > SHARED_ALONE) {
+        if (x >= p.counts[F::FORM]) return;
+        const int v = __builtin_amdgcn_readfirstlane(static_cast<const int *>(p.unit_seq[F::FORM])[x]);
+        const SeqInfo i = static_cast<const SeqInfo *>(p.before[F::FORM])[v];
+        u = unit_of<F>(p, v, i.tiles, i.c, x - i.units, i.slots);
+        sq = {i.a, i.n, i.all, i.len, i.pos0, 0, 0, 0.0f, i.row, i.lo, i.causal};
+    } else if (many <= 64) {
+        locate_alone<F, 1>(p, G, x, many, u, sq);
+    } else {
+        locate_alone<F, SHARED_ALONE / 64>(p, G, x, many, u, sq);
+    }
 }
 
 template <class F>
@@ -446,9 +458,9 @@ __device__ __forceinline__ void write_info(const CacheAttnParams &p, const Unit 
 }
 
 // Where a row's partial outputs of one of its two ranges lie, for the join of
-// attn_shared: the first one's row among all, and 2 pieces + form (0: none).
+// attn_shared: the first one's row among all, and 4 pieces + form (0: none).
 struct RowInfo {
-    int at, pieces2;
+    int at, pieces4;
 };
 
 // Of the first piece's unit, for its rows: [0][T][Hq] the prefix, [1][T][Hq] the
@@ -457,13 +469,14 @@ template <class F>
 __device__ __forceinline__ void write_info(const SharedAttnParams &p, const Unit &u, const SeqPlan &sq, int row0, int rows)
 {
     if (u.piece != 0) return;
-    const int G = p.Hq / p.b.Hkv, base = F::FORM ? p.slots[0] * FewRows::ROWS + u.slot * F::ROWS : u.slot * F::ROWS;
+    const int G = p.Hq / p.b.Hkv;
+    const int base = u.slot * F::ROWS + (F::FORM > 0 ? p.slots[0] * FewRows::ROWS : 0) + (F::FORM > 1 ? p.slots[1] * ManyRows::ROWS : 0);
     const bool part = joined(p, sq, u.pieces);
     RowInfo *info = static_cast<RowInfo *>(p.rows);
     for (int r = (int)threadIdx.x; r < rows; r += (int)blockDim.x) {
         const int gr = row0 + r, t = gr / G;
         const int64_t row = (int64_t)(sq.a + t) * p.Hq + u.head * G + gr - t * G;
-        info[(sq.causal ? (int64_t)p.b.T * p.Hq : 0) + row] = part ? RowInfo{base + r, 2 * u.pieces + F::FORM} : RowInfo{0, 0};
+        info[(sq.causal ? (int64_t)p.b.T * p.Hq : 0) + row] = part ? RowInfo{base + r, 4 * u.pieces + F::FORM} : RowInfo{0, 0};
         if (sq.causal && sq.lo == 0) info[row] = RowInfo{0, 0};
     }
 }

@@ -14,33 +14,105 @@
 #include <hip/hip_runtime.h>
 
 #include "lamp_cache_many.h"
+#include "lamp_cache_prefix.h"
 
 namespace lamp {
 namespace {
 
-template <int D, int KT>
+// Groups over their prefixes (x < units[2]) beside the form for few rows.
+template <int D, int KT, int NPG>
 __global__ __launch_bounds__(256, 2) void shared_few_kernel(SharedAttnParams p)
 {
-    __shared__ FewShared<D, 4> sh;
-    cache_few<D, KT, 4>(p, (int)blockIdx.x, sh);
-}
-
-template <int D, int KT, int KF, bool WIDE>
-__global__ __launch_bounds__(THREADS, 2) void shared_mixed_kernel(SharedAttnParams p)
-{
-    constexpr size_t A = sizeof(PromptShared<D, KT>), B = sizeof(FewShared<D, WAVES>);
+    constexpr size_t A = sizeof(PrefixShared<D, KT>), B = sizeof(FewShared<D, 4>);
     __shared__ __attribute__((aligned(16))) char sh[A > B ? A : B];
     const int x = (int)blockIdx.x;
-    if (x < p.units[1]) cache_prompt<D, KT, WIDE>(p, x, *reinterpret_cast<PromptShared<D, KT> *>(sh));
-    else cache_few<D, KF, WAVES>(p, x - p.units[1], *reinterpret_cast<FewShared<D, WAVES> *>(sh));
+    if (x < p.units[2]) cache_prefix<D, KT, NPG>(p, x, *reinterpret_cast<PrefixShared<D, KT> *>(sh));
+    else cache_few<D, KT, 4>(p, x - p.units[2], *reinterpret_cast<FewShared<D, 4> *>(sh));
+}
+
+template <int D, int KT, bool WIDE>
+__global__ __launch_bounds__(THREADS, 2) void shared_many_kernel(SharedAttnParams p)
+{
+    __shared__ PromptShared<D, KT> sh;
+    cache_prompt<D, KT, WIDE>(p, (int)blockIdx.x, sh);
+}
+
+// The plan of many groups and sequences, a workgroup for each form: key tiles of a
+// piece from the sum over all, then each one's place and, for each unit, whose it is
+// (units of many are written by the whole wave).  A thread takes a group or sequence
+// of each 1024.  Bound by the latencies of the loads and the scans; the units'
+// workgroups then have two loads to wait for, where planning alone costs each of
+// them about 600 instructions a wave.
+template <class F>
+__device__ void shared_plan(const SharedAttnParams &p)
+{
+    constexpr int BY = 1024, BW = BY / 64, SMALL = 32;
+    __shared__ Work works[BW];
+    __shared__ Before sums[BW];
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), G = p.Hq / p.b.Hkv;
+    const int many = planned<F>(p), rounds = (many + BY - 1) / BY;
+    SeqPlan r;
+    auto plan_of = [&](int k) {
+        const int v = k * BY + tid;
+        r = seq_plan<F>(p, v < many ? v : many - 1, G);
+        if (v >= many) r.tiles = 0;
+    };
+    Work work = {};
+    for (int k = 0; k < rounds; ++k) {
+        plan_of(k);
+        add(work, r);
+    }
+    work = wave_work(work);
+    if (lane == 0) works[wave] = work;
+    __syncthreads();
+    work = {};
+#pragma unroll
+    for (int w = 0; w < BW; ++w) {
+        work.tiles += works[w].tiles;
+        work.most += works[w].most;
+        work.mean += works[w].mean;
+        work.longest = fmaxf(work.longest, works[w].longest);
+    }
+    const Split split = split_of<F>(p, work);
+    SeqInfo *info = static_cast<SeqInfo *>(p.before[F::FORM]);
+    int *unit_seq = static_cast<int *>(p.unit_seq[F::FORM]);
+    Before all = {0, 0};
+    for (int k = 0; k < rounds; ++k) {
+        if (rounds > 1) plan_of(k);
+        const int v = k * BY + tid;
+        const Share h = share_of<F>(p, r, split);
+        const Before upto = {wave_scan(h.units), wave_scan(h.slots)};
+        __syncthreads();   // (the sums before have been read)
+        if (lane == 63) sums[wave] = upto;
+        __syncthreads();
+        Before at = {all.units + upto.units - h.units, all.slots + upto.slots - h.slots};
+#pragma unroll
+        for (int w = 0; w < BW; ++w) {
+            if (w < wave) at.units += sums[w].units, at.slots += sums[w].slots;
+            all.units += sums[w].units;
+            all.slots += sums[w].slots;
+        }
+        if (v < many) info[v] = {at.units, at.slots, h.tiles, h.c, r.row, r.a, r.n, r.all, r.len, r.pos0, r.lo, r.causal};
+        // (tables that break their rules may count past the bounds: units without a place are left out)
+        auto is = [&](int i) { return i >= 0 && i < p.units[F::FORM]; };
+        if (h.units <= SMALL)
+            for (int i = at.units; i < at.units + h.units; ++i)
+                if (is(i)) unit_seq[i] = v;
+        for (uint64_t left = __ballot(h.units > SMALL); left; left &= left - 1) {
+            const int l = __builtin_ctzll(left), first = lane_value(at.units, l), n = lane_value(h.units, l), who = lane_value(v, l);
+            for (int i = lane; i < n; i += 64)
+                if (is(first + i)) unit_seq[first + i] = who;
+        }
+    }
+    if (tid == 0) p.counts[F::FORM] = all.units < 0 ? 0 : (all.units < p.units[F::FORM] ? all.units : p.units[F::FORM]);
 }
 
 __global__ __launch_bounds__(1024) void shared_plan_kernel(SharedAttnParams p)
 {
     if (p.units[blockIdx.x] == 0) return;
-    if (blockIdx.x == 1) plan_form<ManyRows>(p);
-    else if (p.units[1]) plan_form<FewRowsOf<8>>(p);
-    else plan_form<FewRowsOf<4>>(p);
+    if (blockIdx.x == 0) shared_plan<FewRows>(p);
+    else if (blockIdx.x == 1) shared_plan<ManyRows>(p);
+    else shared_plan<PrefixRows>(p);
 }
 
 template <int D>
@@ -52,11 +124,11 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedAttnParams p)
     if (t >= last || t < first) return;
     const RowInfo *info = static_cast<const RowInfo *>(p.rows);
     const RowInfo a = info[row], b = info[rows + row];
-    const int64_t held = (int64_t)p.slots[0] * FewRows::ROWS + (int64_t)p.slots[1] * ManyRows::ROWS;
-    auto step = [](const RowInfo &i) { return i.pieces2 & 1 ? ManyRows::ROWS : FewRows::ROWS; };
+    const int64_t held = (int64_t)p.slots[0] * FewRows::ROWS + (int64_t)p.slots[1] * ManyRows::ROWS + (int64_t)p.slots[2] * PrefixRows::ROWS;
+    auto step = [](const RowInfo &i) { return (i.pieces4 & 3) == 0 ? FewRows::ROWS : ((i.pieces4 & 3) == 1 ? ManyRows::ROWS : PrefixRows::ROWS); };
     // (whatever tables that break their rules leave here, nothing outside the arrays is read)
     auto pieces = [&](const RowInfo &i) {
-        const int n = i.pieces2 >> 1;
+        const int n = i.pieces4 >> 2;
         return n > 0 && i.at >= 0 && i.at + (int64_t)(n - 1) * step(i) < held ? n : 0;
     };
     const int n0 = pieces(a), n1 = pieces(b);
@@ -64,15 +136,15 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedAttnParams p)
     join_row<D>(p.part[0], p.part_ml[0], a.at, step(a), n0, b.at, step(b), n1, p.o + row * D, p.lse + row);
 }
 
-// Groups and sequences of at most FEW rows take the form for few rows.
-constexpr int SHARED_FEW = 64;
+// Groups of up to GROUP_FEW rows and sequences of up to SHARED_FEW take the form for
+// few rows, larger groups of up to GROUP_PREFIX that of lamp_cache_prefix.h.
+constexpr int GROUP_FEW = 16, GROUP_PREFIX = 1024, SHARED_FEW = 64;
 
 struct SharedBounds {
-    int above[2], upto[2], units[2], slots[2];
+    int above[3], upto[3], group_above[3], group_upto[3], units[3], slots[3];
 };
 
-// The new tokens are rows twice, of their groups and of their sequences, `planned`
-// in all.  Units as in lamp_cache_attn.hip; each may have a partial output.
+// Units as in lamp_cache_attn.hip; each may have a partial output.
 template <class F>
 void bound_shared(SharedBounds &b, int64_t pairs, int64_t keys)
 {
@@ -84,23 +156,33 @@ void bound_shared(SharedBounds &b, int64_t pairs, int64_t keys)
 SharedBounds shared_bounds(int64_t T, int64_t S, int64_t groups, int G, int Hkv, int64_t keys)
 {
     SharedBounds b = {};
-    const int64_t rows = T * G, planned = S + groups;
-    const bool few = rows <= SHARED_FEW;
-    const int64_t limit = few ? rows : SHARED_FEW;
-    const int64_t most = 2 * rows / FewRows::ROWS + planned, each = planned * ((limit + FewRows::ROWS - 1) / FewRows::ROWS);
-    b.upto[0] = (int)limit;
-    bound_shared<FewRows>(b, (most < each ? most : each) * Hkv, keys);
-    if (!few) {
-        const int64_t longer = 2 * rows / (limit + 1);
-        b.above[1] = (int)limit;
-        b.upto[1] = (int)rows;
-        bound_shared<ManyRows>(b, (2 * rows / ManyRows::ROWS + (longer < planned ? longer : planned)) * Hkv, keys);
+    const int64_t rows = T * G;   // of all sequences, and of all groups
+    const bool many = rows > GROUP_PREFIX;
+    auto least = [](int64_t x, int64_t y) { return x < y ? x : y; };
+    // row tiles of `rows` rows in `n` ranges of `from` rows at least and `upto` at most
+    auto tiles = [&](int64_t tile, int64_t n, int64_t from, int64_t upto) {
+        const int64_t k = least(n, rows / from);
+        return least(rows / tile + k, k * ((upto + tile - 1) / tile));
+    };
+    b.group_upto[0] = GROUP_FEW;
+    b.upto[0] = many ? SHARED_FEW : (int)rows;
+    bound_shared<FewRows>(b, (tiles(FewRows::ROWS, S, 1, b.upto[0]) + tiles(FewRows::ROWS, groups, 1, GROUP_FEW)) * Hkv, keys);
+    if (rows > GROUP_FEW) {
+        b.group_above[2] = GROUP_FEW;
+        b.group_upto[2] = GROUP_PREFIX;
+        bound_shared<PrefixRows>(b, tiles(PrefixRows::ROWS, groups, GROUP_FEW + 1, GROUP_PREFIX) * Hkv, keys);
+    }
+    if (many) {
+        b.above[1] = SHARED_FEW;
+        b.group_above[1] = GROUP_PREFIX;
+        b.upto[1] = b.group_upto[1] = (int)rows;
+        bound_shared<ManyRows>(b, (tiles(ManyRows::ROWS, S, SHARED_FEW + 1, rows) + tiles(ManyRows::ROWS, groups, GROUP_PREFIX + 1, rows)) * Hkv, keys);
     }
     return b;
 }
 
 struct SharedLayout {
-    size_t before[2], rows, ml, part, total;
+    size_t seqs[3], units[3], rows, ml, part, total;
 };
 
 SharedLayout shared_layout(const SharedBounds &b, int D, int64_t T, int Hq, int64_t planned)
@@ -112,8 +194,12 @@ SharedLayout shared_layout(const SharedBounds &b, int D, int64_t T, int Hq, int6
         at += (bytes + 255) & ~(size_t)255;
         return here;
     };
-    const size_t rows = (size_t)b.slots[0] * FewRows::ROWS + (size_t)b.slots[1] * ManyRows::ROWS;
-    for (int f = 0; f < 2; ++f) l.before[f] = take(planned > PLAN_ALONE && b.units[f] ? planned * sizeof(Before) : 0);
+    const size_t rows = (size_t)b.slots[0] * FewRows::ROWS + (size_t)b.slots[1] * ManyRows::ROWS + (size_t)b.slots[2] * PrefixRows::ROWS;
+    for (int f = 0; f < 3; ++f) {
+        const bool plan = planned > SHARED_ALONE && b.units[f];
+        l.seqs[f] = take(plan ? planned * sizeof(SeqInfo) : 0);
+        l.units[f] = take(plan ? b.units[f] * sizeof(int) : 0);
+    }
     l.rows = take(2 * (size_t)T * Hq * sizeof(RowInfo));
     l.ml = take(rows * 2 * sizeof(float));
     l.part = take(rows * D * sizeof(float));
@@ -121,14 +207,19 @@ SharedLayout shared_layout(const SharedBounds &b, int D, int64_t T, int Hq, int6
     return l;
 }
 
-template <int D, int KT, int KF>
+template <int D, int KT>
 hipError_t launch_shared(const SharedAttnParams &p, hipStream_t s)
 {
-    if (p.b.S + p.groups > PLAN_ALONE) shared_plan_kernel<<<dim3(2), 1024, 0, s>>>(p);
-    const dim3 grid((unsigned)(p.units[0] + p.units[1]));
-    if (!p.units[1]) shared_few_kernel<D, KF><<<grid, 256, 0, s>>>(p);
-    else if (1 << p.b.page_shift >= KT) shared_mixed_kernel<D, KT, KF, true><<<grid, THREADS, 0, s>>>(p);
-    else shared_mixed_kernel<D, KT, KF, false><<<grid, THREADS, 0, s>>>(p);
+    if (p.b.S + p.groups > SHARED_ALONE) shared_plan_kernel<<<dim3(3), 1024, 0, s>>>(p);
+    const int page = 1 << p.b.page_shift;
+    const dim3 grid((unsigned)(p.units[0] + p.units[2]));
+    if (page >= KT) shared_few_kernel<D, KT, 1><<<grid, 256, 0, s>>>(p);
+    else if (KT == 32 || page == 32) shared_few_kernel<D, KT, 2><<<grid, 256, 0, s>>>(p);
+    else shared_few_kernel<D, KT, KT / 16><<<grid, 256, 0, s>>>(p);
+    if (p.units[1]) {
+        if (page >= KT) shared_many_kernel<D, KT, true><<<dim3((unsigned)p.units[1]), THREADS, 0, s>>>(p);
+        else shared_many_kernel<D, KT, false><<<dim3((unsigned)p.units[1]), THREADS, 0, s>>>(p);
+    }
     shared_join_kernel<D><<<dim3((unsigned)(((int64_t)p.b.T * p.Hq + 3) / 4)), 256, 0, s>>>(p);
     return hipGetLastError();
 }
@@ -145,24 +236,28 @@ hipError_t launch_shared_attn(int D, SharedAttnParams &p, void *ws, hipStream_t 
     const SharedBounds b = shared_bounds(p.b.T, p.b.S, p.groups, p.Hq / p.b.Hkv, p.b.Hkv, (int64_t)p.b.width << p.b.page_shift);
     const SharedLayout l = shared_layout(b, D, p.b.T, p.Hq, (int64_t)p.b.S + p.groups);
     char *base = static_cast<char *>(ws);
-    p.apart = 0;
+    p.apart = 1;
     p.counts = reinterpret_cast<int *>(base);
     p.split = base + 16;
     p.rows = base + l.rows;
-    for (int f = 0; f < 2; ++f) {
+    for (int f = 0; f < 3; ++f) {
+        p.group_above[f] = b.group_above[f];
+        p.group_upto[f] = b.group_upto[f];
         p.rows_above[f] = b.above[f];
         p.rows_upto[f] = b.upto[f];
         p.units[f] = b.units[f];
         p.slots[f] = b.slots[f];
-        p.before[f] = base + l.before[f];
-        const size_t first = f ? (size_t)b.slots[0] * FewRows::ROWS : 0;   // (one array of rows for both forms)
+        p.before[f] = base + l.seqs[f];
+        p.unit_seq[f] = base + l.units[f];
+        // (one array of rows for all forms)
+        const size_t first = (f > 0 ? (size_t)b.slots[0] * FewRows::ROWS : 0) + (f > 1 ? (size_t)b.slots[1] * ManyRows::ROWS : 0);
         p.part_ml[f] = reinterpret_cast<float *>(base + l.ml) + first * 2;
         p.part[f] = reinterpret_cast<float *>(base + l.part) + first * D;
     }
     switch (D) {
-    case 64: return launch_shared<64, 64, 64>(p, s);
-    case 128: return launch_shared<128, 64, 64>(p, s);
-    default: return launch_shared<256, 32, 32>(p, s);
+    case 64: return launch_shared<64, 64>(p, s);
+    case 128: return launch_shared<128, 64>(p, s);
+    default: return launch_shared<256, 32>(p, s);
     }
 }
 

@@ -74,17 +74,18 @@ struct CacheAttnParams {
     float *lse;               // [T][Hq]
     int Hq, causal, window;
     float scale_log2;         // logit scale times log2(e)
-    // By form of the kernel (lamp_cache_plan.h; 0: few rows a sequence, 1: many).
-    int rows_above[2], rows_upto[2];   // it takes the sequences with this many rows (new tokens times heads of a group)
-    int units[2];             // workgroups: no lengths give more
-    int slots[2];             // partial outputs of split row tiles that the workspace holds: likewise
+    // By form of the kernel (lamp_cache_plan.h; 0: few rows a sequence, 1: many, 2: a
+    // group over its prefix, of attn_shared alone).
+    int rows_above[3], rows_upto[3];   // it takes the sequences with this many rows (new tokens times heads of a group)
+    int units[3];             // workgroups: no lengths give more
+    int slots[3];             // partial outputs of split row tiles that the workspace holds: likewise
     int apart;                // both forms, in launches of their own
     int *counts;              // those that this call has (workspace)
     void *split;              // the plan of more than PLAN_ALONE sequences: Split of each form (workspace)
-    void *before[2];          // and [S] Before (workspace)
+    void *before[3];          // and [S] Before (workspace)
     void *info[2];            // [slots] PartInfo (workspace)
-    float *part[2];           // [slots][rows of a tile][D] (workspace)
-    float *part_ml[2];        // their running maxima and sums [slots][rows of a tile][2] (workspace)
+    float *part[3];           // [slots][rows of a tile][D] (workspace)
+    float *part_ml[3];        // their running maxima and sums [slots][rows of a tile][2] (workspace)
 };
 
 // Groups of sequences with a shared prefix (lamp_cache_shared.hip): causal, no window.
@@ -92,7 +93,9 @@ struct SharedAttnParams : CacheAttnParams {
     const int *prefix_lens;   // [S]
     const int *group_start;   // [groups + 1], of sequences
     int groups;
+    int group_above[3], group_upto[3];   // as rows_above, rows_upto, of the groups
     void *rows;               // RowInfo [2][T][Hq] (workspace)
+    void *unit_seq[3];        // the group or sequence of each unit, of more than SHARED_ALONE (workspace)
 };
 
 // Attention over the pages of each token's and kv head's list (lamp_cache_pages.hip):
