@@ -544,7 +544,7 @@ int lamp_kv_bounds(const lamp_cache *cache, const lamp_batch *batch, int8_t *bou
 int lamp_select_pages(const uint16_t *q, int64_t q_token, int64_t q_head, int Hq, const lamp_cache *cache,
                       const lamp_batch *batch, const int8_t *bounds, int budget, int first, int last,
                       int32_t *places, void *workspace, size_t workspace_bytes, void *stream);
-size_t lamp_select_pages_workspace_size(int T, int Hkv, int width, int budget);
+size_t lamp_select_pages_workspace_size(int T, int S, int Hq, int Hkv, int d, int width, int budget);
 
 /*
  * lamp_attn_pages -- lamp_attn_cache (causal) where each token and kv head sees only

@@ -5,20 +5,22 @@
 //
 // With h_s = ceil(len_s / page) the places that sequence s holds and n_s the tokens
 // it adds, it needs ceil((len_s + n_s) / page) - h_s pages; sums over the sequences
-// before say which of the ring's, in order.  One workgroup goes over the sequences
-// twice, THREADS at a time: once for the sums, by which the step is admitted or not,
-// and once to write.  The entries of a round's sequences are spread over all
-// threads, by a search in the round's sums (one sequence may need thousands).
+// before say which of the ring's, in order.  One workgroup goes over the sequences,
+// EACH consecutive ones a thread: sums over all, by which the step is admitted or not,
+// and places, sums over those before (saturating in 32 bits, beyond everything that
+// is admitted).  The entries and
+// positions of all of them are then spread over the threads, each of which searches
+// the places in LDS for its sequence (one may have thousands, most have none).
 // Positions of many tokens are written by a second launch.  Bound by the latencies
-// of the loads, scans and barriers of a round.
+// of the loads, the sums and the ring's entries, one after another.
 #include <hip/hip_runtime.h>
 
-#include "lamp_serve.h"
+#include "lamp_cache_plan.h"
 
 namespace lamp {
 namespace {
 
-constexpr int THREADS_ADV = 1024, WAVES_ADV = THREADS_ADV / 64;
+constexpr int ADVANCE_BY = 1024, ADVANCE_WAVES = ADVANCE_BY / 64;
 constexpr int WITHIN = 8192;   // positions that the first launch writes itself
 
 // Why a step is not admitted.
@@ -27,137 +29,192 @@ enum { SHORT_OF_PAGES = 1, BEYOND_TABLE = 2, BEYOND_TOKENS = 4 };
 constexpr int TOO_MANY_BACK = 8;
 
 struct Step {
-    int64_t len, add;    // keys now, and new
-    int64_t held, need, back, kept;   // places held, pages needed, places that go back and those before them
+    int said, len;       // keys now: as said, and with table entries
+    int add;             // new tokens
+    int held, need;      // places held, pages needed
+    int kept, back;      // places that stay and pages that go back behind them
+    bool gone, beyond;   // the sequence leaves; it would not fit the table
 };
 
-__device__ __forceinline__ Step step_of(const AdvanceParams &p, int s)
+__device__ __forceinline__ Step step_of(const AdvanceParams &p, int s, bool is)
 {
     Step r;
-    const int64_t page = 1 << p.page_shift, reach = (int64_t)p.width << p.page_shift;
-    const int64_t len = p.lens[s], add = p.add[s], prefix = p.prefix_lens ? p.prefix_lens[s] : 0;
-    r.len = len < 0 ? 0 : (len < reach ? len : reach);   // (a longer one has no entries: not admitted below)
-    r.add = add > 0 ? add : 0;
+    const int page = 1 << p.page_shift, reach = p.width << p.page_shift;   // (at most 2^30)
+    const int len = p.lens[s], add = p.add[s], prefix = p.prefix_lens ? p.prefix_lens[s] : 0;
+    r.said = len;
+    r.len = len < 0 ? 0 : (len < reach ? len : reach);
+    r.gone = is && add < 0;
+    r.add = is && add > 0 ? add : 0;
+    r.beyond = is && add >= 0 && (int64_t)len + r.add > reach;
     r.held = (r.len + page - 1) >> p.page_shift;
-    r.need = (((len + r.add < reach ? r.len + r.add : reach) + page - 1) >> p.page_shift) - r.held;
-    r.kept = prefix > 0 ? prefix >> p.page_shift : 0;
-    r.kept = r.kept < r.held ? r.kept : r.held;
-    r.back = add < 0 ? r.held - r.kept : 0;
+    const int room = reach - r.len, take = r.add < room ? r.add : room;    // (more is not admitted)
+    r.need = ((r.len + take + page - 1) >> p.page_shift) - r.held;
+    const int kept = prefix > 0 ? prefix >> p.page_shift : 0;
+    r.kept = kept < r.held ? kept : r.held;
+    r.back = r.gone ? r.held - r.kept : 0;
     return r;
 }
 
-__device__ __forceinline__ int64_t wave_sum_upto(int64_t v, int lane)
+__device__ __forceinline__ uint32_t sum(uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); }
+
+// Inclusive sum over the wave's lanes.
+__device__ __forceinline__ uint32_t wave_sums(uint32_t v)
 {
-#pragma unroll
-    for (int k = 1; k < 64; k <<= 1) {
-        const int64_t y = __shfl_up(v, k, 64);
-        v += lane >= k ? y : 0;
-    }
-    return v;
+    return wave_scan_by(v, [](uint32_t a, uint32_t b) { return sum(a, b); });
 }
 
-// Last i < n with at[i] <= x (at[0] <= x; non-decreasing).
-__device__ __forceinline__ int last_of(const int *at, int n, int x)
+// Where a sequence's taken entries, those that go back and its positions begin among
+// all, and where in its row and from which position on.
+struct SeqPlaces {
+    int at[3], from[3];
+};
+
+// Last i < n with at[i].at[which] <= x (those of the first are; non-decreasing).
+template <int N>
+__device__ __forceinline__ int owner(const SeqPlaces *at, int which, int n, int x)
 {
     int lo = 0;
-    for (int half = THREADS_ADV / 2; half; half >>= 1)
-        if (lo + half < n && at[lo + half] <= x) lo += half;
+#pragma unroll
+    for (int half = N / 2; half; half >>= 1)
+        if (lo + half < n && at[lo + half].at[which] <= x) lo += half;
     return lo;
 }
 
-__global__ __launch_bounds__(THREADS_ADV) void advance_kernel(AdvanceParams p)
+template <int EACH>
+__global__ __launch_bounds__(ADVANCE_BY) void advance_kernel(AdvanceParams p)
 {
-    __shared__ int64_t sums[3][WAVES_ADV];
-    __shared__ int why;
-    __shared__ int need_at[THREADS_ADV], back_at[THREADS_ADV], tok_at[THREADS_ADV];   // of a round's sequences, within the round
-    __shared__ int held_at[THREADS_ADV], kept_at[THREADS_ADV], len_at[THREADS_ADV];
-    const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int64_t pages = p.pages;
-    int64_t head = p.state[0] % pages, count = p.state[1];
-    head = head < 0 ? head + pages : head;
-    count = count < 0 ? 0 : (count < pages ? count : pages);
-    if (tid == 0) why = 0;
-    // the sums of all
-    int64_t need = 0, back = 0, add = 0;
+    __shared__ uint32_t sums[3][ADVANCE_WAVES];
+    __shared__ int beyond_any[ADVANCE_WAVES];
+    __shared__ SeqPlaces at_seq[EACH * ADVANCE_BY];   // of a round's sequences
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int pages = p.pages, last = p.S - 1;
+    const int first = p.state[0], free = p.state[1];
+    const int rounds = (p.S + EACH * ADVANCE_BY - 1) / (EACH * ADVANCE_BY);
+    auto sequence = [&](int round, int i) { return (round * ADVANCE_BY + tid) * EACH + i; };
+    // the ring, whatever its state says
+    const int head = first >= 0 ? first % pages : 0;
+    const int count = free < 0 ? 0 : (free < pages ? free : pages);
+    auto in_ring = [&](int64_t i) { return (int)(head + i < pages ? head + i : head + i - pages); };   // (i up to pages)
+
+    Step r[EACH];
+    uint32_t mine[3], upto[3], all[3] = {0, 0, 0};   // needed, going back, added: this thread's, with the lanes before, of all
     bool beyond = false;
-    for (int s = tid; s < p.S; s += THREADS_ADV) {
-        const Step r = step_of(p, s);
-        need += r.need;
-        back += r.back;
-        add += r.add;
-        beyond = beyond || (p.add[s] >= 0 && (int64_t)p.lens[s] + r.add > (int64_t)p.width << p.page_shift);
+    auto load = [&](int round) {
+        mine[0] = mine[1] = mine[2] = 0;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const int s = sequence(round, i);
+            r[i] = step_of(p, s < last ? s : last, s <= last);
+            mine[0] = sum(mine[0], (uint32_t)r[i].need);
+            mine[1] = sum(mine[1], (uint32_t)r[i].back);
+            mine[2] = sum(mine[2], (uint32_t)r[i].add);
+            beyond = beyond || r[i].beyond;
+        }
+    };
+    // this thread's sums among the waves', which LDS holds after the next barrier
+    auto place = [&]() {
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            upto[k] = wave_sums(mine[k]);
+            if (lane == 63) sums[k][wave] = upto[k];
+        }
+    };
+    for (int round = 0; round < rounds; ++round) {
+        load(round);
+        if (round) __syncthreads();   // (the sums of the round before have been read)
+        place();
+        const bool any = __ballot(beyond) != 0;
+        if (lane == 0) beyond_any[wave] = any;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < ADVANCE_WAVES; ++w)
+#pragma unroll
+            for (int k = 0; k < 3; ++k) all[k] = sum(all[k], sums[k][w]);
     }
-    need = wave_sum_upto(need, lane);
-    back = wave_sum_upto(back, lane);
-    add = wave_sum_upto(add, lane);
-    if (lane == 63) sums[0][wave] = need, sums[1][wave] = back, sums[2][wave] = add;
-    __syncthreads();
-    if (beyond) why = BEYOND_TABLE;
-    need = back = add = 0;
-    for (int w = 0; w < WAVES_ADV; ++w) need += sums[0][w], back += sums[1][w], add += sums[2][w];
-    __syncthreads();
-    const int no = why | (need > count ? SHORT_OF_PAGES : 0) | (add > p.T ? BEYOND_TOKENS : 0);
-    const bool ok = no == 0, returns = back <= pages - count;
-    // a round's sequences
-    int64_t need0 = 0, back0 = 0, add0 = 0;
-    for (int s0 = 0; s0 < p.S; s0 += THREADS_ADV) {
-        const int s = s0 + tid, n = p.S - s0 < THREADS_ADV ? p.S - s0 : THREADS_ADV;
-        Step r = {};
-        bool gone = false;
-        if (s < p.S) {
-            r = step_of(p, s);
-            gone = p.add[s] < 0;
-            if (!ok) r.need = r.add = 0;
-            if (!returns) r.back = 0;
+    beyond = false;
+#pragma unroll
+    for (int w = 0; rounds && w < ADVANCE_WAVES; ++w) beyond = beyond || beyond_any[w];
+    const int no = (all[0] > (uint32_t)count ? SHORT_OF_PAGES : 0) | (beyond ? BEYOND_TABLE : 0) | (all[2] > (uint32_t)p.T ? BEYOND_TOKENS : 0);
+    const bool ok = no == 0, returns = all[1] <= (uint32_t)(pages - count);
+
+    int need0 = 0, back0 = 0, add0 = 0;   // of the rounds before
+    for (int round = 0; round < rounds; ++round) {
+        if (rounds > 1) {
+            load(round);
+            __syncthreads();   // (what the round before left in LDS has been read)
+            place();
+            __syncthreads();
         }
-        const int64_t needs = wave_sum_upto(r.need, lane), backs = wave_sum_upto(r.back, lane), adds = wave_sum_upto(r.add, lane);
-        __syncthreads();   // (the round before is done)
-        if (lane == 63) sums[0][wave] = needs, sums[1][wave] = backs, sums[2][wave] = adds;
-        __syncthreads();
-        int64_t before[3] = {0, 0, 0}, all[3] = {0, 0, 0};
-        for (int w = 0; w < WAVES_ADV; ++w)
-            for (int k = 0; k < 3; ++k) {
-                before[k] += w < wave ? sums[k][w] : 0;
-                all[k] += sums[k][w];
+        const int from[3] = {need0, back0, add0};
+        // (what is not admitted, or does not go back, counts as none)
+        int at[3] = {from[0], from[1], from[2]}, end[3] = {from[0], from[1], from[2]};
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            if (k == 1 ? !returns : !ok) continue;
+            at[k] += (int)(upto[k] - mine[k]);
+#pragma unroll
+            for (int w = 0; w < ADVANCE_WAVES; ++w) {
+                at[k] += w < wave ? (int)sums[k][w] : 0;
+                end[k] += (int)sums[k][w];
             }
-        const int64_t tok = add0 + before[2] + adds - r.add;
-        need_at[tid] = (int)(before[0] + needs - r.need);
-        back_at[tid] = (int)(before[1] + backs - r.back);
-        tok_at[tid] = (int)(before[2] + adds - r.add);
-        held_at[tid] = (int)r.held;
-        kept_at[tid] = (int)r.kept;
-        len_at[tid] = (int)r.len;
-        if (s < p.S) {
-            const int len = p.lens[s];
-            p.kv_lens[s] = gone ? 0 : len + (int)r.add;
-            p.q_start[s] = (int)tok;
-            if (s == p.S - 1) p.q_start[p.S] = (int)(tok + r.add);
+        }
+        need0 = end[0];
+        back0 = end[1];
+        add0 = end[2];
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const int s = sequence(round, i);
+            at_seq[tid * EACH + i] = {{at[0], at[1], at[2]}, {r[i].held, r[i].kept, r[i].len}};
+            if (s <= last) {
+                p.kv_lens[s] = r[i].gone ? 0 : r[i].said + (ok ? r[i].add : 0);
+                p.q_start[s] = at[2];
+                if (s == last) p.q_start[p.S] = at[2] + (ok ? r[i].add : 0);
+            }
+            at[0] += ok ? r[i].need : 0;
+            at[1] += returns ? r[i].back : 0;
+            at[2] += ok ? r[i].add : 0;
         }
         __syncthreads();
-        for (int64_t i = tid; i < all[0]; i += THREADS_ADV) {
-            const int l = last_of(need_at, n, (int)i);
-            p.table[(s0 + l) * p.table_stride + held_at[l] + (i - need_at[l])] = p.ring[(head + need0 + i) % pages];
+        const int s0 = round * EACH * ADVANCE_BY, n = p.S - s0 < EACH * ADVANCE_BY ? p.S - s0 : EACH * ADVANCE_BY;
+        auto entry = [&](int which, int i) {
+            const int l = owner<EACH * ADVANCE_BY>(at_seq, which, n, i);
+            return p.table + (int64_t)(s0 + l) * p.table_stride + at_seq[l].from[which] + (i - at_seq[l].at[which]);
+        };
+        // (AT entries of a thread at once: their searches and loads do not wait for each other)
+        constexpr int AT = 4;
+        for (int i0 = from[0] + tid; i0 < need0; i0 += AT * ADVANCE_BY) {
+            int *to[AT], page[AT];
+#pragma unroll
+            for (int k = 0; k < AT; ++k) {
+                const int i = i0 + k * ADVANCE_BY < need0 ? i0 + k * ADVANCE_BY : i0;
+                page[k] = p.ring[in_ring(i)];
+                to[k] = entry(0, i);
+            }
+#pragma unroll
+            for (int k = 0; k < AT; ++k)
+                if (i0 + k * ADVANCE_BY < need0) *to[k] = page[k];
         }
-        for (int64_t i = tid; i < all[1]; i += THREADS_ADV) {
-            const int l = last_of(back_at, n, (int)i);
-            p.ring[(head + count + back0 + i) % pages] = p.table[(s0 + l) * p.table_stride + kept_at[l] + (i - back_at[l])];
+        for (int i0 = from[1] + tid; i0 < back0; i0 += AT * ADVANCE_BY) {
+            int page[AT];
+#pragma unroll
+            for (int k = 0; k < AT; ++k) page[k] = *entry(1, i0 + k * ADVANCE_BY < back0 ? i0 + k * ADVANCE_BY : i0);
+#pragma unroll
+            for (int k = 0; k < AT; ++k)
+                if (i0 + k * ADVANCE_BY < back0) p.ring[in_ring((int64_t)count + i0 + k * ADVANCE_BY)] = page[k];
         }
         if (p.T <= WITHIN)
-            for (int64_t i = tid; i < all[2]; i += THREADS_ADV) {
-                const int l = last_of(tok_at, n, (int)i);
-                p.positions[add0 + i] = len_at[l] + (int)(i - tok_at[l]);
+            for (int i = from[2] + tid; i < add0; i += ADVANCE_BY) {
+                const int l = owner<EACH * ADVANCE_BY>(at_seq, 2, n, i);
+                p.positions[i] = at_seq[l].from[2] + (i - at_seq[l].at[2]);
             }
-        need0 += all[0];
-        back0 += all[1];
-        add0 += all[2];
     }
     if (p.T <= WITHIN)
-        for (int64_t i = add0 + tid; i < p.T; i += THREADS_ADV) p.positions[i] = 0;
+        for (int i = add0 + tid; i < p.T; i += ADVANCE_BY) p.positions[i] = 0;
     if (tid == 0) {
         if (p.S == 0) p.q_start[0] = 0;
-        p.state_out[0] = (int)((head + need0) % pages);
-        p.state_out[1] = (int)(count - need0 + back0);
-        p.state_out[2] = (int)(need < 0x7FFFFFFF ? need : 0x7FFFFFFF);
+        p.state_out[0] = in_ring(need0);
+        p.state_out[1] = count - need0 + back0;
+        p.state_out[2] = (int)(all[0] < 0x7FFFFFFFu ? all[0] : 0x7FFFFFFFu);
         p.state_out[3] = no | (returns ? 0 : TOO_MANY_BACK);
     }
 }
@@ -179,7 +236,8 @@ __global__ __launch_bounds__(256) void positions_kernel(AdvanceParams p, int par
 
 hipError_t launch_advance(const AdvanceParams &p, hipStream_t s)
 {
-    advance_kernel<<<1, THREADS_ADV, 0, s>>>(p);
+    if (p.S <= ADVANCE_BY) advance_kernel<1><<<1, ADVANCE_BY, 0, s>>>(p);
+    else advance_kernel<4><<<1, ADVANCE_BY, 0, s>>>(p);
     if (p.T > WITHIN) {
         // about 256 tokens a wave
         const int64_t want = (p.T + 256 * ((int64_t)p.S + 1) - 1) / (256 * ((int64_t)p.S + 1)), waves = ((int64_t)p.S + 1) * want;

@@ -546,12 +546,12 @@ __device__ __forceinline__ void mark_nan(uint32_t (*marks)[D / 32], uint32_t nan
 // A row's partial outputs joined by a wave and written (attn_shared, attn_pages):
 // n0 of them from row at0 of `part` on, step0 rows apart, then n1 from at1.  A lane
 // holds D/64 channels, and for each 64 partial outputs the maximum and sum of one.
-// Bound by latency: 8 rows are requested at once.
+// Bound by latency: 16 rows are requested at once.  Not written where not `live`.
 template <int D>
 __device__ __forceinline__ void join_row(const float *part, const float *ml, int64_t at0, int64_t step0, int n0, int64_t at1,
-                                         int64_t step1, int n1, uint16_t *o, float *lse)
+                                         int64_t step1, int n1, bool live, uint16_t *o, float *lse)
 {
-    constexpr int C = D / 64, AT = 8;
+    constexpr int C = D / 64, AT = 16;
     const int lane = threadIdx.x & 63, n = n0 + n1;
     auto row_of = [&](int k) { return k < n0 ? at0 + k * step0 : at1 + (k - n0) * step1; };
     float m = NEG_INF, sum = 0.0f, v[C] = {};
@@ -559,6 +559,16 @@ __device__ __forceinline__ void join_row(const float *part, const float *ml, int
         const int mine = c0 + lane, here = n - c0 < 64 ? n - c0 : 64;
         const int64_t at = row_of(mine < n ? mine : c0) * 2;
         const float mc = mine < n ? ml[at] : NEG_INF, lc = ml[at + 1];
+        float x[AT][C];
+        auto request = [&](int k0) {
+#pragma unroll
+            for (int j = 0; j < AT; ++j) {   // (beyond the last: read again, not added)
+                const float *r = part + row_of(c0 + (k0 + j < here ? k0 + j : k0)) * D + C * lane;
+#pragma unroll
+                for (int e = 0; e < C; ++e) x[j][e] = r[e];
+            }
+        };
+        request(0);   // (before the maxima are waited for)
         float mn = mc;
 #pragma unroll
         for (int k = 1; k < 64; k <<= 1) mn = fmaxf(mn, __shfl_xor(mn, k, 64));
@@ -573,13 +583,7 @@ __device__ __forceinline__ void join_row(const float *part, const float *ml, int
 #pragma unroll
         for (int e = 0; e < C; ++e) v[e] *= f0;
         for (int k0 = 0; k0 < here; k0 += AT) {
-            float x[AT][C];
-#pragma unroll
-            for (int j = 0; j < AT; ++j) {   // (beyond the last: read again, not added)
-                const float *r = part + row_of(c0 + (k0 + j < here ? k0 + j : k0)) * D + C * lane;
-#pragma unroll
-                for (int e = 0; e < C; ++e) x[j][e] = r[e];
-            }
+            if (k0) request(k0);
 #pragma unroll
             for (int j = 0; j < AT; ++j) {
                 if (k0 + j >= here) break;
@@ -589,6 +593,7 @@ __device__ __forceinline__ void join_row(const float *part, const float *ml, int
             }
         }
     }
+    if (!live) return;
     const float inv = finish(m, sum);
     if constexpr (C == 1) {
         o[lane] = (uint16_t)pack2(v[0] * inv, 0.0f);
@@ -596,6 +601,50 @@ __device__ __forceinline__ void join_row(const float *part, const float *ml, int
 #pragma unroll
         for (int e = 0; e < C; e += 2) *reinterpret_cast<uint32_t *>(o + C * lane + e) = pack2(v[e] * inv, v[e + 1] * inv);
     }
+    if (lane == 0) *lse = finish_lse(m, sum);
+}
+
+// The same by 16 lanes, for rows of few partial outputs (their weights in each lane).
+template <int D>
+__device__ __forceinline__ void join_row16(const float *part, const float *ml, int64_t at0, int64_t step0, int n0, int64_t at1,
+                                           int64_t step1, int n1, uint16_t *o, float *lse)
+{
+    constexpr int C = D / 16, AT = 2;
+    const int lane = threadIdx.x & 15, n = n0 + n1;
+    auto row_of = [&](int k) { return k < n0 ? at0 + k * step0 : at1 + (k - n0) * step1; };
+    float m = NEG_INF, sum = 0.0f, v[C] = {};
+    for (int c0 = 0; c0 < n; c0 += AT) {
+        float mc[AT], lc[AT];
+        f32x4 x[AT][C / 4];
+#pragma unroll
+        for (int k = 0; k < AT; ++k) {   // (beyond the last: read again, not added)
+            const int64_t at = row_of(c0 + k < n ? c0 + k : c0);
+            mc[k] = ml[at * 2];
+            lc[k] = ml[at * 2 + 1];
+#pragma unroll
+            for (int e = 0; e < C / 4; ++e) x[k][e] = *reinterpret_cast<const f32x4 *>(part + at * D + 4 * (16 * e + lane));
+        }
+        float mn = m;
+#pragma unroll
+        for (int k = 0; k < AT; ++k) mn = fmaxf(mn, mc[k]);
+        const float ms = mn == NEG_INF ? 0.0f : mn, f0 = __builtin_amdgcn_exp2f(m - ms);
+        m = mn;
+        sum *= f0;
+#pragma unroll
+        for (int e = 0; e < C; ++e) v[e] *= f0;
+#pragma unroll
+        for (int k = 0; k < AT; ++k) {
+            if (c0 + k >= n) break;
+            const float f = __builtin_amdgcn_exp2f(mc[k] - ms);
+            sum += lc[k] * f;
+#pragma unroll
+            for (int e = 0; e < C; ++e) v[e] += x[k][e / 4][e % 4] * f;
+        }
+    }
+    const float inv = finish(m, sum);
+#pragma unroll
+    for (int e = 0; e < C; e += 4)
+        *reinterpret_cast<u32x2 *>(o + 4 * (16 * (e / 4) + lane)) = u32x2{pack2(v[e] * inv, v[e + 1] * inv), pack2(v[e + 2] * inv, v[e + 3] * inv)};
     if (lane == 0) *lse = finish_lse(m, sum);
 }
 

@@ -115,15 +115,17 @@ __global__ __launch_bounds__(1024) void shared_plan_kernel(SharedAttnParams p)
     else shared_plan<PrefixRows>(p);
 }
 
-template <int D>
+// LANES: of a row (64, where there may be many partial outputs of a few rows, or 16).
+template <int D, int LANES>
 __global__ __launch_bounds__(256) void shared_join_kernel(SharedAttnParams p)
 {
-    const int64_t row = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), rows = (int64_t)p.b.T * p.Hq;
+    const int64_t row = (int64_t)blockIdx.x * (256 / LANES) + (LANES == 64 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x / LANES) : (int)threadIdx.x / LANES);
+    const int64_t rows = (int64_t)p.b.T * p.Hq;
     if (row >= rows) return;
-    const int t = (int)(row / p.Hq), last = p.b.q_start ? p.b.q_start[p.b.S] : p.b.S, first = p.b.q_start ? p.b.q_start[0] : 0;
-    if (t >= last || t < first) return;
     const RowInfo *info = static_cast<const RowInfo *>(p.rows);
     const RowInfo a = info[row], b = info[rows + row];
+    const int t = (int)((int)row / p.Hq), last = p.b.q_start ? p.b.q_start[p.b.S] : p.b.S, first = p.b.q_start ? p.b.q_start[0] : 0;
+    if (t >= last || t < first) return;
     const int64_t held = (int64_t)p.slots[0] * FewRows::ROWS + (int64_t)p.slots[1] * ManyRows::ROWS + (int64_t)p.slots[2] * PrefixRows::ROWS;
     auto step = [](const RowInfo &i) { return (i.pieces4 & 3) == 0 ? FewRows::ROWS : ((i.pieces4 & 3) == 1 ? ManyRows::ROWS : PrefixRows::ROWS); };
     // (whatever tables that break their rules leave here, nothing outside the arrays is read)
@@ -133,12 +135,14 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedAttnParams p)
     };
     const int n0 = pieces(a), n1 = pieces(b);
     if (n0 + n1 == 0) return;   // (written already)
-    join_row<D>(p.part[0], p.part_ml[0], a.at, step(a), n0, b.at, step(b), n1, p.o + row * D, p.lse + row);
+    if constexpr (LANES == 64) join_row<D>(p.part[0], p.part_ml[0], a.at, step(a), n0, b.at, step(b), n1, true, p.o + row * D, p.lse + row);
+    else join_row16<D>(p.part[0], p.part_ml[0], a.at, step(a), n0, b.at, step(b), n1, p.o + row * D, p.lse + row);
 }
 
 // Groups of up to GROUP_FEW rows and sequences of up to SHARED_FEW take the form for
 // few rows, larger groups of up to GROUP_PREFIX that of lamp_cache_prefix.h.
 constexpr int GROUP_FEW = 16, GROUP_PREFIX = 1024, SHARED_FEW = 64;
+constexpr int64_t JOIN_WIDE = 8192;   // rows up to which a wave joins each
 
 struct SharedBounds {
     int above[3], upto[3], group_above[3], group_upto[3], units[3], slots[3];
@@ -220,7 +224,9 @@ hipError_t launch_shared(const SharedAttnParams &p, hipStream_t s)
         if (page >= KT) shared_many_kernel<D, KT, true><<<dim3((unsigned)p.units[1]), THREADS, 0, s>>>(p);
         else shared_many_kernel<D, KT, false><<<dim3((unsigned)p.units[1]), THREADS, 0, s>>>(p);
     }
-    shared_join_kernel<D><<<dim3((unsigned)(((int64_t)p.b.T * p.Hq + 3) / 4)), 256, 0, s>>>(p);
+    const int64_t rows = (int64_t)p.b.T * p.Hq;
+    if (rows <= JOIN_WIDE) shared_join_kernel<D, 64><<<dim3((unsigned)((rows + 3) / 4)), 256, 0, s>>>(p);
+    else shared_join_kernel<D, 16><<<dim3((unsigned)((rows + 15) / 16)), 256, 0, s>>>(p);
     return hipGetLastError();
 }
 

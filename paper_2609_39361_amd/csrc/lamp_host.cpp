@@ -1151,11 +1151,11 @@ int lamp_kv_bounds(const lamp_cache *cache, const lamp_batch *batch, int8_t *bou
     return LAMP_OK;
 }
 
-size_t lamp_select_pages_workspace_size(int T, int Hkv, int width, int budget)
+size_t lamp_select_pages_workspace_size(int T, int S, int Hq, int Hkv, int d, int width, int budget)
 {
-    if (T <= 0 || Hkv <= 0 || width <= 0 || budget <= 0 || width <= budget) return 0;
-    if (T > 1 << 23 || (int64_t)T * Hkv > (int64_t)1 << 27 || (int64_t)T * Hkv * width > (int64_t)1 << 32) return 0;
-    return lamp::select_workspace(T, Hkv, width);
+    if (T <= 0 || S <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv || width <= 0 || budget <= 0 || (d != 64 && d != 128 && d != 256)) return 0;
+    if (T > 1 << 23 || (int64_t)S * Hkv > 1 << 20 || (int64_t)T * Hq > (int64_t)1 << 27 || (int64_t)T * Hkv * width > (int64_t)1 << 32) return 0;
+    return lamp::select_workspace(d, T, S, Hq / Hkv, Hkv, width, budget);
 }
 
 int lamp_select_pages(const uint16_t *q, int64_t q_token, int64_t q_head, int Hq, const lamp_cache *cache,
@@ -1188,7 +1188,7 @@ int lamp_select_pages(const uint16_t *q, int64_t q_token, int64_t q_head, int Hq
     p.first = first;
     p.last = last;
     void *base = nullptr;
-    rc = serve_ws(lamp_select_pages_workspace_size(batch->T, cache->Hkv, batch->width, budget), workspace, workspace_bytes, stream, &base);
+    rc = serve_ws(lamp_select_pages_workspace_size(batch->T, batch->S, Hq, cache->Hkv, cache->d, batch->width, budget), workspace, workspace_bytes, stream, &base);
     if (rc) return rc;
     HIP_TRY(lamp::launch_select(cache->d, p, base, static_cast<hipStream_t>(stream)));
     return LAMP_OK;

@@ -130,10 +130,24 @@ __device__ __forceinline__ TokenTile token_tile(const PagedBatch &b, int per, in
     const TokenTile none = {-1, 0, 0, 0, 0};
     auto start = [&](int s) { return b.q_start ? b.q_start[s] : s; };
     auto first = [&](int s) { return (int64_t)(start(s) / per) + (per > 1 ? s : 0); };
-    const int s = last_at_most(b.S, x, first);
-    const int a = start(s), e = start(s + 1), i = (int)(x - first(s)) * per;
+    int s, a, e, keys;
+    if (b.S <= 64) {   // (a lane for each sequence: one load's latency; those behind the last repeat it)
+        const int l = (int)(threadIdx.x & 63) < b.S ? (int)(threadIdx.x & 63) : b.S - 1;
+        const int al = start(l), el = start(l + 1), kl = b.kv_lens[l];
+        s = 63 - __builtin_clzll(__ballot(l == 0 || (int64_t)(al / per) + (per > 1 ? l : 0) <= x));
+        s = s < b.S ? s : b.S - 1;
+        a = __builtin_amdgcn_readlane(al, s);
+        e = __builtin_amdgcn_readlane(el, s);
+        keys = __builtin_amdgcn_readlane(kl, s);
+    } else {
+        s = last_at_most(b.S, x, first);
+        a = start(s);
+        e = start(s + 1);
+        keys = b.kv_lens[s];
+    }
+    const int i = (int)(x - ((int64_t)(a / per) + (per > 1 ? s : 0))) * per;
     if (a < 0 || e > b.T || i < 0 || i >= e - a) return none;
-    const int len = b.kv_lens[s] > 0 ? b.kv_lens[s] : 0;
+    const int len = keys > 0 ? keys : 0;
     return {s, a + i, e - a - i < per ? e - a - i : per, len - (e - a) + i, len};
 }
 
@@ -146,28 +160,14 @@ __device__ __forceinline__ int places_of(const PagedBatch &b, int pos, int len)
     return n < b.width ? n : b.width;
 }
 
-// Scores of a tile's tokens and one kv head over `chunk` places: the products of
-// int8 rows [max(q', 0) | min(q', 0)] with the ranges, 16 places a wave at a time.
-// Rows of the operand: row of token t and head g of the group is (t << HS) + g,
-// HS = heads_shift; groups of more than 16 heads go over their heads in rounds.
-template <int D>
-__global__ __launch_bounds__(256) void select_score_kernel(SelectParams p)
+// Largest bf16 magnitude (its bits) of each token's group among finite ones, into
+// amax[16] (LDS, zeroed).  The queries of groups of up to 16 heads stay in `raw`, by
+// the operand's rows.
+template <int D, int THREADS>
+__device__ __forceinline__ void group_amax(const SelectParams &p, const TokenTile &t, int head, uint32_t *amax, u32x4 (*raw)[D / 8])
 {
-    constexpr int KS = 2 * D / 64;                 // 64-channel steps of the product
-    __shared__ u32x4 rows[KS][64];                 // the operand: of lane l in step k
-    __shared__ uint32_t amax[16];
-    const int G = p.Hq / p.b.Hkv, hs = p.heads_shift, per = 16 >> hs;
-    const TokenTile t = token_tile(p.b, per, (int)blockIdx.x);
-    if (t.s < 0) return;
-    const int head = (int)blockIdx.y, tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int many = places_of(p.b, t.pos + t.n - 1, t.len);
-    const int p0 = (int)blockIdx.z * p.chunk, p1 = many - p0 < p.chunk ? many : p0 + p.chunk;
-    if (p0 >= p1 || many <= p.budget) return;      // (all of them: no scores are looked at)
-    const int *table = p.b.table + t.s * p.b.table_stride;
-    // largest magnitude of each token's group
-    if (tid < 16) amax[tid] = 0;
-    __syncthreads();
-    for (int i = tid; i < t.n * G * (D / 8); i += 256) {
+    const int G = p.Hq / p.b.Hkv;
+    for (int i = (int)threadIdx.x; i < t.n * G * (D / 8); i += THREADS) {
         const int r = i / (D / 8), c = i - r * (D / 8), tk = r / G, h = head * G + r - tk * G;
         const u32x4 x = *reinterpret_cast<const u32x4 *>(p.q + (int64_t)(t.tok + tk) * p.q_st + (int64_t)h * p.q_sh + 8 * c);
         uint32_t m = 0;
@@ -178,116 +178,125 @@ __global__ __launch_bounds__(256) void select_score_kernel(SelectParams p)
             m = finite16(b) && b > m ? b : m;
         }
         atomicMax(&amax[tk], m);
-    }
-    i32x4 best[4];                                 // of 4 blocks of 16 places, until the rounds are over
-    for (int q0 = p0; q0 < p1; q0 += 256) {
-        for (int round = 0; round << 4 < G; ++round) {
-            __syncthreads();
-            // lane l's bytes of step k: row l % 16, bytes 2 D / 4 (l / 16) + 16 k of [max | min]
-            for (int i = tid; i < KS * 64; i += 256) {
-                const int k = i >> 6, l = i & 63, r = l & 15, at = (2 * D / 4) * (l >> 4) + 16 * k;
-                const int tk = r >> hs, g = 16 * round + (r & ((1 << hs) - 1));
-                u32x4 w = {0, 0, 0, 0};
-                if (tk < t.n) {
-                    const int h = head * G + (g < G ? g : 0);   // (missing rows repeat the first)
-                    const uint16_t *src = p.q + (int64_t)(t.tok + tk) * p.q_st + (int64_t)h * p.q_sh + at % D;
-                    const u32x4 a = *reinterpret_cast<const u32x4 *>(src), b = *reinterpret_cast<const u32x4 *>(src + 8);
-                    const float inv = __builtin_bit_cast(float, (uint32_t)(127 - step_exponent(amax[tk])) << 23);
-                    const bool neg = at >= D;
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const uint32_t word = e < 8 ? a[e / 2] : b[e / 2 - 4], bits = e & 1 ? word >> 16 : word & 0xFFFFu;
-                        const float x = finite16(bits) ? __builtin_bit_cast(float, bits << 16) * inv : 0.0f;
-                        const int v = (int)__builtin_rintf(x), s = neg ? (v < 0 ? v : 0) : (v > 0 ? v : 0);
-                        w[e / 4] |= (uint32_t)(s & 255) << (8 * (e % 4));
-                    }
-                }
-                rows[k][l] = w;
-            }
-            __syncthreads();
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int place = q0 + 64 * j + 16 * wave + (lane & 15);
-                const int pg = place < p1 ? table[place] : -1;
-                const bool is = pg >= 0 && pg < p.b.pages;
-                const int8_t *src = p.bounds + ((int64_t)(is ? pg : 0) * p.b.Hkv + head) * (2 * D) + (2 * D / 4) * (lane >> 4);
-                i32x4 acc = {0, 0, 0, 0};
-#pragma unroll
-                for (int k = 0; k < KS; ++k)
-                    acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, rows[k][lane]),
-                                                                *reinterpret_cast<const i32x4 *>(src + 16 * k), acc, 0, 0, 0);
-                if (round == 0) best[j] = acc;
-                else
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) best[j][e] = acc[e] > best[j][e] ? acc[e] : best[j][e];
-            }
-        }
-        // lane: place lane % 16, rows 4 (lane / 16) + e
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int place = q0 + 64 * j + 16 * wave + (lane & 15);
-            i32x4 x = best[j];
-            if (hs >= 1) x[0] = x[0] > x[1] ? x[0] : x[1], x[2] = x[2] > x[3] ? x[2] : x[3];
-            if (hs >= 2) x[0] = x[0] > x[2] ? x[0] : x[2];
-            if (hs >= 3) {
-                const int y = __shfl_xor(x[0], 16, 64);
-                x[0] = x[0] > y ? x[0] : y;
-            }
-            if (hs >= 4) {
-                const int y = __shfl_xor(x[0], 32, 64);
-                x[0] = x[0] > y ? x[0] : y;
-            }
-            if (place >= p1) continue;
-            const int pg = table[place];
-            const bool is = pg >= 0 && pg < p.b.pages;
-            const float ks = is ? p.ks[(int64_t)pg * p.b.Hkv + head] : 0.0f;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int r = 4 * (lane >> 4) + e, tk = r >> hs;
-                if ((r & ((1 << hs) - 1)) != 0 || tk >= t.n) continue;
-                const int64_t row = (int64_t)(t.tok + tk) * p.b.Hkv + head;
-                p.scores[row * p.b.width + place] = is ? sortable((float)x[e] * ks) : MISSING;
-            }
-        }
+        if (G <= 16) raw[(tk << p.heads_shift) + r - tk * G][c] = x;
     }
 }
 
-// The `budget` largest of a row's scores, in order of their places.  A workgroup
-// narrows down the smallest key that is taken by 8 bits a step (a histogram in LDS),
-// then counts and writes, a wave a range of consecutive places.
-__global__ __launch_bounds__(256) void select_top_kernel(SelectParams p)
+// The int8 operand [max(q', 0) | min(q', 0)] of 16 rows: of lane l in step k the row
+// l % 16 and its bytes (2 D/4) (l / 16) + 16 k.  Row (t << HS) + g is head 16 round + g
+// of token t's group (HS = heads_shift; rows without a head repeat the first, those
+// without a token are 0).
+template <int D, int THREADS>
+__device__ __forceinline__ void build_rows(const SelectParams &p, const TokenTile &t, int head, int round, const uint32_t *amax,
+                                           const u32x4 (*raw)[D / 8], u32x4 (*rows)[64])
 {
-    __shared__ uint32_t hist[256];
-    __shared__ int found[2], counts[4][2];
-    const int t = (int)blockIdx.x, head = (int)blockIdx.y, tid = (int)threadIdx.x, lane = tid & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const TokenTile tt = token_tile(p.b, 1, t);
-    if (tt.s < 0) return;
-    const int many = places_of(p.b, tt.pos, tt.len);
-    const int64_t row = (int64_t)tt.tok * p.b.Hkv + head;
-    int *out = p.places + row * p.budget;
-    if (many <= p.budget) {
-        for (int i = tid; i < p.budget; i += 256) out[i] = i < many ? i : -1;
-        return;
+    const int G = p.Hq / p.b.Hkv, hs = p.heads_shift;
+    for (int i = (int)threadIdx.x; i < 2 * D; i += THREADS) {   // (2 D/64 steps of 64 lanes)
+        const int k = i >> 6, l = i & 63, r = l & 15, at = (2 * D / 4) * (l >> 4) + 16 * k;
+        const int tk = r >> hs, g = 16 * round + (r & ((1 << hs) - 1));
+        u32x4 w = {0, 0, 0, 0};
+        if (tk < t.n) {
+            const int gg = g < G ? g : 0;
+            const uint16_t *src = p.q + (int64_t)(t.tok + tk) * p.q_st + (int64_t)(head * G + gg) * p.q_sh + at % D;
+            const u32x4 *here = &raw[(tk << hs) + (gg & 15)][at % D / 8];
+            const u32x4 a = G <= 16 ? here[0] : reinterpret_cast<const u32x4 *>(src)[0];
+            const u32x4 b = G <= 16 ? here[1] : reinterpret_cast<const u32x4 *>(src)[1];
+            const float inv = __builtin_bit_cast(float, (uint32_t)(127 - step_exponent(amax[tk])) << 23);
+            const bool neg = at >= D;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const uint32_t word = e < 8 ? a[e / 2] : b[e / 2 - 4], bits = e & 1 ? word >> 16 : word & 0xFFFFu;
+                const float x = finite16(bits) ? __builtin_bit_cast(float, bits << 16) * inv : 0.0f;
+                const int v = (int)__builtin_rintf(x), s = neg ? (v < 0 ? v : 0) : (v > 0 ? v : 0);
+                w[e / 4] |= (uint32_t)(s & 255) << (8 * (e % 4));
+            }
+        }
+        rows[k][l] = w;
     }
-    const uint32_t *scores = p.scores + row * p.b.width;
-    auto key = [&](int i) { return i < p.first || i >= many - p.last ? FORCED : scores[i]; };
-    uint32_t prefix = 0;
-    int need = p.budget;   // of the keys with this prefix
+}
+
+// Products of the operand with the ranges of the pages in table entries pg (each of
+// the lane's place, lane % 16): its rows 4 (lane / 16) + e; and the pages' scales.
+template <int D, int AT>
+__device__ __forceinline__ void place_products(const SelectParams &p, const int *pg, int head, const u32x4 (*rows)[64], i32x4 *acc, float *ks)
+{
+    constexpr int KS = 2 * D / 64;
+    const int lane = threadIdx.x & 63;
+    i32x4 x[AT][KS];
+#pragma unroll
+    for (int j = 0; j < AT; ++j) {
+        const bool is = pg[j] >= 0 && pg[j] < p.b.pages;
+        const int64_t at = (int64_t)(is ? pg[j] : 0) * p.b.Hkv + head;
+        const int8_t *src = p.bounds + at * (2 * D) + (2 * D / 4) * (lane >> 4);
+#pragma unroll
+        for (int k = 0; k < KS; ++k) x[j][k] = *reinterpret_cast<const i32x4 *>(src + 16 * k);
+        ks[j] = p.ks[at];
+    }
+#pragma unroll
+    for (int j = 0; j < AT; ++j) {
+        acc[j] = i32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int k = 0; k < KS; ++k) acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, rows[k][lane]), x[j][k], acc[j], 0, 0, 0);
+    }
+}
+
+// The largest over each token's rows, in the lanes and elements of their first.
+__device__ __forceinline__ void row_max(i32x4 &x, int hs)
+{
+    if (hs >= 1) x[0] = x[0] > x[1] ? x[0] : x[1], x[2] = x[2] > x[3] ? x[2] : x[3];
+    if (hs >= 2) x[0] = x[0] > x[2] ? x[0] : x[2];
+    if (hs >= 3) {
+        const int y = __shfl_xor(x[0], 16, 64);
+        x[0] = x[0] > y ? x[0] : y;
+    }
+    if (hs >= 4) {
+        const int y = __shfl_xor(x[0], 32, 64);
+        x[0] = x[0] > y ? x[0] : y;
+    }
+}
+
+// Token tk's score of the lane's place with page pg, of scale ks, to write(tk, key), by
+// the lane that has it.
+template <class W>
+__device__ __forceinline__ void write_scores(const SelectParams &p, const i32x4 &x, int pg, float ks, int n, W write)
+{
+    const int lane = threadIdx.x & 63, hs = p.heads_shift;
+    const bool is = pg >= 0 && pg < p.b.pages;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int r = 4 * (lane >> 4) + e, tk = r >> hs;
+        if ((r & ((1 << hs) - 1)) == 0 && tk < n) write(tk, is ? sortable((float)x[e] * ks) : MISSING);
+    }
+}
+
+// The smallest key that is taken and how many that equal it, for up to 16 rows at
+// once: 8 bits a step from a histogram of each in LDS.  The waves of a row (whose
+// wave is `first`th of `by`) call each(f) to go over their part of its keys.  All
+// waves call it.
+struct Taken {
+    uint32_t key;
+    int same;
+};
+
+template <class E>
+__device__ __forceinline__ Taken narrow(uint32_t (*hist)[256], int (*found)[2], int rows, int row, bool head_wave, int budget, E each)
+{
+    const int lane = threadIdx.x & 63;
+    Taken t = {0, budget};
     for (int shift = 24; shift >= 0; shift -= 8) {
-        hist[tid] = 0;
+        for (int i = (int)threadIdx.x; i < 256 * rows; i += (int)blockDim.x) hist[0][i] = 0;
         __syncthreads();
         const uint32_t mask = shift == 24 ? 0u : ~0u << (shift + 8);
-        for (int i = tid; i < many; i += 256) {
-            const uint32_t k = key(i);
-            if ((k & mask) == prefix) atomicAdd(&hist[k >> shift & 255], 1u);
-        }
+        if (row < rows)
+            each([&](uint32_t k) {
+                if ((k & mask) == t.key) atomicAdd(&hist[row][k >> shift & 255], 1u);
+            });
         __syncthreads();
-        if (wave == 0) {
+        if (row < rows && head_wave) {
             // lane l: the 4 digits from 252 - 4 l down in order of size
             uint32_t n[4], sum = 0;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sum += n[e] = hist[255 - 4 * lane - e];
+            for (int e = 0; e < 4; ++e) sum += n[e] = hist[row][255 - 4 * lane - e];
             uint32_t upto = sum;
 #pragma unroll
             for (int k = 1; k < 64; k <<= 1) {
@@ -297,40 +306,265 @@ __global__ __launch_bounds__(256) void select_top_kernel(SelectParams p)
             uint32_t above = upto - sum;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                if (above < (uint32_t)need && (uint32_t)need <= above + n[e]) found[0] = 255 - 4 * lane - e, found[1] = (int)above;
+                if (above < (uint32_t)t.same && (uint32_t)t.same <= above + n[e]) found[row][0] = 255 - 4 * lane - e, found[row][1] = (int)above;
                 above += n[e];
             }
         }
         __syncthreads();
-        prefix |= (uint32_t)found[0] << shift;
-        need -= found[1];
+        if (row < rows) {
+            t.key |= (uint32_t)found[row][0] << shift;
+            t.same -= found[row][1];
+        }
     }
-    // keys above `prefix` are taken, and the first `need` that equal it
-    const int each = ((many + 3) / 4 + 63) & ~63, a = wave * each, e = a + each < many ? a + each : many;
+    return t;
+}
+
+// Places of the keys above t.key, and of the first t.same that equal it, in order:
+// the `by` waves of a row take consecutive parts; key(i) for i < many.  All waves
+// call it (those of no row with many 0).
+template <class K>
+__device__ __forceinline__ void write_places(const Taken &t, int many, int wave, int by, int (*counts)[2], int counts_from, int *out, K key)
+{
+    const int lane = threadIdx.x & 63;
+    const int each = ((many + by - 1) / by + 63) & ~63, a = wave * each, e = a + each < many ? a + each : many;
     int above = 0, same = 0;
     for (int i = a + lane; i - lane < e; i += 64) {
         const uint32_t k = i < e ? key(i) : 0;
-        above += __popcll(__ballot(i < e && k > prefix));
-        same += __popcll(__ballot(i < e && k == prefix));
+        above += __popcll(__ballot(i < e && k > t.key));
+        same += __popcll(__ballot(i < e && k == t.key));
     }
-    if (lane == 0) counts[wave][0] = above, counts[wave][1] = same;
+    if (lane == 0) counts[counts_from + wave][0] = above, counts[counts_from + wave][1] = same;
     __syncthreads();
     int at = 0, equal = 0;
     for (int w = 0; w < wave; ++w) {
-        const int left = need - equal > 0 ? need - equal : 0;
-        at += counts[w][0] + (counts[w][1] < left ? counts[w][1] : left);
-        equal += counts[w][1];
+        const int left = t.same - equal > 0 ? t.same - equal : 0, eq = counts[counts_from + w][1];
+        at += counts[counts_from + w][0] + (eq < left ? eq : left);
+        equal += eq;
     }
     const uint64_t below = ((uint64_t)1 << lane) - 1;
     for (int i = a + lane; i - lane < e; i += 64) {
         const uint32_t k = i < e ? key(i) : 0;
-        const uint64_t eq = __ballot(i < e && k == prefix);
-        const bool take = i < e && (k > prefix || (k == prefix && equal + __popcll(eq & below) < need));
+        const uint64_t eq = __ballot(i < e && k == t.key);
+        const bool take = i < e && (k > t.key || (k == t.key && equal + __popcll(eq & below) < t.same));
         const uint64_t got = __ballot(take);
         if (take) out[at + __popcll(got & below)] = i;
         at += __popcll(got);
         equal += __popcll(eq);
     }
+}
+
+// The same by one wave for one row of up to 64 R keys: the largest key that at least
+// `budget` reach, bit by bit, their number counted by ballots, until exactly `budget`
+// reach one.  Then its places.
+template <int R, class K>
+__device__ __forceinline__ void select_row(int many, int budget, int *out, K key)
+{
+    const int lane = threadIdx.x & 63;
+    uint32_t k[R], low = ~0u, high = 0;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        k[r] = 64 * r + lane < many ? key(64 * r + lane) : 0u;   // (0: below whatever counts)
+        if (64 * r + lane < many) low = k[r] < low ? k[r] : low, high = k[r] > high ? k[r] : high;
+    }
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) {
+        const uint32_t a = __shfl_xor(low, x, 64), b = __shfl_xor(high, x, 64);
+        low = a < low ? a : low;
+        high = b > high ? b : high;
+    }
+    // keys that are at least x (>= 1)
+    auto reach = [&](uint32_t x) {
+        int n = 0;
+#pragma unroll
+        for (int r = 0; r < R; ++r) n += __popcll(__ballot(k[r] >= x));
+        return n;
+    };
+    // (the bits that all have in common need no counting)
+    const uint32_t differ = (uint32_t)__builtin_amdgcn_readfirstlane((int)(low ^ high));
+    const int top = differ ? 32 - __builtin_clz(differ) : 0;
+    uint32_t least = top == 32 ? 0 : (uint32_t)__builtin_amdgcn_readfirstlane((int)low) >> top << top;
+    for (int bit = top - 1; bit >= 0; --bit) {
+        const uint32_t x = least | 1u << bit;
+        const int n = reach(x);
+        if (n >= budget) least = x;
+        if (n == budget) break;
+    }
+    const int above = least == ~0u ? 0 : reach(least + 1);
+    int same = budget - above, at = 0;   // of those that equal it, the first
+    const uint64_t below = ((uint64_t)1 << lane) - 1;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const bool is = 64 * r + lane < many;
+        const uint64_t eq = __ballot(is && k[r] == least);
+        const bool take = is && (k[r] > least || (k[r] == least && __popcll(eq & below) < same));
+        const uint64_t got = __ballot(take);
+        if (take) out[at + __popcll(got & below)] = 64 * r + lane;
+        at += __popcll(got);
+        same -= __popcll(eq) < same ? __popcll(eq) : same;
+    }
+}
+
+// A tile's tokens and one kv head, scores in LDS.
+constexpr int SELECT_BY = 512;
+
+template <int D>
+__global__ __launch_bounds__(SELECT_BY) void select_kernel(SelectParams p)
+{
+    constexpr int WAVES = SELECT_BY / 64;
+    __shared__ u32x4 rows[2 * D / 64][64];
+    __shared__ u32x4 raw[16][D / 8];
+    __shared__ uint32_t amax[16], hist[1][256];
+    __shared__ int found[1][2], counts[WAVES][2];
+    extern __shared__ uint32_t keys[];             // [tokens][places]
+    const int G = p.Hq / p.b.Hkv, hs = p.heads_shift;
+    const TokenTile t = token_tile(p.b, p.tokens, (int)blockIdx.x);
+    if (t.s < 0) return;
+    const int head = (int)blockIdx.y, tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int most = places_of(p.b, t.pos + t.n - 1, t.len);
+    auto out_of = [&](int tk) { return p.places + ((int64_t)(t.tok + tk) * p.b.Hkv + head) * p.budget; };
+    if (most > p.budget) {
+        const int *table = p.b.table + t.s * p.b.table_stride;
+        constexpr int AT = D > 128 ? 2 : 4;        // blocks of 16 places of a wave at once
+        int pg[AT];
+        auto look_up = [&](int q0) {
+#pragma unroll
+            for (int j = 0; j < AT; ++j) {
+                const int place = q0 + 16 * j + (lane & 15);
+                pg[j] = place < most ? table[place] : -1;
+            }
+        };
+        look_up(wave * 16 * AT);
+        if (tid < 16) amax[tid] = 0;
+        __syncthreads();
+        group_amax<D, SELECT_BY>(p, t, head, amax, raw);
+        __syncthreads();
+        const int rounds = (G + 15) / 16;
+        for (int round = 0; round < rounds; ++round) {
+            if (round) __syncthreads();
+            build_rows<D, SELECT_BY>(p, t, head, round, amax, raw, rows);
+            __syncthreads();
+            for (int q0 = wave * 16 * AT; q0 < most; q0 += WAVES * 16 * AT) {
+                if (round || q0 >= WAVES * 16 * AT) look_up(q0);
+                i32x4 x[AT];
+                float ks[AT];
+                place_products<D, AT>(p, pg, head, rows, x, ks);
+#pragma unroll
+                for (int j = 0; j < AT; ++j) {
+                    const int place = q0 + 16 * j + (lane & 15);
+                    row_max(x[j], hs);
+                    if (place >= most) continue;
+                    if (rounds == 1) {
+                        write_scores(p, x[j], pg[j], ks[j], t.n, [&](int tk, uint32_t k) { keys[tk * p.b.width + place] = k; });
+                    } else if (lane < 16) {   // (one token a tile: its products' maximum over the rounds first)
+                        const int old = round ? (int)keys[place] : x[j][0], now = x[j][0] > old ? x[j][0] : old;
+                        keys[place] = (uint32_t)now;
+                        if (round == rounds - 1) write_scores(p, i32x4{now, 0, 0, 0}, pg[j], ks[j], 1, [&](int, uint32_t k) { keys[place] = k; });
+                    }
+                }
+            }
+        }
+        __syncthreads();
+    }
+    // a wave for each token, or all for each of long rows
+    const bool alone = most <= 1024;
+    for (int tk = alone ? wave : 0; tk < t.n; tk += alone ? WAVES : 1) {
+        const int many = places_of(p.b, t.pos + tk, t.len);
+        int *out = out_of(tk);
+        auto key = [&](int i) { return i < p.first || i >= many - p.last ? FORCED : keys[tk * p.b.width + i]; };
+        if (many <= p.budget) {
+            for (int i = alone ? lane : tid; i < p.budget; i += alone ? 64 : SELECT_BY) out[i] = i < many ? i : -1;
+        } else if (many <= 256) {
+            select_row<4>(many, p.budget, out, key);
+        } else if (many <= 512) {
+            select_row<8>(many, p.budget, out, key);
+        } else if (many <= 1024) {
+            select_row<16>(many, p.budget, out, key);
+        } else {
+            const Taken taken = narrow(hist, found, 1, 0, wave == 0, p.budget, [&](auto f) {
+                for (int i = tid; i < many; i += SELECT_BY) f(key(i));
+            });
+            write_places(taken, many, wave, WAVES, counts, 0, out, key);
+            __syncthreads();   // (counts have been read)
+        }
+    }
+}
+
+// Where the scores of a tile's tokens do not fit LDS, or one tile's workgroup would
+// have too long a row to itself: scores over `chunk` places to memory, ...
+template <int D>
+__global__ __launch_bounds__(256) void select_score_kernel(SelectParams p)
+{
+    __shared__ u32x4 rows[2 * D / 64][64], raw[16][D / 8];
+    __shared__ uint32_t amax[16];
+    const int G = p.Hq / p.b.Hkv, hs = p.heads_shift;
+    const TokenTile t = token_tile(p.b, p.tokens, (int)blockIdx.x);
+    if (t.s < 0) return;
+    const int head = (int)blockIdx.y, tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int many = places_of(p.b, t.pos + t.n - 1, t.len);
+    const int p0 = (int)blockIdx.z * p.chunk, p1 = many - p0 < p.chunk ? many : p0 + p.chunk;
+    if (p0 >= p1 || many <= p.budget) return;      // (all of them: no scores are looked at)
+    const int *table = p.b.table + t.s * p.b.table_stride;
+    if (tid < 16) amax[tid] = 0;
+    __syncthreads();
+    group_amax<D, 256>(p, t, head, amax, raw);
+    __syncthreads();
+    const int rounds = (G + 15) / 16;
+    constexpr int AT = D > 128 ? 2 : 4;            // blocks of 16 places of a wave at once
+    for (int q0 = p0 + wave * 16 * AT; q0 - wave * 16 * AT < p1; q0 += 64 * AT) {
+        int pg[AT];
+        i32x4 best[AT];
+        float ks[AT];
+#pragma unroll
+        for (int j = 0; j < AT; ++j) {
+            const int place = q0 + 16 * j + (lane & 15);
+            pg[j] = place < p1 ? table[place] : -1;
+        }
+        for (int round = 0; round < rounds; ++round) {
+            if (q0 < p0 + 64 * AT || rounds > 1) {
+                __syncthreads();
+                build_rows<D, 256>(p, t, head, round, amax, raw, rows);
+                __syncthreads();
+            }
+            i32x4 x[AT];
+            place_products<D, AT>(p, pg, head, rows, x, ks);
+#pragma unroll
+            for (int j = 0; j < AT; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) best[j][e] = round == 0 || x[j][e] > best[j][e] ? x[j][e] : best[j][e];
+        }
+#pragma unroll
+        for (int j = 0; j < AT; ++j) {
+            const int place = q0 + 16 * j + (lane & 15);
+            row_max(best[j], hs);
+            if (place >= p1) continue;
+            write_scores(p, best[j], pg[j], ks[j], t.n, [&](int tk, uint32_t k) {
+                p.scores[((int64_t)(t.tok + tk) * p.b.Hkv + head) * p.b.width + place] = k;
+            });
+        }
+    }
+}
+
+// ... and the places of a token and kv head from those.
+__global__ __launch_bounds__(256) void select_top_kernel(SelectParams p)
+{
+    __shared__ uint32_t hist[1][256];
+    __shared__ int found[1][2], counts[4][2];
+    const int head = (int)blockIdx.y, tid = (int)threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const TokenTile t = token_tile(p.b, 1, (int)blockIdx.x);
+    if (t.s < 0) return;
+    const int many = places_of(p.b, t.pos, t.len);
+    const int64_t row = (int64_t)t.tok * p.b.Hkv + head;
+    int *out = p.places + row * p.budget;
+    if (many <= p.budget) {
+        for (int i = tid; i < p.budget; i += 256) out[i] = i < many ? i : -1;
+        return;
+    }
+    const uint32_t *scores = p.scores + row * p.b.width;
+    auto key = [&](int i) { return i < p.first || i >= many - p.last ? FORCED : scores[i]; };
+    const Taken taken = narrow(hist, found, 1, 0, wave == 0, p.budget, [&](auto f) {
+        for (int i = tid; i < many; i += 256) f(key(i));
+    });
+    write_places(taken, many, wave, 4, counts, 0, out, key);
 }
 
 } // namespace
@@ -349,33 +583,64 @@ hipError_t launch_kv_bounds(int D, const BoundsParams &params, hipStream_t s)
     return hipGetLastError();
 }
 
-size_t select_workspace(int64_t T, int Hkv, int64_t width)
+// The tokens of a tile; whether one launch does it all.
+struct SelectShape {
+    int heads_shift, tokens;
+    int64_t tiles;
+    bool one;
+};
+
+// In one launch where a tile's scores fit half of a CU's LDS, and either workgroups
+// fill the device or none reads more than ALONE bytes of ranges.
+constexpr int64_t KEYS = 12288, ALONE = (int64_t)1 << 18;
+
+static SelectShape select_shape(int D, int64_t T, int64_t S, int G, int Hkv, int64_t width)
 {
-    return (size_t)T * Hkv * width * sizeof(uint32_t);
+    SelectShape x = {};
+    while (1 << x.heads_shift < G && x.heads_shift < 4) ++x.heads_shift;
+    x.tokens = 16 >> x.heads_shift;
+    auto tiles = [&](int per) { return per > 1 ? T / per + S : T; };
+    x.tiles = tiles(x.tokens);
+    // (fewer tokens a tile: the operand's other rows are 0)
+    int per = x.tokens;
+    while (per > 1 && (per * width > KEYS || tiles(per) * Hkv < 256)) per /= 2;
+    x.one = width * per <= KEYS && (tiles(per) * Hkv >= 256 || width * 2 * D <= ALONE);
+    if (x.one) x.tokens = per, x.tiles = tiles(per);
+    return x;
+}
+
+size_t select_workspace(int D, int64_t T, int64_t S, int G, int Hkv, int64_t width, int64_t budget)
+{
+    return width <= budget || select_shape(D, T, S, G, Hkv, width).one ? 0 : (size_t)T * Hkv * width * sizeof(uint32_t);
+}
+
+template <int D>
+static hipError_t launch_select_of(const SelectParams &p, const SelectShape &x, hipStream_t s)
+{
+    if (x.one || p.b.width <= p.budget) {
+        const size_t keys = p.b.width <= p.budget ? 0 : (size_t)x.tokens * p.b.width * sizeof(uint32_t);
+        select_kernel<D><<<dim3((unsigned)x.tiles, (unsigned)p.b.Hkv), SELECT_BY, keys, s>>>(p);
+        return hipGetLastError();
+    }
+    select_score_kernel<D><<<dim3((unsigned)x.tiles, (unsigned)p.b.Hkv, (unsigned)((p.b.width + p.chunk - 1) / p.chunk)), 256, 0, s>>>(p);
+    select_top_kernel<<<dim3((unsigned)p.b.T, (unsigned)p.b.Hkv), 256, 0, s>>>(p);
+    return hipGetLastError();
 }
 
 hipError_t launch_select(int D, SelectParams &p, void *ws, hipStream_t s)
 {
-    const int G = p.Hq / p.b.Hkv;
+    const SelectShape x = select_shape(D, p.b.T, p.b.S, p.Hq / p.b.Hkv, p.b.Hkv, p.b.width);
     p.scores = static_cast<uint32_t *>(ws);
-    p.heads_shift = 0;
-    while (1 << p.heads_shift < G && p.heads_shift < 4) ++p.heads_shift;
-    const int per = 16 >> p.heads_shift;
-    const int64_t tiles = per > 1 ? (int64_t)p.b.T / per + p.b.S : p.b.T;
+    p.heads_shift = x.heads_shift;
+    p.tokens = x.tokens;
     // chunks of 64 places at least, and enough of them to fill the device
-    const int64_t most = (p.b.width + 63) / 64, want = (2048 + tiles * p.b.Hkv - 1) / (tiles * p.b.Hkv);
-    const int64_t n = want < most ? want : most;
-    if (p.b.width > p.budget) {
-        p.chunk = (int)(((p.b.width + n - 1) / n + 63) / 64 * 64);
-        const dim3 grid((unsigned)tiles, (unsigned)p.b.Hkv, (unsigned)((p.b.width + p.chunk - 1) / p.chunk));
-        switch (D) {
-        case 64: select_score_kernel<64><<<grid, 256, 0, s>>>(p); break;
-        case 128: select_score_kernel<128><<<grid, 256, 0, s>>>(p); break;
-        default: select_score_kernel<256><<<grid, 256, 0, s>>>(p); break;
-        }
+    const int64_t most = (p.b.width + 63) / 64, want = (2048 + x.tiles * p.b.Hkv - 1) / (x.tiles * p.b.Hkv), n = want < most ? want : most;
+    p.chunk = n > 0 ? (int)(((p.b.width + n - 1) / n + 63) / 64 * 64) : 64;
+    switch (D) {
+    case 64: return launch_select_of<64>(p, x, s);
+    case 128: return launch_select_of<128>(p, x, s);
+    default: return launch_select_of<256>(p, x, s);
     }
-    select_top_kernel<<<dim3((unsigned)p.b.T, (unsigned)p.b.Hkv), 256, 0, s>>>(p);
-    return hipGetLastError();
 }
 
 } // namespace lamp

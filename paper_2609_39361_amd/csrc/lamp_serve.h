@@ -137,11 +137,12 @@ struct SelectParams {
     int *places;              // [T][Hkv][budget]
     int Hq, budget, first, last;
     uint32_t *scores;         // [T][Hkv][width] (workspace)
-    int heads_shift;          // log2 of the heads of a group, rounded up, 16 at most (set by the launcher)
-    int chunk;                // places of a workgroup (set by the launcher)
+    // (set by the launcher) log2 of the heads of a group, rounded up, 16 at most; tokens
+    // of a tile; places of a workgroup
+    int heads_shift, tokens, chunk;
 };
 
-size_t select_workspace(int64_t T, int Hkv, int64_t width);
+size_t select_workspace(int D, int64_t T, int64_t S, int G, int Hkv, int64_t width, int64_t budget);
 hipError_t launch_select(int D, SelectParams &p, void *ws, hipStream_t s);
 
 // A step of a batch (lamp_advance.hip).

@@ -7,6 +7,7 @@ no fallback path.
 """
 import collections
 import ctypes
+import functools
 import math
 import os
 import struct
@@ -88,7 +89,7 @@ def lib():
         L.lamp_kv_bounds.restype = i32
         L.lamp_select_pages.argtypes = [P, i64, i64, i32, P, P, P, i32, i32, i32, P, P, sz, P]
         L.lamp_select_pages.restype = i32
-        L.lamp_select_pages_workspace_size.argtypes = [i32] * 4
+        L.lamp_select_pages_workspace_size.argtypes = [i32] * 7
         L.lamp_select_pages_workspace_size.restype = sz
         L.lamp_attn_pages.argtypes = [P, i64, i64, i32, P, P, P, i32, f64, P, P, P, sz, P]
         L.lamp_attn_pages.restype = i32
@@ -641,21 +642,25 @@ def kv_advance(pool, block_table, kv_lens, add, page, tokens, prefix_lens=None, 
         raise ValueError("block_table must be an int32 CUDA tensor [S, pages of a sequence]")
     dev = block_table.get_device()
     S, width = block_table.shape
-    _must(block_table, "block_table", (_I32,), dev)
+    if not (block_table.dtype is _I32 and ring.dtype is _I32 and state.dtype is _I32 and kv_lens.dtype is _I32 and add.dtype is _I32
+            and ring.get_device() == dev and state.get_device() == dev and kv_lens.get_device() == dev and add.get_device() == dev
+            and state.shape == (4,) and kv_lens.shape == (S,) and add.shape == (S,) and ring.dim() == 1 and ring.is_contiguous()
+            and state.is_contiguous() and kv_lens.is_contiguous() and add.is_contiguous() and (width < 2 or block_table.stride(1) == 1)):
+        _must(block_table, "block_table", (_I32,), dev)
+        _must(ring, "pool.ring", (_I32,), dev, (ring.numel(),))
+        _must(state, "pool.state", (_I32,), dev, (4,))
+        _must(kv_lens, "kv_lens", (_I32,), dev, (S,))
+        _must(add, "add", (_I32,), dev, (S,))
     if S > 1 and block_table.stride(0) < width:   # (written to)
         raise ValueError("rows of block_table share memory")
-    _must(ring, "pool.ring", (_I32,), dev, (ring.numel(),))
-    _must(state, "pool.state", (_I32,), dev, (4,))
-    _must(kv_lens, "kv_lens", (_I32,), dev, (S,))
-    _must(add, "add", (_I32,), dev, (S,))
-    if prefix_lens is not None:
+    if prefix_lens is not None and (prefix_lens.dtype is not _I32 or prefix_lens.get_device() != dev or prefix_lens.shape != (S,)
+                                    or not prefix_lens.is_contiguous()):
         _must(prefix_lens, "prefix_lens", (_I32,), dev, (S,))
     tokens = int(tokens)
     if tokens < 0:
         raise ValueError("tokens must not be negative")
     if out is None:
-        lens, q_start = kv_lens.new_empty(S), kv_lens.new_empty(S + 1)
-        positions, new_state = kv_lens.new_empty(tokens), kv_lens.new_empty(4)
+        lens, q_start, positions, new_state = kv_lens.new_empty(2 * S + tokens + 5).split((S, S + 1, tokens, 4))
     else:
         lens, q_start, positions, new_state = out
         for t, name, n in ((lens, "kv_lens", S), (q_start, "q_start", S + 1), (positions, "positions", tokens),
@@ -705,6 +710,12 @@ def _queries(q, dev, d):
     return q.data_ptr(), q.stride(0), q.stride(1), q.shape[1]
 
 
+@functools.lru_cache(maxsize=1024)
+def _need(name, *sizes):
+    """What a workspace size function of the library (of sizes alone) returns."""
+    return int(getattr(lib(), name)(*sizes))
+
+
 def _workspace(workspace, need, like, dev):
     """(pointer, bytes, the tensor) of a call's workspace: the caller's, or one of torch's of `need` bytes."""
     if workspace is None:
@@ -730,9 +741,9 @@ def _attn_out(q, out, dev):
     return o, lse
 
 
-def select_pages_workspace_size(T, Hkv, width, budget):
+def select_pages_workspace_size(T, S, Hq, Hkv, d, width, budget):
     """Bytes of workspace one select_pages call needs (0: none)."""
-    return int(lib().lamp_select_pages_workspace_size(T, Hkv, width, budget))
+    return int(lib().lamp_select_pages_workspace_size(T, S, Hq, Hkv, d, width, budget))
 
 
 def select_pages(q, cache, bounds, block_table, kv_lens, budget, q_start=None, first=1, last=2, out=None, workspace=None):
@@ -745,7 +756,7 @@ def select_pages(q, cache, bounds, block_table, kv_lens, budget, q_start=None, f
     last `last` places in the token's sight are taken always; ties go to the lower place.  Rows of tokens behind
     q_start[S] are left as they are in `out`.  `workspace` as for attn_cache."""
     T = _tokens(q)
-    c, b, dev, Hkv, _, d, _, width = _paged(cache, block_table, kv_lens, q_start, T)
+    c, b, dev, Hkv, _, d, S, width = _paged(cache, block_table, kv_lens, q_start, T)
     rows = _queries(q, dev, d)
     ranges = _bounds(bounds, dev, (cache.k.shape[0], Hkv, 2, d))
     budget = int(budget)
@@ -755,9 +766,8 @@ def select_pages(q, cache, bounds, block_table, kv_lens, budget, q_start=None, f
         out = kv_lens.new_empty((T, Hkv, budget))
     else:
         _must(out, "out", (_I32,), dev, (T, Hkv, budget))
-    L = lib()
-    ws, size, keep = _workspace(workspace, L.lamp_select_pages_workspace_size(T, Hkv, width, budget), q, dev)
-    _call(dev, L.lamp_select_pages, *rows, c, b, ranges, budget, int(first), int(last), out.data_ptr(), ws, size)
+    ws, size, keep = _workspace(workspace, _need("lamp_select_pages_workspace_size", T, S, rows[3], Hkv, d, width, budget), q, dev)
+    _call(dev, lib().lamp_select_pages, *rows, c, b, ranges, budget, int(first), int(last), out.data_ptr(), ws, size)
     return out
 
 
@@ -780,9 +790,8 @@ def attn_pages(q, cache, block_table, kv_lens, places, q_start=None, scale=None,
         _must(places, "places", (_I32,), dev, places.shape)
     budget = places.shape[2]
     o, lse = _attn_out(q, out, dev)
-    L = lib()
-    ws, size, keep = _workspace(workspace, L.lamp_attn_pages_workspace_size(T, rows[3], Hkv, d, page, budget), q, dev)
-    _call(dev, L.lamp_attn_pages, *rows, c, b, places.data_ptr(), budget, d ** -0.5 if scale is None else float(scale),
+    ws, size, keep = _workspace(workspace, _need("lamp_attn_pages_workspace_size", T, rows[3], Hkv, d, page, budget), q, dev)
+    _call(dev, lib().lamp_attn_pages, *rows, c, b, places.data_ptr(), budget, d ** -0.5 if scale is None else float(scale),
           o.data_ptr(), lse.data_ptr(), ws, size)
     return o, lse
 
@@ -803,15 +812,16 @@ def attn_shared(q, cache, block_table, kv_lens, prefix_lens, group_start, q_star
     T = _tokens(q)
     c, b, dev, Hkv, page, d, S, width = _paged(cache, block_table, kv_lens, q_start, T)
     rows = _queries(q, dev, d)
-    _must(prefix_lens, "prefix_lens", (_I32,), dev, (S,))
     if not isinstance(group_start, torch.Tensor) or group_start.dim() != 1 or group_start.shape[0] < 2:
         raise ValueError("group_start int32 [groups + 1] expected")
-    _must(group_start, "group_start", (_I32,), dev, group_start.shape)
+    if not (prefix_lens.dtype is _I32 and group_start.dtype is _I32 and prefix_lens.get_device() == dev and group_start.get_device() == dev
+            and prefix_lens.shape == (S,) and prefix_lens.is_contiguous() and group_start.is_contiguous()):
+        _must(prefix_lens, "prefix_lens", (_I32,), dev, (S,))
+        _must(group_start, "group_start", (_I32,), dev, group_start.shape)
     groups = group_start.shape[0] - 1
     o, lse = _attn_out(q, out, dev)
-    L = lib()
-    ws, size, keep = _workspace(workspace, L.lamp_attn_shared_workspace_size(T, S, groups, rows[3], Hkv, d, page, width), q, dev)
-    _call(dev, L.lamp_attn_shared, *rows, c, b, prefix_lens.data_ptr(), group_start.data_ptr(), groups,
+    ws, size, keep = _workspace(workspace, _need("lamp_attn_shared_workspace_size", T, S, groups, rows[3], Hkv, d, page, width), q, dev)
+    _call(dev, lib().lamp_attn_shared, *rows, c, b, prefix_lens.data_ptr(), group_start.data_ptr(), groups,
           d ** -0.5 if scale is None else float(scale), o.data_ptr(), lse.data_ptr(), ws, size)
     return o, lse
 

@@ -205,6 +205,17 @@ def test_select(L, lens, Hq, H, d, page, budget, first, last):  # noqa: F811
     _check_select(L, _select_case(lens, Hq, H, d, page, d + page), page, budget, first, last)
 
 
+@pytest.mark.parametrize("lens,Hq,H,d,budget", [
+    ([(195000, 1)], 2, 1, 64, 100),                                        # a row too long for one workgroup
+    ([(150000, 1)] + [(30 + i, 1) for i in range(129)], 4, 2, 64, 60),     # LDS holds as many scores as it may
+    ([(150000, 2)] + [(30 + i, 1) for i in range(29)], 2, 1, 128, 60),     # and not those of two tokens, of few workgroups
+    ([(40, 1)] * 3 + [(40000, 14)], 1, 1, 64, 33),                         # 14 tokens in one tile
+    ([(2500, 40), (900, 7)], 3, 3, 64, 20),
+])
+def test_select_long(L, lens, Hq, H, d, budget):  # noqa: F811
+    _check_select(L, _select_case(lens, Hq, H, d, 16, 77), 16, budget, 1, 2)
+
+
 def test_select_ties_zeros_and_what_is_not_finite(L):  # noqa: F811
     """Equal scores go to the lower places; zero queries and scales; NaN and infinities of the queries count as 0; missing
     pages come last, in the order of their places."""

@@ -76,8 +76,8 @@ def test_bounds_and_select_refusals():
         assert _select(budget=budget, first=first, last=last) == INVALID and "budget" in _err()
     assert _select(budget=(1 << 20) + 1) == UNSUPPORTED
     assert _select(b=_batch(T=1 << 22, width=1 << 20)) == UNSUPPORTED and "T*Hkv*width" in _err()
-    assert _select(b=_batch(width=9), budget=4, ws=P(4096), n=8) == 6          # (too small a workspace)
-    assert _select(b=_batch(width=9), budget=4, ws=P(4100), n=1 << 20) == INVALID and "256" in _err()
+    assert _select(b=_batch(width=5000), budget=4, ws=P(4096), n=8) == 6          # (too small a workspace)
+    assert _select(b=_batch(width=5000), budget=4, ws=P(4100), n=1 << 20) == INVALID and "256" in _err()
 
 
 def test_pages_and_shared_refusals():
@@ -104,8 +104,11 @@ def test_advance_refusals():
 
 def test_workspace_sizes():
     size = lamp.select_pages_workspace_size
-    assert size(3, 2, 10, 10) == 0 and size(0, 2, 10, 4) == 0 and size(3, 2, 10, 4) >= 3 * 2 * 10 * 4
-    assert size(1 << 23, 1 << 20, 1 << 30, 4) == 0
+    assert size(3, 1, 8, 2, 64, 10, 10) == 0 and size(0, 1, 8, 2, 64, 10, 4) == 0 and size(3, 1, 7, 2, 64, 10, 4) == 0
+    # scores in LDS, but for rows too long for it, or for a few workgroups
+    assert size(3, 1, 8, 2, 64, 10, 4) == 0 and size(300, 300, 8, 2, 128, 12288, 4) == 0
+    assert size(300, 300, 8, 2, 128, 12289, 4) == 300 * 2 * 12289 * 4 and size(1, 1, 8, 2, 128, 1025, 4) == 2 * 1025 * 4
+    assert size(1 << 23, 1 << 20, 1, 1, 64, 1 << 20, 4) == 0
     size = lamp.attn_pages_workspace_size
     assert size(2, 4, 3, 64, 16, 4) == 0 and size(1, 4, 2, 80, 16, 4) == 0 and size(1, 4, 2, 64, 24, 4) == 0
     assert size(1, 4, 2, 64, 16, 16) == 0 and size(1, 4, 2, 64, 16, 64) > 0   # (4 tiles of 64 keys a part at least)
