@@ -100,16 +100,16 @@ __device__ __forceinline__ SeqPlan seq_plan(const CacheAttnParams &p, int s, int
 }
 
 // Groups of sequences with a shared prefix (lamp_cache_shared.hip): what is
-// planned is each group's new tokens over the prefix, then each sequence's over
-// the keys behind it.
+// planned is each group's new tokens over the prefix (in the forms 1 and 2), then each
+// sequence's over the keys behind it (in the forms 0 and 1).
 // (Without branches: the loads of several sequences do not wait for each other.)
 template <class F>
 __device__ __forceinline__ SeqPlan seq_plan(const SharedAttnParams &p, int v, int G)
 {
     SeqPlan r;
-    const bool group = F::FORM == 2 || v < p.groups;
-    const int at = group ? v : 0, g0 = p.group_start[at], g1 = p.group_start[at + 1];
-    const int s = group ? g0 : v - p.groups, s1 = group ? g1 : s + 1;
+    const bool group = F::FORM == 2 || (F::FORM == 1 && v < p.groups);
+    const int at = group ? v : 0, g0 = F::FORM == 0 ? 0 : p.group_start[at], g1 = F::FORM == 0 ? 0 : p.group_start[at + 1];
+    const int s = group ? g0 : (F::FORM == 0 ? v : v - p.groups), s1 = group ? g1 : s + 1;
     const bool is = s >= 0 && s1 <= p.b.S && s < s1;
     const int i = is ? s : 0, i1 = is ? s1 : 0;
     const int a = p.b.q_start ? p.b.q_start[i] : i, e = p.b.q_start ? p.b.q_start[i1] : i1;
@@ -159,7 +159,7 @@ __device__ __forceinline__ SeqPlan seq_plan(const PagesAttnParams &p, int t, int
 // What a plan of attn_shared goes over; and whether a sequence's units of `pieces`
 // pieces leave partial outputs to be joined.
 template <class F>
-__device__ __forceinline__ int planned(const SharedAttnParams &p) { return F::FORM == 2 ? p.groups : p.b.S + p.groups; }
+__device__ __forceinline__ int planned(const SharedAttnParams &p) { return F::FORM == 2 ? p.groups : p.b.S + (F::FORM == 1 ? p.groups : 0); }
 __device__ __forceinline__ bool joined(const CacheAttnParams &, const SeqPlan &, int pieces) { return pieces > 1; }
 __device__ __forceinline__ bool joined(const PagesAttnParams &, const SeqPlan &, int pieces) { return pieces > 1; }
 __device__ __forceinline__ bool joined(const SharedAttnParams &, const SeqPlan &r, int pieces)
@@ -257,7 +257,7 @@ __device__ __forceinline__ Split split_of(const CacheAttnParams &p, const Work &
 {
     const int tiles = F::FORM == 1 && p.units[0] && !p.apart ? 8 : F::MIN_TILES;
     const float each = fmaxf(w.most * (float)p.b.Hkv * (1.0f / F::TARGET), (float)tiles);
-    return {each, F::FORM == 1 && w.mean < EVEN * w.tiles * w.longest ? 2 : 1, tiles};
+    return {each, F::FORM == 2 || (F::FORM && w.mean < EVEN * w.tiles * w.longest) ? 2 : 1, tiles};
 }
 
 // Unit `local` of sequence s, whose partial outputs start at `slots`.  (Tables

@@ -139,10 +139,14 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedAttnParams p)
     else join_row16<D>(p.part[0], p.part_ml[0], a.at, step(a), n0, b.at, step(b), n1, p.o + row * D, p.lse + row);
 }
 
-// Groups of up to GROUP_FEW rows and sequences of up to SHARED_FEW take the form for
-// few rows, larger groups of up to GROUP_PREFIX that of lamp_cache_prefix.h.
-constexpr int GROUP_FEW = 16, GROUP_PREFIX = 1024, SHARED_FEW = 64;
-constexpr int64_t JOIN_WIDE = 8192;   // rows up to which a wave joins each
+// Groups of up to GROUP_PREFIX rows take the form of lamp_cache_prefix.h, beside the
+// sequences, in the form for few rows; where the batch holds more rows than that,
+// larger groups, and sequences of more than SHARED_FEW rows, take the form for many
+// in a launch of its own.  Behind 8192 shared keys (32/8 heads, d = 128): one token
+// 18 us in the first form and 22 in that for few rows, 8 tokens 20 and 28, 250 tokens
+// (1000 rows) 78 and 87 in that for many, 1000 tokens 274 and 254.
+constexpr int GROUP_PREFIX = 1024, SHARED_FEW = 64;
+constexpr int64_t JOIN_WIDE = 1024;   // rows up to which a wave joins each (512 rows 21.6 us a call, by 16 lanes 22.5; 8192 rows 77.0 and 75.3)
 
 struct SharedBounds {
     int above[3], upto[3], group_above[3], group_upto[3], units[3], slots[3];
@@ -168,14 +172,10 @@ SharedBounds shared_bounds(int64_t T, int64_t S, int64_t groups, int G, int Hkv,
         const int64_t k = least(n, rows / from);
         return least(rows / tile + k, k * ((upto + tile - 1) / tile));
     };
-    b.group_upto[0] = GROUP_FEW;
     b.upto[0] = many ? SHARED_FEW : (int)rows;
-    bound_shared<FewRows>(b, (tiles(FewRows::ROWS, S, 1, b.upto[0]) + tiles(FewRows::ROWS, groups, 1, GROUP_FEW)) * Hkv, keys);
-    if (rows > GROUP_FEW) {
-        b.group_above[2] = GROUP_FEW;
-        b.group_upto[2] = GROUP_PREFIX;
-        bound_shared<PrefixRows>(b, tiles(PrefixRows::ROWS, groups, GROUP_FEW + 1, GROUP_PREFIX) * Hkv, keys);
-    }
+    bound_shared<FewRows>(b, tiles(FewRows::ROWS, S, 1, b.upto[0]) * Hkv, keys);
+    b.group_upto[2] = GROUP_PREFIX;
+    bound_shared<PrefixRows>(b, tiles(PrefixRows::ROWS, groups, 1, GROUP_PREFIX) * Hkv, keys);
     if (many) {
         b.above[1] = SHARED_FEW;
         b.group_above[1] = GROUP_PREFIX;

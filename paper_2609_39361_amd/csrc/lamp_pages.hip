@@ -13,84 +13,104 @@
 // whatever order it is summed, and the same pages are selected everywhere.
 #include <hip/hip_runtime.h>
 
-#include "lamp_search.h"
-#include "lamp_serve.h"
+#include "lamp_cache_plan.h"
 
 namespace lamp {
 namespace {
 
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef short i16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int RANGE_UNIT = 4;      // code values of a step of a range
-constexpr int NONE = 1000;         // beyond every range: no key yet
 
-__device__ __forceinline__ i16x2 max2(i16x2 a, i16x2 b) { return __builtin_elementwise_max(a, b); }
-__device__ __forceinline__ i16x2 min2(i16x2 a, i16x2 b) { return __builtin_elementwise_min(a, b); }
+// The number where the other is a quiet NaN, as conversions make them.  (The compiler
+// quiets the operands of its own maximum first: two instructions more for each.  Lane
+// exchanges do not read what these write: the compiler does not see their hazards.)
+__device__ __forceinline__ f16x2 max2(f16x2 a, f16x2 b)
+{
+    f16x2 r;
+    asm("v_pk_max_f16 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
 
-// One workgroup ranges over the keys of one page and head that received tokens;
-// a thread takes 16 channels of every 256/(D/16)-th key.
+__device__ __forceinline__ f16x2 min2(f16x2 a, f16x2 b)
+{
+    f16x2 r;
+    asm("v_pk_min_f16 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
+
+// Max and min over the lanes whose numbers differ in bits of `from` and up, in all of
+// them: within rows of 16 lanes by rotation, then over the rows.
+template <int FROM, class OP>
+__device__ __forceinline__ f16x2 over_lanes(f16x2 v, OP op)
+{
+    auto bits = [](f16x2 x) { return __builtin_bit_cast(int, x); };
+    auto pair = [](int x) { return __builtin_bit_cast(f16x2, x); };
+    v = __builtin_elementwise_canonicalize(v);
+    if constexpr (FROM <= 4) v = op(v, pair(__builtin_amdgcn_update_dpp(0, bits(v), 0x124, 0xf, 0xf, false)));   // row_ror:4
+    if constexpr (FROM <= 8) v = op(v, pair(__builtin_amdgcn_update_dpp(0, bits(v), 0x128, 0xf, 0xf, false)));   // row_ror:8
+    const auto a = __builtin_amdgcn_permlane16_swap((uint32_t)bits(v), (uint32_t)bits(v), false, false);
+    v = op(pair((int)a[0]), pair((int)a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap((uint32_t)bits(v), (uint32_t)bits(v), false, false);
+    return op(pair((int)b[0]), pair((int)b[1]));
+}
+
+// A wave ranges over the keys of one page and head that received tokens; a lane
+// takes 16 channels of every 64/(D/16)-th key, AT of them at once.  Bound by HBM for
+// prompts, by the latencies of starts, lengths, table and codes for single tokens.
 template <int D>
 __global__ __launch_bounds__(256) void kv_bounds_kernel(BoundsParams p)
 {
-    constexpr int LPR = D / 16, RPB = 256 / LPR;   // threads of a key, keys of a pass
-    __shared__ i16x2 red[2][4][D / 2];
+    constexpr int LPR = D / 16, KEYS = 64 / LPR, AT = 8;   // lanes of a key, keys of a load
     const PageWork w = page_work(p.b, p.by_token, (int)blockIdx.x);
     if (w.count == 0) return;   // (the whole workgroup)
-    const int tid = (int)threadIdx.x, head = (int)blockIdx.y, page = 1 << p.b.page_shift, keys = w.first + w.count;
-    const uint8_t *codes = p.kc + (w.page * p.b.Hkv + head) * (int64_t)page * D + 16 * (tid % LPR);
-    float hi[16], lo[16];
+    const int lane = threadIdx.x & 63, page = 1 << p.b.page_shift, keys = w.first + w.count;
+    const int head = (int)blockIdx.y * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    if (head >= p.b.Hkv) return;
+    const uint8_t *codes = p.kc + (w.page * p.b.Hkv + head) * (int64_t)page * D;
+    // (e4m3 is exact in fp16: two channels a word)
+    const _Float16 inf = (_Float16)__builtin_inff();
+    f16x2 hi[8], lo[8];
 #pragma unroll
-    for (int c = 0; c < 16; ++c) hi[c] = -(float)(NONE * RANGE_UNIT), lo[c] = (float)(NONE * RANGE_UNIT);
-    for (int k = tid / LPR; k < keys; k += RPB) {
-        const u32x4 x = *reinterpret_cast<const u32x4 *>(codes + (int64_t)k * D);
+    for (int c = 0; c < 8; ++c) hi[c] = f16x2{-inf, -inf}, lo[c] = f16x2{inf, inf};
+    for (int k0 = lane / LPR; k0 - lane / LPR < keys; k0 += AT * KEYS) {
+        u32x4 x[AT];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)x[i], false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)x[i], true);
-            const float v[4] = {a[0], a[1], b[0], b[1]};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) hi[4 * i + e] = fmaxf(hi[4 * i + e], v[e]), lo[4 * i + e] = fminf(lo[4 * i + e], v[e]);   // (NaN: left out)
+        for (int a = 0; a < AT; ++a) {   // (beyond the last key: the last again)
+            const int k = k0 + a * KEYS;
+            x[a] = *reinterpret_cast<const u32x4 *>(codes + (k < keys ? k : keys - 1) * D + 16 * (lane % LPR));
         }
+#pragma unroll
+        for (int a = 0; a < AT; ++a)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const f16x2 u = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x[a][i], 1.0f, false));
+                const f16x2 v = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x[a][i], 1.0f, true));
+                hi[2 * i] = max2(hi[2 * i], u), lo[2 * i] = min2(lo[2 * i], u);
+                hi[2 * i + 1] = max2(hi[2 * i + 1], v), lo[2 * i + 1] = min2(lo[2 * i + 1], v);
+            }
     }
-    // in steps, two channels a word, over the lanes of a channel, then over the waves
-    i16x2 h2[8], l2[8];
+    // over the lanes of a channel, then in steps
+    uint32_t words[2][4] = {};   // of hi and lo, 4 channels each
 #pragma unroll
     for (int c = 0; c < 8; ++c) {
-        h2[c] = i16x2{(short)(int)__builtin_ceilf(hi[2 * c] * (1.0f / RANGE_UNIT)), (short)(int)__builtin_ceilf(hi[2 * c + 1] * (1.0f / RANGE_UNIT))};
-        l2[c] = i16x2{(short)(int)__builtin_floorf(lo[2 * c] * (1.0f / RANGE_UNIT)), (short)(int)__builtin_floorf(lo[2 * c + 1] * (1.0f / RANGE_UNIT))};
-    }
+        const f16x2 a = over_lanes<LPR>(hi[c], [](f16x2 u, f16x2 v) { return __builtin_elementwise_max(u, v); });
+        const f16x2 b = over_lanes<LPR>(lo[c], [](f16x2 u, f16x2 v) { return __builtin_elementwise_min(u, v); });
 #pragma unroll
-    for (int m = LPR; m < 64; m <<= 1)
-#pragma unroll
-        for (int c = 0; c < 8; ++c) {
-            h2[c] = max2(h2[c], __builtin_bit_cast(i16x2, __shfl_xor(__builtin_bit_cast(int, h2[c]), m, 64)));
-            l2[c] = min2(l2[c], __builtin_bit_cast(i16x2, __shfl_xor(__builtin_bit_cast(int, l2[c]), m, 64)));
+        for (int e = 0; e < 2; ++e) {   // (a channel with no number: 0)
+            const int up = a[e] < -(_Float16)1000 ? 0 : (int)__builtin_ceilf((float)a[e] * (1.0f / RANGE_UNIT));
+            const int down = b[e] > (_Float16)1000 ? 0 : (int)__builtin_floorf((float)b[e] * (1.0f / RANGE_UNIT));
+            words[0][c / 2] |= (uint32_t)(up & 255) << (16 * (c & 1) + 8 * e);
+            words[1][c / 2] |= (uint32_t)(down & 255) << (16 * (c & 1) + 8 * e);
         }
-    if ((tid & 63) < LPR) {
-#pragma unroll
-        for (int c = 0; c < 8; ++c) red[0][tid >> 6][8 * (tid % LPR) + c] = h2[c], red[1][tid >> 6][8 * (tid % LPR) + c] = l2[c];
     }
-    __syncthreads();
-    // 4 channels a thread: D/4 words of hi, then of lo
-    if (tid < D / 2) {
-        const bool is_lo = tid >= D / 4;
-        const int c2 = 2 * (tid % (D / 4));
-        uint32_t word = 0;
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            i16x2 v = red[is_lo][0][c2 + k];
-#pragma unroll
-            for (int wv = 1; wv < 4; ++wv) v = is_lo ? min2(v, red[1][wv][c2 + k]) : max2(v, red[0][wv][c2 + k]);
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int x = v[e] <= -NONE || v[e] >= NONE ? 0 : v[e];   // (a channel with no number)
-                word |= (uint32_t)(x & 255) << (16 * k + 8 * e);
-            }
-        }
-        reinterpret_cast<uint32_t *>(p.bounds + (w.page * p.b.Hkv + head) * (int64_t)(2 * D))[tid] = word;
+    // lanes 0 .. LPR - 1 hold all channels
+    if (lane < LPR) {
+        u32x4 *out = reinterpret_cast<u32x4 *>(p.bounds + (w.page * p.b.Hkv + head) * (int64_t)(2 * D));
+        out[lane] = u32x4{words[0][0], words[0][1], words[0][2], words[0][3]};
+        out[LPR + lane] = u32x4{words[1][0], words[1][1], words[1][2], words[1][3]};
     }
 }
 
@@ -160,25 +180,39 @@ __device__ __forceinline__ int places_of(const PagedBatch &b, int pos, int len)
     return n < b.width ? n : b.width;
 }
 
+// 8 channels of a tile's queries: chunk i of those of its tokens' groups.
+struct Chunk {
+    int tk, g, c;
+    u32x4 x;
+};
+
+template <int D>
+__device__ __forceinline__ Chunk load_chunk(const SelectParams &p, const TokenTile &t, int head, int i)
+{
+    const int G = p.Hq / p.b.Hkv, r = i / (D / 8), tk = r / G;
+    Chunk k = {tk, r - tk * G, i - r * (D / 8), {0, 0, 0, 0}};
+    if (tk < t.n) k.x = *reinterpret_cast<const u32x4 *>(p.q + (int64_t)(t.tok + tk) * p.q_st + (int64_t)(head * G + k.g) * p.q_sh + 8 * k.c);
+    return k;
+}
+
 // Largest bf16 magnitude (its bits) of each token's group among finite ones, into
-// amax[16] (LDS, zeroed).  The queries of groups of up to 16 heads stay in `raw`, by
-// the operand's rows.
+// amax[16] (LDS, zeroed); `mine` is the thread's first chunk.  The queries of groups
+// of up to 16 heads stay in `raw`, by the operand's rows.
 template <int D, int THREADS>
-__device__ __forceinline__ void group_amax(const SelectParams &p, const TokenTile &t, int head, uint32_t *amax, u32x4 (*raw)[D / 8])
+__device__ __forceinline__ void group_amax(const SelectParams &p, const TokenTile &t, int head, Chunk mine, uint32_t *amax, u32x4 (*raw)[D / 8])
 {
     const int G = p.Hq / p.b.Hkv;
     for (int i = (int)threadIdx.x; i < t.n * G * (D / 8); i += THREADS) {
-        const int r = i / (D / 8), c = i - r * (D / 8), tk = r / G, h = head * G + r - tk * G;
-        const u32x4 x = *reinterpret_cast<const u32x4 *>(p.q + (int64_t)(t.tok + tk) * p.q_st + (int64_t)h * p.q_sh + 8 * c);
+        if (i >= THREADS) mine = load_chunk<D>(p, t, head, i);
         uint32_t m = 0;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const uint32_t a = x[k] & 0x7FFFu, b = x[k] >> 16 & 0x7FFFu;
+            const uint32_t a = mine.x[k] & 0x7FFFu, b = mine.x[k] >> 16 & 0x7FFFu;
             m = finite16(a) && a > m ? a : m;
             m = finite16(b) && b > m ? b : m;
         }
-        atomicMax(&amax[tk], m);
-        if (G <= 16) raw[(tk << p.heads_shift) + r - tk * G][c] = x;
+        atomicMax(&amax[mine.tk], m);
+        if (G <= 16) raw[(mine.tk << p.heads_shift) + mine.g][mine.c] = mine.x;
     }
 }
 
@@ -215,30 +249,38 @@ __device__ __forceinline__ void build_rows(const SelectParams &p, const TokenTil
     }
 }
 
-// Products of the operand with the ranges of the pages in table entries pg (each of
-// the lane's place, lane % 16): its rows 4 (lane / 16) + e; and the pages' scales.
+// The ranges of the pages in table entries pg (each of the lane's place, lane % 16),
+// and their scales; and their products with the operand: its rows 4 (lane / 16) + e.
 template <int D, int AT>
-__device__ __forceinline__ void place_products(const SelectParams &p, const int *pg, int head, const u32x4 (*rows)[64], i32x4 *acc, float *ks)
-{
-    constexpr int KS = 2 * D / 64;
-    const int lane = threadIdx.x & 63;
-    i32x4 x[AT][KS];
+struct Ranges {
+    i32x4 x[AT][2 * D / 64];
+    float ks[AT];
+
+    __device__ __forceinline__ void load(const SelectParams &p, const int *pg, int head)
+    {
+        const int lane = threadIdx.x & 63;
 #pragma unroll
-    for (int j = 0; j < AT; ++j) {
-        const bool is = pg[j] >= 0 && pg[j] < p.b.pages;
-        const int64_t at = (int64_t)(is ? pg[j] : 0) * p.b.Hkv + head;
-        const int8_t *src = p.bounds + at * (2 * D) + (2 * D / 4) * (lane >> 4);
+        for (int j = 0; j < AT; ++j) {
+            const bool is = pg[j] >= 0 && pg[j] < p.b.pages;
+            const int64_t at = (int64_t)(is ? pg[j] : 0) * p.b.Hkv + head;
+            const int8_t *src = p.bounds + at * (2 * D) + (2 * D / 4) * (lane >> 4);
 #pragma unroll
-        for (int k = 0; k < KS; ++k) x[j][k] = *reinterpret_cast<const i32x4 *>(src + 16 * k);
-        ks[j] = p.ks[at];
+            for (int k = 0; k < 2 * D / 64; ++k) x[j][k] = *reinterpret_cast<const i32x4 *>(src + 16 * k);
+            ks[j] = p.ks[at];
+        }
     }
+
+    __device__ __forceinline__ void multiply(const u32x4 (*rows)[64], i32x4 *acc) const
+    {
+        const int lane = threadIdx.x & 63;
 #pragma unroll
-    for (int j = 0; j < AT; ++j) {
-        acc[j] = i32x4{0, 0, 0, 0};
+        for (int j = 0; j < AT; ++j) {
+            acc[j] = i32x4{0, 0, 0, 0};
 #pragma unroll
-        for (int k = 0; k < KS; ++k) acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, rows[k][lane]), x[j][k], acc[j], 0, 0, 0);
+            for (int k = 0; k < 2 * D / 64; ++k) acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, rows[k][lane]), x[j][k], acc[j], 0, 0, 0);
+        }
     }
-}
+};
 
 // The largest over each token's rows, in the lanes and elements of their first.
 __device__ __forceinline__ void row_max(i32x4 &x, int hs)
@@ -360,18 +402,17 @@ template <int R, class K>
 __device__ __forceinline__ void select_row(int many, int budget, int *out, K key)
 {
     const int lane = threadIdx.x & 63;
-    uint32_t k[R], low = ~0u, high = 0;
+    uint32_t k[R], low = 0, high = 0;   // (low: of the complements)
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        k[r] = 64 * r + lane < many ? key(64 * r + lane) : 0u;   // (0: below whatever counts)
-        if (64 * r + lane < many) low = k[r] < low ? k[r] : low, high = k[r] > high ? k[r] : high;
+        const bool is = 64 * r + lane < many;
+        k[r] = is ? key(64 * r + lane) : 0u;   // (0: below whatever counts)
+        high = k[r] > high ? k[r] : high;
+        low = is && ~k[r] > low ? ~k[r] : low;
     }
-#pragma unroll
-    for (int x = 1; x < 64; x <<= 1) {
-        const uint32_t a = __shfl_xor(low, x, 64), b = __shfl_xor(high, x, 64);
-        low = a < low ? a : low;
-        high = b > high ? b : high;
-    }
+    auto largest = [](uint32_t v) { return (uint32_t)lane_value((int)wave_scan_by(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; }), 63); };
+    high = largest(high);
+    low = ~largest(low);
     // keys that are at least x (>= 1)
     auto reach = [&](uint32_t x) {
         int n = 0;
@@ -380,9 +421,9 @@ __device__ __forceinline__ void select_row(int many, int budget, int *out, K key
         return n;
     };
     // (the bits that all have in common need no counting)
-    const uint32_t differ = (uint32_t)__builtin_amdgcn_readfirstlane((int)(low ^ high));
+    const uint32_t differ = low ^ high;
     const int top = differ ? 32 - __builtin_clz(differ) : 0;
-    uint32_t least = top == 32 ? 0 : (uint32_t)__builtin_amdgcn_readfirstlane((int)low) >> top << top;
+    uint32_t least = top == 32 ? 0 : low >> top << top;
     for (int bit = top - 1; bit >= 0; --bit) {
         const uint32_t x = least | 1u << bit;
         const int n = reach(x);
@@ -425,6 +466,7 @@ __global__ __launch_bounds__(SELECT_BY) void select_kernel(SelectParams p)
     if (most > p.budget) {
         const int *table = p.b.table + t.s * p.b.table_stride;
         constexpr int AT = D > 128 ? 2 : 4;        // blocks of 16 places of a wave at once
+        const Chunk mine = load_chunk<D>(p, t, head, tid);   // (first: loads come back in order)
         int pg[AT];
         auto look_up = [&](int q0) {
 #pragma unroll
@@ -434,9 +476,11 @@ __global__ __launch_bounds__(SELECT_BY) void select_kernel(SelectParams p)
             }
         };
         look_up(wave * 16 * AT);
+        Ranges<D, AT> ranges;
+        ranges.load(p, pg, head);   // (while the queries are made ready)
         if (tid < 16) amax[tid] = 0;
         __syncthreads();
-        group_amax<D, SELECT_BY>(p, t, head, amax, raw);
+        group_amax<D, SELECT_BY>(p, t, head, mine, amax, raw);
         __syncthreads();
         const int rounds = (G + 15) / 16;
         for (int round = 0; round < rounds; ++round) {
@@ -444,21 +488,23 @@ __global__ __launch_bounds__(SELECT_BY) void select_kernel(SelectParams p)
             build_rows<D, SELECT_BY>(p, t, head, round, amax, raw, rows);
             __syncthreads();
             for (int q0 = wave * 16 * AT; q0 < most; q0 += WAVES * 16 * AT) {
-                if (round || q0 >= WAVES * 16 * AT) look_up(q0);
+                if (round || q0 >= WAVES * 16 * AT) {
+                    look_up(q0);
+                    ranges.load(p, pg, head);
+                }
                 i32x4 x[AT];
-                float ks[AT];
-                place_products<D, AT>(p, pg, head, rows, x, ks);
+                ranges.multiply(rows, x);
 #pragma unroll
                 for (int j = 0; j < AT; ++j) {
                     const int place = q0 + 16 * j + (lane & 15);
                     row_max(x[j], hs);
                     if (place >= most) continue;
                     if (rounds == 1) {
-                        write_scores(p, x[j], pg[j], ks[j], t.n, [&](int tk, uint32_t k) { keys[tk * p.b.width + place] = k; });
+                        write_scores(p, x[j], pg[j], ranges.ks[j], t.n, [&](int tk, uint32_t k) { keys[tk * p.b.width + place] = k; });
                     } else if (lane < 16) {   // (one token a tile: its products' maximum over the rounds first)
                         const int old = round ? (int)keys[place] : x[j][0], now = x[j][0] > old ? x[j][0] : old;
                         keys[place] = (uint32_t)now;
-                        if (round == rounds - 1) write_scores(p, i32x4{now, 0, 0, 0}, pg[j], ks[j], 1, [&](int, uint32_t k) { keys[place] = k; });
+                        if (round == rounds - 1) write_scores(p, i32x4{now, 0, 0, 0}, pg[j], ranges.ks[j], 1, [&](int, uint32_t k) { keys[place] = k; });
                     }
                 }
             }
@@ -506,19 +552,20 @@ __global__ __launch_bounds__(256) void select_score_kernel(SelectParams p)
     const int *table = p.b.table + t.s * p.b.table_stride;
     if (tid < 16) amax[tid] = 0;
     __syncthreads();
-    group_amax<D, 256>(p, t, head, amax, raw);
+    group_amax<D, 256>(p, t, head, load_chunk<D>(p, t, head, tid), amax, raw);
     __syncthreads();
     const int rounds = (G + 15) / 16;
     constexpr int AT = D > 128 ? 2 : 4;            // blocks of 16 places of a wave at once
     for (int q0 = p0 + wave * 16 * AT; q0 - wave * 16 * AT < p1; q0 += 64 * AT) {
         int pg[AT];
         i32x4 best[AT];
-        float ks[AT];
 #pragma unroll
         for (int j = 0; j < AT; ++j) {
             const int place = q0 + 16 * j + (lane & 15);
             pg[j] = place < p1 ? table[place] : -1;
         }
+        Ranges<D, AT> ranges;
+        ranges.load(p, pg, head);
         for (int round = 0; round < rounds; ++round) {
             if (q0 < p0 + 64 * AT || rounds > 1) {
                 __syncthreads();
@@ -526,7 +573,7 @@ __global__ __launch_bounds__(256) void select_score_kernel(SelectParams p)
                 __syncthreads();
             }
             i32x4 x[AT];
-            place_products<D, AT>(p, pg, head, rows, x, ks);
+            ranges.multiply(rows, x);
 #pragma unroll
             for (int j = 0; j < AT; ++j)
 #pragma unroll
@@ -537,7 +584,7 @@ __global__ __launch_bounds__(256) void select_score_kernel(SelectParams p)
             const int place = q0 + 16 * j + (lane & 15);
             row_max(best[j], hs);
             if (place >= p1) continue;
-            write_scores(p, best[j], pg[j], ks[j], t.n, [&](int tk, uint32_t k) {
+            write_scores(p, best[j], pg[j], ranges.ks[j], t.n, [&](int tk, uint32_t k) {
                 p.scores[((int64_t)(t.tok + tk) * p.b.Hkv + head) * p.b.width + place] = k;
             });
         }
@@ -574,7 +621,7 @@ hipError_t launch_kv_bounds(int D, const BoundsParams &params, hipStream_t s)
     BoundsParams p = params;
     const int64_t slots = (int64_t)(p.b.T >> p.b.page_shift) + 2 * (int64_t)p.b.S;   // (as for kv_append)
     p.by_token = p.b.T <= slots;
-    const dim3 grid((unsigned)(p.by_token ? p.b.T : slots), (unsigned)p.b.Hkv);
+    const dim3 grid((unsigned)(p.by_token ? p.b.T : slots), (unsigned)((p.b.Hkv + 3) / 4));
     switch (D) {
     case 64: kv_bounds_kernel<64><<<grid, 256, 0, s>>>(p); break;
     case 128: kv_bounds_kernel<128><<<grid, 256, 0, s>>>(p); break;
@@ -592,7 +639,7 @@ struct SelectShape {
 
 // In one launch where a tile's scores fit half of a CU's LDS, and either workgroups
 // fill the device or none reads more than ALONE bytes of ranges.
-constexpr int64_t KEYS = 12288, ALONE = (int64_t)1 << 18;
+constexpr int64_t KEYS = 12288, ALONE = (int64_t)1 << 17;
 
 static SelectShape select_shape(int D, int64_t T, int64_t S, int G, int Hkv, int64_t width)
 {
