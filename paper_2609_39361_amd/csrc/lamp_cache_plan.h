@@ -128,7 +128,7 @@ __device__ __forceinline__ SeqPlan seq_plan(const SharedAttnParams &p, int v, in
     r.tiles = rows > above && rows <= upto ? (rows + F::ROWS - 1) / F::ROWS : 0;
     const int span = r.len > r.lo ? r.len - r.lo : 0;
     r.kt = (span + TILE - 1) / TILE;
-    r.mean = r.causal ? fmaxf(0.0f, fminf((float)r.kt, ((float)span - 0.5f * (float)r.n) * (1.0f / TILE))) : (float)r.kt;
+    r.mean = group ? 1.0f : 0.0f;                    // (what split_of counts here)
     return r;
 }
 
@@ -212,24 +212,28 @@ struct Share {
     int tiles, c, units, slots;   // row tiles, pieces of each, and theirs of all kv heads
 };
 
+constexpr float ANY = 1.02f, NEVER = 2.0f;   // (of Split.two)
+
 // How row tiles are cut: those of kt key tiles in kt / each pieces, rounded down,
-// but in `least` where that is above 1, and no shorter than `tiles`.
+// but in two where that is above `two`, and no shorter than `tiles`.
 struct Split {
-    float each;
-    int least, tiles;
+    float each, two;
+    int tiles;
 };
 
 template <class F, class P>
 __device__ __forceinline__ Share share_of(const P &p, const SeqPlan &r, Split split)
 {
     const float x = (float)r.kt * (1.0f / split.each) + 0.01f;   // (an even share stays one under the sums' rounding)
-    const int c = x > 1.02f && x < 2.0f ? split.least : (int)x, most = r.kt / split.tiles, fit = c < most ? c : most;
+    const float two = std::is_same_v<P, SharedAttnParams> && F::FORM == 1 && r.causal ? ANY : split.two;
+    const int c = x > two && x < 2.0f ? 2 : (int)x, most = r.kt / split.tiles, fit = c < most ? c : most;
     const int pieces = fit < 1 ? 1 : fit, units = r.tiles * p.b.Hkv * pieces;
     return {r.tiles, pieces, units, joined(p, r, pieces) ? units : 0};
 }
 
 // Sums over a form's row tiles (of one head): their number, the key tiles they
-// visit at most and on average; and the most that one visits.
+// visit at most and on average (of attn_shared, instead: the number of its groups'
+// row tiles); and the most that one visits.
 struct Work {
     float tiles, most, mean, longest;
 };
@@ -257,7 +261,21 @@ __device__ __forceinline__ Split split_of(const CacheAttnParams &p, const Work &
 {
     const int tiles = F::FORM == 1 && p.units[0] && !p.apart ? 8 : F::MIN_TILES;
     const float each = fmaxf(w.most * (float)p.b.Hkv * (1.0f / F::TARGET), (float)tiles);
-    return {each, F::FORM == 2 || (F::FORM && w.mean < EVEN * w.tiles * w.longest) ? 2 : 1, tiles};
+    return {each, F::FORM && w.mean < EVEN * w.tiles * w.longest ? ANY : NEVER, tiles};
+}
+
+// Of attn_shared: two of the workgroups of the form for prefixes share a CU, and are
+// cut as soon as they can.  The row tiles of prefixes in the form for many are cut in
+// two where all halves start at once or not even all whole ones do (questions of 100 to
+// 300 tokens about documents: 128 row tiles of 1.98 shares 339 us, uncut 477; 264 of 0.7
+// and 1.1: 227, uncut 289; but 232 of 1.0 and 1.1: 190, uncut 163; 168 of 1.45: 195 and
+// 166); those of sequences, which are fewer and shorter, always.
+template <class F>
+__device__ __forceinline__ Split split_of(const SharedAttnParams &p, const Work &w)
+{
+    const float each = fmaxf(w.most * (float)p.b.Hkv * (1.0f / F::TARGET), (float)F::MIN_TILES);
+    const float whole = w.mean * (float)p.b.Hkv * (1.0f / F::TARGET);
+    return {each, F::FORM == 2 || (F::FORM == 1 && (whole <= 0.5f || whole > 1.0f)) ? ANY : NEVER, F::MIN_TILES};
 }
 
 // Unit `local` of sequence s, whose partial outputs start at `slots`.  (Tables

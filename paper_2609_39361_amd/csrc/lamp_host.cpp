@@ -1130,6 +1130,8 @@ int lamp_kv_advance(const int32_t *lens, const int32_t *add, const int32_t *pref
         return fail(LAMP_ERR_UNSUPPORTED, "S above 2^20, T above 2^23 or width*page above 2^30");
     if (!ring || !state || !q_start || !state_out || (S > 0 && (!lens || !add || !kv_lens || (width > 0 && !table))) || (T > 0 && !positions))
         return fail(LAMP_ERR_INVALID_ARG, "null pointer among the step's arrays");
+    if (S > 1 && (table_stride < 0 ? -table_stride : table_stride) < width)
+        return fail(LAMP_ERR_INVALID_ARG, "rows of the table share memory (table_stride=%lld, width=%d)", (long long)table_stride, width);
     int ps = 4;
     while (1 << ps != page) ++ps;
     const lamp::AdvanceParams p = {lens, add, prefix_lens, table, table_stride, ring, state, kv_lens, q_start, positions, state_out,

@@ -209,7 +209,8 @@ def test_select(L, lens, Hq, H, d, page, budget, first, last):  # noqa: F811
     ([(195000, 1)], 2, 1, 64, 100),                                        # a row too long for one workgroup
     ([(150000, 1)] + [(30 + i, 1) for i in range(129)], 4, 2, 64, 60),     # LDS holds as many scores as it may
     ([(150000, 2)] + [(30 + i, 1) for i in range(29)], 2, 1, 128, 60),     # and not those of two tokens, of few workgroups
-    ([(40, 1)] * 3 + [(40000, 14)], 1, 1, 64, 33),                         # 14 tokens in one tile
+    ([(195000, 1)] + [(30 + i % 50, 1) for i in range(257)], 2, 1, 256, 60),
+    ([(40, 1)] * 3 + [(40000, 14)], 1, 1, 64, 33),                         # 14 tokens of a sequence
     ([(2500, 40), (900, 7)], 3, 3, 64, 20),
 ])
 def test_select_long(L, lens, Hq, H, d, budget):  # noqa: F811
@@ -422,6 +423,73 @@ def test_shared_both_forms_every_page(L, d, page):  # noqa: F811
 def test_shared_long(L):  # noqa: F811
     _run_shared(L, _shared_case([(8192, [(37 * i % 300, 1) for i in range(24)])], 8, 2, 128, 64, seed=70), 64)
     _run_shared(L, _shared_case([(6000, [(0, 200), (10, 150)])], 4, 1, 128, 16, seed=71), 16, scale=-0.1)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("page", [16, 32, 64])
+def test_shared_scales_values_far_apart_and_growing_logits(L, d, page):  # noqa: F811
+    """Logits of either sign and none; pages of values 2^140 apart and of scale 0; keys whose logits rise by hundreds along the
+    prefix; in the forms for prefixes and (1100 rows) for many rows."""
+    for groups in ([(320, [(10, 1), (0, 3), (70, 1)])], [(320, [(10, 250), (30, 25)])]):
+        case = _shared_case(groups, 4, 1, d, page, seed=80)
+        for scale in (-0.1, 0.0):
+            _run_shared(L, case, page, scale=scale)
+        q, parts, table, kv, starts, prefix, gs = case
+        for j in range(table.shape[1]):
+            for s in range(table.shape[0]):
+                if int(table[s, j]) >= 0:
+                    parts[3][int(table[s, j])] = [2.0 ** 70, 2.0 ** -70, 1.0, 0.0, 2.0 ** -100][j % 5]
+        _run_shared(L, case, page)
+        q, parts, table, kv, starts, prefix, gs = case = _shared_case(groups, 4, 1, d, page, seed=81)
+        for j in range(320 // page):
+            parts[2][int(table[0, j])] = 2.0 ** (-6 + 2 * ((j * page) // 64))
+        _run_shared(L, case, page)
+
+
+def test_shared_of_lengths_beyond_the_table_and_of_nothing(L):  # noqa: F811
+    """Rows that see keys beyond the table are NaN; no tokens, no sequences with tokens; a prefix as long as the table."""
+    q, parts, table, kv, starts, prefix, gs = _shared_case([(64, [(30, 2), (3, 1)])], 4, 2, 64, 16, seed=82)
+    c = _device_cache(L, parts)
+    args = (_i32(prefix), _i32(gs), _i32(starts))
+    o, lse = L.attn_shared(q.cuda(), c, table[:, :5].contiguous().cuda(), _i32(kv), *args)
+    assert torch.isnan(o[:2]).all() and torch.isnan(lse[:2]).all() and torch.isfinite(o[2:].float()).all()
+    o, lse = L.attn_shared(q.cuda()[:0], c, table.cuda(), _i32(kv), _i32(prefix), _i32(gs), _i32([0, 0, 0]))
+    assert o.shape[0] == 0
+    out = (torch.full((3, 4, 64), 7.0, dtype=torch.bfloat16, device="cuda"), torch.full((3, 4), 7.0, device="cuda"))
+    L.attn_shared(q.cuda(), c, table.cuda(), _i32(kv), _i32(prefix), _i32(gs), _i32([0, 0, 0]), out=out)
+    assert bool((out[0] == 7).all()) and bool((out[1] == 7).all())
+    none = table[:, :0].contiguous().cuda()
+    o, lse = L.attn_shared(q.cuda(), c, none, _i32(kv), *args)
+    assert torch.isnan(o).all()
+
+
+def test_pages_and_select_on_another_stream_while_the_first_is_busy(L):  # noqa: F811
+    """Calls on two streams with their own workspaces give what they give alone."""
+    cases = [_attn_case(L, [(900 + i, 1) for i in range(20)], 8, 2, 64, 16, seed=83 + k) for k in range(2)]
+    work = []
+    for q, parts, table, kv, starts in cases:
+        places = _lists(table, kv, starts, 2, 16, 30, 5).cuda()
+        cache = _device_cache(L, parts)
+        rng = torch.randint(-100, 100, (cache.k.shape[0], 2, 2, 64), generator=_gen(84)).sort(2, descending=True)[0].to(torch.int8).cuda()
+        work.append((q.cuda(), cache, table.cuda(), _i32(kv), places, rng.contiguous(), _i32([0, 20]), _i32([16] * 20), _i32(starts)))
+
+    def run(q, cache, table, kv, places, rng, gs, prefix, starts):
+        return (*L.attn_pages(q, cache, table, kv, places, starts), L.select_pages(q, cache, rng, table, kv, 20, starts),
+                *L.attn_pages(q[:1], cache, table[:1], kv[:1], places[:1].contiguous()))
+
+    alone = [run(*w) for w in work]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in work]
+    both = [[], []]
+    for _ in range(20):
+        for k, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                both[k].append(run(*work[k]))
+    torch.cuda.synchronize()
+    for k in range(2):
+        for got in both[k]:
+            for x, y in zip(got, alone[k]):
+                assert torch.equal(x, y)
 
 
 @pytest.mark.parametrize("n", [150, 700])

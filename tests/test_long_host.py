@@ -100,6 +100,7 @@ def test_advance_refusals():
         assert _advance(page=page) == UNSUPPORTED and "page" in _err()
     assert _advance(S=(1 << 20) + 1) == UNSUPPORTED and _advance(T=(1 << 23) + 1) == UNSUPPORTED
     assert _advance(width=(1 << 24) + 1) == UNSUPPORTED
+    assert _advance(stride=3) == INVALID and _advance(stride=0) == INVALID and "share" in _err()
 
 
 def test_workspace_sizes():
