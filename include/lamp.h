@@ -539,7 +539,8 @@ int lamp_kv_bounds(const lamp_cache *cache, const lamp_batch *batch, int8_t *bou
  * Nothing is written for tokens from q_start[S] on.
  *
  * workspace: lamp_select_pages_workspace_size(...) bytes, as for lamp_attn_cache.
- * budget up to 2^20, T*Hkv*width up to 2^32; other limits as for lamp_attn_cache.
+ * T up to 2^22, budget up to 2^20, T*Hkv*width up to 2^32; other limits as for
+ * lamp_attn_cache.
  */
 int lamp_select_pages(const uint16_t *q, int64_t q_token, int64_t q_head, int Hq, const lamp_cache *cache,
                       const lamp_batch *batch, const int8_t *bounds, int budget, int first, int last,
@@ -552,7 +553,7 @@ size_t lamp_select_pages_workspace_size(int T, int S, int Hq, int Hkv, int d, in
  * each place at most once; entries outside [0, width) and places behind the
  * token's position hold no keys.  Edges as for lamp_attn_cache: a row without keys
  * has o = 0 and lse = -infinity, one with a listed place without a page is NaN.
- * T*Hq*ceil(budget/1024) up to 2^24; other limits as for lamp_attn_cache.
+ * T*Hq*ceil(budget/1024) below 2^24; other limits as for lamp_attn_cache.
  */
 int lamp_attn_pages(const uint16_t *q, int64_t q_token, int64_t q_head, int Hq, const lamp_cache *cache,
                     const lamp_batch *batch, const int32_t *places, int budget, double scale, uint16_t *o, float *lse,

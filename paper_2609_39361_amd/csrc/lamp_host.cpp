@@ -1130,7 +1130,7 @@ int lamp_kv_advance(const int32_t *lens, const int32_t *add, const int32_t *pref
         return fail(LAMP_ERR_UNSUPPORTED, "S above 2^20, T above 2^23 or width*page above 2^30");
     if (!ring || !state || !q_start || !state_out || (S > 0 && (!lens || !add || !kv_lens || (width > 0 && !table))) || (T > 0 && !positions))
         return fail(LAMP_ERR_INVALID_ARG, "null pointer among the step's arrays");
-    if (S > 1 && (table_stride < 0 ? -table_stride : table_stride) < width)
+    if (S > 1 && table_stride < width && table_stride > -(int64_t)width)
         return fail(LAMP_ERR_INVALID_ARG, "rows of the table share memory (table_stride=%lld, width=%d)", (long long)table_stride, width);
     int ps = 4;
     while (1 << ps != page) ++ps;
@@ -1156,7 +1156,7 @@ int lamp_kv_bounds(const lamp_cache *cache, const lamp_batch *batch, int8_t *bou
 size_t lamp_select_pages_workspace_size(int T, int S, int Hq, int Hkv, int d, int width, int budget)
 {
     if (T <= 0 || S <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv || width <= 0 || budget <= 0 || (d != 64 && d != 128 && d != 256)) return 0;
-    if (T > 1 << 23 || (int64_t)S * Hkv > 1 << 20 || (int64_t)T * Hq > (int64_t)1 << 27 || (int64_t)T * Hkv * width > (int64_t)1 << 32) return 0;
+    if (T > 1 << 22 || (int64_t)S * Hkv > 1 << 20 || (int64_t)T * Hq > (int64_t)1 << 27 || (int64_t)T * Hkv * width > (int64_t)1 << 32) return 0;
     return lamp::select_workspace(d, T, S, Hq / Hkv, Hkv, width, budget);
 }
 
@@ -1170,9 +1170,9 @@ int lamp_select_pages(const uint16_t *q, int64_t q_token, int64_t q_head, int Hq
     if (Hq <= 0 || Hq % cache->Hkv) return fail(LAMP_ERR_INVALID_ARG, "Hq=%d is not a multiple of Hkv=%d", Hq, cache->Hkv);
     if (first < 0 || last < 0 || budget <= 0 || (int64_t)first + last > budget)
         return fail(LAMP_ERR_INVALID_ARG, "budget=%d must be positive and at least first=%d + last=%d", budget, first, last);
-    if ((int64_t)batch->T * Hq > (int64_t)1 << 27 || Hq > 65536 || budget > 1 << 20
+    if (batch->T > 1 << 22 || (int64_t)batch->T * Hq > (int64_t)1 << 27 || Hq > 65536 || budget > 1 << 20
         || (int64_t)batch->T * cache->Hkv * batch->width > (int64_t)1 << 32)
-        return fail(LAMP_ERR_UNSUPPORTED, "T*Hq above 2^27, Hq above 65536, budget above 2^20 or T*Hkv*width above 2^32");
+        return fail(LAMP_ERR_UNSUPPORTED, "T above 2^22, T*Hq above 2^27, Hq above 65536, budget above 2^20 or T*Hkv*width above 2^32");
     if (batch->S == 0 || batch->T == 0) return LAMP_OK;
     const int64_t qs[2] = {q_token, q_head}, sizes[2] = {batch->T, Hq};
     rc = check_rows("q", q, false, qs, sizes, 2);
@@ -1196,8 +1196,8 @@ int lamp_select_pages(const uint16_t *q, int64_t q_token, int64_t q_head, int Hq
     return LAMP_OK;
 }
 
-// (lists of more than 1024 entries are cut in any case)
-static bool too_many_lists(int64_t T, int64_t Hq, int64_t budget) { return T * Hq * ((budget + 1023) / 1024) > (int64_t)1 << 24; }
+// (lists of more than 1024 entries are cut in any case; a launch has less than 2^32 threads)
+static bool too_many_lists(int64_t T, int64_t Hq, int64_t budget) { return T * Hq * ((budget + 1023) / 1024) >= (int64_t)1 << 24; }
 
 size_t lamp_attn_pages_workspace_size(int T, int Hq, int Hkv, int d, int page, int budget)
 {
@@ -1215,7 +1215,7 @@ int lamp_attn_pages(const uint16_t *q, int64_t q_token, int64_t q_head, int Hq, 
     if (rc) return rc;
     if (budget <= 0) return fail(LAMP_ERR_INVALID_ARG, "budget=%d must be positive", budget);
     if (budget > 1 << 20 || too_many_lists(batch->T, Hq, budget))
-        return fail(LAMP_ERR_UNSUPPORTED, "budget above 2^20 or T*Hq*ceil(budget/1024) above 2^24");
+        return fail(LAMP_ERR_UNSUPPORTED, "budget above 2^20 or T*Hq*ceil(budget/1024) not below 2^24");
     if (batch->S == 0 || batch->T == 0) return LAMP_OK;
     if (!places) return fail(LAMP_ERR_INVALID_ARG, "null pointer: places");
     p.places = places;

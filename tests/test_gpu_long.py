@@ -446,6 +446,15 @@ def test_shared_scales_values_far_apart_and_growing_logits(L, d, page):  # noqa:
         _run_shared(L, case, page)
 
 
+def test_shared_of_fewer_keys_than_new_tokens(L):  # noqa: F811
+    """Tokens before position 0 see nothing: o = 0, lse = -infinity; in both forms."""
+    q, parts, table, kv, starts, prefix, gs = _shared_case([(0, [(3, 9)]), (32, [(0, 4), (2, 1)]), (0, [(0, 300)])], 4, 1, 64, 16, seed=85)
+    kv[0], kv[3] = 2, 150
+    got = _run_shared(L, (q, parts, table, kv, starts, prefix, gs), 16)
+    for rows in (slice(0, 7), slice(14, 164)):
+        assert not got[0][rows].any() and bool((got[1][rows] == -math.inf).all())
+
+
 def test_shared_of_lengths_beyond_the_table_and_of_nothing(L):  # noqa: F811
     """Rows that see keys beyond the table are NaN; no tokens, no sequences with tokens; a prefix as long as the table."""
     q, parts, table, kv, starts, prefix, gs = _shared_case([(64, [(30, 2), (3, 1)])], 4, 2, 64, 16, seed=82)

@@ -75,6 +75,7 @@ def test_bounds_and_select_refusals():
     for budget, first, last in ((0, 0, 0), (-1, 0, 0), (4, -1, 0), (4, 0, -1), (4, 3, 2), (2, 2 ** 31 - 1, 2 ** 31 - 1)):
         assert _select(budget=budget, first=first, last=last) == INVALID and "budget" in _err()
     assert _select(budget=(1 << 20) + 1) == UNSUPPORTED
+    assert _select(b=_batch(T=(1 << 22) + 1)) == UNSUPPORTED and "T above" in _err()
     assert _select(b=_batch(T=1 << 22, width=1 << 20)) == UNSUPPORTED and "T*Hkv*width" in _err()
     assert _select(b=_batch(width=5000), budget=4, ws=P(4096), n=8) == 6          # (too small a workspace)
     assert _select(b=_batch(width=5000), budget=4, ws=P(4100), n=1 << 20) == INVALID and "256" in _err()
@@ -85,6 +86,7 @@ def test_pages_and_shared_refusals():
     assert _pages(budget=0) == INVALID and _pages(budget=-3) == INVALID
     assert _pages(budget=(1 << 20) + 1) == UNSUPPORTED
     assert _pages(b=_batch(T=(1 << 12) + 1), budget=1 << 20) == UNSUPPORTED   # (2^24 + 4096)
+    assert _pages(b=_batch(T=1 << 12), budget=1 << 20) == UNSUPPORTED and _pages(b=_batch(T=1 << 22), budget=1) == UNSUPPORTED   # (2^24)
     assert _pages(budget=64, ws=P(4096), n=8) == 6
     assert _shared(prefix=0) == INVALID and _shared(start=0) == INVALID
     assert _shared(groups=0) == INVALID and _shared(groups=3) == INVALID and "groups" in _err()   # (of 2 sequences)
@@ -114,6 +116,7 @@ def test_workspace_sizes():
     assert size(2, 4, 3, 64, 16, 4) == 0 and size(1, 4, 2, 80, 16, 4) == 0 and size(1, 4, 2, 64, 24, 4) == 0
     assert size(1, 4, 2, 64, 16, 16) == 0 and size(1, 4, 2, 64, 16, 64) > 0   # (4 tiles of 64 keys a part at least)
     assert size(1, 4, 2, 64, 16, 5000) > 0 and size(1 << 24, 4, 2, 64, 16, 1) == 0
+    assert size((1 << 21) - 1, 4, 2, 64, 16, 1025) > 0 and size(1 << 21, 4, 2, 64, 16, 1025) == 0   # (2^24)
     size = lamp.attn_shared_workspace_size
     assert size(1, 1, 2, 4, 2, 64, 16, 4) == 0 and size(1, 1, 0, 4, 2, 64, 16, 4) == 0 and size(1, 1, 1, 4, 2, 64, 16, 4) > 0
     assert size(1 << 22, 1, 1, 4, 2, 64, 16, 4) == 0
