@@ -26,7 +26,7 @@ __global__ __launch_bounds__(256) void pages_join_kernel(PagesAttnParams p)
     const int64_t row = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), rows = (int64_t)p.b.T * p.Hq;
     if (row >= rows) return;
     const int t = (int)row / p.Hq, last = p.b.q_start ? p.b.q_start[p.b.S] : p.b.S, first = p.b.q_start ? p.b.q_start[0] : 0;
-    join_row<D>(p.part[0], p.part_ml[0], row, rows, p.pieces, 0, 0, 0, t < last && t >= first, p.o + row * D, p.lse + row);
+    join_row<D>(p.part[0], p.part_ml[0], (int)row, (int)rows, p.pieces, 0, 0, 0, t < last && t >= first, p.o + row * D, p.lse + row);
 }
 
 struct Cut {

@@ -35,11 +35,14 @@ struct FewRowsOf {     // single tokens and short chunks (lamp_cache_few.h): 8 w
     static constexpr int ROWS = 16, TARGET = 2048 / WAVES, MIN_TILES = WAVES, FORM = 0;
 };
 using FewRows = FewRowsOf<4>;
-struct ManyRows {      // prompts (lamp_cache_prompt.hip; 32 row tiles' window of 1024: 31 us with pieces of 5 tiles at least, 37 of 8)
+struct ManyRows {      // prompts (lamp_cache_many.h; 32 row tiles' window of 1024: 31 us with pieces of 5 tiles at least, 37 of 8)
     static constexpr int ROWS = 256, TARGET = 256, MIN_TILES = 5, FORM = 1;
 };
 
-struct PrefixRows {    // a group's rows over their shared prefix (lamp_cache_prefix.h): 8 waves fill a CU's registers
+// A group's rows over their shared prefix (lamp_cache_prefix.h).  Two workgroups fill a
+// CU's registers, but share its issue: units for one a CU (behind 8192 shared keys: 32
+// tokens 22 us, 64 tokens 30; for two 30 and 35).
+struct PrefixRows {
     static constexpr int ROWS = 32, TARGET = 256, MIN_TILES = 8, FORM = 2;
 };
 
@@ -212,7 +215,7 @@ struct Share {
     int tiles, c, units, slots;   // row tiles, pieces of each, and theirs of all kv heads
 };
 
-constexpr float ANY = 1.02f, NEVER = 2.0f;   // (of Split.two)
+constexpr float SOON = 1.02f, NEVER = 2.0f;   // (of Split.two)
 
 // How row tiles are cut: those of kt key tiles in kt / each pieces, rounded down,
 // but in two where that is above `two`, and no shorter than `tiles`.
@@ -225,7 +228,7 @@ template <class F, class P>
 __device__ __forceinline__ Share share_of(const P &p, const SeqPlan &r, Split split)
 {
     const float x = (float)r.kt * (1.0f / split.each) + 0.01f;   // (an even share stays one under the sums' rounding)
-    const float two = std::is_same_v<P, SharedAttnParams> && F::FORM == 1 && r.causal ? ANY : split.two;
+    const float two = std::is_same_v<P, SharedAttnParams> && F::FORM == 1 && r.causal ? SOON : split.two;
     const int c = x > two && x < 2.0f ? 2 : (int)x, most = r.kt / split.tiles, fit = c < most ? c : most;
     const int pieces = fit < 1 ? 1 : fit, units = r.tiles * p.b.Hkv * pieces;
     return {r.tiles, pieces, units, joined(p, r, pieces) ? units : 0};
@@ -261,7 +264,7 @@ __device__ __forceinline__ Split split_of(const CacheAttnParams &p, const Work &
 {
     const int tiles = F::FORM == 1 && p.units[0] && !p.apart ? 8 : F::MIN_TILES;
     const float each = fmaxf(w.most * (float)p.b.Hkv * (1.0f / F::TARGET), (float)tiles);
-    return {each, F::FORM && w.mean < EVEN * w.tiles * w.longest ? ANY : NEVER, tiles};
+    return {each, F::FORM && w.mean < EVEN * w.tiles * w.longest ? SOON : NEVER, tiles};
 }
 
 // Of attn_shared: two of the workgroups of the form for prefixes share a CU, and are
@@ -275,7 +278,7 @@ __device__ __forceinline__ Split split_of(const SharedAttnParams &p, const Work 
 {
     const float each = fmaxf(w.most * (float)p.b.Hkv * (1.0f / F::TARGET), (float)F::MIN_TILES);
     const float whole = w.mean * (float)p.b.Hkv * (1.0f / F::TARGET);
-    return {each, F::FORM == 2 || (F::FORM == 1 && (whole <= 0.5f || whole > 1.0f)) ? ANY : NEVER, F::MIN_TILES};
+    return {each, F::FORM == 2 || (F::FORM == 1 && (whole <= 0.5f || whole > 1.0f)) ? SOON : NEVER, F::MIN_TILES};
 }
 
 // Unit `local` of sequence s, whose partial outputs start at `slots`.  (Tables
@@ -561,54 +564,68 @@ __device__ __forceinline__ void mark_nan(uint32_t (*marks)[D / 32], uint32_t nan
     }
 }
 
+// Over all lanes of the wave, in all of them.
+template <class OP>
+__device__ __forceinline__ float wave_all(float v, OP op)
+{
+    auto step = [&](auto ctrl) {
+        const int x = __builtin_bit_cast(int, v);
+        v = op(v, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(x, x, decltype(ctrl)::value, 0xf, 0xf, false)));
+    };
+    step(std::integral_constant<int, 0xB1>{});    // quad_perm 1,0,3,2
+    step(std::integral_constant<int, 0x4E>{});    // quad_perm 2,3,0,1
+    step(std::integral_constant<int, 0x141>{});   // row_half_mirror
+    step(std::integral_constant<int, 0x140>{});   // row_mirror
+    const auto a = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+    v = op(__builtin_bit_cast(float, (uint32_t)a[0]), __builtin_bit_cast(float, (uint32_t)a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+    return op(__builtin_bit_cast(float, (uint32_t)b[0]), __builtin_bit_cast(float, (uint32_t)b[1]));
+}
+
 // A row's partial outputs joined by a wave and written (attn_shared, attn_pages):
 // n0 of them from row at0 of `part` on, step0 rows apart, then n1 from at1.  A lane
 // holds D/64 channels, and for each 64 partial outputs the maximum and sum of one.
-// Bound by latency: 16 rows are requested at once.  Not written where not `live`.
+// Bound by latency: 16 rows are requested at once, the first before the maxima are
+// waited for (16 partial outputs of 32 rows 3.6 us; with the loads one after another
+// 7.2).  Not written where not `live`.
 template <int D>
-__device__ __forceinline__ void join_row(const float *part, const float *ml, int64_t at0, int64_t step0, int n0, int64_t at1,
-                                         int64_t step1, int n1, bool live, uint16_t *o, float *lse)
+__device__ __forceinline__ void join_row(const float *part, const float *ml, int at0, int step0, int n0, int at1, int step1, int n1, bool live,
+                                         uint16_t *o, float *lse)
 {
     constexpr int C = D / 64, AT = 16;
     const int lane = threadIdx.x & 63, n = n0 + n1;
     auto row_of = [&](int k) { return k < n0 ? at0 + k * step0 : at1 + (k - n0) * step1; };
-    float m = NEG_INF, sum = 0.0f, v[C] = {};
+    float m = NEG_INF, sum = 0.0f, v[C] = {}, x[AT][C];
+    auto request = [&](int k0) {
+#pragma unroll
+        for (int j = 0; j < AT; ++j) {   // (beyond the last: read again, not added)
+            const float *r = part + (int64_t)row_of(k0 + j < n ? k0 + j : k0) * D + C * lane;
+#pragma unroll
+            for (int e = 0; e < C; ++e) x[j][e] = r[e];
+        }
+    };
+    request(0);
     for (int c0 = 0; c0 < n; c0 += 64) {
-        const int mine = c0 + lane, here = n - c0 < 64 ? n - c0 : 64;
-        const int64_t at = row_of(mine < n ? mine : c0) * 2;
-        const float mc = mine < n ? ml[at] : NEG_INF, lc = ml[at + 1];
-        float x[AT][C];
-        auto request = [&](int k0) {
-#pragma unroll
-            for (int j = 0; j < AT; ++j) {   // (beyond the last: read again, not added)
-                const float *r = part + row_of(c0 + (k0 + j < here ? k0 + j : k0)) * D + C * lane;
-#pragma unroll
-                for (int e = 0; e < C; ++e) x[j][e] = r[e];
-            }
-        };
-        request(0);   // (before the maxima are waited for)
-        float mn = mc;
-#pragma unroll
-        for (int k = 1; k < 64; k <<= 1) mn = fmaxf(mn, __shfl_xor(mn, k, 64));
-        mn = fmaxf(mn, m);
+        const int mine = c0 + lane;
+        const int64_t at = (int64_t)row_of(mine < n ? mine : c0) * 2;
+        const float m_at = ml[at], l_at = ml[at + 1], mc = mine < n ? m_at : NEG_INF;
+        const float mn = fmaxf(wave_all(mc, [](float a, float b) { return fmaxf(a, b); }), m);
         const float ms = mn == NEG_INF ? 0.0f : mn, f0 = __builtin_amdgcn_exp2f(m - ms);
         const float f = __builtin_amdgcn_exp2f(mc - ms);
-        float l = mine < n ? lc * f : 0.0f;
-#pragma unroll
-        for (int k = 1; k < 64; k <<= 1) l += __shfl_xor(l, k, 64);
         m = mn;
-        sum = sum * f0 + l;
+        sum = sum * f0 + wave_all(mine < n ? l_at * f : 0.0f, [](float a, float b) { return a + b; });
 #pragma unroll
         for (int e = 0; e < C; ++e) v[e] *= f0;
-        for (int k0 = 0; k0 < here; k0 += AT) {
-            if (k0) request(k0);
+        const int end = n - c0 < 64 ? n : c0 + 64;
+        for (int k0 = c0; k0 < end; k0 += AT) {
 #pragma unroll
             for (int j = 0; j < AT; ++j) {
-                if (k0 + j >= here) break;
-                const float fj = __builtin_bit_cast(float, lane_value(__builtin_bit_cast(int, f), k0 + j));
+                const bool is = k0 + j < end;   // (no branch: loads would wait in it, one after another)
+                const float fj = __builtin_bit_cast(float, lane_value(__builtin_bit_cast(int, f), k0 + j - c0));
 #pragma unroll
-                for (int e = 0; e < C; ++e) v[e] += x[j][e] * fj;
+                for (int e = 0; e < C; ++e) v[e] += is ? x[j][e] * fj : 0.0f;
             }
+            if (k0 + AT < n) request(k0 + AT);
         }
     }
     if (!live) return;
@@ -624,8 +641,8 @@ __device__ __forceinline__ void join_row(const float *part, const float *ml, int
 
 // The same by 16 lanes, for rows of few partial outputs (their weights in each lane).
 template <int D>
-__device__ __forceinline__ void join_row16(const float *part, const float *ml, int64_t at0, int64_t step0, int n0, int64_t at1,
-                                           int64_t step1, int n1, uint16_t *o, float *lse)
+__device__ __forceinline__ void join_row16(const float *part, const float *ml, int at0, int step0, int n0, int at1, int step1, int n1,
+                                           uint16_t *o, float *lse)
 {
     constexpr int C = D / 16, AT = 2;
     const int lane = threadIdx.x & 15, n = n0 + n1;
@@ -636,7 +653,7 @@ __device__ __forceinline__ void join_row16(const float *part, const float *ml, i
         f32x4 x[AT][C / 4];
 #pragma unroll
         for (int k = 0; k < AT; ++k) {   // (beyond the last: read again, not added)
-            const int64_t at = row_of(c0 + k < n ? c0 + k : c0);
+            const int64_t at = row_of(c0 + k < n ? c0 + k : c0);   // (below 2^31 partial outputs)
             mc[k] = ml[at * 2];
             lc[k] = ml[at * 2 + 1];
 #pragma unroll
@@ -652,11 +669,11 @@ __device__ __forceinline__ void join_row16(const float *part, const float *ml, i
         for (int e = 0; e < C; ++e) v[e] *= f0;
 #pragma unroll
         for (int k = 0; k < AT; ++k) {
-            if (c0 + k >= n) break;
+            const bool is = c0 + k < n;
             const float f = __builtin_amdgcn_exp2f(mc[k] - ms);
-            sum += lc[k] * f;
+            sum += is ? lc[k] * f : 0.0f;
 #pragma unroll
-            for (int e = 0; e < C; ++e) v[e] += x[k][e / 4][e % 4] * f;
+            for (int e = 0; e < C; ++e) v[e] += is ? x[k][e / 4][e % 4] * f : 0.0f;
         }
     }
     const float inv = finish(m, sum);

@@ -146,7 +146,7 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedAttnParams p)
 // 18 us in the first form and 22 in that for few rows, 8 tokens 20 and 28, 250 tokens
 // (1000 rows) 78 and 87 in that for many, 1000 tokens 274 and 254.
 constexpr int GROUP_PREFIX = 1024, SHARED_FEW = 64;
-constexpr int64_t JOIN_WIDE = 1024;   // rows up to which a wave joins each (512 rows 21.6 us a call, by 16 lanes 22.5; 8192 rows 77.0 and 75.3)
+constexpr int64_t JOIN_WIDE = 4096;   // rows up to which a wave joins each (a call with 2048 rows 36.6 us, by 16 lanes 37.2; with 8000 rows 107 and 103)
 
 struct SharedBounds {
     int above[3], upto[3], group_above[3], group_upto[3], units[3], slots[3];
