@@ -12,7 +12,9 @@
 // positions of all of them are then spread over the threads, each of which searches
 // the places in LDS for its sequence (one may have thousands, most have none).
 // Positions of many tokens are written by a second launch.  Bound by the latencies
-// of the loads, the sums and the ring's entries, one after another.
+// of the loads, the sums, the searches and the ring's entries, one after another (32
+// sequences 5.6 us, of which a launch is 3.7; 4096 whose step takes 4200 pages and
+// gives 12700 back 14.4 with the positions' launch).
 #include <hip/hip_runtime.h>
 
 #include "lamp_cache_plan.h"
@@ -63,21 +65,30 @@ __device__ __forceinline__ uint32_t wave_sums(uint32_t v)
     return wave_scan_by(v, [](uint32_t a, uint32_t b) { return sum(a, b); });
 }
 
-// Where a sequence's taken entries, those that go back and its positions begin among
-// all, and where in its row and from which position on.
+// Where the sequences' taken entries, those that go back and their positions begin
+// among all, and where in their rows and from which position on.
+template <int N>
 struct SeqPlaces {
-    int at[3], from[3];
+    int at[3][N], from[3][N];
 };
 
-// Last i < n with at[i].at[which] <= x (those of the first are; non-decreasing).
-template <int N>
-__device__ __forceinline__ int owner(const SeqPlaces *at, int which, int n, int x)
+// Last i with at[i] <= x for each x (those of the first are, those behind the last
+// sequence are not; non-decreasing): without branches, as the reads of one search wait
+// for each other.
+template <int N, int AT>
+__device__ __forceinline__ void owners(const int *at, const int (&x)[AT], int (&i)[AT])
 {
-    int lo = 0;
 #pragma unroll
-    for (int half = N / 2; half; half >>= 1)
-        if (lo + half < n && at[lo + half].at[which] <= x) lo += half;
-    return lo;
+    for (int k = 0; k < AT; ++k) i[k] = 0;
+#pragma unroll
+    for (int half = N / 2; half; half >>= 1) {
+        int y[AT];
+#pragma unroll
+        for (int k = 0; k < AT; ++k) y[k] = at[i[k] + half];
+        __builtin_amdgcn_sched_barrier(0);   // (the compiler would take one search after another)
+#pragma unroll
+        for (int k = 0; k < AT; ++k) i[k] += y[k] <= x[k] ? half : 0;
+    }
 }
 
 template <int EACH>
@@ -85,7 +96,8 @@ __global__ __launch_bounds__(ADVANCE_BY) void advance_kernel(AdvanceParams p)
 {
     __shared__ uint32_t sums[3][ADVANCE_WAVES];
     __shared__ int beyond_any[ADVANCE_WAVES];
-    __shared__ SeqPlaces at_seq[EACH * ADVANCE_BY];   // of a round's sequences
+    constexpr int N = EACH * ADVANCE_BY;
+    __shared__ SeqPlaces<N> places;   // of a round's sequences
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int pages = p.pages, last = p.S - 1;
     const int first = p.state[0], free = p.state[1];
@@ -164,7 +176,9 @@ __global__ __launch_bounds__(ADVANCE_BY) void advance_kernel(AdvanceParams p)
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
             const int s = sequence(round, i);
-            at_seq[tid * EACH + i] = {{at[0], at[1], at[2]}, {r[i].held, r[i].kept, r[i].len}};
+            const int place = tid * EACH + i, begin[3] = {r[i].held, r[i].kept, r[i].len};
+#pragma unroll
+            for (int k = 0; k < 3; ++k) places.at[k][place] = at[k], places.from[k][place] = begin[k];
             if (s <= last) {
                 p.kv_lens[s] = r[i].gone ? 0 : r[i].said + (ok ? r[i].add : 0);
                 p.q_start[s] = at[2];
@@ -175,38 +189,44 @@ __global__ __launch_bounds__(ADVANCE_BY) void advance_kernel(AdvanceParams p)
             at[2] += ok ? r[i].add : 0;
         }
         __syncthreads();
-        const int s0 = round * EACH * ADVANCE_BY, n = p.S - s0 < EACH * ADVANCE_BY ? p.S - s0 : EACH * ADVANCE_BY;
-        auto entry = [&](int which, int i) {
-            const int l = owner<EACH * ADVANCE_BY>(at_seq, which, n, i);
-            return p.table + (int64_t)(s0 + l) * p.table_stride + at_seq[l].from[which] + (i - at_seq[l].at[which]);
-        };
-        // (AT entries of a thread at once: their searches and loads do not wait for each other)
-        constexpr int AT = 4;
-        for (int i0 = from[0] + tid; i0 < need0; i0 += AT * ADVANCE_BY) {
-            int *to[AT], page[AT];
+        // (AT entries of a thread at once, whose searches and loads do not wait for each other: 4096
+        // sequences one token each 8.7 us, one by one 9.3; 1000, which have few, 9.3, four at once 10.4)
+        const int s0 = round * N;
+        constexpr int AT = EACH;
+        auto each = [&](int which, int end, auto work) {
+            for (int i0 = from[which] + tid; i0 < end; i0 += AT * ADVANCE_BY) {
+                int x[AT], of[AT];
 #pragma unroll
-            for (int k = 0; k < AT; ++k) {
-                const int i = i0 + k * ADVANCE_BY < need0 ? i0 + k * ADVANCE_BY : i0;
-                page[k] = p.ring[in_ring(i)];
-                to[k] = entry(0, i);
+                for (int k = 0; k < AT; ++k) x[k] = i0 + k * ADVANCE_BY < end ? i0 + k * ADVANCE_BY : i0;   // (beyond the last: the first again, with the same outcome)
+                owners<N>(places.at[which], x, of);
+                work(x, of);
             }
-#pragma unroll
-            for (int k = 0; k < AT; ++k)
-                if (i0 + k * ADVANCE_BY < need0) *to[k] = page[k];
-        }
-        for (int i0 = from[1] + tid; i0 < back0; i0 += AT * ADVANCE_BY) {
+        };
+        auto entry = [&](int which, int x, int l) {
+            return p.table + (int64_t)(s0 + l) * p.table_stride + places.from[which][l] + (x - places.at[which][l]);
+        };
+        each(0, need0, [&](const int (&x)[AT], const int (&of)[AT]) {
             int page[AT];
 #pragma unroll
-            for (int k = 0; k < AT; ++k) page[k] = *entry(1, i0 + k * ADVANCE_BY < back0 ? i0 + k * ADVANCE_BY : i0);
+            for (int k = 0; k < AT; ++k) page[k] = p.ring[in_ring(x[k])];
 #pragma unroll
             for (int k = 0; k < AT; ++k)
-                if (i0 + k * ADVANCE_BY < back0) p.ring[in_ring((int64_t)count + i0 + k * ADVANCE_BY)] = page[k];
-        }
+                *entry(0, x[k], of[k]) = page[k];
+        });
+        each(1, back0, [&](const int (&x)[AT], const int (&of)[AT]) {
+            int page[AT];
+#pragma unroll
+            for (int k = 0; k < AT; ++k) page[k] = *entry(1, x[k], of[k]);
+#pragma unroll
+            for (int k = 0; k < AT; ++k)
+                p.ring[in_ring((int64_t)count + x[k])] = page[k];
+        });
         if (p.T <= WITHIN)
-            for (int i = from[2] + tid; i < add0; i += ADVANCE_BY) {
-                const int l = owner<EACH * ADVANCE_BY>(at_seq, 2, n, i);
-                p.positions[i] = at_seq[l].from[2] + (i - at_seq[l].at[2]);
-            }
+            each(2, add0, [&](const int (&x)[AT], const int (&of)[AT]) {
+#pragma unroll
+                for (int k = 0; k < AT; ++k)
+                    p.positions[x[k]] = places.from[2][of[k]] + (x[k] - places.at[2][of[k]]);
+            });
     }
     if (p.T <= WITHIN)
         for (int i = add0 + tid; i < p.T; i += ADVANCE_BY) p.positions[i] = 0;

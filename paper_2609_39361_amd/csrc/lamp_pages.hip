@@ -191,36 +191,38 @@ __device__ __forceinline__ Chunk load_chunk(const SelectParams &p, const TokenTi
 {
     const int G = p.Hq / p.b.Hkv, r = i / (D / 8), tk = r / G;
     Chunk k = {tk, r - tk * G, i - r * (D / 8), {0, 0, 0, 0}};
-    if (tk < t.n) k.x = *reinterpret_cast<const u32x4 *>(p.q + (int64_t)(t.tok + tk) * p.q_st + (int64_t)(head * G + k.g) * p.q_sh + 8 * k.c);
+    const int there = tk < t.n ? tk : 0;   // (tokens behind the last: whatever, loaded without a branch that would wait)
+    k.x = *reinterpret_cast<const u32x4 *>(p.q + (int64_t)(t.tok + there) * p.q_st + (int64_t)(head * G + k.g) * p.q_sh + 8 * k.c);
     return k;
 }
 
 // Largest bf16 magnitude (its bits) of each token's group among finite ones, into
-// amax[16] (LDS, zeroed); `mine` is the thread's first chunk.  The queries of groups
-// of up to 16 heads stay in `raw`, by the operand's rows.
-template <int D, int THREADS>
-__device__ __forceinline__ void group_amax(const SelectParams &p, const TokenTile &t, int head, Chunk mine, uint32_t *amax, u32x4 (*raw)[D / 8])
+// amax[16] (LDS, zeroed); `mine` is the thread's first chunk.  RAW (groups of up to 16
+// heads): the queries stay in `raw`, by the operand's rows.
+template <int D, int THREADS, bool RAW>
+__device__ __forceinline__ void group_amax(const SelectParams &p, const TokenTile &t, int head, const Chunk &mine, uint32_t *amax, u32x4 (*raw)[D / 8])
 {
-    const int G = p.Hq / p.b.Hkv;
-    for (int i = (int)threadIdx.x; i < t.n * G * (D / 8); i += THREADS) {
-        if (i >= THREADS) mine = load_chunk<D>(p, t, head, i);
+    const int G = p.Hq / p.b.Hkv, many = t.n * G * (D / 8);
+    auto take = [&](const Chunk &c) {
         uint32_t m = 0;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const uint32_t a = mine.x[k] & 0x7FFFu, b = mine.x[k] >> 16 & 0x7FFFu;
+            const uint32_t a = c.x[k] & 0x7FFFu, b = c.x[k] >> 16 & 0x7FFFu;
             m = finite16(a) && a > m ? a : m;
             m = finite16(b) && b > m ? b : m;
         }
-        atomicMax(&amax[mine.tk], m);
-        if (G <= 16) raw[(mine.tk << p.heads_shift) + mine.g][mine.c] = mine.x;
-    }
+        atomicMax(&amax[c.tk], m);
+        if (RAW) raw[(c.tk << p.heads_shift) + c.g][c.c] = c.x;
+    };
+    if ((int)threadIdx.x < many) take(mine);   // (not in the loop, whose loads would be waited for with all that are on the way)
+    for (int i = (int)threadIdx.x + THREADS; i < many; i += THREADS) take(load_chunk<D>(p, t, head, i));
 }
 
 // The int8 operand [max(q', 0) | min(q', 0)] of 16 rows: of lane l in step k the row
 // l % 16 and its bytes (2 D/4) (l / 16) + 16 k.  Row (t << HS) + g is head 16 round + g
 // of token t's group (HS = heads_shift; rows without a head repeat the first, those
 // without a token are 0).
-template <int D, int THREADS>
+template <int D, int THREADS, bool RAW>
 __device__ __forceinline__ void build_rows(const SelectParams &p, const TokenTile &t, int head, int round, const uint32_t *amax,
                                            const u32x4 (*raw)[D / 8], u32x4 (*rows)[64])
 {
@@ -232,9 +234,7 @@ __device__ __forceinline__ void build_rows(const SelectParams &p, const TokenTil
         if (tk < t.n) {
             const int gg = g < G ? g : 0;
             const uint16_t *src = p.q + (int64_t)(t.tok + tk) * p.q_st + (int64_t)(head * G + gg) * p.q_sh + at % D;
-            const u32x4 *here = &raw[(tk << hs) + (gg & 15)][at % D / 8];
-            const u32x4 a = G <= 16 ? here[0] : reinterpret_cast<const u32x4 *>(src)[0];
-            const u32x4 b = G <= 16 ? here[1] : reinterpret_cast<const u32x4 *>(src)[1];
+            const u32x4 *from = RAW ? &raw[(tk << hs) + gg][at % D / 8] : reinterpret_cast<const u32x4 *>(src), a = from[0], b = from[1];
             const float inv = __builtin_bit_cast(float, (uint32_t)(127 - step_exponent(amax[tk])) << 23);
             const bool neg = at >= D;
 #pragma unroll
@@ -448,7 +448,7 @@ __device__ __forceinline__ void select_row(int many, int budget, int *out, K key
 // A tile's tokens and one kv head, scores in LDS.
 constexpr int SELECT_BY = 512;
 
-template <int D>
+template <int D, bool RAW>
 __global__ __launch_bounds__(SELECT_BY) void select_kernel(SelectParams p)
 {
     constexpr int WAVES = SELECT_BY / 64;
@@ -472,7 +472,8 @@ __global__ __launch_bounds__(SELECT_BY) void select_kernel(SelectParams p)
 #pragma unroll
             for (int j = 0; j < AT; ++j) {
                 const int place = q0 + 16 * j + (lane & 15);
-                pg[j] = place < most ? table[place] : -1;
+                const int entry = table[place < most ? place : most - 1];
+                pg[j] = place < most ? entry : -1;
             }
         };
         look_up(wave * 16 * AT);
@@ -480,12 +481,12 @@ __global__ __launch_bounds__(SELECT_BY) void select_kernel(SelectParams p)
         ranges.load(p, pg, head);   // (while the queries are made ready)
         if (tid < 16) amax[tid] = 0;
         __syncthreads();
-        group_amax<D, SELECT_BY>(p, t, head, mine, amax, raw);
+        group_amax<D, SELECT_BY, RAW>(p, t, head, mine, amax, raw);
         __syncthreads();
         const int rounds = (G + 15) / 16;
         for (int round = 0; round < rounds; ++round) {
             if (round) __syncthreads();
-            build_rows<D, SELECT_BY>(p, t, head, round, amax, raw, rows);
+            build_rows<D, SELECT_BY, RAW>(p, t, head, round, amax, raw, rows);
             __syncthreads();
             for (int q0 = wave * 16 * AT; q0 < most; q0 += WAVES * 16 * AT) {
                 if (round || q0 >= WAVES * 16 * AT) {
@@ -537,7 +538,7 @@ __global__ __launch_bounds__(SELECT_BY) void select_kernel(SelectParams p)
 
 // Where the scores of a tile's tokens do not fit LDS, or one tile's workgroup would
 // have too long a row to itself: scores over `chunk` places to memory, ...
-template <int D>
+template <int D, bool RAW>
 __global__ __launch_bounds__(256) void select_score_kernel(SelectParams p)
 {
     __shared__ u32x4 rows[2 * D / 64][64], raw[16][D / 8];
@@ -552,7 +553,7 @@ __global__ __launch_bounds__(256) void select_score_kernel(SelectParams p)
     const int *table = p.b.table + t.s * p.b.table_stride;
     if (tid < 16) amax[tid] = 0;
     __syncthreads();
-    group_amax<D, 256>(p, t, head, load_chunk<D>(p, t, head, tid), amax, raw);
+    group_amax<D, 256, RAW>(p, t, head, load_chunk<D>(p, t, head, tid), amax, raw);
     __syncthreads();
     const int rounds = (G + 15) / 16;
     constexpr int AT = D > 128 ? 2 : 4;            // blocks of 16 places of a wave at once
@@ -562,14 +563,15 @@ __global__ __launch_bounds__(256) void select_score_kernel(SelectParams p)
 #pragma unroll
         for (int j = 0; j < AT; ++j) {
             const int place = q0 + 16 * j + (lane & 15);
-            pg[j] = place < p1 ? table[place] : -1;
+            const int entry = table[place < p1 ? place : p1 - 1];
+            pg[j] = place < p1 ? entry : -1;
         }
         Ranges<D, AT> ranges;
         ranges.load(p, pg, head);
         for (int round = 0; round < rounds; ++round) {
             if (q0 < p0 + 64 * AT || rounds > 1) {
                 __syncthreads();
-                build_rows<D, 256>(p, t, head, round, amax, raw, rows);
+                build_rows<D, 256, RAW>(p, t, head, round, amax, raw, rows);
                 __syncthreads();
             }
             i32x4 x[AT];
@@ -661,15 +663,15 @@ size_t select_workspace(int D, int64_t T, int64_t S, int G, int Hkv, int64_t wid
     return width <= budget || select_shape(D, T, S, G, Hkv, width).one ? 0 : (size_t)T * Hkv * width * sizeof(uint32_t);
 }
 
-template <int D>
+template <int D, bool RAW>
 static hipError_t launch_select_of(const SelectParams &p, const SelectShape &x, hipStream_t s)
 {
     if (x.one || p.b.width <= p.budget) {
         const size_t keys = p.b.width <= p.budget ? 0 : (size_t)x.tokens * p.b.width * sizeof(uint32_t);
-        select_kernel<D><<<dim3((unsigned)x.tiles, (unsigned)p.b.Hkv), SELECT_BY, keys, s>>>(p);
+        select_kernel<D, RAW><<<dim3((unsigned)x.tiles, (unsigned)p.b.Hkv), SELECT_BY, keys, s>>>(p);
         return hipGetLastError();
     }
-    select_score_kernel<D><<<dim3((unsigned)x.tiles, (unsigned)p.b.Hkv, (unsigned)((p.b.width + p.chunk - 1) / p.chunk)), 256, 0, s>>>(p);
+    select_score_kernel<D, RAW><<<dim3((unsigned)x.tiles, (unsigned)p.b.Hkv, (unsigned)((p.b.width + p.chunk - 1) / p.chunk)), 256, 0, s>>>(p);
     select_top_kernel<<<dim3((unsigned)p.b.T, (unsigned)p.b.Hkv), 256, 0, s>>>(p);
     return hipGetLastError();
 }
@@ -683,10 +685,11 @@ hipError_t launch_select(int D, SelectParams &p, void *ws, hipStream_t s)
     // chunks of 64 places at least, and enough of them to fill the device
     const int64_t most = (p.b.width + 63) / 64, want = (2048 + x.tiles * p.b.Hkv - 1) / (x.tiles * p.b.Hkv), n = want < most ? want : most;
     p.chunk = n > 0 ? (int)(((p.b.width + n - 1) / n + 63) / 64 * 64) : 64;
+    const bool raw = p.Hq / p.b.Hkv <= 16;   // (queries in LDS: with a branch in the kernel every wait would be for all loads)
     switch (D) {
-    case 64: return launch_select_of<64>(p, x, s);
-    case 128: return launch_select_of<128>(p, x, s);
-    default: return launch_select_of<256>(p, x, s);
+    case 64: return raw ? launch_select_of<64, true>(p, x, s) : launch_select_of<64, false>(p, x, s);
+    case 128: return raw ? launch_select_of<128, true>(p, x, s) : launch_select_of<128, false>(p, x, s);
+    default: return raw ? launch_select_of<256, true>(p, x, s) : launch_select_of<256, false>(p, x, s);
     }
 }
 
