@@ -311,76 +311,64 @@ __device__ __forceinline__ void write_scores(const SelectParams &p, const i32x4 
     }
 }
 
-// The smallest key that is taken and how many that equal it, for up to 16 rows at
-// once: 8 bits a step from a histogram of each in LDS.  The waves of a row (whose
-// wave is `first`th of `by`) call each(f) to go over their part of its keys.  All
-// waves call it.
+// The smallest key of a row that is taken and how many that equal it: 8 bits a step
+// from a histogram in LDS.  each(f) goes over the thread's part of the keys.
 struct Taken {
     uint32_t key;
     int same;
 };
 
-template <class E>
-__device__ __forceinline__ Taken narrow(uint32_t (*hist)[256], int (*found)[2], int rows, int row, bool head_wave, int budget, E each)
+template <int BY, class E>
+__device__ __forceinline__ Taken narrow(uint32_t (&hist)[256], int (&found)[2], int budget, E each)
 {
-    const int lane = threadIdx.x & 63;
+    const int tid = (int)threadIdx.x, lane = tid & 63;
     Taken t = {0, budget};
     for (int shift = 24; shift >= 0; shift -= 8) {
-        for (int i = (int)threadIdx.x; i < 256 * rows; i += (int)blockDim.x) hist[0][i] = 0;
+        if (tid < 256) hist[tid] = 0;
         __syncthreads();
         const uint32_t mask = shift == 24 ? 0u : ~0u << (shift + 8);
-        if (row < rows)
-            each([&](uint32_t k) {
-                if ((k & mask) == t.key) atomicAdd(&hist[row][k >> shift & 255], 1u);
-            });
+        each([&](uint32_t k) {
+            if ((k & mask) == t.key) atomicAdd(&hist[k >> shift & 255], 1u);
+        });
         __syncthreads();
-        if (row < rows && head_wave) {
+        if (tid < 64) {
             // lane l: the 4 digits from 252 - 4 l down in order of size
             uint32_t n[4], sum = 0;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sum += n[e] = hist[row][255 - 4 * lane - e];
-            uint32_t upto = sum;
-#pragma unroll
-            for (int k = 1; k < 64; k <<= 1) {
-                const uint32_t y = __shfl_up(upto, k, 64);
-                upto += lane >= k ? y : 0;
-            }
-            uint32_t above = upto - sum;
+            for (int e = 0; e < 4; ++e) sum += n[e] = hist[255 - 4 * lane - e];
+            uint32_t above = wave_scan(sum) - sum;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                if (above < (uint32_t)t.same && (uint32_t)t.same <= above + n[e]) found[row][0] = 255 - 4 * lane - e, found[row][1] = (int)above;
+                if (above < (uint32_t)t.same && (uint32_t)t.same <= above + n[e]) found[0] = 255 - 4 * lane - e, found[1] = (int)above;
                 above += n[e];
             }
         }
         __syncthreads();
-        if (row < rows) {
-            t.key |= (uint32_t)found[row][0] << shift;
-            t.same -= found[row][1];
-        }
+        t.key |= (uint32_t)found[0] << shift;
+        t.same -= found[1];
     }
     return t;
 }
 
 // Places of the keys above t.key, and of the first t.same that equal it, in order:
-// the `by` waves of a row take consecutive parts; key(i) for i < many.  All waves
-// call it (those of no row with many 0).
-template <class K>
-__device__ __forceinline__ void write_places(const Taken &t, int many, int wave, int by, int (*counts)[2], int counts_from, int *out, K key)
+// the waves take consecutive parts; key(i) for i < many.
+template <int BY, class K>
+__device__ __forceinline__ void write_places(const Taken &t, int many, int (&counts)[BY / 64][2], int *out, K key)
 {
-    const int lane = threadIdx.x & 63;
-    const int each = ((many + by - 1) / by + 63) & ~63, a = wave * each, e = a + each < many ? a + each : many;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int each = ((many + BY / 64 - 1) / (BY / 64) + 63) & ~63, a = wave * each, e = a + each < many ? a + each : many;
     int above = 0, same = 0;
     for (int i = a + lane; i - lane < e; i += 64) {
         const uint32_t k = i < e ? key(i) : 0;
         above += __popcll(__ballot(i < e && k > t.key));
         same += __popcll(__ballot(i < e && k == t.key));
     }
-    if (lane == 0) counts[counts_from + wave][0] = above, counts[counts_from + wave][1] = same;
+    if (lane == 0) counts[wave][0] = above, counts[wave][1] = same;
     __syncthreads();
     int at = 0, equal = 0;
     for (int w = 0; w < wave; ++w) {
-        const int left = t.same - equal > 0 ? t.same - equal : 0, eq = counts[counts_from + w][1];
-        at += counts[counts_from + w][0] + (eq < left ? eq : left);
+        const int left = t.same - equal > 0 ? t.same - equal : 0, eq = counts[w][1];
+        at += counts[w][0] + (eq < left ? eq : left);
         equal += eq;
     }
     const uint64_t below = ((uint64_t)1 << lane) - 1;
@@ -446,7 +434,7 @@ __device__ __forceinline__ void select_row(int many, int budget, int *out, K key
 }
 
 // A tile's tokens and one kv head, scores in LDS.
-constexpr int SELECT_BY = 512;
+constexpr int SELECT_BY = 512, WIDEST = 1024;   // threads; places of a row
 
 template <int D, bool RAW>
 __global__ __launch_bounds__(SELECT_BY) void select_kernel(SelectParams p)
@@ -454,8 +442,7 @@ __global__ __launch_bounds__(SELECT_BY) void select_kernel(SelectParams p)
     constexpr int WAVES = SELECT_BY / 64;
     __shared__ u32x4 rows[2 * D / 64][64];
     __shared__ u32x4 raw[16][D / 8];
-    __shared__ uint32_t amax[16], hist[1][256];
-    __shared__ int found[1][2], counts[WAVES][2];
+    __shared__ uint32_t amax[16];
     extern __shared__ uint32_t keys[];             // [tokens][places]
     const int G = p.Hq / p.b.Hkv, hs = p.heads_shift;
     const TokenTile t = token_tile(p.b, p.tokens, (int)blockIdx.x);
@@ -512,32 +499,24 @@ __global__ __launch_bounds__(SELECT_BY) void select_kernel(SelectParams p)
         }
         __syncthreads();
     }
-    // a wave for each token, or all for each of long rows
-    const bool alone = most <= 1024;
-    for (int tk = alone ? wave : 0; tk < t.n; tk += alone ? WAVES : 1) {
+    // a wave for each token
+    for (int tk = wave; tk < t.n; tk += WAVES) {
         const int many = places_of(p.b, t.pos + tk, t.len);
         int *out = out_of(tk);
         auto key = [&](int i) { return i < p.first || i >= many - p.last ? FORCED : keys[tk * p.b.width + i]; };
         if (many <= p.budget) {
-            for (int i = alone ? lane : tid; i < p.budget; i += alone ? 64 : SELECT_BY) out[i] = i < many ? i : -1;
+            for (int i = lane; i < p.budget; i += 64) out[i] = i < many ? i : -1;
         } else if (many <= 256) {
             select_row<4>(many, p.budget, out, key);
         } else if (many <= 512) {
             select_row<8>(many, p.budget, out, key);
-        } else if (many <= 1024) {
-            select_row<16>(many, p.budget, out, key);
-        } else {
-            const Taken taken = narrow(hist, found, 1, 0, wave == 0, p.budget, [&](auto f) {
-                for (int i = tid; i < many; i += SELECT_BY) f(key(i));
-            });
-            write_places(taken, many, wave, WAVES, counts, 0, out, key);
-            __syncthreads();   // (counts have been read)
+        } else {   // (up to WIDEST)
+            select_row<WIDEST / 64>(many, p.budget, out, key);
         }
     }
 }
 
-// Where the scores of a tile's tokens do not fit LDS, or one tile's workgroup would
-// have too long a row to itself: scores over `chunk` places to memory, ...
+// Where rows are too long for a workgroup each: scores over `chunk` places to memory, ...
 template <int D, bool RAW>
 __global__ __launch_bounds__(256) void select_score_kernel(SelectParams p)
 {
@@ -593,27 +572,28 @@ __global__ __launch_bounds__(256) void select_score_kernel(SelectParams p)
     }
 }
 
-// ... and the places of a token and kv head from those.
-__global__ __launch_bounds__(256) void select_top_kernel(SelectParams p)
+// ... and the places of a token and kv head from those, by a workgroup.
+template <int BY>
+__global__ __launch_bounds__(BY) void select_top_kernel(SelectParams p)
 {
-    __shared__ uint32_t hist[1][256];
-    __shared__ int found[1][2], counts[4][2];
-    const int head = (int)blockIdx.y, tid = (int)threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    __shared__ uint32_t hist[256];
+    __shared__ int found[2], counts[BY / 64][2];
+    const int head = (int)blockIdx.y, tid = (int)threadIdx.x;
     const TokenTile t = token_tile(p.b, 1, (int)blockIdx.x);
     if (t.s < 0) return;
     const int many = places_of(p.b, t.pos, t.len);
     const int64_t row = (int64_t)t.tok * p.b.Hkv + head;
     int *out = p.places + row * p.budget;
     if (many <= p.budget) {
-        for (int i = tid; i < p.budget; i += 256) out[i] = i < many ? i : -1;
+        for (int i = tid; i < p.budget; i += BY) out[i] = i < many ? i : -1;
         return;
     }
     const uint32_t *scores = p.scores + row * p.b.width;
     auto key = [&](int i) { return i < p.first || i >= many - p.last ? FORCED : scores[i]; };
-    const Taken taken = narrow(hist, found, 1, 0, wave == 0, p.budget, [&](auto f) {
-        for (int i = tid; i < many; i += 256) f(key(i));
+    const Taken taken = narrow<BY>(hist, found, p.budget, [&](auto f) {
+        for (int i = tid; i < many; i += BY) f(key(i));
     });
-    write_places(taken, many, wave, 4, counts, 0, out, key);
+    write_places<BY>(taken, many, counts, out, key);
 }
 
 } // namespace
@@ -639,9 +619,19 @@ struct SelectShape {
     bool one;
 };
 
-// In one launch where a tile's scores fit half of a CU's LDS, and either workgroups
-// fill the device or none reads more than ALONE bytes of ranges.
-constexpr int64_t KEYS = 12288, ALONE = (int64_t)1 << 17;
+// In one launch where a workgroup for each tile is no worse than more of them and a
+// second launch: with one token a sequence where it reads up to ALONE bytes of ranges
+// (8 heads, d = 128, GPU time one / two: 1 token of 313 places 11.1 / 12.2 us; 32 tokens of
+// 500 places 17.7 / 17.6, of 625 26.8 / 23.7, of 1250 42.6 / 32.3; but a call of two
+// launches costs 4 us more on the host); with chunks of several, whose tokens share what
+// is read and are selected from side by side, up to WIDEST places where the tiles fill the
+// device (32 times 8 tokens of 781 places 42.8 / 44.7; 4 times 500 of 625 157 / 186, but 2000
+// of 1250 608 / 449).  The scores of a tile fit half of a CU's LDS, KEYS of them.
+constexpr int64_t KEYS = 12288, ALONE = (int64_t)1 << 17, CHUNK = 4;
+// Places in the table from which a row's workgroup in the second launch is of 1024
+// threads (6250 places of 32 tokens and 8 heads: 14 us; of one token and 8 heads 15, of 256
+// threads 28).
+constexpr int TOP_WIDE = 1024;
 
 static SelectShape select_shape(int D, int64_t T, int64_t S, int G, int Hkv, int64_t width)
 {
@@ -653,7 +643,7 @@ static SelectShape select_shape(int D, int64_t T, int64_t S, int G, int Hkv, int
     // (fewer tokens a tile: the operand's other rows are 0)
     int per = x.tokens;
     while (per > 1 && (per * width > KEYS || tiles(per) * Hkv < 256)) per /= 2;
-    x.one = width * per <= KEYS && (tiles(per) * Hkv >= 256 || width * 2 * D <= ALONE);
+    x.one = width * per <= KEYS && width <= WIDEST && (width * 2 * D <= ALONE || (T >= CHUNK * S && tiles(per) * Hkv >= 256));
     if (x.one) x.tokens = per, x.tiles = tiles(per);
     return x;
 }
@@ -672,7 +662,9 @@ static hipError_t launch_select_of(const SelectParams &p, const SelectShape &x, 
         return hipGetLastError();
     }
     select_score_kernel<D, RAW><<<dim3((unsigned)x.tiles, (unsigned)p.b.Hkv, (unsigned)((p.b.width + p.chunk - 1) / p.chunk)), 256, 0, s>>>(p);
-    select_top_kernel<<<dim3((unsigned)p.b.T, (unsigned)p.b.Hkv), 256, 0, s>>>(p);
+    const dim3 rows((unsigned)p.b.T, (unsigned)p.b.Hkv);
+    if (p.b.width > TOP_WIDE) select_top_kernel<1024><<<rows, 1024, 0, s>>>(p);
+    else select_top_kernel<256><<<rows, 256, 0, s>>>(p);
     return hipGetLastError();
 }
 

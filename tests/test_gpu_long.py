@@ -207,11 +207,14 @@ def test_select(L, lens, Hq, H, d, page, budget, first, last):  # noqa: F811
 
 @pytest.mark.parametrize("lens,Hq,H,d,budget", [
     ([(195000, 1)], 2, 1, 64, 100),                                        # a row too long for one workgroup
-    ([(150000, 1)] + [(30 + i, 1) for i in range(129)], 4, 2, 64, 60),     # LDS holds as many scores as it may
-    ([(150000, 2)] + [(30 + i, 1) for i in range(29)], 2, 1, 128, 60),     # and not those of two tokens, of few workgroups
+    ([(150000, 1)] + [(30 + i, 1) for i in range(129)], 4, 2, 64, 60),     # among many short ones
+    ([(150000, 2)] + [(30 + i, 1) for i in range(29)], 2, 1, 128, 60),
     ([(195000, 1)] + [(30 + i % 50, 1) for i in range(257)], 2, 1, 256, 60),
     ([(40, 1)] * 3 + [(40000, 14)], 1, 1, 64, 33),                         # 14 tokens of a sequence
     ([(2500, 40), (900, 7)], 3, 3, 64, 20),
+    ([(15900, 30)], 32, 32, 64, 70),                                       # a chunk of tokens with rows as long as one workgroup takes
+    ([(8000, 1), (8191, 1), (16368, 1)], 8, 8, 64, 9),                     # single tokens of rows up to that length
+    ([(8000, 1), (8191, 1), (16384, 1)], 8, 8, 64, 9),                     # and beyond it
 ])
 def test_select_long(L, lens, Hq, H, d, budget):  # noqa: F811
     _check_select(L, _select_case(lens, Hq, H, d, 16, 77), 16, budget, 1, 2)

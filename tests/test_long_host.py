@@ -108,9 +108,10 @@ def test_advance_refusals():
 def test_workspace_sizes():
     size = lamp.select_pages_workspace_size
     assert size(3, 1, 8, 2, 64, 10, 10) == 0 and size(0, 1, 8, 2, 64, 10, 4) == 0 and size(3, 1, 7, 2, 64, 10, 4) == 0
-    # scores in LDS, but for rows too long for it, or for a few workgroups
-    assert size(3, 1, 8, 2, 64, 10, 4) == 0 and size(300, 300, 8, 2, 128, 12288, 4) == 0
-    assert size(300, 300, 8, 2, 128, 12289, 4) == 300 * 2 * 12289 * 4 and size(1, 1, 8, 2, 128, 513, 4) == 2 * 513 * 4
+    # scores in LDS, but for rows too long for it, or for a workgroup each
+    assert size(3, 1, 8, 2, 64, 10, 4) == 0 and size(300, 300, 8, 2, 128, 512, 4) == 0 and size(300, 300, 8, 2, 64, 1024, 4) == 0
+    assert size(300, 300, 8, 2, 128, 513, 4) == 300 * 2 * 513 * 4 and size(1, 1, 8, 2, 128, 513, 4) == 2 * 513 * 4
+    assert size(2000, 300, 8, 2, 128, 1024, 4) == 0 and size(2000, 300, 8, 2, 128, 1025, 4) == 2000 * 2 * 1025 * 4
     assert size(1 << 23, 1 << 20, 1, 1, 64, 1 << 20, 4) == 0
     size = lamp.attn_pages_workspace_size
     assert size(2, 4, 3, 64, 16, 4) == 0 and size(1, 4, 2, 80, 16, 4) == 0 and size(1, 4, 2, 64, 24, 4) == 0
