@@ -501,7 +501,8 @@ size_t lamp_attn_cache_workspace_size(int T, int S, int Hq, int Hkv, int d, int 
  * (kv_lens = lens, q_start = 0, no page is taken); sequences leave all the same.
  * 8 (in any case) more pages would go back than the ring has room for, and none does.
  *
- * kv_lens may be lens, and state_out state; no other two arrays may overlap.  page:
+ * kv_lens may be lens, and state_out state; no other two arrays may overlap, nor the
+ * table's rows (|table_stride| below width is refused).  page:
  * 16, 32, 64, 128 or 256; S up to 2^20, T up to 2^23, width*page up to 2^30.
  * Values that break these rules give wrong results, never an access outside the
  * arrays.
@@ -549,9 +550,9 @@ size_t lamp_select_pages_workspace_size(int T, int S, int Hq, int Hkv, int d, in
 
 /*
  * lamp_attn_pages -- lamp_attn_cache (causal) where each token and kv head sees only
- * the keys of the places in its list, places int32 [T][Hkv][budget]: any order,
- * each place at most once; entries outside [0, width) and places behind the
- * token's position hold no keys.  Edges as for lamp_attn_cache: a row without keys
+ * the keys of the places in its list, places int32 [T][Hkv][budget]: any order
+ * (a place listed twice counts twice); entries outside [0, width) and places behind
+ * the token's position hold no keys.  Edges as for lamp_attn_cache: a row without keys
  * has o = 0 and lse = -infinity, one with a listed place without a page is NaN.
  * T*Hq*ceil(budget/1024) below 2^24; other limits as for lamp_attn_cache.
  */

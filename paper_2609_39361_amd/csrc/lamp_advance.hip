@@ -13,8 +13,8 @@
 // the places in LDS for its sequence (one may have thousands, most have none).
 // Positions of many tokens are written by a second launch.  Bound by the latencies
 // of the loads, the sums, the searches and the ring's entries, one after another (32
-// sequences 5.6 us, of which a launch is 3.7; 4096 whose step takes 4200 pages and
-// gives 12700 back 14.4 with the positions' launch).
+// sequences 5.6 us, of which a launch is 3.7; 4096 whose step takes 3554 pages and
+// gives 3208 back 14.4 with the positions' launch).
 #include <hip/hip_runtime.h>
 
 #include "lamp_cache_plan.h"
@@ -23,7 +23,7 @@ namespace lamp {
 namespace {
 
 constexpr int ADVANCE_BY = 1024, ADVANCE_WAVES = ADVANCE_BY / 64;
-constexpr int WITHIN = 8192;   // positions that the first launch writes itself
+constexpr int WITHIN = 8192;   // positions that the first launch writes itself (eight a thread; a launch is 3.7 us)
 
 // Why a step is not admitted.
 enum { SHORT_OF_PAGES = 1, BEYOND_TABLE = 2, BEYOND_TOKENS = 4 };

@@ -18,14 +18,18 @@ namespace {
 // and both products take their summed axis in the order that makes a lane's bytes
 // contiguous: K's channels h D/2 .. of a key, V's KT/2 keys of a channel.
 //
-// A wave loads a tile's codes in the order of memory (64 lanes, 1 KB; lanes that
-// read rows of their own instead take the load path four times as long, 3.0 us a
-// tile), keeps them in registers until they are due, and passes them through a
-// stretch of LDS of its own, K first, then V, with rows a 16-byte unit longer than
-// their bytes (and the upper half of the keys 64 bytes on), so that 8 lanes reading
-// a unit of their rows use all banks.  No barrier is needed until the waves join.
-// Nothing is masked but whole groups of 16 keys behind the prefix's end, which is a
-// page's.
+// A wave loads a tile's codes in the order of memory (64 lanes, 1 KB), keeps them in
+// registers until they are due, and passes them through a stretch of LDS of its own, K
+// first, then V, with rows a 16-byte unit longer than their bytes (and the upper half
+// of the keys 64 bytes on), so that 8 lanes reading a unit of their rows use all
+// banks.  No barrier is needed until the waves join.  Nothing is masked but whole
+// groups of 16 keys behind the prefix's end, which is a page's.
+//
+// Bound by issue (d = 128): a tile's 290 vector and 32 matrix instructions take a wave
+// 1.85 us alone on its SIMD and 2.8 beside another (lanes that read rows of their own
+// straight into operands: 3.0), whatever the caches hold: touching L2 a tile ahead
+// gained nothing.  64 tokens of 32/8 heads behind 8192 shared keys and 20 to 1500 of
+// their own: 33 us with the form for few rows beside it (all in that form: 51).
 template <int D, int KT>
 struct PrefixShared {
     static constexpr int DC = D == 128 ? 128 : 64;      // channels joined at a time (two workgroups a CU hold theirs)

@@ -8,9 +8,14 @@
 // Every row sees the whole prefix, so that the new tokens of all sequences of a group
 // are the rows of one product without a mask, and the prefix's codes are read once
 // for all.  Both kinds of part, cut further where they do not fill the device, are
-// units of one launch (lamp_cache_plan.h: what is planned is the groups, then the
-// sequences), in the form for few rows or that for many; a second launch joins each
-// row's partial outputs, whose places the first pieces leave (RowInfo).
+// units (lamp_cache_plan.h: what is planned is the groups, then the sequences): of one
+// launch the groups' in the form of lamp_cache_prefix.h and the sequences' in that for
+// few rows, and, where the batch may hold so many rows, of a second in the form for
+// many.  The last launch joins each row's partial outputs, whose places the first
+// pieces leave (RowInfo).  (Units of groups and of sequences in turn instead of one
+// after the other: slower.)  Four samples of one prompt (1000 keys, 8/8 heads, d = 64): 7.7 us
+// and 4.1 for the join; questions of 100 to 300 tokens about two documents of some 4000 keys
+// (121 GFLOP): 148 us, 14 for the join of 61 MB.
 #include <hip/hip_runtime.h>
 
 #include "lamp_cache_many.h"

@@ -778,7 +778,8 @@ def attn_pages_workspace_size(T, Hq, Hkv, d, page, budget):
 
 def attn_pages(q, cache, block_table, kv_lens, places, q_start=None, scale=None, out=None, workspace=None):
     """attn_cache (causal) where each new token and kv head sees only the keys of the places in its list: places int32
-    [T,Hkv,budget], of select_pages or any others, each at most once; what is not a place of the table holds no keys.
+    [T,Hkv,budget], of select_pages or any others (one listed twice counts twice); what is not a place of the table holds
+    no keys.
     Returns (o bf16 [T,Hq,d], lse fp32 [T,Hq])."""
     T = _tokens(q)
     c, b, dev, Hkv, page, d, _, _ = _paged(cache, block_table, kv_lens, q_start, T)

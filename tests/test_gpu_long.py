@@ -352,6 +352,16 @@ def test_pages_empty_lists_missing_pages_and_nan(L):  # noqa: F811
     assert not got[0][0].any() and bool((got[1][0] == -math.inf).all())
 
 
+def test_pages_listed_twice_count_twice(L):  # noqa: F811
+    case = _attn_case(L, [(400, 3), (1000, 1)], 4, 2, 64, 16, seed=6)
+    places = torch.full((4, 2, 200), -1, dtype=torch.int32)
+    for t in range(4):
+        for h in range(2):
+            mine = [3, 7, 3, 0, 9, 9, 9, 25 if t < 3 else 62, 3] + list(range(20)) * (8 * (t == 3))
+            places[t, h, :len(mine)] = torch.tensor(mine, dtype=torch.int32)
+    _run_pages(L, case, 16, 4, places)
+
+
 def test_pages_tokens_behind_the_last_and_one_each(L):  # noqa: F811
     q, parts, table, kv, starts = _attn_case(L, [(300, 1), (100, 1)], 4, 2, 64, 16, seed=5, trailing=3)
     places = _lists(table, kv, starts, 2, 16, 6, 7)
