@@ -515,6 +515,8 @@ __global__ __launch_bounds__(SELECT_BY) void select_kernel(SelectParams p)
             select_row<4>(many, p.budget, out, key);
         } else if (many <= 512) {
             select_row<8>(many, p.budget, out, key);
+        } else if (many <= 768) {
+            select_row<12>(many, p.budget, out, key);
         } else {   // (up to WIDEST)
             select_row<WIDEST / 64>(many, p.budget, out, key);
         }
