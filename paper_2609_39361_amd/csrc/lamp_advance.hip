@@ -5,16 +5,16 @@
 //
 // With h_s = ceil(len_s / page) the places that sequence s holds and n_s the tokens
 // it adds, it needs ceil((len_s + n_s) / page) - h_s pages; sums over the sequences
-// before say which of the ring's, in order.  One workgroup goes over the sequences,
+// before say which of the ring's, in order.  A workgroup goes over the sequences,
 // EACH consecutive ones a thread: sums over all, by which the step is admitted or not,
 // and places, sums over those before (saturating in 32 bits, beyond everything that
-// is admitted).  The entries and
-// positions of all of them are then spread over the threads, each of which searches
-// the places in LDS for its sequence (one may have thousands, most have none).
-// Positions of many tokens are written by a second launch.  Bound by the latencies
-// of the loads, the sums, the searches and the ring's entries, one after another (32
-// sequences 5.6 us, of which a launch is 3.7; 4096 whose step takes 3554 pages and
-// gives 3208 back 14.4 with the positions' launch).
+// is admitted).  The entries and positions of all of them are then spread over the
+// threads, each of which searches the places in LDS for its sequence (one may have
+// thousands, most have none).  Where there may be many, several workgroups do all of
+// this and share the entries and positions.  The lengths, starts and state are the
+// first one's to write; in place they are a second launch's, as the others still read
+// what they replace.  Bound by the latencies of the loads, the sums, the searches and
+// the ring's entries, one after another (FIGURES).
 #include <hip/hip_runtime.h>
 
 #include "lamp_cache_plan.h"
@@ -23,7 +23,7 @@ namespace lamp {
 namespace {
 
 constexpr int ADVANCE_BY = 1024, ADVANCE_WAVES = ADVANCE_BY / 64;
-constexpr int WITHIN = 8192;   // positions that the first launch writes itself (eight a thread; a launch is 3.7 us)
+constexpr int SHARE = 4096;    // entries or positions for which a workgroup more is taken
 
 // Why a step is not admitted.
 enum { SHORT_OF_PAGES = 1, BEYOND_TABLE = 2, BEYOND_TOKENS = 4 };
@@ -65,6 +65,9 @@ __device__ __forceinline__ uint32_t wave_sums(uint32_t v)
     return wave_scan_by(v, [](uint32_t a, uint32_t b) { return sum(a, b); });
 }
 
+// What a launch writes: entries and positions, and the rest.
+enum { ENTRIES = 1, OUTPUTS = 2 };
+
 // Where the sequences' taken entries, those that go back and their positions begin
 // among all, and where in their rows and from which position on.
 template <int N>
@@ -92,7 +95,7 @@ __device__ __forceinline__ void owners(const int *at, const int (&x)[AT], int (&
 }
 
 template <int EACH>
-__global__ __launch_bounds__(ADVANCE_BY) void advance_kernel(AdvanceParams p)
+__global__ __launch_bounds__(ADVANCE_BY) void advance_kernel(AdvanceParams p, int what)
 {
     __shared__ uint32_t sums[3][ADVANCE_WAVES];
     __shared__ int beyond_any[ADVANCE_WAVES];
@@ -100,6 +103,8 @@ __global__ __launch_bounds__(ADVANCE_BY) void advance_kernel(AdvanceParams p)
     __shared__ SeqPlaces<N> places;   // of a round's sequences
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int pages = p.pages, last = p.S - 1;
+    const int part = (int)blockIdx.x * ADVANCE_BY + tid, stride = (int)gridDim.x * ADVANCE_BY;   // of entries and positions
+    const bool outputs = (what & OUTPUTS) != 0 && blockIdx.x == 0;
     const int first = p.state[0], free = p.state[1];
     const int rounds = (p.S + EACH * ADVANCE_BY - 1) / (EACH * ADVANCE_BY);
     auto sequence = [&](int round, int i) { return (round * ADVANCE_BY + tid) * EACH + i; };
@@ -179,7 +184,7 @@ __global__ __launch_bounds__(ADVANCE_BY) void advance_kernel(AdvanceParams p)
             const int place = tid * EACH + i, begin[3] = {r[i].held, r[i].kept, r[i].len};
 #pragma unroll
             for (int k = 0; k < 3; ++k) places.at[k][place] = at[k], places.from[k][place] = begin[k];
-            if (s <= last) {
+            if (outputs && s <= last) {
                 p.kv_lens[s] = r[i].gone ? 0 : r[i].said + (ok ? r[i].add : 0);
                 p.q_start[s] = at[2];
                 if (s == last) p.q_start[p.S] = at[2] + (ok ? r[i].add : 0);
@@ -188,16 +193,20 @@ __global__ __launch_bounds__(ADVANCE_BY) void advance_kernel(AdvanceParams p)
             at[1] += returns ? r[i].back : 0;
             at[2] += ok ? r[i].add : 0;
         }
+        if (!(what & ENTRIES)) continue;
         __syncthreads();
         // (AT entries of a thread at once, whose searches and loads do not wait for each other: 4096
         // sequences one token each 8.7 us, one by one 9.3; 1000, which have few, 9.3, four at once 10.4)
         const int s0 = round * N;
         constexpr int AT = EACH;
         auto each = [&](int which, int end, auto work) {
-            for (int i0 = from[which] + tid; i0 < end; i0 += AT * ADVANCE_BY) {
+            for (int64_t i0 = (int64_t)from[which] + part; i0 < end; i0 += (int64_t)AT * stride) {
                 int x[AT], of[AT];
 #pragma unroll
-                for (int k = 0; k < AT; ++k) x[k] = i0 + k * ADVANCE_BY < end ? i0 + k * ADVANCE_BY : i0;   // (beyond the last: the first again, with the same outcome)
+                for (int k = 0; k < AT; ++k) {   // (beyond the last: the first again, with the same outcome)
+                    const int64_t at = i0 + (int64_t)k * stride;
+                    x[k] = (int)(at < end ? at : i0);
+                }
                 owners<N>(places.at[which], x, of);
                 work(x, of);
             }
@@ -221,16 +230,14 @@ __global__ __launch_bounds__(ADVANCE_BY) void advance_kernel(AdvanceParams p)
             for (int k = 0; k < AT; ++k)
                 p.ring[in_ring((int64_t)count + x[k])] = page[k];
         });
-        if (p.T <= WITHIN)
-            each(2, add0, [&](const int (&x)[AT], const int (&of)[AT]) {
+        each(2, add0, [&](const int (&x)[AT], const int (&of)[AT]) {
 #pragma unroll
-                for (int k = 0; k < AT; ++k)
-                    p.positions[x[k]] = places.from[2][of[k]] + (x[k] - places.at[2][of[k]]);
-            });
+            for (int k = 0; k < AT; ++k) p.positions[x[k]] = places.from[2][of[k]] + (x[k] - places.at[2][of[k]]);
+        });
     }
-    if (p.T <= WITHIN)
-        for (int i = add0 + tid; i < p.T; i += ADVANCE_BY) p.positions[i] = 0;
-    if (tid == 0) {
+    if (what & ENTRIES)
+        for (int i = add0 + part; i < p.T; i += stride) p.positions[i] = 0;   // (T up to 2^23)
+    if (outputs && tid == 0) {
         if (p.S == 0) p.q_start[0] = 0;
         p.state_out[0] = in_ring(need0);
         p.state_out[1] = count - need0 + back0;
@@ -239,29 +246,25 @@ __global__ __launch_bounds__(ADVANCE_BY) void advance_kernel(AdvanceParams p)
     }
 }
 
-// Positions of the tokens of sequence x / parts, a part of them a wave (sequence S:
-// the tokens behind the last).
-__global__ __launch_bounds__(256) void positions_kernel(AdvanceParams p, int parts)
+void launch_part(const AdvanceParams &p, int parts, int what, hipStream_t s)
 {
-    const int64_t x = (int64_t)blockIdx.x * 4 + ((int)threadIdx.x >> 6);
-    const int s = (int)(x / parts), part = (int)(x - (int64_t)s * parts), lane = (int)threadIdx.x & 63;
-    if (s > p.S) return;
-    const int a = p.q_start[s], e = s < p.S ? p.q_start[s + 1] : p.T, n = e - a;
-    const int pos0 = s < p.S ? p.kv_lens[s] - n : 0;
-    const int64_t lo = (int64_t)n * part / parts, hi = (int64_t)n * (part + 1) / parts;
-    for (int64_t i = lo + lane; i < hi; i += 64) p.positions[a + i] = s < p.S ? pos0 + (int)i : 0;
+    if (p.S <= ADVANCE_BY) advance_kernel<1><<<parts, ADVANCE_BY, 0, s>>>(p, what);
+    else advance_kernel<4><<<parts, ADVANCE_BY, 0, s>>>(p, what);
 }
 
 } // namespace
 
 hipError_t launch_advance(const AdvanceParams &p, hipStream_t s)
 {
-    if (p.S <= ADVANCE_BY) advance_kernel<1><<<1, ADVANCE_BY, 0, s>>>(p);
-    else advance_kernel<4><<<1, ADVANCE_BY, 0, s>>>(p);
-    if (p.T > WITHIN) {
-        // about 256 tokens a wave
-        const int64_t want = (p.T + 256 * ((int64_t)p.S + 1) - 1) / (256 * ((int64_t)p.S + 1)), waves = ((int64_t)p.S + 1) * want;
-        positions_kernel<<<dim3((unsigned)((waves + 3) / 4)), 256, 0, s>>>(p, (int)want);
+    // as many entries as a 64th of the tables
+    const int64_t entries = (int64_t)p.S * p.width / 64, most = (p.T > entries ? p.T : entries) / SHARE;
+    const int parts = 1 + (int)(most < 63 ? most : 63);
+    const bool in_place = p.kv_lens == p.lens || p.state_out == p.state;
+    if (parts == 1 || !in_place) {
+        launch_part(p, parts, ENTRIES | OUTPUTS, s);
+    } else {
+        launch_part(p, parts, ENTRIES, s);
+        launch_part(p, 1, OUTPUTS, s);
     }
     return hipGetLastError();
 }

@@ -84,6 +84,22 @@ def test_advance_many(L, S, T):  # noqa: F811
     assert _check_step(L, lens, add, prefix, 16, T, *_pool_case(lens, add, prefix, 16, 7, S))[3][3] == 0
 
 
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("S,longest,new,T", [(700, 20000, 40, 30000), (1500, 6000, 3, 3000), (4500, 900, 60, 200000), (3, 40, 20000, 60001)])
+def test_advance_by_several_workgroups(L, S, longest, new, T, in_place):  # noqa: F811
+    """Many entries and positions, in one launch or (in place) two; steps that are not admitted among them."""
+    g = _gen(S + longest)
+    lens = torch.randint(0, longest, (S,), generator=g).tolist()
+    add = torch.where(torch.rand(S, generator=g) < 0.2, -1, torch.randint(0, new, (S,), generator=g)).tolist()
+    prefix = [32 * (s % 3) for s in range(S)]
+    lens = [max(n, p) for n, p in zip(lens, prefix)]
+    table, ring, state = _pool_case(lens, add, prefix, 16, 7, S)
+    want = _check_step(L, lens, add, prefix, 16, T, table, ring, state, in_place=in_place)
+    assert want[3][3] == 0 and want[1][-1] > 0
+    short = [state[0], want[3][2] - 1, 0, 0]
+    assert _check_step(L, lens, add, prefix, 16, T, table, ring, short, in_place=in_place)[3][3] == 1
+
+
 def test_advance_refuses_steps(L):  # noqa: F811
     """Too few free pages, tokens, places: nothing is added, sequences leave all the same; too many pages going back: none."""
     lens, add = [40, 20, 100, 0], [30, -1, 1, 16]
