@@ -14,7 +14,9 @@
 // this and share the entries and positions.  The lengths, starts and state are the
 // first one's to write; in place they are a second launch's, as the others still read
 // what they replace.  Bound by the latencies of the loads, the sums, the searches and
-// the ring's entries, one after another (FIGURES).
+// the ring's entries, one after another: 32 sequences 5.1 us, of which a launch is 3.7;
+// 4096 whose step takes 3554 pages, gives 3208 back and has 26832 tokens, by 35
+// workgroups 8.8 (by 7 13.4; by one, and a launch for the positions, 14.4).
 #include <hip/hip_runtime.h>
 
 #include "lamp_cache_plan.h"
@@ -23,7 +25,7 @@ namespace lamp {
 namespace {
 
 constexpr int ADVANCE_BY = 1024, ADVANCE_WAVES = ADVANCE_BY / 64;
-constexpr int SHARE = 4096;    // entries or positions for which a workgroup more is taken
+constexpr int SHARE = 1024;    // entries and positions for which a workgroup more is taken
 
 // Why a step is not admitted.
 enum { SHORT_OF_PAGES = 1, BEYOND_TABLE = 2, BEYOND_TOKENS = 4 };
@@ -72,14 +74,14 @@ enum { ENTRIES = 1, OUTPUTS = 2 };
 // among all, and where in their rows and from which position on.
 template <int N>
 struct SeqPlaces {
-    int at[3][N], from[3][N];
+    int at[3 * N], from[3 * N];
 };
 
-// Last i with at[i] <= x for each x (those of the first are, those behind the last
-// sequence are not; non-decreasing): without branches, as the reads of one search wait
-// for each other.
+// Last i with at[which N + i] <= x for each x (those of the first are, those behind the
+// last sequence are not; non-decreasing): without branches, as the reads of one search
+// wait for each other.
 template <int N, int AT>
-__device__ __forceinline__ void owners(const int *at, const int (&x)[AT], int (&i)[AT])
+__device__ __forceinline__ void owners(const int *at, const int (&which)[AT], const int (&x)[AT], int (&i)[AT])
 {
 #pragma unroll
     for (int k = 0; k < AT; ++k) i[k] = 0;
@@ -87,7 +89,7 @@ __device__ __forceinline__ void owners(const int *at, const int (&x)[AT], int (&
     for (int half = N / 2; half; half >>= 1) {
         int y[AT];
 #pragma unroll
-        for (int k = 0; k < AT; ++k) y[k] = at[i[k] + half];
+        for (int k = 0; k < AT; ++k) y[k] = at[which[k] * N + i[k] + half];
         __builtin_amdgcn_sched_barrier(0);   // (the compiler would take one search after another)
 #pragma unroll
         for (int k = 0; k < AT; ++k) i[k] += y[k] <= x[k] ? half : 0;
@@ -183,7 +185,7 @@ __global__ __launch_bounds__(ADVANCE_BY) void advance_kernel(AdvanceParams p, in
             const int s = sequence(round, i);
             const int place = tid * EACH + i, begin[3] = {r[i].held, r[i].kept, r[i].len};
 #pragma unroll
-            for (int k = 0; k < 3; ++k) places.at[k][place] = at[k], places.from[k][place] = begin[k];
+            for (int k = 0; k < 3; ++k) places.at[k * N + place] = at[k], places.from[k * N + place] = begin[k];
             if (outputs && s <= last) {
                 p.kv_lens[s] = r[i].gone ? 0 : r[i].said + (ok ? r[i].add : 0);
                 p.q_start[s] = at[2];
@@ -195,45 +197,39 @@ __global__ __launch_bounds__(ADVANCE_BY) void advance_kernel(AdvanceParams p, in
         }
         if (!(what & ENTRIES)) continue;
         __syncthreads();
-        // (AT entries of a thread at once, whose searches and loads do not wait for each other: 4096
-        // sequences one token each 8.7 us, one by one 9.3; 1000, which have few, 9.3, four at once 10.4)
-        const int s0 = round * N;
-        constexpr int AT = EACH;
-        auto each = [&](int which, int end, auto work) {
-            for (int64_t i0 = (int64_t)from[which] + part; i0 < end; i0 += (int64_t)AT * stride) {
-                int x[AT], of[AT];
+        // entries to take, those that go back and positions as one list, AT of a thread at once, whose
+        // searches and loads do not wait for each other (a call of up to 1024 sequences 5.1 to 5.9 us, of one
+        // at once 5.8 to 6.3; the step of 4096 8.8, of two 9.6, of four 11.2)
+        constexpr int AT = EACH == 1 ? 2 : 1;
+        const int64_t taken = need0 - from[0], moved = taken + back0 - from[1], total = moved + add0 - from[2];
+        for (int64_t i0 = part; i0 < total; i0 += (int64_t)AT * stride) {
+            int which[AT], x[AT], of[AT], value[AT];
+            const int *source[AT];
+            int *target[AT];
 #pragma unroll
-                for (int k = 0; k < AT; ++k) {   // (beyond the last: the first again, with the same outcome)
-                    const int64_t at = i0 + (int64_t)k * stride;
-                    x[k] = (int)(at < end ? at : i0);
-                }
-                owners<N>(places.at[which], x, of);
-                work(x, of);
+            for (int k = 0; k < AT; ++k) {   // (beyond the last: the first again, with the same outcome)
+                const int64_t at = i0 + (int64_t)k * stride, i = at < total ? at : i0;
+                which[k] = i < taken ? 0 : (i < moved ? 1 : 2);
+                x[k] = (int)(i < taken ? from[0] + i : (i < moved ? from[1] + i - taken : from[2] + i - moved));
             }
-        };
-        auto entry = [&](int which, int x, int l) {
-            return p.table + (int64_t)(s0 + l) * p.table_stride + places.from[which][l] + (x - places.at[which][l]);
-        };
-        each(0, need0, [&](const int (&x)[AT], const int (&of)[AT]) {
-            int page[AT];
+            owners<N>(places.at, which, x, of);
 #pragma unroll
-            for (int k = 0; k < AT; ++k) page[k] = p.ring[in_ring(x[k])];
+            for (int k = 0; k < AT; ++k) {
+                const int l = of[k], begin = places.from[which[k] * N + l] + (x[k] - places.at[which[k] * N + l]);
+                int *entry = p.table + (int64_t)(round * N + l) * p.table_stride + begin;
+                int *ring = p.ring + (which[k] == 2 ? 0 : in_ring(which[k] == 1 ? (int64_t)count + x[k] : x[k]));
+                source[k] = which[k] == 1 ? entry : ring;   // (of positions: whatever the ring's first entry is)
+                target[k] = which[k] == 0 ? entry : (which[k] == 1 ? ring : p.positions + x[k]);
+                value[k] = begin;
+            }
 #pragma unroll
-            for (int k = 0; k < AT; ++k)
-                *entry(0, x[k], of[k]) = page[k];
-        });
-        each(1, back0, [&](const int (&x)[AT], const int (&of)[AT]) {
-            int page[AT];
+            for (int k = 0; k < AT; ++k) {
+                const int page = *source[k];
+                value[k] = which[k] == 2 ? value[k] : page;
+            }
 #pragma unroll
-            for (int k = 0; k < AT; ++k) page[k] = *entry(1, x[k], of[k]);
-#pragma unroll
-            for (int k = 0; k < AT; ++k)
-                p.ring[in_ring((int64_t)count + x[k])] = page[k];
-        });
-        each(2, add0, [&](const int (&x)[AT], const int (&of)[AT]) {
-#pragma unroll
-            for (int k = 0; k < AT; ++k) p.positions[x[k]] = places.from[2][of[k]] + (x[k] - places.at[2][of[k]]);
-        });
+            for (int k = 0; k < AT; ++k) *target[k] = value[k];
+        }
     }
     if (what & ENTRIES)
         for (int i = add0 + part; i < p.T; i += stride) p.positions[i] = 0;   // (T up to 2^23)
@@ -257,7 +253,7 @@ void launch_part(const AdvanceParams &p, int parts, int what, hipStream_t s)
 hipError_t launch_advance(const AdvanceParams &p, hipStream_t s)
 {
     // as many entries as a 64th of the tables
-    const int64_t entries = (int64_t)p.S * p.width / 64, most = (p.T > entries ? p.T : entries) / SHARE;
+    const int64_t entries = (int64_t)p.S * p.width / 64, most = (p.T + entries) / SHARE;
     const int parts = 1 + (int)(most < 63 ? most : 63);
     const bool in_place = p.kv_lens == p.lens || p.state_out == p.state;
     if (parts == 1 || !in_place) {
