@@ -19,7 +19,6 @@ namespace lamp {
 namespace {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int RANGE_UNIT = 4;      // code values of a step of a range
@@ -634,7 +633,7 @@ struct SelectShape {
 // is read and are selected from side by side, up to WIDEST places where the tiles fill the
 // device (32 times 8 tokens of 781 places 42.8 / 44.7; 4 times 500 of 625 157 / 186, but 2000
 // of 1250 608 / 449).  The scores of a tile fit half of a CU's LDS, KEYS of them.
-constexpr int64_t KEYS = 12288, ALONE = (int64_t)1 << 17, CHUNK = 4;
+constexpr int64_t KEYS = 12288, ALONE = (int64_t)1 << 17, CHUNK_TOKENS = 4;
 // Places in the table from which a row's workgroup in the second launch is of 1024
 // threads (6250 places of 32 tokens and 8 heads: 14 us; of one token and 8 heads 15, of 256
 // threads 28).
@@ -650,7 +649,7 @@ static SelectShape select_shape(int D, int64_t T, int64_t S, int G, int Hkv, int
     // (fewer tokens a tile: the operand's other rows are 0)
     int per = x.tokens;
     while (per > 1 && (per * width > KEYS || tiles(per) * Hkv < 256)) per /= 2;
-    x.one = width * per <= KEYS && width <= WIDEST && (width * 2 * D <= ALONE || (T >= CHUNK * S && tiles(per) * Hkv >= 256));
+    x.one = width * per <= KEYS && width <= WIDEST && (width * 2 * D <= ALONE || (T >= CHUNK_TOKENS * S && tiles(per) * Hkv >= 256));
     if (x.one) x.tokens = per, x.tiles = tiles(per);
     return x;
 }
