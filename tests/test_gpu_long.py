@@ -100,6 +100,37 @@ def test_advance_by_several_workgroups(L, S, longest, new, T, in_place):  # noqa
     assert _check_step(L, lens, add, prefix, 16, T, table, ring, short, in_place=in_place)[3][3] == 1
 
 
+def test_advance_captured_in_place_by_several_workgroups(L):  # noqa: F811
+    """A captured step in place goes on from step to step as the plain one does, until one is not admitted."""
+    S, page, T, g = 600, 16, 20000, _gen(9)
+    lens, pages = torch.randint(0, 3000, (S,), generator=g).tolist(), 130000
+    table = torch.full((S, 1000), -1, dtype=torch.int32)
+    order, at = torch.randperm(pages, generator=g).int(), 0
+    for s, n in enumerate(lens):
+        held = -(-n // page)
+        table[s, :held] = order[at:at + held]
+        at += held
+    ring, state = torch.cat([order[at:], torch.full((at,), -9, dtype=torch.int32)]), [0, pages - at, 0, 0]
+    rd, sd, td, ld, ad = ring.cuda(), _i32(state), table.cuda(), _i32(lens), _i32([0] * S)
+    out = (ld, _i32([0] * (S + 1)), _i32([0] * T), sd)
+    stream = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        L.kv_advance(L.KVPool(rd, sd), td, ld, ad, page, T, None, out)
+    seen = set()
+    for step in range(6):
+        add = torch.where(torch.rand(S, generator=g) < 0.2, -1, torch.randint(0, 60 if step < 5 else 200, (S,), generator=g)).int()
+        ad.copy_(add)
+        graph.replay()
+        torch.cuda.synchronize()
+        lens, starts, positions, state, table, ring = Q.advance(lens, add.tolist(), None, table, page, T, ring, state)
+        for got, want in zip(out, (lens, starts, positions, state)):
+            assert got.tolist() == list(want)
+        assert torch.equal(td.cpu(), table) and torch.equal(rd.cpu(), ring)
+        seen.add(state[3])
+    assert seen == {0, 4}
+
+
 def test_advance_refuses_steps(L):  # noqa: F811
     """Too few free pages, tokens, places: nothing is added, sequences leave all the same; too many pages going back: none."""
     lens, add = [40, 20, 100, 0], [30, -1, 1, 16]
