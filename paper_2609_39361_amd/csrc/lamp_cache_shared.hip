@@ -147,9 +147,10 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedAttnParams p)
 // Groups of up to GROUP_PREFIX rows take the form of lamp_cache_prefix.h, beside the
 // sequences, in the form for few rows; where the batch holds more rows than that,
 // larger groups, and sequences of more than SHARED_FEW rows, take the form for many
-// in a launch of its own.  Behind 8192 shared keys (32/8 heads, d = 128): one token
-// 18 us in the first form and 22 in that for few rows, 8 tokens 20 and 28, 250 tokens
-// (1000 rows) 78 and 87 in that for many, 1000 tokens 274 and 254.
+// in a launch of its own.  Behind 8192 shared keys (32/8 heads, d = 128): 100 tokens (400
+// rows) 39 us in the first form and 52 in that for many, 250 tokens 74 and 83, 1000
+// tokens 269 and 247; one token 18 and 22 in that for few rows, 8 tokens 20 and 28 (with
+// an earlier join; now 14 and 16 in the first).
 constexpr int GROUP_PREFIX = 1024, SHARED_FEW = 64;
 constexpr int64_t JOIN_WIDE = 4096;   // rows up to which a wave joins each (a call with 2048 rows 36.6 us, by 16 lanes 37.2; with 8000 rows 107 and 103)
 
