@@ -88,6 +88,8 @@ __device__ __forceinline__ void cache_few(const P &p, int x, SH &sh)
 
     const int *table = p.b.table + sq.row * p.b.table_stride;
     const int ps = p.b.page_shift, pmask = (1 << ps) - 1;
+    // the page of keys that no row sees: none (any entry of the table may be a missing page's)
+    constexpr int UNSEEN = -1;
     if constexpr (PAGES) {
         if (threadIdx.x == 0) sh.listed = sh.seen = 0;
         __syncthreads();
@@ -96,7 +98,7 @@ __device__ __forceinline__ void cache_few(const P &p, int x, SH &sh)
         for (int i = (int)threadIdx.x; i < many; i += 64 * WAVES) {
             const int place = list[i];
             const bool is = place >= 0 && place < p.b.width && place << ps < hi_any;
-            sh.page[i] = is ? table[place] : INT_MIN;
+            sh.page[i] = is ? table[place] : UNSEEN;
             sh.key[i] = is ? place << ps : INT_MAX / 2;
             if (is) atomicMax(&sh.listed, i + 1), sh.seen = 1;
         }
@@ -105,8 +107,7 @@ __device__ __forceinline__ void cache_few(const P &p, int x, SH &sh)
         end = __builtin_amdgcn_readfirstlane(((sh.listed << ps) + KT - 1) / KT);
     }
     // page of the KPL keys from `key` (a page holds them whole): as the table has it (not looked at before its first use, a tile
-    // on), or UNSEEN by every row
-    constexpr int UNSEEN = INT_MIN;
+    // on), or UNSEEN
     auto page_at = [&](int key) {
         int pg = UNSEEN;
         if constexpr (PAGES) {
@@ -121,7 +122,7 @@ __device__ __forceinline__ void cache_few(const P &p, int x, SH &sh)
         if constexpr (PAGES) return key >> ps < sh.listed ? sh.key[key >> ps] + (key & pmask) : INT_MAX / 2;
         else return key;
     };
-    auto held = [&](int pg) { return pg >= 0 && pg < p.b.pages; };   // (otherwise UNSEEN or missing)
+    auto held = [&](int pg) { return pg >= 0 && pg < p.b.pages; };   // (otherwise missing or UNSEEN)
     const int kgrp = ((n >> 2) * KPL);   // the lane's key group as a row of K, its first key in the tile
     uint32_t kreg[NT][KW], vreg[DT][VW];
     float kscale = 0.0f, vscale = 0.0f;
@@ -144,7 +145,7 @@ __device__ __forceinline__ void cache_few(const P &p, int x, SH &sh)
     auto load_v = [&](int t) {
         const bool is = held(pgv);
         const int64_t at = (int64_t)(is ? pgv : 0) * p.b.Hkv + u.head;
-        bad = !is && pgv != UNSEEN;
+        bad = !is && position(t * KT + g * KPL) < hi_any;
         kscale = p.ks[at] * p.scale_log2;
         vscale = is ? p.vs[at] : 1.0f;   // (its probabilities are 0 or NaN)
         const uint8_t *c = p.vc + at * ((int64_t)D << ps) + (int64_t)n * (1 << ps) + ((t * KT + g * KPL) & pmask);

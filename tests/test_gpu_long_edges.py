@@ -1,0 +1,53 @@
+"""Values at the edges of what the operators of long contexts and changing batches are told: table entries, scales,
+sizes."""
+import pytest
+import torch
+
+from test_gpu_long import _lists, _run_pages, _run_shared, _shared_case
+from test_gpu_serve import L, _attn_case, _run_attn  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+NO_PAGE = [-1, 10 ** 6, 2 ** 31 - 1, -2 ** 31]
+
+
+@pytest.mark.parametrize("entry", NO_PAGE)
+@pytest.mark.parametrize("d,page", [(64, 16), (128, 64), (256, 32)])
+def test_attn_cache_every_missing_entry(L, entry, d, page):  # noqa: F811
+    """Rows that see a place whose entry is no page are NaN, whatever the entry: single tokens, chunks, and (300 tokens) a
+    prompt in the form for many rows."""
+    for lens in ([(700, 1), (60, 3)], [(700, 300), (300, 40)]):
+        q, parts, table, kv, starts = _attn_case(L, lens, 4, 2, d, page, seed=d)
+        table[0, 2] = entry
+        for window in (0, 100):
+            got = _run_attn(L, q, parts, table, kv, starts, page, 4, window=window)
+            assert torch.isnan(got[0][0]).all() == (window == 0) and torch.isfinite(got[0][starts[1]:].float()).all()
+
+
+@pytest.mark.parametrize("entry", NO_PAGE)
+@pytest.mark.parametrize("d,page", [(64, 16), (128, 64), (256, 32)])
+def test_attn_pages_every_missing_entry(L, entry, d, page):  # noqa: F811
+    q, parts, table, kv, starts = _attn_case(L, [(700, 2), (900, 1)], 4, 2, d, page, seed=d)
+    table[0, 2] = entry
+    places = _lists(table, kv, starts, 2, page, 5, 1)
+    places[0, 0] = torch.tensor([0, 2, 5, -1, -1])
+    places[1, 1] = torch.tensor([1, 3, 2, 6, 9])
+    places[0, 1, places[0, 1] == 2] = 1
+    got = _run_pages(L, (q, parts, table, kv, starts), page, 4, places)
+    assert torch.isnan(got[0][0, :2]).all() and torch.isnan(got[0][1, 2:]).all()
+    assert torch.isfinite(got[0][0, 2:].float()).all() and torch.isfinite(got[0][2].float()).all()
+
+
+@pytest.mark.parametrize("entry", NO_PAGE)
+@pytest.mark.parametrize("d,page", [(64, 16), (128, 64), (256, 32)])
+def test_attn_shared_every_missing_entry(L, entry, d, page):  # noqa: F811
+    """Of a prefix, and of one sequence's own keys; in the forms for few rows, for prefixes, and for many rows."""
+    for groups in ([(256, [(100, 1), (30, 2)]), (64, [(70, 1)])], [(256, [(100, 260), (30, 2)]), (64, [(70, 1)])]):
+        q, parts, table, kv, starts, prefix, gs = _shared_case(groups, 4, 1, d, page, seed=d)
+        for places in ((range(2), 128 // page), ((1,), 256 // page)):
+            hole = table.clone()
+            for s in places[0]:
+                hole[s, places[1]] = entry
+            got = _run_shared(L, (q, parts, hole, kv, starts, prefix, gs), page)
+            assert torch.isnan(got[0][starts[1]:starts[2]]).all() and torch.isfinite(got[0][starts[2]:].float()).all()
+            assert torch.isnan(got[0][0]).all() == (len(places[0]) == 2)
