@@ -531,12 +531,13 @@ int lamp_kv_bounds(const lamp_cache *cache, const lamp_batch *batch, int8_t *bou
  * q' = q / 2^e (to nearest even), e >= -100 the smallest with |q'| <= 127 for all of
  * them (what is not finite counts as 0).  A page's score is
  *   k_scale * max over the heads of sum_c max(q'_c bounds[0]_c, q'_c bounds[1]_c),
- * an integer times a power of two, exact in fp32: in units of 2^(e+2) an upper
- * bound of q.k for the rounded query.  Places are those of the keys that the token
- * sees, [0, p/page] at position p, and within the table.  The first `first` and the
- * last `last` of them are taken always, then those of the largest score, ties to the
- * lower place; places without a page come after all others.  places int32
- * [T][Hkv][budget]: ascending, -1 behind the last.  budget >= first + last.
+ * an integer times a power of two, compared exactly whatever power of two (or 0)
+ * k_scale is: in units of 2^(e+2) an upper bound of q.k for the rounded query.  Places
+ * are those of the keys that the token sees, [0, p/page] at position p, and within the
+ * table.  The first `first` and the last `last` of them are taken always, then those of
+ * the largest score, ties to the lower place; places without a page come after all
+ * others.  places int32 [T][Hkv][budget]: ascending, -1 behind the last.
+ * budget >= first + last.
  * Nothing is written for tokens from q_start[S] on.
  *
  * workspace: lamp_select_pages_workspace_size(...) bytes, as for lamp_attn_cache.

@@ -9,8 +9,8 @@
 // (|hi|, |lo| <= 448 / 4 = 112; a quarter of the codes' bytes would hold them
 // exactly, but integers make the score exact), and the queries of a token and kv
 // head are rounded to int8 under one power of two (|q'_c| <= 127).  So a score is
-// an integer below 2 d 127 112 < 2^23 times a power of two: exact in fp32 in
-// whatever order it is summed, and the same pages are selected everywhere.
+// an integer up to d 127 112 < 2^22, exact in whatever order it is summed, times a
+// power of two, and the same pages are selected everywhere.
 #include <hip/hip_runtime.h>
 
 #include "lamp_cache_plan.h"
@@ -130,11 +130,25 @@ __device__ __forceinline__ int step_exponent(uint32_t amax)
     return e < -100 ? -100 : e;
 }
 
-// Order-preserving bits of a finite fp32 number, above 1 and below ~0u - 1.
-__device__ __forceinline__ uint32_t sortable(float x)
+// Order-preserving bits, above MISSING and below FORCED, of x ks: x below 2^22, ks any
+// fp32 power of two or 0.  The product passes fp32's range at both ends, so that the
+// exponent of ks, from -148 to 128, is added to that of x times its mantissa: 9 bits;
+// the last bit of the product's mantissa, 0 for such ks, makes room.
+struct Scale {
+    float mantissa;
+    uint32_t exponent;   // above 0, in place in the bits of an fp32 number
+};
+
+__device__ __forceinline__ Scale scale_of(float ks)
 {
-    const uint32_t b = __builtin_bit_cast(uint32_t, x + 0.0f);   // (-0 as 0)
-    return b & 0x80000000u ? ~b : b | 0x80000000u;
+    return {__builtin_amdgcn_frexp_mantf(ks), (uint32_t)(__builtin_amdgcn_frexp_expf(ks) + 149) << 23};
+}
+
+__device__ __forceinline__ uint32_t sortable(int x, const Scale &s)
+{
+    const float y = (float)x * s.mantissa;
+    const uint32_t b = __builtin_bit_cast(uint32_t, y), m = y == 0.0f ? 0u : ((b & 0x7FFFFFFFu) + s.exponent) >> 1;
+    return 0x80000000u + (b & 0x80000000u ? 0u - m : m);
 }
 
 constexpr uint32_t MISSING = 0, FORCED = ~0u;
@@ -305,10 +319,11 @@ __device__ __forceinline__ void write_scores(const SelectParams &p, const i32x4 
 {
     const int lane = threadIdx.x & 63, hs = p.heads_shift;
     const bool is = pg >= 0 && pg < p.b.pages;
+    const Scale scale = scale_of(ks);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         const int r = 4 * (lane >> 4) + e, tk = r >> hs;
-        if ((r & ((1 << hs) - 1)) == 0 && tk < n) write(tk, is ? sortable((float)x[e] * ks) : MISSING);
+        if ((r & ((1 << hs) - 1)) == 0 && tk < n) write(tk, is ? sortable(x[e], scale) : MISSING);
     }
 }
 

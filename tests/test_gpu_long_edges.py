@@ -3,7 +3,7 @@ sizes."""
 import pytest
 import torch
 
-from test_gpu_long import _lists, _run_pages, _run_shared, _shared_case
+from test_gpu_long import _check_select, _lists, _run_pages, _run_shared, _select_case, _shared_case
 from test_gpu_serve import L, _attn_case, _run_attn  # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -51,3 +51,16 @@ def test_attn_shared_every_missing_entry(L, entry, d, page):  # noqa: F811
             got = _run_shared(L, (q, parts, hole, kv, starts, prefix, gs), page)
             assert torch.isnan(got[0][starts[1]:starts[2]]).all() and torch.isfinite(got[0][starts[2]:].float()).all()
             assert torch.isnan(got[0][0]).all() == (len(places[0]) == 2)
+
+
+@pytest.mark.parametrize("lo,hi", [(100, 120), (-149, -110), (-149, 128), (120, 128)])
+@pytest.mark.parametrize("Hq,H,d,keys", [(4, 2, 64, 6000), (1, 1, 256, 4000), (40, 2, 64, 3000), (8, 1, 128, 30000), (34, 1, 128, 17000)])
+def test_select_scales_of_the_whole_range(L, Hq, H, d, keys, lo, hi):  # noqa: F811
+    """Scores pass fp32's largest number, and its smallest normal one, in order all the same; in one launch and in two."""
+    q, rng, ks, table, kv, starts = _select_case([(keys, 2), (keys // 3, 1)], Hq, H, d, 16, hi - lo)
+    g = torch.Generator().manual_seed(hi)
+    ks = (2.0 ** torch.randint(lo, hi, ks.shape, generator=g).double()).float()
+    assert bool((ks > 0).all()) and bool(torch.isfinite(ks).all())
+    q[0] *= 0.01
+    for budget in (5, 40):
+        _check_select(L, (q, rng, ks, table, kv, starts), 16, budget, 1, 1)
