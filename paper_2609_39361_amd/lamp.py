@@ -621,6 +621,14 @@ def attn_cache(q, cache, block_table, kv_lens, q_start=None, causal=True, window
 KVPool = collections.namedtuple("KVPool", "ring state")
 
 
+def _c_int(x, name):
+    """A size as the library takes it (ctypes would take the low 32 bits of others)."""
+    x = int(x)
+    if not -0x80000000 <= x <= 0x7FFFFFFF:
+        raise ValueError("%s=%d is beyond a C int" % (name, x))
+    return x
+
+
 def kv_pool(pages, device="cuda"):
     """A KVPool in which the pages 0 .. pages-1 are free."""
     return KVPool(torch.arange(pages, dtype=_I32, device=device), torch.tensor([0, pages, 0, 0], dtype=_I32, device=device))
@@ -656,7 +664,7 @@ def kv_advance(pool, block_table, kv_lens, add, page, tokens, prefix_lens=None, 
     if prefix_lens is not None and (prefix_lens.dtype is not _I32 or prefix_lens.get_device() != dev or prefix_lens.shape != (S,)
                                     or not prefix_lens.is_contiguous()):
         _must(prefix_lens, "prefix_lens", (_I32,), dev, (S,))
-    tokens = int(tokens)
+    page, tokens = _c_int(page, "page"), _c_int(tokens, "tokens")
     if tokens < 0:
         raise ValueError("tokens must not be negative")
     if out is None:
@@ -668,7 +676,7 @@ def kv_advance(pool, block_table, kv_lens, add, page, tokens, prefix_lens=None, 
             _must(t, "out: " + name, (_I32,), dev, (n,))
     _call(dev, lib().lamp_kv_advance, kv_lens.data_ptr(), add.data_ptr(),
           None if prefix_lens is None else prefix_lens.data_ptr(), block_table.data_ptr(), block_table.stride(0), S, width,
-          int(page), tokens, ring.data_ptr(), ring.numel(), state.data_ptr(), lens.data_ptr(), q_start.data_ptr(),
+          page, tokens, ring.data_ptr(), ring.numel(), state.data_ptr(), lens.data_ptr(), q_start.data_ptr(),
           positions.data_ptr(), new_state.data_ptr())
     return lens, q_start, positions, KVPool(ring, new_state)
 
@@ -690,7 +698,7 @@ def kv_bounds(cache, bounds, block_table, kv_lens, tokens, q_start=None):
     """Bring `bounds` (of kv_page_bounds) up to date for the pages that a batch of `tokens` new tokens went to, after
     kv_append with the same block_table, kv_lens and q_start: the range of each channel over a page's keys in units of 4
     code values, bounds[:,:,0] the largest (rounded up), bounds[:,:,1] the smallest (rounded down).  Returns bounds."""
-    c, b, dev, Hkv, _, d, _, _ = _paged(cache, block_table, kv_lens, q_start, int(tokens))
+    c, b, dev, Hkv, _, d, _, _ = _paged(cache, block_table, kv_lens, q_start, _c_int(tokens, "tokens"))
     _call(dev, lib().lamp_kv_bounds, c, b, _bounds(bounds, dev, (cache.k.shape[0], Hkv, 2, d)))
     return bounds
 
@@ -759,7 +767,7 @@ def select_pages(q, cache, bounds, block_table, kv_lens, budget, q_start=None, f
     c, b, dev, Hkv, _, d, S, width = _paged(cache, block_table, kv_lens, q_start, T)
     rows = _queries(q, dev, d)
     ranges = _bounds(bounds, dev, (cache.k.shape[0], Hkv, 2, d))
-    budget = int(budget)
+    budget, first, last = _c_int(budget, "budget"), _c_int(first, "first"), _c_int(last, "last")
     if budget <= 0:
         raise ValueError("budget must be positive")
     if out is None:
@@ -767,7 +775,7 @@ def select_pages(q, cache, bounds, block_table, kv_lens, budget, q_start=None, f
     else:
         _must(out, "out", (_I32,), dev, (T, Hkv, budget))
     ws, size, keep = _workspace(workspace, _need("lamp_select_pages_workspace_size", T, S, rows[3], Hkv, d, width, budget), q, dev)
-    _call(dev, lib().lamp_select_pages, *rows, c, b, ranges, budget, int(first), int(last), out.data_ptr(), ws, size)
+    _call(dev, lib().lamp_select_pages, *rows, c, b, ranges, budget, first, last, out.data_ptr(), ws, size)
     return out
 
 

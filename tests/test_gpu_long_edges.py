@@ -3,7 +3,7 @@ sizes."""
 import pytest
 import torch
 
-from test_gpu_long import _check_select, _lists, _run_pages, _run_shared, _select_case, _shared_case
+from test_gpu_long import _cache_of_scales, _check_select, _i32, _lists, _run_pages, _run_shared, _select_case, _shared_case
 from test_gpu_serve import L, _attn_case, _run_attn  # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -64,3 +64,26 @@ def test_select_scales_of_the_whole_range(L, Hq, H, d, keys, lo, hi):  # noqa: F
     q[0] *= 0.01
     for budget in (5, 40):
         _check_select(L, (q, rng, ks, table, kv, starts), 16, budget, 1, 1)
+
+
+def test_sizes_beyond_a_c_int_are_refused(L):  # noqa: F811
+    """Not taken by their low 32 bits."""
+    q, rng, ks, table, kv, starts = _select_case([(500, 2)], 4, 2, 64, 16, 3)
+    cache = _cache_of_scales(L, ks, 16, 64)
+    args = (q.cuda(), cache, rng.cuda(), table.cuda(), _i32(kv))
+    out = torch.full((2, 2, 6), -2, dtype=torch.int32, device="cuda")
+    for big in (2 ** 32, 2 ** 32 + 1, -2 ** 32, 2 ** 31, -2 ** 31 - 1, 2 ** 64 + 1):
+        for kw in (dict(first=big), dict(last=big)):
+            with pytest.raises(ValueError):
+                L.select_pages(*args, 6, _i32(starts), out=out, **kw)
+        with pytest.raises(ValueError):
+            L.select_pages(*args, big, _i32(starts))
+    assert bool((out == -2).all())
+    pool, t, n = L.kv_pool(8), torch.full((2, 4), -1, dtype=torch.int32, device="cuda"), _i32([0, 0])
+    for page, tokens in ((2 ** 32 + 16, 4), (16, 2 ** 32 + 4), (-2 ** 32 + 16, 4)):
+        with pytest.raises(ValueError):
+            L.kv_advance(pool, t, n, _i32([1, 1]), page, tokens, None, (n, _i32([0] * 3), _i32([0] * 4), pool.state))
+    assert pool.state.tolist() == [0, 8, 0, 0] and bool((t == -1).all()) and n.tolist() == [0, 0]
+    bounds = L.kv_page_bounds(cache)
+    with pytest.raises(ValueError):
+        L.kv_bounds(cache, bounds, table.cuda(), _i32(kv), 2 ** 32 + 2, _i32(starts))
