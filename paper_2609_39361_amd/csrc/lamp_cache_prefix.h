@@ -22,7 +22,8 @@ namespace {
 // registers until they are due, and passes them through a stretch of LDS of its own, K
 // first, then V, with rows a 16-byte unit longer than their bytes (and the upper half
 // of the keys 64 bytes on), so that 8 lanes reading a unit of their rows use all
-// banks.  No barrier is needed until the waves join.  Nothing is masked but whole
+// banks.  No barrier is needed until the waves join: a wave's accesses of LDS are
+// executed in order, and the compiler is kept to it.  Nothing is masked but whole
 // groups of 16 keys behind the prefix's end, which is a page's.
 //
 // Bound by issue (d = 128): a tile's 290 vector and 32 matrix instructions take a wave
@@ -132,6 +133,13 @@ __device__ __forceinline__ void cache_prefix(const SharedAttnParams &p, int x, P
             *reinterpret_cast<u32x4 *>(s + (i - g * (NL / NPG)) * (1024 / PAGE) * SH::VROW + g * PAGE) = vr[i];
         }
     };
+    // What lanes have stored is there for the others of the wave, and what they have read may be stored over.  (The
+    // compiler looks at one lane, whose loads and stores could be told apart.  No instruction comes of it.)
+    auto in_order = [] {
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+    };
     // the lane's key in the tile as row n of the K operand b; its keys of V and of logits, 16 for each b
     auto key_of = [&](int b) { return (KT / 2) * (n >> 2 & 1) + 16 * b + 8 * (n >> 4) + 4 * (n >> 3 & 1) + (n & 3); };
     auto group_of = [&](int b) { return (KT / 2) * h + 16 * b; };
@@ -169,7 +177,9 @@ __device__ __forceinline__ void cache_prefix(const SharedAttnParams &p, int x, P
         for (int e = 0; e < 16; ++e) o[i][e] = 0.0f;
     float m = LOWEST, l = 0.0f;   // (l: of this lane's keys)
     for (; t < end; t += WAVES) {
+        in_order();
         store_k();
+        in_order();
         load_k(t + WAVES);
         f32x16 s[NB];
 #pragma unroll
@@ -222,7 +232,9 @@ __device__ __forceinline__ void cache_prefix(const SharedAttnParams &p, int x, P
             const auto halves = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, mt), __builtin_bit_cast(uint32_t, mt), false, false);
             mt = fmaxf(__builtin_bit_cast(float, (uint32_t)halves[0]), __builtin_bit_cast(float, (uint32_t)halves[1]));
         }
+        in_order();
         store_v();
+        in_order();
         load_v(t + WAVES);
         look_up(t + 2 * WAVES);
         if (__ballot(mt > m + LAZY)) {
