@@ -248,9 +248,7 @@ hipError_t launch_shared_attn(int D, SharedAttnParams &p, void *ws, hipStream_t 
     const SharedBounds b = shared_bounds(p.b.T, p.b.S, p.groups, p.Hq / p.b.Hkv, p.b.Hkv, (int64_t)p.b.width << p.b.page_shift);
     const SharedLayout l = shared_layout(b, D, p.b.T, p.Hq, (int64_t)p.b.S + p.groups);
     char *base = static_cast<char *>(ws);
-    p.apart = 1;
     p.counts = reinterpret_cast<int *>(base);
-    p.split = base + 16;
     p.rows = base + l.rows;
     for (int f = 0; f < 3; ++f) {
         p.group_above[f] = b.group_above[f];
