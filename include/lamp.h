@@ -570,7 +570,11 @@ size_t lamp_attn_pages_workspace_size(int T, int Hq, int Hkv, int d, int page, i
  * first sequence.  group_start int32 [groups+1], non-decreasing, from 0 to S;
  * prefix_lens int32 [S], at most the keys before the sequence's new tokens (0: none).
  * The same results as lamp_attn_cache's but for the order of fp32 sums.
- * T*Hq up to 2^23; other limits as for lamp_attn_cache.
+ * groups from 1 to S, T*Hq up to 2^23; other limits as for lamp_attn_cache.
+ * The workspace has room for two fp32 partial outputs of every row that a batch of T
+ * tokens could have, whatever the lengths turn out to be: from about 8 d bytes for each
+ * of T*Hq (65536 tokens of 64 sequences in 4 groups, 32/8 heads, d = 128: 2.4 GB, where
+ * lamp_attn_cache takes 77 MB) to several times that for few tokens (64 tokens 15 MB).
  */
 int lamp_attn_shared(const uint16_t *q, int64_t q_token, int64_t q_head, int Hq, const lamp_cache *cache,
                      const lamp_batch *batch, const int32_t *prefix_lens, const int32_t *group_start, int groups,

@@ -40,8 +40,8 @@ struct ManyRows {      // prompts (lamp_cache_many.h; 32 row tiles' window of 10
 };
 
 // A group's rows over their shared prefix (lamp_cache_prefix.h).  Two workgroups fill a
-// CU's registers, but share its issue: units for one a CU (behind 8192 shared keys: 32
-// tokens 20 us, 64 tokens 27, 250 tokens 74; for two 26, 32 and 80).
+// CU's registers, but share its issue: units for one a CU (behind 8192 shared keys, without
+// others of their own: 32 tokens 20 us, 64 tokens 27, 250 tokens 73; for two 26, 32 and 80).
 struct PrefixRows {
     static constexpr int ROWS = 32, TARGET = 256, MIN_TILES = 8, FORM = 2;
 };
@@ -394,7 +394,7 @@ struct SeqInfo {
     int units, slots, tiles, c;
     int row, a, n, all, len, pos0, lo, causal;
 };
-constexpr int SHARED_ALONE = 128;   // (the launch takes 5.8 us: 250 sequences behind one prefix 74 us with it, 83 without; 160 the same)
+constexpr int SHARED_ALONE = 128;   // (the launch takes 5.8 us: 250 tokens behind 8192 keys, without others of their own, 74 us with it, 83 without; 160 the same)
 
 // Unit x and its sequence's plan, by a wave that plans for itself: lane l has the EACH
 // groups and sequences from EACH l, and the plan comes from the lane that has it.

@@ -13,9 +13,9 @@
 // few rows, and, where the batch may hold so many rows, of a second in the form for
 // many.  The last launch joins each row's partial outputs, whose places the first
 // pieces leave (RowInfo).  (Units of groups and of sequences in turn instead of one
-// after the other: slower.)  Four samples of one prompt (1000 keys, 8/8 heads, d = 64): 7.7 us
+// after the other: slower.)  Four samples of one prompt (1000 keys, 8/8 heads, d = 64): 7.6 us
 // and 4.1 for the join; questions of 100 to 300 tokens about two documents of some 4000 keys
-// (121 GFLOP): 148 us, 14 for the join of 61 MB.
+// (121 GFLOP): 147 us, 14 for the join of 61 MB.
 #include <hip/hip_runtime.h>
 
 #include "lamp_cache_many.h"
@@ -147,10 +147,11 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedAttnParams p)
 // Groups of up to GROUP_PREFIX rows take the form of lamp_cache_prefix.h, beside the
 // sequences, in the form for few rows; where the batch holds more rows than that,
 // larger groups, and sequences of more than SHARED_FEW rows, take the form for many
-// in a launch of its own.  Behind 8192 shared keys (32/8 heads, d = 128): 100 tokens (400
-// rows) 39 us in the first form and 52 in that for many, 250 tokens 74 and 83, 1000
-// tokens 269 and 247; one token 18 and 22 in that for few rows, 8 tokens 20 and 28 (with
-// an earlier join; now 14 and 16 in the first).
+// in a launch of its own.  Single tokens behind 8192 shared keys, without other keys of
+// their own (32/8 heads, d = 128): 100 tokens (400 rows) 40 us in the first form and 53 in
+// that for many, 250 tokens 73 and 83, 300 tokens 97 and 96, 600 tokens 163 and 160, 1000
+// tokens 268 and 247.  One token 14.4, 8 tokens 16.1, where attn_cache, which reads each
+// one's keys in the form for few rows, takes 14.1 and 25.2.
 constexpr int GROUP_PREFIX = 1024, SHARED_FEW = 64;
 constexpr int64_t JOIN_WIDE = 4096;   // rows up to which a wave joins each (a call with 2048 rows 36.6 us, by 16 lanes 37.2; with 8000 rows 107 and 103)
 
