@@ -90,6 +90,8 @@ __device__ __forceinline__ void cache_few(const P &p, int x, SH &sh)
     const int ps = p.b.page_shift, pmask = (1 << ps) - 1;
     // the page of keys that no row sees: none (any entry of the table may be a missing page's)
     constexpr int UNSEEN = -1;
+    // and their position in a list: behind every key, a page below the largest number
+    constexpr int BEHIND = INT_MAX - 512;
     if constexpr (PAGES) {
         if (threadIdx.x == 0) sh.listed = sh.seen = 0;
         __syncthreads();
@@ -99,7 +101,7 @@ __device__ __forceinline__ void cache_few(const P &p, int x, SH &sh)
             const int place = list[i];
             const bool is = place >= 0 && place < p.b.width && place << ps < hi_any;
             sh.page[i] = is ? table[place] : UNSEEN;
-            sh.key[i] = is ? place << ps : INT_MAX / 2;
+            sh.key[i] = is ? place << ps : BEHIND;
             if (is) atomicMax(&sh.listed, i + 1), sh.seen = 1;
         }
         __syncthreads();
@@ -119,7 +121,7 @@ __device__ __forceinline__ void cache_few(const P &p, int x, SH &sh)
     };
     // position of the first of the KPL keys from `key`
     auto position = [&](int key) {
-        if constexpr (PAGES) return key >> ps < sh.listed ? sh.key[key >> ps] + (key & pmask) : INT_MAX / 2;
+        if constexpr (PAGES) return key >> ps < sh.listed ? sh.key[key >> ps] + (key & pmask) : BEHIND;
         else return key;
     };
     auto held = [&](int pg) { return pg >= 0 && pg < p.b.pages; };   // (otherwise missing or UNSEEN)

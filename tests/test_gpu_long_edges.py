@@ -87,3 +87,18 @@ def test_sizes_beyond_a_c_int_are_refused(L):  # noqa: F811
     bounds = L.kv_page_bounds(cache)
     with pytest.raises(ValueError):
         L.kv_bounds(cache, bounds, table.cuda(), _i32(kv), 2 ** 32 + 2, _i32(starts))
+
+
+@pytest.mark.parametrize("d,page", [(64, 256), (128, 64), (256, 16)])
+def test_attn_pages_of_the_longest_sequences(L, d, page):  # noqa: F811
+    """Entries of a list that hold no keys hold none of a sequence as long as a table reaches (2^30 keys, of a few pages)."""
+    q, parts, table, kv, starts = _attn_case(L, [(40 * page, 3)], 4, 2, d, page, seed=d)
+    width = 2 ** 30 // page
+    long = table[0, torch.arange(width) % 40].unsqueeze(0).contiguous()
+    places = torch.full((3, 2, 7), -1, dtype=torch.int32)
+    places[0, :, 3] = width - 1
+    places[1, 0, :6] = torch.tensor([-1, 5, 2 ** 31 - 1, width - 1, width, width - 2])
+    places[1, 1, 6] = 0
+    places[2, :, 1:5:2] = torch.tensor([width // 2 + 3, width - 1])
+    got = _run_pages(L, (q, parts, long, [2 ** 30], [0, 3]), page, 4, places)
+    assert torch.isfinite(got[0].float()).all() and torch.isfinite(got[1]).all()
