@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from test_gpu_long import _cache_of_scales, _check_select, _i32, _lists, _run_pages, _run_shared, _select_case, _shared_case
-from test_gpu_serve import L, _attn_case, _run_attn  # noqa: F401
+from test_gpu_serve import L, _attn_case, _device_cache, _run_attn  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -102,3 +102,29 @@ def test_attn_pages_of_the_longest_sequences(L, d, page):  # noqa: F811
     places[2, :, 1:5:2] = torch.tensor([width // 2 + 3, width - 1])
     got = _run_pages(L, (q, parts, long, [2 ** 30], [0, 3]), page, 4, places)
     assert torch.isfinite(got[0].float()).all() and torch.isfinite(got[1]).all()
+
+
+def test_caches_whose_offsets_pass_32_bits(L):  # noqa: F811
+    """The pages of small cases at the end of a cache of 4.6 GB of keys: ranges, selection, attention over places and over a
+    shared prefix are those of the small cache."""
+    page, H, d, many = 64, 8, 128, 70000
+    q, parts, table, kv, starts, prefix, gs = _shared_case([(320, [(100, 2), (30, 1)]), (0, [(700, 1), (5, 90)])], 16, H, d, page, seed=3)
+    small = _device_cache(L, parts)
+    n = parts[0].shape[0]
+    assert (many - n) * H * page * d > 2 ** 32
+    big = L.kv_cache(many, H, d, page)
+    for x, y in zip(big, small):
+        x[many - n:] = y
+    far = torch.where(table >= 0, table + many - n, table).cuda()
+    args = _i32(kv), _i32(starts)
+    got = []
+    for cache, tab in ((small, table.cuda()), (big, far)):
+        rng = L.kv_bounds(cache, L.kv_page_bounds(cache), tab, args[0], starts[-1], args[1])
+        rng = L.kv_bounds(cache, rng, tab, args[0], sum(kv), _i32([0, *torch.tensor(kv).cumsum(0).tolist()]))   # (every key as new)
+        places = L.select_pages(q.cuda(), cache, rng, tab, args[0], 4, args[1])
+        got.append((rng[-n:], places, *L.attn_pages(q.cuda(), cache, tab, args[0], places, args[1]),
+                    *L.attn_shared(q.cuda(), cache, tab, args[0], _i32(prefix), _i32(gs), args[1])))
+    assert bool(got[0][0].any()) and bool((got[0][1] >= 0).any())
+    for x, y in zip(*got):
+        assert torch.equal(x, y)
+    _run_shared(L, (q, parts, table, kv, starts, prefix, gs), page)

@@ -128,3 +128,80 @@ def test_advance_around_the_second_workgroup(L, S, in_place):  # noqa: F811
     assert 0 < last and sum(max(0, a) for a in add) <= last
     for T in (last, last + 1):
         assert _check_step(L, lens, add, None, 16, T, *case, in_place=in_place)[3][3] == 0
+
+
+# ---------------------------------------------------------------- captured
+
+def test_captured_forms_follow_lengths_that_change(L):  # noqa: F811
+    """One graph of attn_shared planned by a launch of its own, with the forms for prefixes and for many rows and the join of
+    many rows, of select_pages in two launches and attn_pages in pieces: replayed over batches of other lengths and groups,
+    with eager work between, each replay against the eager calls."""
+    page, d, H, Hq, S, groups, T = 16, 64, 2, 8, 150, 12, 900
+    g = _gen(21)
+    pages, width = 5000, 1100
+    parts = R.random_cache(pages, H, page, d, g)
+    cache = _device_cache(L, parts)
+    hi = torch.randint(-20, 113, (pages, H, d), generator=g)
+    rng = torch.stack([hi, torch.minimum(hi, torch.randint(-112, 21, (pages, H, d), generator=g))], 2).to(torch.int8).cuda()
+    assert S + groups > _constant("lamp_cache_plan.h", "SHARED_ALONE") and T * Hq > _constant("lamp_cache_shared.hip", "JOIN_WIDE")
+    assert T * (Hq // H) > _constant("lamp_cache_shared.hip", "GROUP_PREFIX")
+    assert L.select_pages_workspace_size(T, S, Hq, H, d, width, 20) > 0 and L.attn_pages_workspace_size(40, Hq, H, d, page, 100) > 0
+    q = torch.randn(T, Hq, d, generator=g).to(torch.bfloat16).cuda()
+    lists = torch.randint(-1, 300, (40, H, 100), generator=g).int().cuda()
+    z = dict(device="cuda", dtype=torch.int32)
+    st = dict(table=torch.zeros((S, width), **z), kv=torch.zeros(S, **z), starts=torch.zeros(S + 1, **z), prefix=torch.zeros(S, **z),
+              gs=torch.zeros(groups + 1, **z))
+
+    def batch(seed):
+        """A batch whose first group holds many rows (but for seed 1), some tokens behind the last."""
+        b = _gen(seed)
+        cut = sorted(torch.randperm(S - 1, generator=b)[:groups - 1].add(1).tolist())
+        gs = [0, *cut, S]
+        table = torch.randint(0, pages, (S, width), generator=b).int()
+        new = torch.randint(0, 4, (S,), generator=b)
+        new[0] = 300 if seed != 1 else 2
+        prefix, own = torch.zeros(S, dtype=torch.long), torch.randint(0, 200, (S,), generator=b)
+        for a, e in zip(gs, gs[1:]):
+            prefix[a:e] = 16 * int(torch.randint(0, 60, (1,), generator=b))
+            table[a:e, :60] = table[a, :60].clone()
+        own[S - 1] = 15000
+        return dict(table=table, kv=(prefix + own + new).int(), starts=torch.cat([torch.zeros(1), new.cumsum(0)]).int(), prefix=prefix.int(),
+                    gs=torch.tensor(gs, dtype=torch.int32))
+
+    def step():
+        o = L.attn_shared(q, cache, st["table"], st["kv"], st["prefix"], st["gs"], st["starts"])
+        return (*o, L.select_pages(q, cache, rng, st["table"], st["kv"], 20, st["starts"]),
+                *L.attn_pages(q[:40], cache, st["table"][:40], st["kv"][:40], lists))
+
+    def load(seed):
+        for k, v in batch(seed).items():
+            st[k].copy_(v)
+
+    load(0)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for seed in (1, 2, 0, 3, 1):
+        load(seed)
+        graph.replay()
+        want = step()
+        torch.cuda.synchronize()
+        n = int(st["starts"][-1])
+        assert 300 <= n < T or seed == 1
+        for x, y in zip(held[:3], want[:3]):
+            assert torch.equal(x[:n], y[:n]), seed
+        for x, y in zip(held[3:], want[3:]):
+            assert torch.equal(x, y), seed
+        torch.randn(1000, 1000, device="cuda").sum().item()
+    b = batch(2)
+    load(2)
+    o, lse, ob, lb = R.attention(q[:int(b["starts"][-1])].cpu(), R.Cache(*parts), b["table"], b["kv"].tolist(), b["starts"].tolist(), page)
+    graph.replay()
+    R.near(held[0][:len(o)], o, ob, "o")
+    R.near(held[1][:len(o)], lse, lb, "lse")
