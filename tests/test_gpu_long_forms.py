@@ -86,11 +86,11 @@ def test_select_on_both_sides_of_its_borders(L, d, lens, one):  # noqa: F811
         _check_select(L, case, 16, budget, min(budget, 1), 0 if budget == 1 else 2)
 
 
-@pytest.mark.parametrize("G", [1, 3, 4, 8, 16, 17, 40])
-@pytest.mark.parametrize("keys", [9000, 30000])
-def test_select_in_two_launches_of_every_group_size(L, G, keys):  # noqa: F811
+@pytest.mark.parametrize("d,keys,G", [(128, keys, G) for keys in (9000, 30000) for G in (1, 3, 4, 8, 16, 17, 40)]
+                         + [(64, 17000, 2), (64, 17000, 20), (256, 5000, 20), (256, 17000, 5)])
+def test_select_in_two_launches_of_every_group_size(L, d, keys, G):  # noqa: F811
     """Groups within the matrix product's rows and beyond them, rows of up to 1024 places and of more; several tokens a tile."""
-    case = _select_case([(keys, 3), (0, 2), (keys // 2, 5)], 2 * G, 2, 128, 16, G)
+    case = _select_case([(keys, 3), (0, 2), (keys // 2, 5)], 2 * G, 2, d, 16, G)
     assert _two_launches(L, case, 30)
     _check_select(L, case, 16, 30, 1, 2)
 
